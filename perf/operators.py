@@ -240,9 +240,10 @@ def _dims(kvg, case, layers):
 
 
 class _Memory:
-    """Device memory of the library as a torch tensor."""
+    """Device memory of the library as a torch tensor, which keeps its owner alive."""
 
-    def __init__(self, ptr, n):
+    def __init__(self, owner, ptr, n):
+        self.owner = owner
         self.__cuda_array_interface__ = {"shape": (n,), "typestr": "|u1", "data": (int(ptr), False), "version": 3}
 
 
@@ -251,7 +252,7 @@ def _append_cache(case, layers, total):
     from paper_2607_14431_gb300 import kvg
     hq, hkv, d, page, _ = _geo(case)
     cache = kvg.Cache(_dims(kvg, case, layers), _pages(total, page)[1], len(total), max(total))
-    pool = torch.as_tensor(_Memory(cache.view.pool, cache.view.pool_bytes), device="cuda")
+    pool = torch.as_tensor(_Memory(cache, cache.view.pool, cache.view.pool_bytes), device="cuda")
     pool.zero_()
     kind = torch.float8_e4m3fn if case.get("fp8") else torch.bfloat16
     return kvg, cache, pool.view(kind).view(layers, 2, -1, hkv, page, d)
