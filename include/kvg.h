@@ -61,6 +61,8 @@ typedef enum kvg_status {
 
 enum { KVG_RESIDENCY_HBM = 0, KVG_RESIDENCY_PINNED_HOST = 1, KVG_RESIDENCY_CACHE_POOL = 2 };
 enum { KVG_ROPE_HALF = 0, KVG_ROPE_INTERLEAVED = 1 };
+/* Scaling of the rotation frequencies for long contexts (kvg_rotary_desc). */
+enum { KVG_ROPE_SCALING_NONE = 0, KVG_ROPE_SCALING_LINEAR = 1, KVG_ROPE_SCALING_YARN = 2 };
 enum { KVG_GRAFT_VERIFY = 1u, KVG_GRAFT_SYNC = 2u };
 enum { KVG_SHA256_PLAIN = 0, KVG_SHA256_PAGED = 1 };
 enum { KVG_DECODE_MERGE = 1u };
@@ -287,6 +289,74 @@ kvg_status kvg_cache_append(kvg_cache *cache, int32_t seq, const void *k, const 
  * run out (nothing is written); KVG_ERR_ARG on repeated ids. */
 kvg_status kvg_cache_append_batch(kvg_cache *cache, const int32_t *seq_ids, int32_t B, const void *k,
                                   const void *v, const int32_t *positions, void *stream);
+
+/* Rotary positions: pair i of the first rotary_dim dimensions of a head turns
+ * by position * f_i, f_i = theta^(-2i / rotary_dim); the rest of the head is
+ * left as it is.  style pairs dimension i with i + rotary_dim / 2
+ * (KVG_ROPE_HALF) or 2i with 2i + 1 (KVG_ROPE_INTERLEAVED): (a, b) becomes
+ * m (a cos - b sin, b cos + a sin), m = attention_factor.
+ * scaling: KVG_ROPE_SCALING_NONE; KVG_ROPE_SCALING_LINEAR: every f_i divided
+ * by factor; KVG_ROPE_SCALING_YARN: a pair that turns r times over
+ * original_positions keeps f_i for r >= beta_fast, has it divided by factor
+ * for r <= beta_slow, and takes the blend linear in r in between ("YaRN",
+ * Peng et al. 2023, whose attention factor is 0.1 ln(factor) + 1).
+ * The angle is formed from a 64-bit fixed-point fraction of a turn, so it is
+ * good to fp32 at every int32 position.
+ * A block's relocation (kvg_graft with delta != 0) rotates whole heads by
+ * kvg_dims.rope_theta / rope_style: it fits rows appended with rotary_dim =
+ * head_dim, the same base and style, and no scaling.
+ * Supported: rotary_dim a multiple of 16 in [0, head_dim]; theta >= 1; factor
+ * >= 1 (KVG_ERR_ARG otherwise).  A host object: no GPU memory, usable with
+ * every cache of its head_dim, from several threads at once. */
+typedef struct kvg_rotary_desc {
+    int32_t head_dim, rotary_dim, style, scaling;
+    double theta, factor, beta_fast, beta_slow;
+    int32_t original_positions;
+    float attention_factor;
+} kvg_rotary_desc;
+typedef struct kvg_rotary kvg_rotary;
+kvg_status kvg_rotary_create(const kvg_rotary_desc *desc, kvg_rotary **out);
+void kvg_rotary_destroy(kvg_rotary *rotary);
+
+/* Projections of T packed tokens (device, bf16): head h of token t (and run
+ * layer l) starts at + t * x_token + l * x_layer + h * head_dim elements, so
+ * slices of one projection's output are taken as they are (the x_layer are
+ * read only by a call over all layers).
+ * q_norm, k_norm: bf16 weights [layers run][head_dim], or null for no norm:
+ * x / sqrt(mean(x^2) + eps) * (weight + norm_offset) over each head. */
+typedef struct kvg_qkv {
+    const void *q, *k, *v;
+    int64_t q_token, k_token, v_token;
+    int64_t q_layer, k_layer, v_layer;
+    const void *q_norm, *k_norm;
+    float eps, norm_offset;
+    int32_t n_q_heads; /* 0: keys and values only (q and q_out null) */
+    int32_t reserved;
+} kvg_qkv;
+
+/* New tokens from their projections (the queries and rows that Sec. 3.2
+ * computes on top of a restored block): queries and keys are normalised
+ * (optional) and rotated to their positions, keys and values appended to the
+ * paged cache, queries written to q_out, in one pass, in fp32 with one
+ * rounding (to bf16, or for an fp8 cache's keys and values to E4M3 as
+ * kvg_cache_append quantizes).
+ * Packed rows: sequence seq_ids[b] (host array, distinct ids, B <= 4096) gets
+ * the next n_rows[b] (host array, >= 0) of the T = sum n_rows tokens at its
+ * end.  A decode step is n_rows of 1 throughout.  positions: device int32 [T].
+ * q_out: device bf16 [layers run][T][n_q_heads][head_dim]; it may be q itself
+ * where that has the same layout, and overlaps nothing else.
+ * rotary: null for no rotation.
+ * layer -1 does all layers in one call.  A model that runs layer by layer
+ * calls layer 0 first: like -1 it opens the rows (slots, pages, position
+ * tags); a call for layer l > 0 fills that layer of the same rows, which must
+ * still be the sequence's last (KVG_ERR_ARG otherwise), in any order of l and
+ * as often as wanted.  A row's other layers are undefined until filled.
+ * Errors (no state change): KVG_ERR_CAPACITY (slots or pages), KVG_ERR_ARG
+ * (null or misaligned buffers (16 bytes), strides that are no multiples of 8
+ * elements, repeated ids, a rotary of another head_dim). */
+kvg_status kvg_cache_append_qkv(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                int32_t B, const kvg_qkv *in, const kvg_rotary *rotary, const int32_t *positions,
+                                void *q_out, void *stream);
 
 /* Returns the sequence's pages to the free list and clears its page table,
  * fills and position tags: the serving slot is empty again, ready for the

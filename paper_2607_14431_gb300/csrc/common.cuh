@@ -192,6 +192,34 @@ struct AppendBatchParams {
     int32_t slot[kMaxBatchPerLaunch];
 };
 
+// ------------------------------------------------------------ append qkv --
+// New tokens' projections: queries rotated into q_out, keys and values into
+// the cache.  A launch takes up to kMaxBatchPerLaunch segments (consecutive
+// slots of a sequence) over up to kMaxQkvPages pages.
+constexpr int kMaxQkvPages = 4096;
+struct QkvParams {
+    const uint16_t *q, *k, *v;           // head h of a token at + h * head_dim
+    int64_t q_token, k_token, v_token;   // elements between tokens
+    int64_t q_layer, k_layer, v_layer;   // elements between run layers
+    const uint16_t *q_norm, *k_norm;     // [n_layers_run][D] or null
+    float eps, norm_offset;
+    const int32_t *pos;                  // [n_tokens]
+    uint16_t *q_out;                     // [n_layers_run][n_tokens][Hq][D]
+    uint8_t *pool;
+    int64_t pool_pages, n_tokens, tok0;  // tokens of the call, first of this launch
+    int32_t n_layers_run, layer0, n_q_heads, n_kv_heads, page_size, max_pages, max_slots, n_seg;
+    int32_t *page_table, *page_fill, *positions;
+    int32_t write_meta;                  // page table, fills and position tags too
+    int32_t rotary_dim, rotary_half;
+    float attention_factor, k_inv_scale, v_inv_scale;
+    uint64_t turn[kMaxHalfDim];          // 2^64 turns per position of each pair
+    int32_t seq[kMaxBatchPerLaunch];
+    int32_t first[kMaxBatchPerLaunch + 1];  // first token of each segment, from tok0
+    int32_t slot0[kMaxBatchPerLaunch];
+    int32_t pid0[kMaxBatchPerLaunch];    // the segment's first page in pids
+    int32_t pids[kMaxQkvPages];
+};
+
 // --------------------------------------------------------------- deposit --
 // What surrounds a serialized block's rows: its header and the alignment gaps
 // after the position tags and after the page digests, which the layout
@@ -374,6 +402,7 @@ cudaError_t launch_graft_batch_pages(const GraftBatchParams &p, const uint32_t *
                                      uint32_t call, cudaStream_t s);
 cudaError_t launch_append(const AppendParams &p, int n_sm, cudaStream_t s);
 cudaError_t launch_append_batch(const AppendBatchParams &p, int n_sm, cudaStream_t s);
+cudaError_t launch_append_qkv(int head_dim, bool fp8, const QkvParams &p, cudaStream_t s);
 cudaError_t launch_gather(const GatherParams &p, int n_sm, cudaStream_t s);
 cudaError_t launch_alias(const AliasParams &p, int n_sm, cudaStream_t s);
 // One 4-byte load per `stride` bytes of [base, base + bytes) (base 4-byte

@@ -16,6 +16,7 @@
 #include <cstring>
 #include <deque>
 #include <mutex>
+#include <new>
 #include <string>
 #include <unordered_map>
 #include <thread>
@@ -772,6 +773,9 @@ struct kvg_cache {
     std::vector<std::vector<int32_t>> seq_pages;
     std::vector<std::vector<int32_t>> seq_fill;  // host copy of page_fill for each sequence's pages
     std::vector<int32_t> n_slots;
+    // rows that kvg_cache_append_qkv's layer 0 opened at the end of each
+    // sequence, for the calls of the other layers
+    std::vector<int32_t> open_slot, open_rows;
     std::vector<int32_t> layer_window;  // per layer: 0 = global attention, W > 0 = last W tokens
     Scratch leaf, part_o, part_ml;
     // the split-K partials are shared by every decode of the cache: a decode
@@ -992,6 +996,8 @@ extern "C" kvg_status kvg_cache_create(const kvg_dims *dims, int32_t n_pages, in
     c->alias.assign(n_pages, 0);
     c->seq_pages.assign(max_seqs, {});
     c->n_slots.assign(max_seqs, 0);
+    c->open_slot.assign(max_seqs, 0);
+    c->open_rows.assign(max_seqs, 0);
     c->seq_fill.resize(max_seqs);
     c->layer_window.assign(dims->n_layers, 0);
     if (cudaDeviceSynchronize() != cudaSuccess) return cleanup(fail(KVG_ERR_CUDA, "init sync failed"));
@@ -1203,6 +1209,179 @@ extern "C" kvg_status kvg_cache_append_batch(kvg_cache *c, const int32_t *seq_id
     return KVG_OK;
 }
 
+// ------------------------------------------------- rotary positions, append --
+
+// 2^64 turns per position of each pair, so that a wrapping integer product
+// with the position is the fraction of a turn.
+struct kvg_rotary {
+    kvg_rotary_desc desc;
+    uint64_t turn[kMaxHalfDim];
+};
+
+extern "C" kvg_status kvg_rotary_create(const kvg_rotary_desc *d, kvg_rotary **out) {
+    if (!d || !out) return fail(KVG_ERR_ARG, "null argument");
+    *out = nullptr;
+    if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256)
+        return fail(KVG_ERR_ARG, "head_dim must be 64, 128 or 256");
+    if (d->rotary_dim < 0 || d->rotary_dim > d->head_dim || d->rotary_dim % 16)
+        return fail(KVG_ERR_ARG, "rotary_dim must be a multiple of 16 in [0, head_dim]");
+    if (d->style != KVG_ROPE_HALF && d->style != KVG_ROPE_INTERLEAVED) return fail(KVG_ERR_ARG, "bad style %d", d->style);
+    if (!(std::isfinite(d->theta) && d->theta >= 1.0)) return fail(KVG_ERR_ARG, "theta must be finite and >= 1");
+    if (!std::isfinite(d->attention_factor)) return fail(KVG_ERR_ARG, "attention_factor must be finite");
+    if (d->scaling != KVG_ROPE_SCALING_NONE && d->scaling != KVG_ROPE_SCALING_LINEAR &&
+        d->scaling != KVG_ROPE_SCALING_YARN)
+        return fail(KVG_ERR_ARG, "bad scaling %d", d->scaling);
+    if (d->scaling != KVG_ROPE_SCALING_NONE && !(std::isfinite(d->factor) && d->factor >= 1.0))
+        return fail(KVG_ERR_ARG, "factor must be finite and >= 1");
+    if (d->scaling == KVG_ROPE_SCALING_YARN &&
+        !(d->original_positions > 0 && std::isfinite(d->beta_fast) && std::isfinite(d->beta_slow) &&
+          d->beta_fast > d->beta_slow))
+        return fail(KVG_ERR_ARG, "blended scaling needs original_positions > 0 and beta_fast > beta_slow");
+    const double two_pi = 6.283185307179586476925286766559;
+    kvg_rotary *r = new (std::nothrow) kvg_rotary();
+    if (!r) return fail(KVG_ERR_OOM, "rotary table");
+    r->desc = *d;
+    for (int i = 0; i < d->rotary_dim / 2; ++i) {
+        double f = std::pow(d->theta, -2.0 * i / d->rotary_dim);
+        if (d->scaling == KVG_ROPE_SCALING_LINEAR) f /= d->factor;
+        if (d->scaling == KVG_ROPE_SCALING_YARN) {
+            const double turns = d->original_positions * f / two_pi;
+            const double keep = std::min(1.0, std::max(0.0, (turns - d->beta_slow) / (d->beta_fast - d->beta_slow)));
+            f = f * keep + f / d->factor * (1.0 - keep);
+        }
+        r->turn[i] = (uint64_t)(f / two_pi * 18446744073709551616.0);  // f <= 1: below 2^62
+    }
+    *out = r;
+    return KVG_OK;
+}
+
+extern "C" void kvg_rotary_destroy(kvg_rotary *r) { delete r; }
+
+extern "C" kvg_status kvg_cache_append_qkv(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                           int32_t B, const kvg_qkv *in, const kvg_rotary *rotary,
+                                           const int32_t *positions, void *q_out, void *stream) {
+    Trace trace_("kvg_cache_append_qkv");
+    if (!c || !seq_ids || !n_rows || !in || !positions) return fail(KVG_ERR_ARG, "null argument");
+    const kvg_dims &d = c->dims;
+    if (layer < -1 || layer >= d.n_layers) return fail(KVG_ERR_ARG, "bad layer %d", layer);
+    if (B <= 0 || B > 4096) return fail(KVG_ERR_ARG, "B must be in [1, 4096]");
+    if (!in->k || !in->v) return fail(KVG_ERR_ARG, "null k or v");
+    if (in->n_q_heads < 0 || (in->n_q_heads > 0) != (in->q != nullptr) || (in->n_q_heads > 0) != (q_out != nullptr))
+        return fail(KVG_ERR_ARG, "q and q_out go with n_q_heads > 0");
+    if (in->n_q_heads > 1024) return fail(KVG_ERR_ARG, "n_q_heads must be at most 1024");
+    if (rotary && rotary->desc.head_dim != d.head_dim)
+        return fail(KVG_ERR_ARG, "rotary made for head_dim %d, cache has %d", rotary->desc.head_dim, d.head_dim);
+    if (!(in->eps >= 0.f) || !std::isfinite(in->eps) || !std::isfinite(in->norm_offset))
+        return fail(KVG_ERR_ARG, "eps must be finite and >= 0, norm_offset finite");
+    const uintptr_t ptrs = reinterpret_cast<uintptr_t>(in->q) | reinterpret_cast<uintptr_t>(in->k) |
+                           reinterpret_cast<uintptr_t>(in->v) | reinterpret_cast<uintptr_t>(in->q_norm) |
+                           reinterpret_cast<uintptr_t>(in->k_norm) | reinterpret_cast<uintptr_t>(q_out);
+    if (ptrs & 15) return fail(KVG_ERR_ARG, "q, k, v, norms and q_out must be 16-byte aligned");
+    const int n_run = layer < 0 ? d.n_layers : 1;
+    int64_t strides = in->k_token | in->v_token | (in->q ? in->q_token : 0);
+    if (n_run > 1) strides |= in->k_layer | in->v_layer | (in->q ? in->q_layer : 0);
+    if (strides & 7) return fail(KVG_ERR_ARG, "strides must be multiples of 8 elements");
+    const int64_t P = d.page_size;
+    const bool opens = layer <= 0;
+    std::vector<char> seen(c->max_seqs, 0);
+    int64_t need = 0, total = 0;
+    for (int32_t b = 0; b < B; ++b) {
+        const int32_t sq = seq_ids[b];
+        const int64_t n = n_rows[b];
+        if (sq < 0 || sq >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", sq);
+        if (seen[sq]) return fail(KVG_ERR_ARG, "seq id %d repeated", sq);
+        seen[sq] = 1;
+        if (n < 0) return fail(KVG_ERR_ARG, "negative n_rows");
+        total += n;
+        if (n == 0) continue;
+        if (opens) {
+            if (c->n_slots[sq] + n > c->max_slots) return fail(KVG_ERR_CAPACITY, "append past max_slots (seq %d)", sq);
+            need += std::max<int64_t>(0, (c->n_slots[sq] + n + P - 1) / P - (int64_t)c->seq_pages[sq].size());
+        } else if (c->open_rows[sq] != n || c->open_slot[sq] + n != c->n_slots[sq]) {
+            return fail(KVG_ERR_ARG, "layer %d: seq %d's last %lld rows were not opened by a call for layer 0", layer, sq,
+                        (long long)n);
+        }
+    }
+    if (need > (int64_t)c->free_list.size()) return fail(KVG_ERR_CAPACITY, "out of free pages");
+    if (total > 0x7fffffff) return fail(KVG_ERR_ARG, "more than 2^31 - 1 rows");
+    if (total == 0) return KVG_OK;
+    DeviceGuard g(c->device);
+    QkvParams p{};
+    p.q = static_cast<const uint16_t *>(in->q);
+    p.k = static_cast<const uint16_t *>(in->k);
+    p.v = static_cast<const uint16_t *>(in->v);
+    p.q_token = in->q_token, p.k_token = in->k_token, p.v_token = in->v_token;
+    p.q_layer = in->q_layer, p.k_layer = in->k_layer, p.v_layer = in->v_layer;
+    p.q_norm = in->q ? static_cast<const uint16_t *>(in->q_norm) : nullptr;
+    p.k_norm = static_cast<const uint16_t *>(in->k_norm);
+    p.eps = in->eps;
+    p.norm_offset = in->norm_offset;
+    p.pos = positions;
+    p.q_out = static_cast<uint16_t *>(q_out);
+    p.pool = c->pool;
+    p.pool_pages = c->n_pages;
+    p.n_tokens = total;
+    p.n_layers_run = n_run;
+    p.layer0 = std::max(layer, 0);
+    p.n_q_heads = in->n_q_heads;
+    p.n_kv_heads = d.n_kv_heads;
+    p.page_size = d.page_size;
+    p.max_pages = c->max_pages;
+    p.max_slots = c->max_slots;
+    p.page_table = c->page_table;
+    p.page_fill = c->page_fill;
+    p.positions = c->positions;
+    p.write_meta = opens;
+    p.attention_factor = 1.f;
+    if (rotary) {
+        p.rotary_dim = rotary->desc.rotary_dim;
+        p.rotary_half = rotary->desc.style == KVG_ROPE_HALF;
+        p.attention_factor = rotary->desc.attention_factor;
+        memcpy(p.turn, rotary->turn, sizeof p.turn);
+    }
+    if (d.kv_dtype == KVG_KV_E4M3) {
+        p.k_inv_scale = 1.0f / d.k_scale;
+        p.v_inv_scale = 1.0f / d.v_scale;
+    }
+    int32_t n_pids = 0;
+    auto launch = [&]() {
+        if (p.n_seg == 0) return cudaSuccess;
+        const cudaError_t e = launch_append_qkv(d.head_dim, d.kv_dtype == KVG_KV_E4M3, p, static_cast<cudaStream_t>(stream));
+        p.tok0 += p.first[p.n_seg];
+        p.n_seg = n_pids = 0;
+        return e;
+    };
+    for (int32_t b = 0; b < B; ++b) {
+        const int32_t sq = seq_ids[b];
+        const int64_t n = n_rows[b], s0 = opens ? c->n_slots[sq] : c->open_slot[sq];
+        if (n == 0) continue;
+        auto &sp = c->seq_pages[sq];
+        if (opens) {
+            const auto got = take_pages(c, std::max<int64_t>(0, (s0 + n + P - 1) / P - (int64_t)sp.size()));
+            sp.insert(sp.end(), got.begin(), got.end());
+            c->n_slots[sq] = (int32_t)(s0 + n);
+            c->open_slot[sq] = (int32_t)s0;
+            c->open_rows[sq] = (int32_t)n;
+            note_fills(c, sq, s0, s0 + n);
+        }
+        for (int64_t s = s0; s < s0 + n;) {  // segments of up to the launch's free pages
+            if (p.n_seg == kMaxBatchPerLaunch || n_pids == kMaxQkvPages) KVG_CUDA(launch());
+            const int64_t pg = s / P;
+            const int64_t end = std::min<int64_t>(s0 + n, (pg + kMaxQkvPages - n_pids) * P);
+            const int32_t i = p.n_seg++;
+            if (i == 0) p.first[0] = 0;
+            p.seq[i] = sq;
+            p.slot0[i] = (int32_t)s;
+            p.pid0[i] = n_pids;
+            p.first[i + 1] = p.first[i] + (int32_t)(end - s);
+            for (int64_t j = pg; j * P < end; ++j) p.pids[n_pids++] = sp[j];
+            s = end;
+        }
+    }
+    KVG_CUDA(launch());
+    return KVG_OK;
+}
+
 extern "C" kvg_status kvg_cache_release(kvg_cache *c, int32_t seq, void *stream) {
     Trace trace_("kvg_cache_release");
     if (!c) return fail(KVG_ERR_ARG, "null cache");
@@ -1217,6 +1396,7 @@ extern "C" kvg_status kvg_cache_release(kvg_cache *c, int32_t seq, void *stream)
     c->seq_pages[seq].clear();
     c->seq_fill[seq].clear();
     c->n_slots[seq] = 0;
+    c->open_rows[seq] = 0;
     KVG_CUDA(launch_reset_seq(c->page_table + (int64_t)seq * c->max_pages,
                               c->page_fill + (int64_t)seq * c->max_pages, c->max_pages,
                               c->positions + (int64_t)seq * c->max_slots, c->max_slots,

@@ -22,6 +22,7 @@ KVG_ERR_CAPACITY, KVG_ERR_POSITION, KVG_ERR_DIGEST, KVG_ERR_FORMAT = -5, -6, -7,
 KVG_ERR_TIMEOUT, KVG_ERR_DEVICE_CHECK = -9, -10
 KVG_RESIDENCY_HBM, KVG_RESIDENCY_PINNED_HOST, KVG_RESIDENCY_CACHE_POOL = 0, 1, 2
 KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED = 0, 1
+KVG_ROPE_SCALING_NONE, KVG_ROPE_SCALING_LINEAR, KVG_ROPE_SCALING_YARN = 0, 1, 2
 KVG_GRAFT_VERIFY, KVG_GRAFT_SYNC = 1, 2
 KVG_SHA256_PLAIN, KVG_SHA256_PAGED = 0, 1
 KVG_DECODE_MERGE = 1
@@ -64,6 +65,21 @@ class kvg_graft_report(ctypes.Structure):
                 ("mismatch_pages", ctypes.c_int32 * KVG_REPORT_MAX_PAGES)]
 
 
+class kvg_rotary_desc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("style", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("original_positions", ctypes.c_int32), ("attention_factor", ctypes.c_float)]
+
+
+class kvg_qkv(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_token", ctypes.c_int64), ("k_token", ctypes.c_int64), ("v_token", ctypes.c_int64),
+                ("q_layer", ctypes.c_int64), ("k_layer", ctypes.c_int64), ("v_layer", ctypes.c_int64),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("norm_offset", ctypes.c_float), ("n_q_heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 _vp, _i32, _i64, _u32, _u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
 _P = ctypes.POINTER
 
@@ -86,6 +102,9 @@ _SIGNATURES = {
     "kvg_cache_seq_info": ([_vp, _i32, _P(_i32), _P(_i32)], _i32),
     "kvg_cache_append": ([_vp, _i32, _vp, _vp, _vp, _i32, _vp], _i32),
     "kvg_cache_append_batch": ([_vp, _vp, _i32, _vp, _vp, _vp, _vp], _i32),
+    "kvg_rotary_create": ([_P(kvg_rotary_desc), _P(_vp)], _i32),
+    "kvg_rotary_destroy": ([_vp], None),
+    "kvg_cache_append_qkv": ([_vp, _i32, _vp, _vp, _i32, _P(kvg_qkv), _vp, _vp, _vp, _vp], _i32),
     "kvg_cache_release": ([_vp, _i32, _vp], _i32),
     "kvg_deposit": ([_vp, _vp, _i32, _i32, _i32, _vp, _P(_u64)], _i32),
     "kvg_graft": ([_vp, _u64, _vp, _i32, _i32, _i64, _u32, _vp, _P(kvg_graft_report)], _i32),
@@ -244,6 +263,51 @@ def kvg_cache_append_batch(cache, seq_ids, k_ptr: int, v_ptr: int, pos_ptr: int,
     _check(lib().kvg_cache_append_batch(cache, ids, len(seq_ids), k_ptr, v_ptr, pos_ptr, _stream(stream)))
 
 
+def kvg_rotary_create(desc: kvg_rotary_desc):
+    h = _vp()
+    _check(lib().kvg_rotary_create(ctypes.byref(desc), ctypes.byref(h)))
+    return h
+
+
+def kvg_rotary_destroy(rotary):
+    lib().kvg_rotary_destroy(rotary)
+
+
+def make_qkv(q, k, v, q_norm=None, k_norm=None, eps: float = 1e-6, norm_offset: float = 0.0) -> kvg_qkv:
+    """kvg_qkv of tensors [tokens][heads][head_dim] or [layers][tokens][heads][head_dim] (q None: keys and
+    values only), which may be slices of one buffer as long as a token's heads are adjacent.  The tensors must
+    stay alive as long as the struct is used."""
+    def strides(x):
+        if x is None:
+            return 0, 0
+        if x.element_size() != 2 or x.dim() not in (3, 4):
+            raise ValueError("q, k and v are bf16 [tokens][heads][head_dim] or [layers][tokens][heads][head_dim]")
+        if (x.shape[-1] > 1 and x.stride(-1) != 1) or (x.shape[-2] > 1 and x.stride(-2) != x.shape[-1]):
+            raise ValueError("a token's heads must be adjacent")
+        return x.stride(-3), x.stride(0) if x.dim() == 4 else 0
+
+    def ptr(x):
+        return None if x is None else x.data_ptr()
+
+    for w in (q_norm, k_norm):
+        if w is not None and not (w.is_contiguous() and w.element_size() == 2):
+            raise ValueError("norm weights are contiguous bf16")
+    (qt, ql), (kt, kl), (vt, vl) = strides(q), strides(k), strides(v)
+    return kvg_qkv(ptr(q), ptr(k), ptr(v), qt, kt, vt, ql, kl, vl, ptr(q_norm), ptr(k_norm), float(eps),
+                   float(norm_offset), 0 if q is None else q.shape[-2], 0)
+
+
+def kvg_cache_append_qkv(cache, layer: int, seq_ids, n_rows, qkv: kvg_qkv, rotary, pos_ptr: int, q_out_ptr,
+                         stream=None):
+    """rotary: a handle (Rotary.h) or None; q_out_ptr: None when qkv has no queries."""
+    if len(n_rows) != len(seq_ids):
+        raise ValueError("seq_ids and n_rows differ in length")
+    ids = (ctypes.c_int32 * len(seq_ids))(*seq_ids)
+    rows = (ctypes.c_int32 * len(seq_ids))(*n_rows)
+    _check(lib().kvg_cache_append_qkv(cache, layer, ids, rows, len(seq_ids), ctypes.byref(qkv), rotary, pos_ptr,
+                                      q_out_ptr, _stream(stream)))
+
+
 def kvg_cache_release(cache, seq: int, stream=None):
     _check(lib().kvg_cache_release(cache, seq, _stream(stream)))
 
@@ -379,7 +443,31 @@ class PoolStore(Store):
 
     def __init__(self, cache: "Cache", capacity_bytes: int):
         self.dims = cache.dims
+        self.cache = cache  # destroyed after the store
         self.h = kvg_store_create_in_cache(cache.h, capacity_bytes)
+
+
+class Rotary:
+    """Rotary positions of heads of head_dim (see kvg_rotary_desc in kvg.h)."""
+
+    def __init__(self, head_dim: int, rotary_dim: int, theta: float = 10000.0, style: int = KVG_ROPE_HALF,
+                 scaling: int = KVG_ROPE_SCALING_NONE, factor: float = 1.0, original_positions: int = 0,
+                 beta_fast: float = 32.0, beta_slow: float = 1.0, attention_factor: float = 1.0):
+        self.h = None
+        self.h = kvg_rotary_create(kvg_rotary_desc(head_dim, rotary_dim, style, scaling, float(theta), float(factor),
+                                                   float(beta_fast), float(beta_slow), original_positions,
+                                                   float(attention_factor)))
+
+    def close(self):
+        if self.h:
+            kvg_rotary_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Cache:
