@@ -591,6 +591,24 @@ kvg_status kvg_decode_attention_noalloc(kvg_cache *cache, int32_t layer, const i
                                         int32_t B, const void *q, int32_t n_q_heads, void *out,
                                         float scale, void *stream);
 
+/* Prompt attention (Sec. 3.2: new queries computed on top of a restored block
+ * at [N, N + q)): the last n_rows[b] slots of sequence seq_ids[b] (host
+ * arrays, n_rows[b] >= 0, B <= 4096, T = sum n_rows packed rows) are its
+ * query rows, their keys and values already in the cache
+ * (kvg_cache_append_qkv or kvg_cache_append).  The row at slot s attends to
+ * every valid row in slots up to s, its own included — on a windowed layer to
+ * the last W of them — as kvg_decode_attention does for a sequence that ends
+ * there: o = sum softmax(scale * q . k) v per query head, its KV head being
+ * h / (n_q_heads / n_kv_heads), accumulated in fp32 and rounded to bf16.
+ * q, out: device bf16 [n_layers_run][T][n_q_heads][head_dim], 16-byte
+ * aligned; layer as for kvg_decode_attention.  A value row that a query does
+ * not attend to does not reach its output, whatever bits it holds.  Where
+ * every n_rows[b] is 1 this is kvg_decode_attention.
+ * Errors: KVG_ERR_ARG as for kvg_decode_attention, for more query rows than
+ * slots, and where a graft left unfilled slots among a sequence's query rows. */
+kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                int32_t B, const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
+
 /* ------------------------------------------------------------- digest -- */
 
 /* SHA-256 (FIPS 180-4) on the GPU.

@@ -347,6 +347,28 @@ inline int64_t decode_slots(const std::vector<DecodeParams> &plan, int64_t w_max
     return most;
 }
 
+// ---------------------------------------------------- prompt attention --
+// Query rows of up to kMaxBatchPerLaunch sequences over layers of one window.
+struct PromptParams {
+    const uint8_t *pool;
+    int64_t pool_pages;
+    int32_t n_kv_heads, page_size, n_q_heads, n_layers_run;
+    const int32_t *page_table, *page_fill;
+    int32_t max_pages, n_seq, window;
+    float qscale, vscale;      // softmax scale * log2(e) (* k_scale), 1 or v_scale
+    const __nv_bfloat16 *q;    // [layers][q_rows][Hq][D]
+    __nv_bfloat16 *out;
+    int64_t q_rows;            // packed rows of the whole call
+    DevStatus *status;
+    int16_t layers[kMaxLayersPerLaunch];   // run layer -> cache layer
+    int16_t qlayers[kMaxLayersPerLaunch];  // run layer -> layer of q and out
+    int32_t seq[kMaxBatchPerLaunch];
+    int32_t first[kMaxBatchPerLaunch + 1]; // prefix sums of the query rows
+    int32_t row0[kMaxBatchPerLaunch];      // first packed row
+    int32_t slot0[kMaxBatchPerLaunch];     // its slot
+    uint8_t holes[kMaxBatchPerLaunch];     // a page before the last is not full
+};
+
 // -------------------------------------------------------------- launchers --
 // Every launcher counts the kernels it launches (kvg_launch_count()).
 void count_launches(uint64_t n);
@@ -450,6 +472,7 @@ bool sha256_parts_ok();
 // number of co-resident warps the decode kernel can keep on the device.
 // Split-decode state -> bf16 output: out[r][d] = o / l (0 where l = 0), for
 // n_rows rows of D + 4 floats.
+cudaError_t launch_prompt(int head_dim, bool fp8, const PromptParams &p, cudaStream_t s);
 cudaError_t launch_state_finish(const float *state, int64_t n_rows, int head_dim, __nv_bfloat16 *out,
                                 cudaStream_t s);
 cudaError_t launch_decode(int head_dim, int group, bool fp8, const DecodeParams &p, const CUtensorMap &pool_map,

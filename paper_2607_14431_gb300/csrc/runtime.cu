@@ -2241,6 +2241,25 @@ struct WindowGroup {
     std::vector<std::pair<int32_t, int32_t>> layers;
 };
 
+// The layers run (all for layer -1) grouped by window, in order of first
+// appearance, in parts of at most kMaxLayersPerLaunch.
+static std::vector<WindowGroup> layer_parts(const kvg_cache *c, int32_t layer) {
+    const kvg_dims &d = c->dims;
+    std::vector<WindowGroup> parts;
+    for (int32_t l = layer < 0 ? 0 : layer; l < (layer < 0 ? d.n_layers : layer + 1); ++l) {
+        const int32_t w = c->layer_window[l];
+        auto it = std::find_if(parts.begin(), parts.end(), [w](const WindowGroup &g) {
+            return g.window == w && g.layers.size() < kMaxLayersPerLaunch;
+        });
+        if (it == parts.end()) {
+            parts.push_back({w, {}});
+            it = parts.end() - 1;
+        }
+        it->layers.push_back({l, layer < 0 ? l : 0});
+    }
+    return parts;
+}
+
 // The launches of one decode call: the layers run are grouped by their
 // window (one group when no layer is windowed), each group split into parts
 // of at most kMaxLayersPerLaunch layers, and each launch takes one part, or
@@ -2266,18 +2285,7 @@ static kvg_status plan_decode(const kvg_cache *c, int32_t layer, const int32_t *
     const kvg_dims &d = c->dims;
     const int TOK = decode_tile_tokens(d.head_dim, d.kv_dtype == KVG_KV_E4M3, d.page_size);
     const int tpp = (d.page_size + TOK - 1) / TOK;
-    std::vector<WindowGroup> parts;  // in order of first appearance
-    for (int32_t l = layer < 0 ? 0 : layer; l < (layer < 0 ? d.n_layers : layer + 1); ++l) {
-        const int32_t w = c->layer_window[l];
-        auto it = std::find_if(parts.begin(), parts.end(), [w](const WindowGroup &g) {
-            return g.window == w && g.layers.size() < kMaxLayersPerLaunch;
-        });
-        if (it == parts.end()) {
-            parts.push_back({w, {}});
-            it = parts.end() - 1;
-        }
-        it->layers.push_back({l, layer < 0 ? l : 0});
-    }
+    const std::vector<WindowGroup> parts = layer_parts(c, layer);
     plan->clear();
     const int32_t nb_max = std::min<int32_t>(B, kMaxBatchPerLaunch);
     const int64_t slots = (int64_t)((kStaticScratchBytes - 256) / partial_slot_bytes(G, d.head_dim));
@@ -2448,6 +2456,88 @@ extern "C" kvg_status kvg_decode_state_finish(const float *state, int64_t n_rows
         return fail(KVG_ERR_ARG, "state/out must be 16-byte aligned");
     KVG_CUDA(launch_state_finish(state, n_rows, head_dim, static_cast<__nv_bfloat16 *>(out),
                                  static_cast<cudaStream_t>(stream)));
+    return KVG_OK;
+}
+
+// -------------------------------------------------------- prompt attention --
+
+extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                           int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
+                                           void *stream) {
+    Trace trace_("kvg_prompt_attention");
+    if (!c || !seq_ids || !n_rows || !q || !out) return fail(KVG_ERR_ARG, "kvg_prompt_attention: null argument");
+    const kvg_dims &d = c->dims;
+    if (layer < -1 || layer >= d.n_layers) return fail(KVG_ERR_ARG, "bad layer %d", layer);
+    if (B <= 0 || B > 4096) return fail(KVG_ERR_ARG, "B must be in [1, 4096]");
+    if (n_q_heads <= 0 || n_q_heads % d.n_kv_heads) return fail(KVG_ERR_ARG, "n_q_heads must be a multiple of n_kv_heads");
+    const int G = n_q_heads / d.n_kv_heads;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    if (!decode_supported(d.head_dim, G, fp8))
+        return fail(KVG_ERR_ARG, "unsupported head_dim %d / group %d%s", d.head_dim, G, fp8 ? " (fp8)" : "");
+    if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)
+        return fail(KVG_ERR_ARG, "q/out must be 16-byte aligned");
+    const int64_t P = d.page_size;
+    int64_t total = 0;
+    bool single = true;
+    for (int32_t b = 0; b < B; ++b) {
+        const int32_t sq = seq_ids[b];
+        if (sq < 0 || sq >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", sq);
+        if (n_rows[b] < 0 || n_rows[b] > c->n_slots[sq])
+            return fail(KVG_ERR_ARG, "seq %d: %d query rows of %d slots", sq, n_rows[b], c->n_slots[sq]);
+        // the rows' slots must all be valid: no graft's unfilled page tail among them
+        const auto &f = c->seq_fill[sq];
+        for (int64_t pg = (c->n_slots[sq] - n_rows[b]) / P; n_rows[b] && pg + 1 < (int64_t)f.size(); ++pg)
+            if (f[pg] < P) return fail(KVG_ERR_ARG, "seq %d: unfilled slots among its last %d", sq, n_rows[b]);
+        total += n_rows[b];
+        single = single && n_rows[b] == 1;
+    }
+    if (total > 0x7fffffff / n_q_heads) return fail(KVG_ERR_ARG, "more than 2^31 - 1 query rows x heads");
+    if (total == 0) return KVG_OK;
+    // prompts of one token are a decode step
+    if (single)
+        return decode_impl("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0, INT32_MAX,
+                           nullptr, 0);
+    DeviceGuard g(c->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    PromptParams p{};
+    p.pool = c->pool;
+    p.pool_pages = c->n_pages;
+    p.n_kv_heads = d.n_kv_heads;
+    p.page_size = d.page_size;
+    p.n_q_heads = n_q_heads;
+    p.page_table = c->page_table;
+    p.page_fill = c->page_fill;
+    p.max_pages = c->max_pages;
+    p.qscale = scale * 1.4426950408889634f * (fp8 ? d.k_scale : 1.f);
+    p.vscale = fp8 ? d.v_scale : 1.f;
+    p.q = static_cast<const __nv_bfloat16 *>(q);
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.q_rows = total;
+    p.status = c->status;
+    for (const WindowGroup &part : layer_parts(c, layer)) {
+        p.window = part.window;
+        p.n_layers_run = (int32_t)part.layers.size();
+        for (int32_t i = 0; i < p.n_layers_run; ++i) {
+            p.layers[i] = (int16_t)part.layers[i].first;
+            p.qlayers[i] = (int16_t)part.layers[i].second;
+        }
+        int32_t row = 0;
+        for (int32_t b = 0; b < B;) {
+            p.n_seq = 0;
+            for (; b < B && p.n_seq < kMaxBatchPerLaunch; ++b) {
+                if (n_rows[b] == 0) continue;
+                const int32_t i = p.n_seq++, sq = seq_ids[b];
+                const auto &f = c->seq_fill[sq];
+                p.seq[i] = sq;
+                p.row0[i] = row;
+                p.slot0[i] = c->n_slots[sq] - n_rows[b];
+                p.holes[i] = std::any_of(f.begin(), f.end() - 1, [P](int32_t x) { return x < P; });
+                p.first[i + 1] = p.first[i] + n_rows[b];
+                row += n_rows[b];
+            }
+            if (p.n_seq) KVG_CUDA(launch_prompt(d.head_dim, fp8, p, st));
+        }
+    }
     return KVG_OK;
 }
 

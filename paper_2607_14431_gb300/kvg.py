@@ -116,6 +116,7 @@ _SIGNATURES = {
     "kvg_decode_attention_range": ([_vp, _i32, _vp, _i32, _vp, _i32, ctypes.c_float, _i32, _i32, _u32, _vp, _vp],
                                    _i32),
     "kvg_decode_state_finish": ([_vp, _i64, _i32, _vp, _vp], _i32),
+    "kvg_prompt_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_digest": ([_vp, _u64, _i32, _u64, _vp, _vp], _i32),
     "kvg_sync": ([_vp, _vp, ctypes.c_double, _P(kvg_graft_report)], _i32),
     "kvg_selftest_bounded_wait": ([_vp, _u64, _vp], _i32),
@@ -388,6 +389,17 @@ def kvg_decode_attention_range(cache, layer: int, seq_ids, q_ptr: int, n_q_heads
 def kvg_decode_state_finish(state_ptr: int, n_rows: int, head_dim: int, out_ptr: int, stream=None):
     """bf16 output o / l of a split decode's state rows."""
     _check(lib().kvg_decode_state_finish(state_ptr, int(n_rows), int(head_dim), out_ptr, _stream(stream)))
+
+
+def kvg_prompt_attention(cache, layer: int, seq_ids, n_rows, q_ptr: int, n_q_heads: int, out_ptr: int, scale: float,
+                         stream=None):
+    """Causal attention of each sequence's last n_rows[b] slots, packed; q and out [Lrun][sum n_rows][Hq][D] bf16."""
+    if len(n_rows) != len(seq_ids):
+        raise ValueError("seq_ids and n_rows differ in length")
+    ids = (ctypes.c_int32 * len(seq_ids))(*seq_ids)
+    rows = (ctypes.c_int32 * len(seq_ids))(*n_rows)
+    _check(lib().kvg_prompt_attention(cache, layer, ids, rows, len(seq_ids), q_ptr, n_q_heads, out_ptr, float(scale),
+                                      _stream(stream)))
 
 
 def kvg_digest(ptr: int, n: int, mode: int, page_bytes: int, out_ptr: int, stream=None):
