@@ -864,19 +864,18 @@ cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuui
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, bool fp8, int page_size, uint64_t rows) {
+cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, bool fp8, int box_rows, uint64_t rows) {
     const EncodeTiled encode = tensor_map_encoder();
     if (!encode) return cudaErrorSymbolNotFound;
     if (fp8 && head_dim % 128) {  // no fp8 decode for this head_dim: nothing to map
         memset(out, 0, sizeof *out);
         return cudaSuccess;
     }
-    const int tok = decode_tile_tokens(head_dim, fp8, page_size);  // the box height the kernel for this element type expects
-    if (tok == 0 || rows == 0 || rows > 0x7fffffffull) return cudaErrorInvalidValue;
+    if (box_rows <= 0 || rows == 0 || rows > 0x7fffffffull) return cudaErrorInvalidValue;
     // 128-byte rows per box: 64 bf16 columns, or 128 fp8 columns
     const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)head_dim * (fp8 ? 1 : 2)};
-    const cuuint32_t box[2] = {fp8 ? 128u : 64u, (cuuint32_t)tok};
+    const cuuint32_t box[2] = {fp8 ? 128u : 64u, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
     const CUresult r = encode(out, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, pool,
                               dims, strides, box, estr,

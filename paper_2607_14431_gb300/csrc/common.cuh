@@ -349,13 +349,19 @@ inline int64_t decode_slots(const std::vector<DecodeParams> &plan, int64_t w_max
 
 // ---------------------------------------------------- prompt attention --
 // Query rows of up to kMaxBatchPerLaunch sequences over layers of one window.
+// shared: "sequences" are groups of batch rows whose sequences have the same
+// first pages; a group's rows are its members, seq is one of them.
 struct PromptParams {
     const uint8_t *pool;
     int64_t pool_pages;
     int32_t n_kv_heads, page_size, n_q_heads, n_layers_run;
     const int32_t *page_table, *page_fill;
-    int32_t max_pages, n_seq, window;
-    float qscale, vscale;      // softmax scale * log2(e) (* k_scale), 1 or v_scale
+    int32_t max_pages, n_seq, window, shared;
+    int32_t n_units;           // run layers x KV heads
+    int32_t pages_per_tile;    // key tiles: whole pages that one holds (0: a page takes several)
+    int32_t tiles_per_page, page_rows, box_rows;  // rows of a page in a tile, of a copy
+    float qscale, vscale;      // |softmax scale| * log2(e) (* k_scale), 1 or v_scale
+    int32_t negate;            // the scale is negative
     const __nv_bfloat16 *q;    // [layers][q_rows][Hq][D]
     __nv_bfloat16 *out;
     int64_t q_rows;            // packed rows of the whole call
@@ -365,8 +371,16 @@ struct PromptParams {
     int32_t seq[kMaxBatchPerLaunch];
     int32_t first[kMaxBatchPerLaunch + 1]; // prefix sums of the query rows
     int32_t row0[kMaxBatchPerLaunch];      // first packed row
-    int32_t slot0[kMaxBatchPerLaunch];     // its slot
+    int32_t slot0[kMaxBatchPerLaunch];     // its slot (shared: the last slot of the common pages)
+    int32_t begin[kMaxBatchPerLaunch];     // no row attends to an earlier slot (with holes, or shared)
     uint8_t holes[kMaxBatchPerLaunch];     // a page before the last is not full
+    int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
+    int32_t splits[kMaxBatchPerLaunch];    // key ranges that a query tile's items divide
+    int64_t part0[kMaxBatchPerLaunch];     // first partial result
+    float *part_o;                         // [slots][D]
+    float2 *part_ml;                       // [slots] (m, l)
+    int32_t member[kMaxBatchPerLaunch];    // shared: batch row of each member
+    int32_t lo[kMaxBatchPerLaunch];        // shared: first slot that it attends to
 };
 
 // -------------------------------------------------------------- launchers --
@@ -472,15 +486,24 @@ bool sha256_parts_ok();
 // number of co-resident warps the decode kernel can keep on the device.
 // Split-decode state -> bf16 output: out[r][d] = o / l (0 where l = 0), for
 // n_rows rows of D + 4 floats.
-cudaError_t launch_prompt(int head_dim, bool fp8, const PromptParams &p, cudaStream_t s);
+// Many query rows over the same pages, on the tensor cores: p.item0[n_seq]
+// work items (query tile x KV head x layer x key range), streams query tiles of
+// 128 rows each; then the join of the rows whose keys were split.  `map`: the
+// pool as boxes of 128 bytes x p.box_rows rows (make_pool_tensor_map).
+int prompt_streams(int head_dim, int64_t most_rows);
+void prompt_tiling(int page_size, PromptParams *p);
+cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
+                          cudaStream_t s);
+cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t s);
 cudaError_t launch_state_finish(const float *state, int64_t n_rows, int head_dim, __nv_bfloat16 *out,
                                 cudaStream_t s);
 cudaError_t launch_decode(int head_dim, int group, bool fp8, const DecodeParams &p, const CUtensorMap &pool_map,
                           cudaStream_t s);
-// Tensor map of a cache pool for the decode kernel: a 2-D bf16 tensor of
-// head_dim columns and n_layers*2*n_pages*n_kv_heads*page_size rows, boxes of
-// 64 columns x decode_tile_tokens(head_dim, fp8, page_size) rows, 128-byte swizzle.
-cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, bool fp8, int page_size, uint64_t rows);
+// Tensor map of a cache pool: a 2-D bf16 (or fp8) tensor of head_dim columns
+// and n_layers*2*n_pages*n_kv_heads*page_size rows, boxes of 128 bytes x
+// box_rows rows, 128-byte swizzle.  The decode kernel's boxes have
+// decode_tile_tokens(head_dim, fp8, page_size) rows.
+cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, bool fp8, int box_rows, uint64_t rows);
 // A rank-`rank` bf16 tensor map (no swizzle, zero fill out of bounds): dims
 // innermost first, byte strides of dims 1.., box extents per dim.
 cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuuint64_t *dims,

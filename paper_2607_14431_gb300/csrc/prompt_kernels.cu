@@ -1,21 +1,192 @@
-// prompt_kernels.cu — causal attention of packed prompt rows over a paged
-// cache (Sec. 3.2: new queries are computed on top of a restored block).
+// prompt_kernels.cu — attention of many query rows over the same pages of a
+// paged cache, on the 5th-generation tensor cores.
 //
-// Query row i of a sequence, at slot s_i, attends to its valid rows (below
-// their page's fill) in slots [lo_i, s_i]:
+// Two calls use it: a prompt's rows over its sequence (Sec. 3.2: new queries
+// are computed on top of a restored block), and the rows of a batch over the
+// pages of a block that its sequences share.  Query row i attends to the valid
+// rows (below their page's fill) in slots [lo_i, hi_i]:
 //   o_i = sum_j softmax_j(scale q_i . k_j) v_j
-// with lo_i = 0, or the slot of the last `window` valid rows up to s_i.
+// For a prompt hi_i is the row's own slot and lo_i 0 or the slot of the last
+// `window` valid rows up to it; for a shared block hi_i is its last slot.
 //
-// A warp takes a query head's row and walks its slots, a lane D / 32 of the
-// dimensions: right for every case, and bound by the reduction per key.
+// A work item is a KV head, a tile of query rows (tokens x the group's heads,
+// so that a KV head's queries share its keys) and a range of key tiles; a CTA
+// takes one.  Key tiles are 128 columns: the page's rows, or as many whole
+// pages as fit when pages are smaller, each at a multiple of 8 rows so that
+// its copy starts on a swizzle atom.
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+
 #include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace kvg {
 
 namespace {
 
-constexpr int kRowThreads = 128;
+constexpr int kTile = 128;       // query rows of a stream, columns of a key tile
+constexpr int kMaskSlots = 16;   // key tiles whose column masks are kept
+constexpr int kConvertWarps = 2;
+// The running maximum that the weights refer to is moved only when a row's
+// maximum passes it by more than this (in powers of two): weights then reach
+// at most 2^8, which costs no precision in bf16 or fp16, and the accumulator
+// is rarely rescaled.
+constexpr float kMaxSlack = 8.f;
 
+// STREAMS tiles of query rows share each key tile: with two, one's products
+// run while the other's weights are formed.  head_dim 256 has tensor memory
+// for one (256 columns of output); it keeps two score buffers instead, so that
+// the next tile's scores are formed ahead.
+template <int D_, bool FP8_, int STREAMS_>
+struct Cfg {
+    static constexpr int D = D_, STREAMS = STREAMS_;
+    static constexpr bool FP8 = FP8_;
+    static constexpr int DC = D < 128 ? D : 128;     // dimensions of a chunk
+    static constexpr int NCH = D / DC;               // chunks of a key (or value) tile
+    static constexpr int BOXES = DC / 64;            // 128-byte wide boxes of a 16-bit chunk
+    static constexpr int BOX = kTile * 128;
+    static constexpr int CHUNK = BOXES * BOX;
+    static constexpr int RAW = FP8 ? kTile * DC : 0; // an fp8 chunk as it is in the cache
+    static constexpr int Q_BYTES = STREAMS * kTile * D * 2;
+    static constexpr int STAGES = D == 64 ? 8 : FP8 ? (Q_BYTES > 32768 ? 3 : 4) : Q_BYTES > 32768 ? 5 : 6;
+    static constexpr int RAW_STAGES = FP8 ? 4 : 0;
+    static constexpr int SOFTMAX_WARPS = 4 * STREAMS;
+    static constexpr int LOAD_WARP = SOFTMAX_WARPS, MMA_WARP = LOAD_WARP + 1, CONVERT_WARP = MMA_WARP + 1;
+    static constexpr int THREADS = 32 * (CONVERT_WARP + (FP8 ? kConvertWarps : 0));
+    static constexpr int SMEM = Q_BYTES + STAGES * CHUNK + RAW_STAGES * RAW + 1024;  // + alignment slack
+    static_assert(D <= 128 || STREAMS == 1, "tensor memory");
+    static_assert(SMEM <= 230 * 1024, "shared memory");
+};
+constexpr int kScoreCols = 0, kOutCols = 256;  // tensor memory: scores (and weights), outputs
+
+struct Bars {
+    uint64_t full[8], empty[8], raw_full[4], raw_empty[4];
+    uint64_t scores[2], weights[2], out[2];  // a score tile is there; its weights are; their product is added
+    uint64_t queries, drained;
+    uint32_t mask[kMaskSlots][4];            // valid columns of key tile j % kMaskSlots
+    uint32_t tmem;
+    int abort;
+};
+
+// Bounded wait that also ends when another warp gave up.
+__device__ __noinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, DevStatus *status) {
+    const uint64_t t0 = global_timer_ns();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 63) == 0) {
+            if (*abort) return false;
+            if (global_timer_ns() - t0 > 2000000000ull) {
+                *abort = 1;
+                record_error(status, KVG_ERR_DEVICE_CHECK, 20);
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ bool wait_bar(Bars &s, uint64_t *bar, uint32_t parity, DevStatus *status) {
+    const bool ok = mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, status);
+    return __all_sync(0xffffffffu, ok);
+}
+
+// ------------------------------------------------------------ a work item --
+struct Item {
+    int b, split, lr, g;
+    int gs;         // log2 of the group
+    int row0, rows; // of the sequence's rows (token x head of the group), those of the item
+    int k0, k1;     // key tiles
+    int last_slot;  // of the sequence's pages that the item reads
+};
+
+// Key tile and column of a slot.
+__device__ __forceinline__ void tile_of(const PromptParams &p, int slot, int &tile, int &col) {
+    const int pg = slot / p.page_size, r = slot - pg * p.page_size;
+    if (p.pages_per_tile) {
+        tile = pg / p.pages_per_tile;
+        col = (pg - tile * p.pages_per_tile) * p.page_rows + r;
+    } else {
+        tile = pg * p.tiles_per_page + r / kTile;
+        col = r % kTile;
+    }
+}
+__device__ __forceinline__ int first_slot(const PromptParams &p, int tile) {
+    return p.pages_per_tile ? tile * p.pages_per_tile * p.page_size
+                            : tile / p.tiles_per_page * p.page_size + tile % p.tiles_per_page * kTile;
+}
+
+// First slot that the row at `slot` attends to.
+__device__ int window_first(const PromptParams &p, int b, int slot) {
+    if (p.window <= 0) return 0;
+    if (!p.holes[b]) return max(0, slot - p.window + 1);
+    // pages that are not full lie in between: count valid rows back
+    const int32_t *fill = p.page_fill + (int64_t)p.seq[b] * p.max_pages;
+    int pg = slot / p.page_size, n = slot % p.page_size + 1, left = p.window;
+    while (n < left && pg > 0) {
+        left -= n;
+        n = fill[--pg];
+    }
+    return pg * p.page_size + max(0, n - left);
+}
+__device__ __forceinline__ int row_first(const PromptParams &p, const Item &it, int tok) {
+    return p.shared ? p.lo[p.row0[it.b] + tok] : window_first(p, it.b, p.slot0[it.b] + tok);
+}
+__device__ __forceinline__ int row_last(const PromptParams &p, const Item &it, int tok) {
+    return p.slot0[it.b] + (p.shared ? 0 : tok);
+}
+// Row of q and out.
+__device__ __forceinline__ int64_t q_row(const PromptParams &p, const Item &it, int row) {
+    const int at = p.row0[it.b] + (row >> it.gs);
+    return ((int64_t)p.qlayers[it.lr] * p.q_rows + (p.shared ? p.member[at] : at)) * p.n_q_heads + (it.g << it.gs) +
+           (row & ((1 << it.gs) - 1));
+}
+// Slot of a row's partial result.
+__device__ __forceinline__ int64_t part_slot(const PromptParams &p, int b, int gs, int split, int unit, int row) {
+    const int64_t n = (int64_t)(p.first[b + 1] - p.first[b]) << gs;
+    return p.part0[b] + ((int64_t)split * p.n_units + unit) * n + row;
+}
+
+__device__ __forceinline__ int search(const int32_t *first, int n, int64_t at) {
+    int b = 0;
+    for (int hi = n - 1; b < hi;) {  // largest b with first[b] <= at
+        const int mid = (b + hi + 1) >> 1;
+        if (first[mid] <= at)
+            b = mid;
+        else
+            hi = mid - 1;
+    }
+    return b;
+}
+
+// The longest tiles of a sequence (its last rows) come first.
+__device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_rows) {
+    Item it;
+    const int b = search(p.item0, p.n_seq, at);
+    it.b = b;
+    it.gs = 31 - __clz(p.n_q_heads / p.n_kv_heads);
+    const int n = (p.first[b + 1] - p.first[b]) << it.gs, nt = (n + tile_rows - 1) / tile_rows;
+    int rem = at - p.item0[b];
+    const int per_tile = p.splits[b] * p.n_units;
+    const int t = nt - 1 - rem / per_tile;
+    rem %= per_tile;
+    it.split = rem / p.n_units;
+    rem %= p.n_units;
+    it.lr = rem / p.n_kv_heads;
+    it.g = rem % p.n_kv_heads;
+    it.row0 = t * tile_rows;
+    it.rows = min(tile_rows, n - it.row0);
+    it.last_slot = row_last(p, it, (it.row0 + it.rows - 1) >> it.gs);
+    const int from = p.shared || p.holes[b] ? p.begin[b] : window_first(p, b, p.slot0[b] + (it.row0 >> it.gs));
+    int ka, kb, col;
+    tile_of(p, from, ka, col);
+    tile_of(p, it.last_slot, kb, col);
+    const int len = kb + 1 - ka;
+    it.k0 = ka + (int)((int64_t)len * it.split / p.splits[b]);
+    it.k1 = ka + (int)((int64_t)len * (it.split + 1) / p.splits[b]);
+    return it;
+}
+
+// ------------------------------------------------------- one row, scalar ----
 // D / 32 consecutive elements of a row as floats.
 template <int D, bool FP8>
 __device__ __forceinline__ void load_row(const uint8_t *row, int lane, float (&x)[D / 32]) {
@@ -40,93 +211,648 @@ __device__ __forceinline__ void load_row(const uint8_t *row, int lane, float (&x
     }
 }
 
-// First slot that the row at `slot` attends to.
-__device__ __forceinline__ int window_first(const PromptParams &p, int b, int slot) {
-    if (p.window <= 0) return 0;
-    if (!p.holes[b]) return max(0, slot - p.window + 1);
-    // pages that are not full lie in between: count valid rows back
-    const int32_t *fill = p.page_fill + (int64_t)p.seq[b] * p.max_pages;
-    int pg = slot / p.page_size, n = slot % p.page_size + 1, left = p.window;
-    while (n < left && pg > 0) {
-        left -= n;
-        n = fill[--pg];
-    }
-    return pg * p.page_size + max(0, n - left);
+// K row (V: + v_off bytes) of a slot, null where it is not valid.
+template <int D, bool FP8>
+__device__ __forceinline__ const uint8_t *row_at(const PromptParams &p, const Item &it, int slot, int64_t &v_off) {
+    constexpr int E = FP8 ? 1 : 2;
+    const int pg = slot / p.page_size, r = slot - pg * p.page_size;
+    const int64_t at = (int64_t)p.seq[it.b] * p.max_pages + pg;
+    const int pid = p.page_table[at];
+    v_off = p.pool_pages * p.n_kv_heads * p.page_size * D * E;
+    if (r >= p.page_fill[at] || pid < 0 || pid >= p.pool_pages) return nullptr;
+    const int64_t page = (int64_t)p.layers[it.lr] * 2 * p.pool_pages + pid;
+    return p.pool + (((page * p.n_kv_heads + it.g) * p.page_size) + r) * D * E;
 }
 
+// A warp: attention of one query row over slots [first, last].
 template <int D, bool FP8>
-__global__ void __launch_bounds__(kRowThreads) prompt_rows_kernel(const __grid_constant__ PromptParams p) {
+__device__ __noinline__ void attend_row(const PromptParams &p, const Item &it, int row, int first, int last,
+                                        float (&o)[D / 32], float &m, float &l) {
     constexpr int N = D / 32;
-    after_previous();
     const int lane = threadIdx.x & 31;
-    const int64_t n = (int64_t)p.first[p.n_seq] * p.n_q_heads;
-    const int64_t at = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) >> 5;
-    if (at >= n) return;
-    const int row = (int)(at / p.n_q_heads), h = (int)(at - (int64_t)row * p.n_q_heads), lr = blockIdx.y;
-    int b = 0;
-    for (int hi = p.n_seq - 1; b < hi;) {
-        const int mid = (b + hi + 1) >> 1;
-        if (p.first[mid] <= row)
-            b = mid;
-        else
-            hi = mid - 1;
-    }
-    const int t = row - p.first[b], slot = p.slot0[b] + t, P = p.page_size;
-    const int g = h / (p.n_q_heads / p.n_kv_heads);
-    const int64_t qrow = ((int64_t)p.qlayers[lr] * p.q_rows + p.row0[b] + t) * p.n_q_heads + h;
-    float q[N], o[N], m = -INFINITY, l = 0.f;
-    load_row<D, false>(reinterpret_cast<const uint8_t *>(p.q + qrow * D), lane, q);
+    float q[N];
+    load_row<D, false>(reinterpret_cast<const uint8_t *>(p.q + q_row(p, it, row) * D), lane, q);
+    m = -INFINITY;
+    l = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = 0.f;
-    const int first = window_first(p, b, slot);
-    constexpr int E = FP8 ? 1 : 2;
-    for (int pg = first / P; pg <= slot / P; ++pg) {
-        const int pid = p.page_table[(int64_t)p.seq[b] * p.max_pages + pg];
-        const int fill = p.page_fill[(int64_t)p.seq[b] * p.max_pages + pg];
-        if (pid < 0 || pid >= p.pool_pages) {
-            record_error(p.status, KVG_ERR_DEVICE_CHECK, 1);
-            continue;
-        }
-        const int64_t page = (int64_t)p.layers[lr] * 2 * p.pool_pages + pid;
-        const uint8_t *k = p.pool + ((page * p.n_kv_heads + g) * P) * D * E;
-        const uint8_t *v = k + p.pool_pages * p.n_kv_heads * P * D * E;
-        const int r1 = min(fill, slot - pg * P + 1);
-        for (int r = max(0, first - pg * P); r < r1; ++r) {
-            float x[N], s = 0.f;
-            load_row<D, FP8>(k + (int64_t)r * D * E, lane, x);
+    for (int slot = first; slot <= last; ++slot) {
+        int64_t v_off;
+        const uint8_t *k = row_at<D, FP8>(p, it, slot, v_off);
+        if (!k) continue;
+        float x[N], s = 0.f;
+        load_row<D, FP8>(k, lane, x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s = __fmaf_rn(q[i], x[i], s);
+        for (int i = 0; i < N; ++i) s = __fmaf_rn(q[i], x[i], s);
 #pragma unroll
-            for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-            s *= p.qscale;
-            const float mn = fmaxf(m, s);
-            const float base = mn == -INFINITY ? 0.f : mn;
-            const float a = exp2f(m - base), w = exp2f(s - base);
-            m = mn;
-            l = __fmaf_rn(l, a, w);
-            load_row<D, FP8>(v + (int64_t)r * D * E, lane, x);
+        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        s *= p.negate ? -p.qscale : p.qscale;
+        const float mn = fmaxf(m, s);
+        const float base = mn == -INFINITY ? 0.f : mn;
+        const float a = exp2f(m - base), w = exp2f(s - base);
+        m = mn;
+        l = __fmaf_rn(l, a, w);
+        load_row<D, FP8>(k + v_off, lane, x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = __fmaf_rn(o[i], a, w * x[i]);
-        }
-    }
-    const float inv = p.vscale / l;
-    uint32_t *out = reinterpret_cast<uint32_t *>(p.out + qrow * D + lane * N);
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        const __nv_bfloat162 y = __floats2bfloat162_rn(o[2 * i] * inv, o[2 * i + 1] * inv);
-        out[i] = *reinterpret_cast<const uint32_t *>(&y);
+        for (int i = 0; i < N; ++i) o[i] = __fmaf_rn(o[i], a, w * x[i]);
     }
 }
+
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// A value row that is not finite reaches, as 0 x inf, the outputs of rows of
+// its tile that do not attend to it.  The warp whose outputs are not finite
+// looks for such rows among the columns that its tiles masked, and computes the
+// output rows that one reached over again.  (A not finite output whose masked
+// values are all finite is as it should be.)
+template <int D, bool FP8>
+__device__ __noinline__ void repair(const PromptParams &p, const Item &it, int first_row, bool bad, int lo, int hi,
+                                    bool partial) {
+    constexpr int N = D / 32;
+    const int lane = threadIdx.x & 31;
+    int tile_lo, tile_hi, col;
+    tile_of(p, lo, tile_lo, col);
+    tile_of(p, hi, tile_hi, col);
+    if (hi < lo) tile_hi = 0x7fffffff;  // not a row of the item's
+    const int from = __reduce_min_sync(0xffffffffu, tile_hi), to = __reduce_max_sync(0xffffffffu, tile_lo);
+    bool redo = false;
+    for (int kt = it.k0; kt < it.k1; ++kt) {
+        if (kt < from && kt > to) continue;  // no row of the warp masks valid columns of it
+        const int end = min(first_slot(p, kt + 1), it.last_slot / p.page_size * p.page_size + p.page_size);
+        for (int slot = first_slot(p, kt); slot < end; ++slot) {
+            int64_t v_off;
+            const uint8_t *k = row_at<D, FP8>(p, it, slot, v_off);
+            if (!k) continue;
+            float x[N];
+            load_row<D, FP8>(k + v_off, lane, x);
+            bool fine = true;
+#pragma unroll
+            for (int i = 0; i < N; ++i) fine = fine && isfinite(x[i]);
+            if (__any_sync(0xffffffffu, !fine)) redo = redo || slot < lo || slot > hi;
+        }
+    }
+    const uint32_t todo = __ballot_sync(0xffffffffu, bad && redo);
+    for (int i = 0; i < 32; ++i) {
+        if (!(todo >> i & 1)) continue;
+        const int row = first_row + i;
+        const int f = max(__shfl_sync(0xffffffffu, lo, i), first_slot(p, it.k0));
+        const int l_ = min(__shfl_sync(0xffffffffu, hi, i), first_slot(p, it.k1) - 1);
+        float o[N], m, l;
+        attend_row<D, FP8>(p, it, row, f, l_, o, m, l);
+        if (partial) {
+            const int64_t at = part_slot(p, it.b, it.gs, it.split, it.lr * p.n_kv_heads + it.g, row);
+#pragma unroll
+            for (int e = 0; e < N; ++e) p.part_o[at * D + lane * N + e] = o[e];
+            if (lane == 0) p.part_ml[at] = make_float2(m, l);
+        } else {
+            const float inv = p.vscale / l;
+            uint32_t *out = reinterpret_cast<uint32_t *>(p.out + q_row(p, it, row) * D + lane * N);
+#pragma unroll
+            for (int e = 0; e < N / 2; ++e) out[e] = pack_out(o[2 * e] * inv, o[2 * e + 1] * inv);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ kernel --
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, 1)
+    prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map) {
+    constexpr int D = C::D, DC = C::DC, NCH = C::NCH, STREAMS = C::STREAMS, STAGES = C::STAGES;
+    constexpr bool FP8 = C::FP8;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ Bars s;
+    uint8_t *const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    uint8_t *const ring = smem + C::Q_BYTES;
+    uint8_t *const raw = ring + STAGES * C::CHUNK;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            mbar_init(&s.full[i], FP8 ? 32 * kConvertWarps : 1);
+            mbar_init(&s.empty[i], 1);
+        }
+        for (int i = 0; i < C::RAW_STAGES; ++i) {
+            mbar_init(&s.raw_full[i], 1);
+            mbar_init(&s.raw_empty[i], 32 * kConvertWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.scores[i], 1);
+            mbar_init(&s.weights[i], 128);
+            mbar_init(&s.out[i], 1);
+        }
+        mbar_init(&s.queries, 32 * C::SOFTMAX_WARPS);
+        mbar_init(&s.drained, 1);
+        s.abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == C::MMA_WARP) tmem_alloc<512>(&s.tmem);
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = s.tmem;
+
+    after_previous();
+    const Item it = item_of(p, blockIdx.x, STREAMS * kTile);
+    const int n = it.k1 - it.k0;
+    const bool partial = p.splits[it.b] > 1 || p.shared;
+
+    if (warp == C::LOAD_WARP) {
+        // ---- keys and values of tile j: K0, then K(j + 1) and V(j) in turn
+        struct Pages {
+            int rows;       // valid rows of the lane's page in the tile
+            int32_t at;     // its first row in the pool, of the layer's keys
+            uint32_t bytes; // of a chunk's copies, all lanes'
+        };
+        const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
+        const int last_page = it.last_slot / p.page_size;
+        auto find = [&](int j) {
+            const int kt = it.k0 + j;
+            Pages r{0, 0, 0};
+            int pg, sub = 0;
+            if (p.pages_per_tile) {
+                pg = lane < p.pages_per_tile ? kt * p.pages_per_tile + lane : last_page + 1;
+            } else {
+                pg = lane == 0 ? kt / p.tiles_per_page : last_page + 1;
+                sub = kt % p.tiles_per_page * kTile;
+            }
+            if (pg <= last_page) {
+                const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
+                const int pid = p.page_table[e];
+                r.rows = min(p.pages_per_tile ? p.page_size : kTile, p.page_fill[e] - sub);
+                if (r.rows < 0) r.rows = 0;
+                if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
+                    record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
+                    r.rows = 0;
+                }
+                r.at = (int32_t)((int64_t)p.layers[it.lr] * 2 * plane +
+                                 ((int64_t)pid * p.n_kv_heads + it.g) * p.page_size + sub);
+            }
+            return r;
+        };
+        int chunk = 0;  // of the ring that the copies land in
+        constexpr int LANDS = FP8 ? C::RAW_STAGES : STAGES;
+        uint64_t *const landed = FP8 ? s.raw_full : s.full;
+        uint64_t *const freed = FP8 ? s.raw_empty : s.empty;
+        const int box_bytes = p.box_rows * 128;
+        auto copy = [&](const Pages &r, bool values) {
+            const int n_pages = __popc(__ballot_sync(0xffffffffu, r.rows > 0));
+            for (int c = 0; c < NCH; ++c, ++chunk) {
+                const int st = chunk % LANDS;
+                if (chunk >= LANDS && !wait_bar(s, &freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
+                if (lane == 0) {
+                    if (n_pages)
+                        mbar_arrive_expect_tx(&landed[st], n_pages * box_bytes * (FP8 ? 1 : C::BOXES));
+                    else
+                        mbar_arrive(&landed[st]);
+                }
+                __syncwarp();
+                if (r.rows > 0) {
+                    const int32_t y = r.at + (values ? (int32_t)plane : 0);
+                    uint8_t *dst = (FP8 ? raw + st * C::RAW : ring + st * C::CHUNK) + lane * p.page_rows * 128;
+                    if constexpr (FP8) {
+                        tma_load_2d(dst, &map, c * DC, y, &landed[st]);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < C::BOXES; ++x)
+                            tma_load_2d(dst + x * C::BOX, &map, c * DC + 64 * x, y, &landed[st]);
+                    }
+                }
+            }
+            return true;
+        };
+        auto note_mask = [&](const Pages &r, int j) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int a = lane * p.page_rows - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
+                uint32_t bits = 0;
+                if (r.rows > 0 && a < 32 && e > 0)
+                    bits = (e >= 32 ? ~0u : (1u << e) - 1) & ~(a > 0 ? (1u << a) - 1 : 0u);
+                bits = __reduce_or_sync(0xffffffffu, bits);
+                if (lane == 0) s.mask[j % kMaskSlots][w] = bits;
+            }
+            __syncwarp();
+        };
+        Pages now = find(0), next = now;
+        bool ok = n > 0;
+        if (ok) {
+            note_mask(now, 0);
+            ok = copy(now, false);
+        }
+        if (n > 1) next = find(1);
+        for (int j = 0; ok && j < n; ++j) {
+            if (j + 1 < n) {
+                note_mask(next, j + 1);
+                ok = copy(next, false);
+            }
+            if (ok) ok = copy(now, true);
+            now = next;
+            if (j + 2 < n) next = find(j + 2);
+        }
+        if (!ok && n > 0)  // gave up: no copy may still be landing when the CTA ends
+            for (int c = max(0, chunk - LANDS); c < chunk; ++c) (void)mbar_wait_bounded(&landed[c % LANDS], (c / LANDS) & 1);
+    } else if (warp == C::MMA_WARP) {
+        // ---- products: one lane issues; the warp clears value rows that are not valid
+        constexpr uint32_t QK = mma_desc(kTile, kTile, FP8, false), PV = mma_desc(kTile, DC, FP8, true);
+        const uint32_t qk = QK | (p.negate ? kMmaNegateA : 0u);
+        const uint32_t q_s = smem_addr(smem), ring_s = smem_addr(ring);
+        bool ok = n > 0 && wait_bar(s, &s.queries, 0, p.status);
+        tc_after_sync();
+        int chunk = 0;
+        auto arrived = [&](int c) { return wait_bar(s, &s.full[c % STAGES], (c / STAGES) & 1, p.status); };
+        // S = Q K^T of a stream into score columns `buf`, keys in chunks from c0
+        auto scores = [&](int stream, int buf, int c0) {
+            if (lane == 0) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    const uint32_t k_s = ring_s + (c0 + ks / (DC / 16)) % STAGES * C::CHUNK + ks % (DC / 16) / 4 * C::BOX;
+                    mma_ss(tmem + kScoreCols + buf * kTile,
+                           smem_desc(q_s + stream * (kTile * D * 2) + ks / 4 * C::BOX + ks % 4 * 32, 0, 1024),
+                           smem_desc(k_s + ks % 4 * 32, 0, 1024), qk, ks > 0);
+                }
+                mma_commit(&s.scores[buf]);
+            }
+        };
+        // O += P V of a stream, weights in score columns `buf`, chunk c of the values at ring chunk at
+        auto product = [&](int stream, int buf, int c, int at, bool add) {
+            if (lane == 0) {
+                const uint32_t v_s = ring_s + at % STAGES * C::CHUNK;
+#pragma unroll
+                for (int ks = 0; ks < kTile / 16; ++ks)
+                    mma_ts(tmem + kOutCols + stream * kTile + c * DC, tmem + kScoreCols + buf * kTile + ks * 8,
+                           smem_desc(v_s + ks * 2048, C::BOX, 1024), PV, add || ks > 0);
+            }
+        };
+        auto release = [&](int c) {
+            if (lane == 0) mma_commit(&s.empty[c % STAGES]);
+        };
+        // the value rows of tile j that are not valid hold anything: zero weights must meet zeros
+        auto clear = [&](int j, int at) {
+            if constexpr (!FP8) {
+                const uint32_t *m = s.mask[j % kMaskSlots];
+                if ((m[0] & m[1] & m[2] & m[3]) == ~0u) return;
+                uint8_t *v = ring + at % STAGES * C::CHUNK;
+                for (int r = lane / 8; r < kTile; r += 4)
+                    if (!(m[r / 32] >> (r % 32) & 1))
+#pragma unroll
+                        for (int x = 0; x < C::BOXES; ++x)
+                            reinterpret_cast<uint4 *>(v + x * C::BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
+                fence_proxy_async_shared();
+                __syncwarp();
+            }
+        };
+        auto keys = [&]() {
+            for (int c = 0; ok && c < NCH; ++c) ok = arrived(chunk + c);
+        };
+        if (ok) keys();
+        if (ok) {
+            for (int st = 0; st < STREAMS; ++st) scores(st, st, chunk);
+            for (int c = 0; c < NCH; ++c) release(chunk + c);
+            chunk += NCH;
+        }
+        for (int j = 0; ok && j < n; ++j) {
+            const int k_at = chunk;
+            const bool more = j + 1 < n;
+            if (more) {
+                keys();
+                if (!ok) break;
+                chunk += NCH;
+                if (STREAMS == 1) {  // the next scores, beside this tile's weights
+                    // (their buffer's weights, of tile j - 1, were multiplied before)
+                    scores(0, (j + 1) & 1, k_at);
+                    for (int c = 0; c < NCH; ++c) release(k_at + c);
+                }
+            }
+            const int v_at = chunk;
+            for (int st = 0; ok && st < STREAMS; ++st) {
+                const int buf = STREAMS == 1 ? j & 1 : st;
+                for (int c = 0; ok && c < NCH; ++c) {
+                    if (st == 0) {
+                        ok = arrived(v_at + c);
+                        if (ok) clear(j, v_at + c);
+                    }
+                    if (ok && c == 0) {
+                        ok = wait_bar(s, &s.weights[buf], (STREAMS == 1 ? j >> 1 : j) & 1, p.status);
+                        tc_after_sync();
+                    }
+                    if (ok) product(st, buf, c, v_at + c, j > 0);
+                }
+                if (ok && lane == 0) mma_commit(&s.out[st]);
+                if (ok && STREAMS == 2 && more) scores(st, st, k_at);
+            }
+            if (!ok) break;
+            if (STREAMS == 2 && more) release(k_at);
+            for (int c = 0; c < NCH; ++c) release(v_at + c);
+            chunk += NCH;
+        }
+        // all products have completed before the tensor memory is given back
+        if (lane == 0) mma_commit(&s.drained);
+        __syncwarp();
+        (void)mbar_wait_bounded(&s.drained, 0);
+    } else if (FP8 && warp >= C::CONVERT_WARP) {
+        // ---- E4M3 codes to fp16 (exact), chunk by chunk
+        const int t = threadIdx.x - 32 * C::CONVERT_WARP, u = t % 8;
+        bool ok = true;
+        for (int i = 0; ok && i < 2 * n * NCH; ++i) {
+            const int rs = i % C::RAW_STAGES, st = i % STAGES;
+            // chunks come as K0, then K(j + 1) and V(j), the last V alone
+            const int tile2 = i / NCH;
+            const bool values = tile2 > 0 && ((tile2 & 1) == 0 || tile2 == 2 * n - 1);
+            const int j = tile2 == 2 * n - 1 ? n - 1 : tile2 / 2 - 1;
+            ok = wait_bar(s, &s.raw_full[rs], (i / C::RAW_STAGES) & 1, p.status);
+            if (ok && i >= STAGES) ok = wait_bar(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
+            if (!ok) break;
+            const uint8_t *src = raw + rs * C::RAW;
+            uint8_t *dst = ring + st * C::CHUNK + u / 4 * C::BOX;
+#pragma unroll 4
+            for (int r = t / 8; r < kTile; r += 4 * kConvertWarps) {
+                uint4 x = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
+                if (values && !(s.mask[j % kMaskSlots][r / 32] >> (r % 32) & 1)) x = make_uint4(0, 0, 0, 0);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                uint32_t y[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint16_t lo = (uint16_t)w[e], hi = (uint16_t)(w[e] >> 16);
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(lo));
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(hi));
+                }
+                const int u2 = u % 4 * 2;
+                *reinterpret_cast<uint4 *>(dst + r * 128 + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4 *>(dst + r * 128 + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+            }
+            fence_proxy_async_shared();
+            mbar_arrive(&s.full[st]);
+            mbar_arrive(&s.raw_empty[rs]);
+        }
+    } else if (warp < C::SOFTMAX_WARPS) {
+        // ---- queries to shared memory (rows past the item's as zeros)
+        {
+            constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR;
+            const int u = lane % LPR;
+#pragma unroll 4
+            for (int i = 0; i < 32; i += RPI) {
+                const int r = warp * 32 + i + lane / LPR, rt = r % kTile;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (r < it.rows) {
+                    x = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + r) * D)[u];
+                    if constexpr (FP8) {
+                        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                            w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                        }
+                        x = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * C::BOX + rt * 128 +
+                                           ((u % 8 ^ (rt & 7)) << 4)) = x;
+            }
+            fence_proxy_async_shared();
+            mbar_arrive(&s.queries);
+        }
+        // ---- weights: a thread has a query row
+        const int stream = warp / 4;
+        const int r = threadIdx.x, row = it.row0 + r;  // of the item, of the sequence
+        const bool mine = r < it.rows;
+        const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // tensor memory lanes of the warp
+        int lo = 0, hi = -1, tile_lo = 0, col_lo = 0, tile_hi = -1, col_hi = 0;
+        if (mine) {
+            lo = row_first(p, it, row >> it.gs);
+            hi = row_last(p, it, row >> it.gs);
+            tile_of(p, lo, tile_lo, col_lo);
+            tile_of(p, hi, tile_hi, col_hi);
+        }
+        const float c = p.qscale;
+        float m = -INFINITY;               // what the weights refer to
+        float2 sum = make_float2(0.f, 0.f);
+        const uint32_t o_at = tmem + lanes + kOutCols + stream * kTile;
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            const int buf = STREAMS == 1 ? j & 1 : stream;
+            const uint32_t s_at = tmem + lanes + kScoreCols + buf * kTile;
+            ok = wait_bar(s, &s.scores[buf], (STREAMS == 1 ? j >> 1 : j) & 1, p.status);
+            if (!ok) break;
+            tc_after_sync();
+            float x[kTile];
+#pragma unroll
+            for (int i = 0; i < kTile; i += 32) tmem_ld32(s_at + i, reinterpret_cast<uint32_t *>(x) + i);
+            tmem_wait_ld();
+            // columns [from, to) of the tile are the row's
+            const int kt = it.k0 + j;
+            const int from = kt < tile_lo ? kTile : kt == tile_lo ? col_lo : 0;
+            const int to = kt > tile_hi ? 0 : kt == tile_hi ? col_hi + 1 : kTile;
+            const uint32_t *valid = s.mask[j % kMaskSlots];
+            const bool whole = from == 0 && to == kTile && (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
+            if (!__all_sync(0xffffffffu, whole)) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int a = from - 32 * w, e = to - 32 * w;
+                    const uint32_t bits = valid[w] & (e >= 32 ? ~0u : e <= 0 ? 0u : (1u << e) - 1) &
+                                          (a >= 32 ? 0u : a <= 0 ? ~0u : ~((1u << a) - 1));
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[32 * w + i] = bits >> i & 1 ? x[32 * w + i] : -INFINITY;
+                }
+            }
+            float t[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+            for (int i = 4; i < kTile; i += 4)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = fmaxf(t[e], x[i + e]);
+            const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+            // move the reference?  (-inf: no column so far, nothing to rescale)
+            const bool move = top > m && (m == -INFINITY || (top - m) * c > kMaxSlack);
+            const bool rescale = move && m != -INFINITY;
+            if (__any_sync(0xffffffffu, rescale)) {
+                const float a = rescale ? exp2_approx((m - top) * c) : 1.f;
+                sum.x *= a;
+                sum.y *= a;
+                ok = wait_bar(s, &s.out[stream], (j - 1) & 1, p.status);
+                if (!ok) break;
+                tc_after_sync();
+#pragma unroll 1
+                for (int i = 0; i < D; i += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(o_at + i, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+                    tmem_st32(o_at + i, o);
+                }
+            }
+            if (move) m = top;
+            const float base = m == -INFINITY ? 0.f : -m * c;
+            const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
+            float2 part[4] = {};
+#pragma unroll
+            for (int i = 0; i < kTile; i += 64) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    float2 y = fma2(make_float2(x[i + 2 * e], x[i + 2 * e + 1]), c2, b2);
+                    y.x = exp2_approx(y.x);
+                    y.y = exp2_approx(y.y);
+                    // weights in the products' 16 bits.  The sum adds the rounded
+                    // bf16 weights: where one is far above the others, its rounding
+                    // (2^-9) then divides out; fp16's (2^-12) stays below the output's.
+                    if constexpr (FP8) {
+                        const __half2 h = __floats2half2_rn(y.x, y.y);
+                        w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                    } else {
+                        w[e] = pack_out(y.x, y.y);
+                        y = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                    }
+                    part[e % 4] = add2(part[e % 4], y);
+                }
+                tmem_st32(s_at + i / 2, w);
+            }
+            sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
+            tmem_wait_st();
+            tc_before_sync();
+            // the wait after the last tile tells its product from the one before
+            // only if that one is known to be done
+            if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
+            if (!ok) break;
+            mbar_arrive(&s.weights[buf]);
+        }
+        // ---- output
+        if (ok && n > 0) ok = wait_bar(s, &s.out[stream], (n - 1) & 1, p.status);
+        if (ok) {
+            tc_after_sync();
+            const float l = sum.x + sum.y;
+            const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
+            bool bad = false;
+            int64_t at = 0;
+            float inv = 1.f;
+            if (mine && partial) {
+                at = part_slot(p, it.b, it.gs, it.split, it.lr * p.n_kv_heads + it.g, row);
+                p.part_ml[at] = make_float2(m * c, l);
+            } else if (mine) {
+                at = q_row(p, it, row);
+                inv = __fdiv_rn(p.vscale, l);
+            }
+            if (n > 0) {
+#pragma unroll 1
+                for (int i = 0; i < D; i += 32) {
+                    float o[32];
+                    tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
+                    tmem_wait_ld();
+                    if (!mine || (partial && empty)) continue;
+                    float2 z = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) z = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), z);
+                    bad = bad || !(z.x + z.y == 0.f);
+                    if (partial) {
+                        float4 *to = reinterpret_cast<float4 *>(p.part_o + at * D + i);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    } else {
+                        uint4 *to = reinterpret_cast<uint4 *>(p.out + at * D + i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            to[e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                               pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                    }
+                }
+            }
+            if (__any_sync(0xffffffffu, bad)) {
+                __syncwarp();
+                repair<D, FP8>(p, it, it.row0 + warp * 32, bad, lo, hi, partial);
+            }
+        }
+    }
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    if (warp == C::MMA_WARP) tmem_free<512>(tmem);
+}
+
+// Joins the splits of each row: a warp per row of the sequences that were split.
+template <int D>
+__global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant__ PromptParams p) {
+    constexpr int N = D / 32;
+    after_previous();
+    const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
+    const int lane = threadIdx.x & 31, gs = 31 - __clz(p.n_q_heads / p.n_kv_heads);
+    if (at >= ((int64_t)p.first[p.n_seq] << gs) * p.n_units) return;
+    Item it{};
+    it.gs = gs;
+    const int64_t row_of_all = at / p.n_units;
+    it.b = search(p.first, p.n_seq, row_of_all >> gs);
+    if (p.splits[it.b] == 1) return;
+    const int unit = (int)(at - row_of_all * p.n_units), row = (int)(row_of_all - ((int64_t)p.first[it.b] << gs));
+    it.lr = unit / p.n_kv_heads;
+    it.g = unit % p.n_kv_heads;
+    float M = -INFINITY, L = 0.f, o[N] = {};
+    for (int i = 0; i < p.splits[it.b]; ++i) M = fmaxf(M, p.part_ml[part_slot(p, it.b, gs, i, unit, row)].x);
+    for (int i = 0; i < p.splits[it.b]; ++i) {
+        const int64_t slot = part_slot(p, it.b, gs, i, unit, row);
+        const float2 ml = p.part_ml[slot];
+        if (ml.y == 0.f) continue;
+        const float a = exp2f(ml.x - M);
+        L = __fmaf_rn(ml.y, a, L);
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] = __fmaf_rn(p.part_o[slot * D + lane * N + e], a, o[e]);
+    }
+    const float inv = __fdiv_rn(p.vscale, L);
+    uint32_t *out = reinterpret_cast<uint32_t *>(p.out + q_row(p, it, row) * D + lane * N);
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) out[e] = pack_out(o[2 * e] * inv, o[2 * e + 1] * inv);
+}
+
+template <class C>
+struct PromptLaunch {
+    static cudaError_t run(const PromptParams &p, const CUtensorMap &map, cudaStream_t s) {
+        static std::atomic<int> ready[kMaxDevices];  // the shared-memory attribute is per device
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+        if (!ready[dev].load()) {
+            e = cudaFuncSetAttribute(prompt_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+            if (e != cudaSuccess) return e;
+            ready[dev].store(1);
+        }
+        return launch_after(prompt_kernel<C>, p.item0[p.n_seq], C::THREADS, C::SMEM, s, p, map);
+    }
+};
 
 }  // namespace
 
-cudaError_t launch_prompt(int head_dim, bool fp8, const PromptParams &p, cudaStream_t s) {
-    const int64_t warps = (int64_t)p.first[p.n_seq] * p.n_q_heads;
-    const dim3 grid((unsigned)((warps + kRowThreads / 32 - 1) / (kRowThreads / 32)), p.n_layers_run);
+// Two streams of query tiles unless no sequence has rows for the second.
+int prompt_streams(int head_dim, int64_t most_rows) { return head_dim <= 128 && most_rows > kTile ? 2 : 1; }
+
+// How pages fill the 128 columns of a key tile.
+void prompt_tiling(int page_size, PromptParams *p) {
+    const int rows = (page_size + 7) / 8 * 8;
+    p->page_rows = rows;
+    p->pages_per_tile = rows <= kTile ? kTile / rows : 0;
+    p->tiles_per_page = (page_size + kTile - 1) / kTile;
+    p->box_rows = std::min(rows, kTile);
+}
+
+cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
+                          cudaStream_t s) {
+    if (head_dim == 64 && !fp8)
+        return streams == 2 ? PromptLaunch<Cfg<64, false, 2>>::run(p, map, s) : PromptLaunch<Cfg<64, false, 1>>::run(p, map, s);
+    if (head_dim == 128 && !fp8)
+        return streams == 2 ? PromptLaunch<Cfg<128, false, 2>>::run(p, map, s) : PromptLaunch<Cfg<128, false, 1>>::run(p, map, s);
+    if (head_dim == 128)
+        return streams == 2 ? PromptLaunch<Cfg<128, true, 2>>::run(p, map, s) : PromptLaunch<Cfg<128, true, 1>>::run(p, map, s);
+    if (head_dim == 256)
+        return fp8 ? PromptLaunch<Cfg<256, true, 1>>::run(p, map, s) : PromptLaunch<Cfg<256, false, 1>>::run(p, map, s);
+    return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t s) {
+    const int64_t rows = (int64_t)p.first[p.n_seq] * (p.n_q_heads / p.n_kv_heads) * p.n_units;
+    const int64_t grid = (rows + 3) / 4;
     switch (head_dim) {
-        case 64: return launch_after(prompt_rows_kernel<64, false>, grid, kRowThreads, 0, s, p);
-        case 128: return launch_after(fp8 ? prompt_rows_kernel<128, true> : prompt_rows_kernel<128, false>, grid, kRowThreads, 0, s, p);
-        case 256: return launch_after(fp8 ? prompt_rows_kernel<256, true> : prompt_rows_kernel<256, false>, grid, kRowThreads, 0, s, p);
+        case 64: return launch_after(prompt_join_kernel<64>, (unsigned)grid, 128, 0, s, p);
+        case 128: return launch_after(prompt_join_kernel<128>, (unsigned)grid, 128, 0, s, p);
+        case 256: return launch_after(prompt_join_kernel<256>, (unsigned)grid, 128, 0, s, p);
     }
     return cudaErrorInvalidValue;
 }

@@ -785,6 +785,7 @@ struct kvg_cache {
     cudaStream_t part_stream = nullptr;
     bool part_used = false;
     CUtensorMap pool_map;  // decode kernel's 2-D view of the pool
+    CUtensorMap prompt_map;  // prompt kernel's
     // library streams and events for hashing a host-store graft's pages while
     // the next pages still cross the host link (made on first use)
     cudaStream_t aux[kHostHashStreams] = {};
@@ -983,9 +984,12 @@ extern "C" kvg_status kvg_cache_create(const kvg_dims *dims, int32_t n_pages, in
     if (pool_rows > 0x7fffffffull)
         return cleanup(fail(KVG_ERR_ARG, "pool of %llu rows exceeds the decode kernel's 2^31-row addressing",
                             (unsigned long long)pool_rows));
-    if (make_pool_tensor_map(&c->pool_map, c->pool, dims->head_dim, dims->kv_dtype == KVG_KV_E4M3, dims->page_size,
-                             pool_rows) !=
-        cudaSuccess)
+    const bool fp8 = dims->kv_dtype == KVG_KV_E4M3;
+    PromptParams tiling{};
+    prompt_tiling(dims->page_size, &tiling);
+    if (make_pool_tensor_map(&c->pool_map, c->pool, dims->head_dim, fp8,
+                             decode_tile_tokens(dims->head_dim, fp8, dims->page_size), pool_rows) != cudaSuccess ||
+        make_pool_tensor_map(&c->prompt_map, c->pool, dims->head_dim, fp8, tiling.box_rows, pool_rows) != cudaSuccess)
         return cleanup(fail(KVG_ERR_CUDA, "tensor map of the pool could not be encoded"));
     // the allocation-free decode's static scratch becomes resident on this
     // device now, while the caller expects allocations, not at its first call
@@ -2461,6 +2465,124 @@ extern "C" kvg_status kvg_decode_state_finish(const float *state, int64_t n_rows
 
 // -------------------------------------------------------- prompt attention --
 
+// The split partials are shared by every attention of the cache: a call on
+// another stream than the previous one waits for that one's last kernel.
+static cudaError_t use_partials(kvg_cache *c, cudaStream_t st) {
+    if (!c->part_ev)
+        if (cudaError_t e = cudaEventCreateWithFlags(&c->part_ev, cudaEventDisableTiming); e != cudaSuccess) return e;
+    return c->part_used && st != c->part_stream ? cudaStreamWaitEvent(st, c->part_ev, 0) : cudaSuccess;
+}
+static kvg_status used_partials(kvg_cache *c, cudaStream_t st) {
+    KVG_CUDA(cudaEventRecord(c->part_ev, st));
+    c->part_stream = st;
+    c->part_used = true;
+    return KVG_OK;
+}
+
+static void prompt_params(const kvg_cache *c, const void *q, int32_t n_q_heads, void *out, float scale,
+                          PromptParams *p) {
+    const kvg_dims &d = c->dims;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    p->pool = c->pool;
+    p->pool_pages = c->n_pages;
+    p->n_kv_heads = d.n_kv_heads;
+    p->page_size = d.page_size;
+    p->n_q_heads = n_q_heads;
+    p->page_table = c->page_table;
+    p->page_fill = c->page_fill;
+    p->max_pages = c->max_pages;
+    prompt_tiling(d.page_size, p);
+    // a masked score is -inf times the scale: a scale of 0 becomes one that
+    // keeps it (2^(1e-30 x) is 1)
+    p->negate = scale < 0.f;
+    p->qscale = std::max(std::fabs(scale) * 1.4426950408889634f * (fp8 ? d.k_scale : 1.f), 1e-30f);
+    p->vscale = fp8 ? d.v_scale : 1.f;
+    p->q = static_cast<const __nv_bfloat16 *>(q);
+    p->out = static_cast<__nv_bfloat16 *>(out);
+    p->status = c->status;
+}
+
+static void prompt_layers(const WindowGroup &part, PromptParams *p) {
+    p->window = part.window;
+    p->n_layers_run = (int32_t)part.layers.size();
+    p->n_units = p->n_layers_run * p->n_kv_heads;
+    for (int32_t i = 0; i < p->n_layers_run; ++i) {
+        p->layers[i] = (int16_t)part.layers[i].first;
+        p->qlayers[i] = (int16_t)part.layers[i].second;
+    }
+}
+
+// Query rows (x heads of the group) of a sequence, over the slots [begin, slot
+// of the row] (or up to `last` for all of them when tokens is 0).
+struct PromptWork {
+    int64_t rows;
+    int32_t tokens, begin, last;
+};
+constexpr int kPromptRows = 128;  // rows of a query tile, columns of a key tile
+
+// Work items of a launch: how many key ranges each sequence's query tiles are
+// split into.  An item costs its key tiles and kItemTiles more for its start,
+// its output and its part of the join; the SMs take items one each at a time,
+// so the time is about the rounds of items times the length of one.  The
+// splits tried halve the longest tile step by step; the best estimate wins.
+// Returns the partial results' slots (0: nothing is split).
+static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &work, int G, int tile_rows, bool always,
+                           PromptParams *p) {
+    constexpr double kItemTiles = 3.0;
+    const int P = p->page_size;
+    const double slots_per_tile = p->pages_per_tile ? (double)p->pages_per_tile * P : (double)P / p->tiles_per_page;
+    struct Row {
+        double longest, mean;
+        int64_t tiles;
+    };
+    std::vector<Row> rows;
+    double longest = 1.0;
+    for (const PromptWork &w : work) {
+        const int64_t nt = (w.rows + tile_rows - 1) / tile_rows;
+        const double far = (w.last + std::max(w.tokens, 1) - w.begin) / slots_per_tile + 1.0;
+        const double near = (w.last + std::min<int64_t>(std::max(w.tokens, 1), tile_rows / G) - w.begin) / slots_per_tile + 1.0;
+        const double cap = p->window > 0 ? (p->window + tile_rows / G) / slots_per_tile + 2.0 : far;
+        rows.push_back({std::min(far, cap), (std::min(far, cap) + std::min(near, cap)) / 2, nt});
+        longest = std::max(longest, rows.back().longest);
+    }
+    double best = INFINITY, best_len = longest;
+    for (double len = longest; len >= 1.0; len *= 0.84) {
+        double items = 0, total = 0, top = 0;
+        for (const Row &r : rows) {
+            const double s = std::max(1.0, std::ceil(r.longest / len - 1e-9));
+            items += s * r.tiles * p->n_units;
+            total += r.tiles * p->n_units * (r.mean + s * kItemTiles);
+            top = std::max(top, r.longest / s + kItemTiles);
+        }
+        const double mean = total / items;
+        const double est = std::max(top, std::ceil(items / c->n_sm) * mean) + (len < longest ? kItemTiles : 0.0);
+        if (est < best) {
+            best = est;
+            best_len = len;
+        }
+    }
+    int64_t slots = 0;
+    p->item0[0] = 0;
+    for (size_t i = 0; i < rows.size(); ++i) {
+        const int32_t s = (int32_t)std::max(1.0, std::ceil(rows[i].longest / best_len - 1e-9));
+        p->splits[i] = s;
+        p->item0[i + 1] = p->item0[i] + (int32_t)(rows[i].tiles * s * p->n_units);
+        p->part0[i] = slots;
+        if (s > 1 || always) slots += work[i].rows * p->n_units * s;
+    }
+    return slots;
+}
+
+static kvg_status prompt_partials(kvg_cache *c, int64_t slots, PromptParams *p) {
+    if (slots) {
+        KVG_CUDA(c->part_o.ensure((size_t)slots * c->dims.head_dim * sizeof(float)));
+        KVG_CUDA(c->part_ml.ensure((size_t)slots * sizeof(float2)));
+    }
+    p->part_o = static_cast<float *>(c->part_o.ptr);
+    p->part_ml = static_cast<float2 *>(c->part_ml.ptr);
+    return KVG_OK;
+}
+
 extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
                                            int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
                                            void *stream) {
@@ -2500,30 +2622,16 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
     DeviceGuard g(c->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     PromptParams p{};
-    p.pool = c->pool;
-    p.pool_pages = c->n_pages;
-    p.n_kv_heads = d.n_kv_heads;
-    p.page_size = d.page_size;
-    p.n_q_heads = n_q_heads;
-    p.page_table = c->page_table;
-    p.page_fill = c->page_fill;
-    p.max_pages = c->max_pages;
-    p.qscale = scale * 1.4426950408889634f * (fp8 ? d.k_scale : 1.f);
-    p.vscale = fp8 ? d.v_scale : 1.f;
-    p.q = static_cast<const __nv_bfloat16 *>(q);
-    p.out = static_cast<__nv_bfloat16 *>(out);
+    prompt_params(c, q, n_q_heads, out, scale, &p);
     p.q_rows = total;
-    p.status = c->status;
+    KVG_CUDA(use_partials(c, st));
     for (const WindowGroup &part : layer_parts(c, layer)) {
-        p.window = part.window;
-        p.n_layers_run = (int32_t)part.layers.size();
-        for (int32_t i = 0; i < p.n_layers_run; ++i) {
-            p.layers[i] = (int16_t)part.layers[i].first;
-            p.qlayers[i] = (int16_t)part.layers[i].second;
-        }
+        prompt_layers(part, &p);
         int32_t row = 0;
         for (int32_t b = 0; b < B;) {
             p.n_seq = 0;
+            std::vector<PromptWork> work;
+            int64_t most = 0;
             for (; b < B && p.n_seq < kMaxBatchPerLaunch; ++b) {
                 if (n_rows[b] == 0) continue;
                 const int32_t i = p.n_seq++, sq = seq_ids[b];
@@ -2532,13 +2640,29 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
                 p.row0[i] = row;
                 p.slot0[i] = c->n_slots[sq] - n_rows[b];
                 p.holes[i] = std::any_of(f.begin(), f.end() - 1, [P](int32_t x) { return x < P; });
+                p.begin[i] = 0;
+                if (p.window > 0) {  // what the first row's window reaches back to
+                    p.begin[i] = std::max(0, p.slot0[i] - p.window + 1);
+                    if (p.holes[i]) {
+                        int32_t pg, in_page;
+                        window_start(c, sq, (int64_t)p.window + n_rows[b] - 1, &pg, &in_page);
+                        p.begin[i] = pg * d.page_size + in_page;
+                    }
+                }
                 p.first[i + 1] = p.first[i] + n_rows[b];
                 row += n_rows[b];
+                most = std::max<int64_t>(most, (int64_t)n_rows[b] * G);
+                work.push_back({(int64_t)n_rows[b] * G, n_rows[b], p.begin[i], p.slot0[i]});
             }
-            if (p.n_seq) KVG_CUDA(launch_prompt(d.head_dim, fp8, p, st));
+            if (p.n_seq == 0) continue;
+            const int streams = prompt_streams(d.head_dim, most);
+            const int64_t slots = plan_prompt(c, work, G, kPromptRows * streams, false, &p);
+            if (kvg_status r = prompt_partials(c, slots, &p); r != KVG_OK) return r;
+            KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
+            if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
         }
     }
-    return KVG_OK;
+    return used_partials(c, st);
 }
 
 // ------------------------------------------------------------------ digest --

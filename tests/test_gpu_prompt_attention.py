@@ -45,7 +45,8 @@ class Bed:
 
     def append(self, seq, n, seed, scale=1.0):
         if n:
-            k, v = (normal(seed + i, self.dims.n_layers, n, self.hkv, self.d) * scale for i in (0, 1))
+            k, v = (normal(seed + i, self.dims.n_layers, n, self.hkv, self.d) for i in (0, 1))
+            k = k * scale  # the gate's absolute bound is one for N(0, 1) values
             pos = torch.arange(n, dtype=torch.int32, device="cuda")
             self.kvg.kvg_cache_append(self.cache.h, seq, k.data_ptr(), v.data_ptr(), pos.data_ptr(), n)
             torch.cuda.synchronize()
