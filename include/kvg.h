@@ -609,6 +609,19 @@ kvg_status kvg_decode_attention_noalloc(kvg_cache *cache, int32_t layer, const i
 kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
                                 int32_t B, const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
 
+/* kvg_decode_attention for a batch whose sequences were given the same stored
+ * block (a pool-resident block grafted into each, Sec. 4.4: their page tables
+ * point at the same pages): the pages that rows of the batch have in common
+ * are read once for all of them instead of once per row, the rows' own pages
+ * as by kvg_decode_attention.  Rows are grouped by their first page; a group's
+ * common pages are the leading ones that all its sequences have.  Nothing has
+ * to be declared, and a batch without common pages, or with so few that
+ * reading them again costs less, is kvg_decode_attention.
+ * Arguments, results (within the rounding of the merge; bitwise reproducible
+ * for the same batch) and errors as for kvg_decode_attention. */
+kvg_status kvg_decode_attention_shared(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, int32_t B,
+                                       const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
+
 /* ------------------------------------------------------------- digest -- */
 
 /* SHA-256 (FIPS 180-4) on the GPU.

@@ -656,8 +656,10 @@ struct Merged {
 };
 constexpr int kCombineMaxThreads = 512;
 
-template <int D, int COLS>
-__device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, int col0, int b, int lr) {
+// SHARED: the row's partials over shared pages follow the decode's own.
+template <int D, int COLS, bool SHARED = false>
+__device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, int col0, int b, int lr,
+                                                 const SharedParts *sp = nullptr) {
     constexpr int LANES = COLS / 4;
     __shared__ float4 sum_o[kCombineMaxThreads];
     __shared__ float sum_l[kCombineMaxThreads / LANES];
@@ -668,7 +670,8 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     const int grp = lr >= p.layer1;
     const int32_t *pref = p.rows[grp].pref_tiles;
     const int64_t Tb = pref[b + 1] - pref[b];
-    if (Tb <= 0) {  // the whole block
+    const int n_shared = SHARED ? sp->splits[b] : 0;
+    if (Tb + n_shared <= 0) {  // the whole block
         after_previous();
         return res;
     }
@@ -676,15 +679,29 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     const int64_t unit = ((int64_t)lr * p.B + b) * p.n_kv_heads + g;
     const int64_t first = (int64_t)g * Tb +  // of the group's tiles
                           (int64_t)p.n_kv_heads * ((int64_t)(lr - (grp ? p.layer1 : 0)) * pref[p.B] + pref[b]);
-    const int64_t wa = warp_of(first, T, W);
-    const int n = (int)(warp_of(first + Tb - 1, T, W) - wa) + 1;
+    const int64_t wa = Tb > 0 ? warp_of(first, T, W) : 0;
+    const int n_own = Tb > 0 ? (int)(warp_of(first + Tb - 1, T, W) - wa) + 1 : 0, n = n_own + n_shared;
     const int64_t slot = unit + wa + (grp ? p.n_warps[0] : 0);
     const float2 *ml = p.part_ml + slot * G + hh;
     const float4 *po = reinterpret_cast<const float4 *>(p.part_o + (slot * G + hh) * D + col0) + d4;
     const int64_t step = (int64_t)G * (D / 4);  // float4 between consecutive partials
+    auto shared_slot = [&](int i) {
+        const int64_t u = (int64_t)(i - n_own) * sp->units + p.qlayers[lr] * p.n_kv_heads + g;
+        return sp->at[b] + u * sp->rows[b] + hh;
+    };
+    auto ml_at = [&](int i) {
+        if constexpr (SHARED)
+            if (i >= n_own) return sp->part_ml[shared_slot(i)];
+        return ml[(int64_t)i * G];
+    };
+    auto o_at = [&](int i) {
+        if constexpr (SHARED)
+            if (i >= n_own) return reinterpret_cast<const float4 *>(sp->part_o + shared_slot(i) * D + col0)[d4];
+        return po[i * step];
+    };
     after_previous();
     float M = -INFINITY;
-    for (int i = threadIdx.x & 31; i < n; i += 32) M = fmaxf(M, ml[(int64_t)i * G].x);
+    for (int i = threadIdx.x & 31; i < n; i += 32) M = fmaxf(M, ml_at(i).x);
 #pragma unroll
     for (int x = 16; x; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
     res.M = M;
@@ -697,8 +714,8 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * R;
                 if (i < n) {
-                    x[u] = ml[(int64_t)i * G];
-                    v[u] = po[i * step];
+                    x[u] = ml_at(i);
+                    v[u] = o_at(i);
                 }
             }
 #pragma unroll
@@ -732,19 +749,33 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     return res;
 }
 
-template <int D, int COLS>
-__global__ void __launch_bounds__(kCombineMaxThreads) combine_kernel(const DecodeParams p) {
-    constexpr int PARTS = D / COLS;
-    const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
-    const Merged m = merge_partials<D, COLS>(p, h, col0, b, lr);
+// (o / l) vscale of a head's columns as bf16 (SHARED: a sum that is NaN gives NaN).
+template <int D, int COLS, bool SHARED = false>
+__device__ __forceinline__ void store_merged(const DecodeParams &p, const Merged &m, int h, int col0, int b, int lr) {
     if (threadIdx.x >= COLS / 4) return;
     float r[4] = {m.o.x, m.o.y, m.o.z, m.o.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = m.L > 0.f ? __fdiv_rn(r[e], m.L) * p.vscale : 0.f;
+    for (int e = 0; e < 4; ++e) r[e] = (SHARED ? m.L != 0.f : m.L > 0.f) ? __fdiv_rn(r[e], m.L) * p.vscale : 0.f;
     const __nv_bfloat162 lo = __floats2bfloat162_rn(r[0], r[1]), hi = __floats2bfloat162_rn(r[2], r[3]);
     uint2 *out = reinterpret_cast<uint2 *>(
         p.out + ((int64_t)(p.qlayers[lr] * p.q_row_stride_b + p.b0 + b) * p.n_q_heads + h) * D + col0);
     out[threadIdx.x] = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+}
+
+template <int D, int COLS>
+__global__ void __launch_bounds__(kCombineMaxThreads) combine_kernel(const DecodeParams p) {
+    constexpr int PARTS = D / COLS;
+    const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
+    store_merged<D, COLS>(p, merge_partials<D, COLS>(p, h, col0, b, lr), h, col0, b, lr);
+}
+
+// The same for rows that read some of their pages together (kvg_decode_attention_shared).
+template <int D, int COLS>
+__global__ void __launch_bounds__(kCombineMaxThreads)
+    combine_shared_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ SharedParts sp) {
+    constexpr int PARTS = D / COLS;
+    const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
+    store_merged<D, COLS, true>(p, merge_partials<D, COLS, true>(p, h, col0, b, lr, &sp), h, col0, b, lr);
 }
 
 // The same merge for a split decode: the unit's partials give (M, L, O) for
@@ -934,7 +965,7 @@ cudaError_t launch_decode(int head_dim, int group, bool fp8, const DecodeParams 
 // Threads of a combine block over `cols` columns of a head: a group of cols / 4
 // lanes per up to four partials of the row with the most of them (the loads
 // one thread keeps in flight).
-static int combine_threads(int cols, const DecodeParams &p) {
+static int combine_threads(int cols, const DecodeParams &p, int n_shared = 0) {
     int64_t most = 1;
     for (int g = 0; g < kMaxWindowGroups; ++g) {
         if (p.group_tiles(g) <= 0) continue;
@@ -943,6 +974,7 @@ static int combine_threads(int cols, const DecodeParams &p) {
             tb = std::max<int64_t>(tb, p.rows[g].pref_tiles[b + 1] - p.rows[g].pref_tiles[b]);
         most = std::max(most, tb * p.n_warps[g] / p.group_tiles(g) + 2);
     }
+    most += n_shared;
     const int lanes = cols / 4;
     int threads = std::max(lanes, 32);
     while (threads < kCombineMaxThreads && (int64_t)(threads / lanes) * 4 < most) threads *= 2;
@@ -962,6 +994,22 @@ cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaSt
         case 256:
             return launch_after(p.state ? combine_state_kernel<256>
                                         : narrow ? combine_kernel<256, 64> : combine_kernel<256, 256>, grid, n, 0, s, p);
+    }
+    return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, int n_sm,
+                                  cudaStream_t s) {
+    const bool narrow = (int64_t)p.n_q_heads * p.B * p.n_layers_run <= n_sm;
+    const int cols = narrow ? 64 : head_dim;
+    const dim3 grid(p.n_q_heads * (head_dim / cols), p.B, p.n_layers_run);
+    const int n = combine_threads(cols, p, *std::max_element(parts.splits, parts.splits + p.B));
+    switch (head_dim) {
+        case 64: return launch_after(combine_shared_kernel<64, 64>, grid, n, 0, s, p, parts);
+        case 128:
+            return launch_after(narrow ? combine_shared_kernel<128, 64> : combine_shared_kernel<128, 128>, grid, n, 0, s, p, parts);
+        case 256:
+            return launch_after(narrow ? combine_shared_kernel<256, 64> : combine_shared_kernel<256, 256>, grid, n, 0, s, p, parts);
     }
     return cudaErrorInvalidValue;
 }

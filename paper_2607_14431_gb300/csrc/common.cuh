@@ -377,10 +377,23 @@ struct PromptParams {
     int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
     int32_t splits[kMaxBatchPerLaunch];    // key ranges that a query tile's items divide
     int64_t part0[kMaxBatchPerLaunch];     // first partial result
+    int32_t part_units;                    // layers of q x KV heads
     float *part_o;                         // [slots][D]
     float2 *part_ml;                       // [slots] (m, l)
     int32_t member[kMaxBatchPerLaunch];    // shared: batch row of each member
     int32_t lo[kMaxBatchPerLaunch];        // shared: first slot that it attends to
+};
+
+// Where the combine of a decode finds its rows' partials over the pages that
+// they share with other rows: of batch row b (of the launch), query head h of
+// layer ql and key range i < splits[b] at slot at[b] + (i * units + ql * Hkv +
+// h / G) * rows[b] + h % G.
+struct SharedParts {
+    const float *part_o;   // [slots][D]
+    const float2 *part_ml; // [slots]
+    int32_t units;         // layers of q x KV heads
+    int32_t rows[kMaxBatchPerLaunch], splits[kMaxBatchPerLaunch];
+    int64_t at[kMaxBatchPerLaunch];
 };
 
 // -------------------------------------------------------------- launchers --
@@ -509,6 +522,9 @@ cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, boo
 cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuuint64_t *dims,
                               const cuuint64_t *strides, const cuuint32_t *box);
 cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaStream_t s);
+// The combine with the partials of the rows' shared pages beside the decode's.
+cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, int n_sm,
+                                  cudaStream_t s);
 bool decode_supported(int head_dim, int group, bool fp8 = false);
 int decode_tile_tokens(int head_dim, bool fp8, int page_size);
 int decode_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);

@@ -141,9 +141,10 @@ __device__ __forceinline__ int64_t q_row(const PromptParams &p, const Item &it, 
            (row & ((1 << it.gs) - 1));
 }
 // Slot of a row's partial result.
-__device__ __forceinline__ int64_t part_slot(const PromptParams &p, int b, int gs, int split, int unit, int row) {
-    const int64_t n = (int64_t)(p.first[b + 1] - p.first[b]) << gs;
-    return p.part0[b] + ((int64_t)split * p.n_units + unit) * n + row;
+__device__ __forceinline__ int64_t part_slot(const PromptParams &p, const Item &it, int split, int row) {
+    const int64_t n = (int64_t)(p.first[it.b + 1] - p.first[it.b]) << it.gs;
+    const int unit = p.qlayers[it.lr] * p.n_kv_heads + it.g;
+    return p.part0[it.b] + ((int64_t)split * p.part_units + unit) * n + row;
 }
 
 __device__ __forceinline__ int search(const int32_t *first, int n, int64_t at) {
@@ -180,7 +181,7 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     int ka, kb, col;
     tile_of(p, from, ka, col);
     tile_of(p, it.last_slot, kb, col);
-    const int len = kb + 1 - ka;
+    const int len = max(0, kb + 1 - ka);  // (a shared block may end before the rows' windows)
     it.k0 = ka + (int)((int64_t)len * it.split / p.splits[b]);
     it.k1 = ka + (int)((int64_t)len * (it.split + 1) / p.splits[b]);
     return it;
@@ -303,10 +304,10 @@ __device__ __noinline__ void repair(const PromptParams &p, const Item &it, int f
         float o[N], m, l;
         attend_row<D, FP8>(p, it, row, f, l_, o, m, l);
         if (partial) {
-            const int64_t at = part_slot(p, it.b, it.gs, it.split, it.lr * p.n_kv_heads + it.g, row);
+            const int64_t at = part_slot(p, it, it.split, row);
 #pragma unroll
             for (int e = 0; e < N; ++e) p.part_o[at * D + lane * N + e] = o[e];
-            if (lane == 0) p.part_ml[at] = make_float2(m, l);
+            if (lane == 0) p.part_ml[at] = make_float2(l == l ? m : 0.f, l);
         } else {
             const float inv = p.vscale / l;
             uint32_t *out = reinterpret_cast<uint32_t *>(p.out + q_row(p, it, row) * D + lane * N);
@@ -727,8 +728,9 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             int64_t at = 0;
             float inv = 1.f;
             if (mine && partial) {
-                at = part_slot(p, it.b, it.gs, it.split, it.lr * p.n_kv_heads + it.g, row);
-                p.part_ml[at] = make_float2(m * c, l);
+                at = part_slot(p, it, it.split, row);
+                // (scores that are all NaN leave m at -inf, which would read as no column)
+                p.part_ml[at] = make_float2(l == l ? m * c : 0.f, l);
             } else if (mine) {
                 at = q_row(p, it, row);
                 inv = __fdiv_rn(p.vscale, l);
@@ -786,9 +788,9 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
     it.lr = unit / p.n_kv_heads;
     it.g = unit % p.n_kv_heads;
     float M = -INFINITY, L = 0.f, o[N] = {};
-    for (int i = 0; i < p.splits[it.b]; ++i) M = fmaxf(M, p.part_ml[part_slot(p, it.b, gs, i, unit, row)].x);
+    for (int i = 0; i < p.splits[it.b]; ++i) M = fmaxf(M, p.part_ml[part_slot(p, it, i, row)].x);
     for (int i = 0; i < p.splits[it.b]; ++i) {
-        const int64_t slot = part_slot(p, it.b, gs, i, unit, row);
+        const int64_t slot = part_slot(p, it, i, row);
         const float2 ml = p.part_ml[slot];
         if (ml.y == 0.f) continue;
         const float a = exp2f(ml.x - M);

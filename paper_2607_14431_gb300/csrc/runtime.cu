@@ -15,6 +15,7 @@
 #include <cstdio>
 #include <cstring>
 #include <deque>
+#include <memory>
 #include <mutex>
 #include <new>
 #include <string>
@@ -2283,9 +2284,10 @@ static std::vector<WindowGroup> layer_parts(const kvg_cache *c, int32_t layer) {
 // workers).
 // page_begin / page_end: only the sequence's pages [page_begin, page_end)
 // are read (a split decode over a slot range); the defaults read them all.
+// row_begin: the first page of each batch row instead.
 static kvg_status plan_decode(const kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B, int G, int w_max,
                               std::vector<DecodeParams> *plan, int32_t page_begin = 0,
-                              int32_t page_end = INT32_MAX) {
+                              int32_t page_end = INT32_MAX, const int32_t *row_begin = nullptr) {
     const kvg_dims &d = c->dims;
     const int TOK = decode_tile_tokens(d.head_dim, d.kv_dtype == KVG_KV_E4M3, d.page_size);
     const int tpp = (d.page_size + TOK - 1) / TOK;
@@ -2320,8 +2322,9 @@ static kvg_status plan_decode(const kvg_cache *c, int32_t layer, const int32_t *
                     int32_t pg = 0, row = 0;
                     if (part.window > 0) window_start(c, sq, part.window, &pg, &row);
                     int32_t t0 = pg * tpp + row / TOK, lo = row % TOK;
-                    if (page_begin > 0 && (int64_t)page_begin * tpp > t0) {
-                        t0 = page_begin * tpp;
+                    const int32_t begin = row_begin ? row_begin[b0 + i] : page_begin;
+                    if (begin > 0 && (int64_t)begin * tpp > t0) {
+                        t0 = begin * tpp;
                         lo = 0;
                     }
                     const int32_t t1 = std::min(np, page_end) * tpp;
@@ -2375,24 +2378,61 @@ extern "C" kvg_status kvg_cache_set_layer_windows(kvg_cache *c, const int32_t *w
     return KVG_OK;
 }
 
+// The split partials are shared by every attention of the cache: a call on
+// another stream than the previous one waits for that one's last kernel.
+static cudaError_t use_partials(kvg_cache *c, cudaStream_t st) {
+    if (!c->part_ev)
+        if (cudaError_t e = cudaEventCreateWithFlags(&c->part_ev, cudaEventDisableTiming); e != cudaSuccess) return e;
+    return c->part_used && st != c->part_stream ? cudaStreamWaitEvent(st, c->part_ev, 0) : cudaSuccess;
+}
+static kvg_status used_partials(kvg_cache *c, cudaStream_t st) {
+    KVG_CUDA(cudaEventRecord(c->part_ev, st));
+    c->part_stream = st;
+    c->part_used = true;
+    return KVG_OK;
+}
+
+// Arguments of a decode; *G: the group.
+static kvg_status check_decode(const char *what, const kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B,
+                               const void *q, int32_t n_q_heads, const void *out, int *G) {
+    if (!c || !seq_ids || !q || !out) return fail(KVG_ERR_ARG, "%s: null argument", what);
+    const kvg_dims &d = c->dims;
+    if (layer < -1 || layer >= d.n_layers) return fail(KVG_ERR_ARG, "bad layer %d", layer);
+    if (B <= 0 || B > 4096) return fail(KVG_ERR_ARG, "B must be in [1, 4096]");
+    if (n_q_heads <= 0 || n_q_heads % d.n_kv_heads) return fail(KVG_ERR_ARG, "n_q_heads must be a multiple of n_kv_heads");
+    *G = n_q_heads / d.n_kv_heads;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    if (!decode_supported(d.head_dim, *G, fp8))
+        return fail(KVG_ERR_ARG, "unsupported head_dim %d / group %d%s", d.head_dim, *G, fp8 ? " (fp8)" : "");
+    if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)
+        return fail(KVG_ERR_ARG, "q/out/state must be 16-byte aligned");
+    for (int32_t b = 0; b < B; ++b)
+        if (seq_ids[b] < 0 || seq_ids[b] >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", seq_ids[b]);
+    return KVG_OK;
+}
+
+// The fields of a planned launch that the call gives.
+static void decode_call(const kvg_cache *c, const void *q, int32_t n_q_heads, void *out, float scale, int32_t B,
+                        int w_max, DecodeParams *p) {
+    const bool fp8 = c->dims.kv_dtype == KVG_KV_E4M3;
+    set_decode_warps(p, w_max);
+    p->n_q_heads = n_q_heads;
+    p->q = static_cast<const __nv_bfloat16 *>(q);
+    p->q_row_stride_b = B;
+    p->qscale = scale * 1.4426950408889634f * (fp8 ? c->dims.k_scale : 1.f);
+    p->vscale = fp8 ? c->dims.v_scale : 1.f;
+    p->out = static_cast<__nv_bfloat16 *>(out);
+}
+
 // Decode attention over the sequences' pages [page_begin, page_end): bf16
 // out (state == null), or the softmax state written or merged into `state`.
 static kvg_status decode_impl(const char *what, kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B,
                               const void *q, int32_t n_q_heads, void *out, float scale, void *stream,
                               int32_t page_begin, int32_t page_end, float *state, int32_t merge) {
-    if (!c || !seq_ids || !q || !(out || state)) return fail(KVG_ERR_ARG, "%s: null argument", what);
+    int G = 0;
+    if (kvg_status r = check_decode(what, c, layer, seq_ids, B, q, n_q_heads, out ? out : state, &G); r != KVG_OK) return r;
     const kvg_dims &d = c->dims;
-    if (layer < -1 || layer >= d.n_layers) return fail(KVG_ERR_ARG, "bad layer %d", layer);
-    if (B <= 0 || B > 4096) return fail(KVG_ERR_ARG, "B must be in [1, 4096]");
-    if (n_q_heads <= 0 || n_q_heads % d.n_kv_heads) return fail(KVG_ERR_ARG, "n_q_heads must be a multiple of n_kv_heads");
-    const int G = n_q_heads / d.n_kv_heads;
     const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
-    if (!decode_supported(d.head_dim, G, fp8))
-        return fail(KVG_ERR_ARG, "unsupported head_dim %d / group %d%s", d.head_dim, G, fp8 ? " (fp8)" : "");
-    if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(state)) & 15)
-        return fail(KVG_ERR_ARG, "q/out/state must be 16-byte aligned");
-    for (int32_t b = 0; b < B; ++b)
-        if (seq_ids[b] < 0 || seq_ids[b] >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", seq_ids[b]);
     DeviceGuard g(c->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int w_max = decode_max_warps(d.head_dim, G, fp8, d.page_size, c->n_sm);
@@ -2401,29 +2441,19 @@ static kvg_status decode_impl(const char *what, kvg_cache *c, int32_t layer, con
     kvg_status r = plan_decode(c, layer, seq_ids, B, G, w_max, &plan, page_begin, page_end);
     if (r != KVG_OK) return r;
     const size_t slots = (size_t)decode_slots(plan, w_max);
-    if (!c->part_ev) KVG_CUDA(cudaEventCreateWithFlags(&c->part_ev, cudaEventDisableTiming));
-    if (c->part_used && st != c->part_stream) KVG_CUDA(cudaStreamWaitEvent(st, c->part_ev, 0));
+    KVG_CUDA(use_partials(c, st));
     KVG_CUDA(c->part_o.ensure(slots * G * d.head_dim * sizeof(float)));
     KVG_CUDA(c->part_ml.ensure(slots * G * sizeof(float2)));
     for (DecodeParams &p : plan) {
-        set_decode_warps(&p, w_max);
-        p.n_q_heads = n_q_heads;
-        p.q = static_cast<const __nv_bfloat16 *>(q);
-        p.q_row_stride_b = B;
-        p.qscale = scale * 1.4426950408889634f * (fp8 ? d.k_scale : 1.f);
-        p.vscale = fp8 ? d.v_scale : 1.f;
+        decode_call(c, q, n_q_heads, out, scale, B, w_max, &p);
         p.part_o = static_cast<float *>(c->part_o.ptr);
         p.part_ml = static_cast<float2 *>(c->part_ml.ptr);
-        p.out = static_cast<__nv_bfloat16 *>(out);
         p.state = state;
         p.state_merge = merge;
         KVG_CUDA(launch_decode(d.head_dim, G, fp8, p, c->pool_map, st));
         KVG_CUDA(launch_combine(d.head_dim, p, c->n_sm, st));
     }
-    KVG_CUDA(cudaEventRecord(c->part_ev, st));
-    c->part_stream = st;
-    c->part_used = true;
-    return KVG_OK;
+    return used_partials(c, st);
 }
 
 extern "C" kvg_status kvg_decode_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B,
@@ -2464,20 +2494,6 @@ extern "C" kvg_status kvg_decode_state_finish(const float *state, int64_t n_rows
 }
 
 // -------------------------------------------------------- prompt attention --
-
-// The split partials are shared by every attention of the cache: a call on
-// another stream than the previous one waits for that one's last kernel.
-static cudaError_t use_partials(kvg_cache *c, cudaStream_t st) {
-    if (!c->part_ev)
-        if (cudaError_t e = cudaEventCreateWithFlags(&c->part_ev, cudaEventDisableTiming); e != cudaSuccess) return e;
-    return c->part_used && st != c->part_stream ? cudaStreamWaitEvent(st, c->part_ev, 0) : cudaSuccess;
-}
-static kvg_status used_partials(kvg_cache *c, cudaStream_t st) {
-    KVG_CUDA(cudaEventRecord(c->part_ev, st));
-    c->part_stream = st;
-    c->part_used = true;
-    return KVG_OK;
-}
 
 static void prompt_params(const kvg_cache *c, const void *q, int32_t n_q_heads, void *out, float scale,
                           PromptParams *p) {
@@ -2562,15 +2578,22 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
         }
     }
     int64_t slots = 0;
-    p->item0[0] = 0;
     for (size_t i = 0; i < rows.size(); ++i) {
         const int32_t s = (int32_t)std::max(1.0, std::ceil(rows[i].longest / best_len - 1e-9));
         p->splits[i] = s;
-        p->item0[i + 1] = p->item0[i] + (int32_t)(rows[i].tiles * s * p->n_units);
         p->part0[i] = slots;
-        if (s > 1 || always) slots += work[i].rows * p->n_units * s;
+        if (s > 1 || always) slots += work[i].rows * p->part_units * s;
     }
     return slots;
+}
+
+// Prefix sums of the items of a launch over p->n_units.
+static void prompt_items(int64_t tile_rows, int G, PromptParams *p) {
+    p->item0[0] = 0;
+    for (int32_t i = 0; i < p->n_seq; ++i) {
+        const int64_t rows = (int64_t)(p->first[i + 1] - p->first[i]) * G;
+        p->item0[i + 1] = p->item0[i] + (int32_t)((rows + tile_rows - 1) / tile_rows * p->splits[i] * p->n_units);
+    }
 }
 
 static kvg_status prompt_partials(kvg_cache *c, int64_t slots, PromptParams *p) {
@@ -2587,23 +2610,16 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
                                            int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
                                            void *stream) {
     Trace trace_("kvg_prompt_attention");
-    if (!c || !seq_ids || !n_rows || !q || !out) return fail(KVG_ERR_ARG, "kvg_prompt_attention: null argument");
+    if (!n_rows) return fail(KVG_ERR_ARG, "kvg_prompt_attention: null argument");
+    int G = 0;
+    if (kvg_status r = check_decode("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, &G); r != KVG_OK) return r;
     const kvg_dims &d = c->dims;
-    if (layer < -1 || layer >= d.n_layers) return fail(KVG_ERR_ARG, "bad layer %d", layer);
-    if (B <= 0 || B > 4096) return fail(KVG_ERR_ARG, "B must be in [1, 4096]");
-    if (n_q_heads <= 0 || n_q_heads % d.n_kv_heads) return fail(KVG_ERR_ARG, "n_q_heads must be a multiple of n_kv_heads");
-    const int G = n_q_heads / d.n_kv_heads;
     const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
-    if (!decode_supported(d.head_dim, G, fp8))
-        return fail(KVG_ERR_ARG, "unsupported head_dim %d / group %d%s", d.head_dim, G, fp8 ? " (fp8)" : "");
-    if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)
-        return fail(KVG_ERR_ARG, "q/out must be 16-byte aligned");
     const int64_t P = d.page_size;
     int64_t total = 0;
     bool single = true;
     for (int32_t b = 0; b < B; ++b) {
         const int32_t sq = seq_ids[b];
-        if (sq < 0 || sq >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", sq);
         if (n_rows[b] < 0 || n_rows[b] > c->n_slots[sq])
             return fail(KVG_ERR_ARG, "seq %d: %d query rows of %d slots", sq, n_rows[b], c->n_slots[sq]);
         // the rows' slots must all be valid: no graft's unfilled page tail among them
@@ -2624,6 +2640,7 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
     PromptParams p{};
     prompt_params(c, q, n_q_heads, out, scale, &p);
     p.q_rows = total;
+    p.part_units = (layer < 0 ? d.n_layers : 1) * d.n_kv_heads;
     KVG_CUDA(use_partials(c, st));
     for (const WindowGroup &part : layer_parts(c, layer)) {
         prompt_layers(part, &p);
@@ -2657,10 +2674,176 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
             if (p.n_seq == 0) continue;
             const int streams = prompt_streams(d.head_dim, most);
             const int64_t slots = plan_prompt(c, work, G, kPromptRows * streams, false, &p);
+            prompt_items(kPromptRows * streams, G, &p);
             if (kvg_status r = prompt_partials(c, slots, &p); r != KVG_OK) return r;
             KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
             if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
         }
+    }
+    return used_partials(c, st);
+}
+
+// ---------------------------------------- decode of a batch with common pages --
+
+// Batch rows whose sequences begin with the same pages.
+struct CommonPages {
+    std::vector<int32_t> rows;
+    int32_t pages;  // leading pages that all of them have, equally filled
+};
+
+static std::vector<CommonPages> common_pages(const kvg_cache *c, const int32_t *seq_ids, int32_t B) {
+    std::vector<CommonPages> groups;
+    std::unordered_map<int32_t, size_t> by_page;  // first page -> group
+    for (int32_t b = 0; b < B; ++b) {
+        const auto &sp = c->seq_pages[seq_ids[b]];
+        if (sp.empty()) continue;
+        const auto it = by_page.emplace(sp[0], groups.size());
+        if (it.second) {
+            groups.push_back({{b}, (int32_t)sp.size()});
+            continue;
+        }
+        CommonPages &g = groups[it.first->second];
+        const int32_t first = seq_ids[g.rows[0]];
+        const auto &fp = c->seq_pages[first];
+        const int32_t most = std::min<int32_t>(g.pages, (int32_t)sp.size());
+        int32_t n = 0;
+        while (n < most && sp[n] == fp[n] && c->seq_fill[seq_ids[b]][n] == c->seq_fill[first][n]) ++n;
+        g.rows.push_back(b);
+        g.pages = n;
+    }
+    return groups;
+}
+
+// Bytes of keys and values not read again from which a group is worth it.
+constexpr double kSharedMinBytes = 1.0;
+
+extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B,
+                                                  const void *q, int32_t n_q_heads, void *out, float scale,
+                                                  void *stream) {
+    Trace trace_("kvg_decode_attention_shared");
+    if (!out) return fail(KVG_ERR_ARG, "null argument");
+    int G = 0;
+    if (kvg_status r = check_decode("kvg_decode_attention_shared", c, layer, seq_ids, B, q, n_q_heads, out, &G); r != KVG_OK)
+        return r;
+    const kvg_dims &d = c->dims;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    const int64_t P = d.page_size;
+    const int32_t n_run = layer < 0 ? d.n_layers : 1;
+    std::vector<CommonPages> groups = common_pages(c, seq_ids, B);
+    // a group's pages are read once instead of once per row where that saves enough
+    const double page_bytes = 2.0 * n_run * (double)c->page_bytes;
+    groups.erase(std::remove_if(groups.begin(), groups.end(), [&](const CommonPages &g) {
+        return (double)(g.rows.size() - 1) * g.pages * page_bytes < kSharedMinBytes;
+    }), groups.end());
+    if (groups.empty())
+        return decode_impl("kvg_decode_attention_shared", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0,
+                           INT32_MAX, nullptr, 0);
+    DeviceGuard g(c->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // ---- the common pages: launches of up to kMaxBatchPerLaunch rows
+    struct Launch {
+        PromptParams p;
+        std::vector<PromptWork> work;
+        int64_t part_base, most;
+        int streams;
+    };
+    std::vector<int32_t> row_begin(B, 0);
+    std::vector<int32_t> row_rows(B, 0), row_splits(B, 0);
+    std::vector<int64_t> row_at(B, 0);
+    std::vector<std::unique_ptr<Launch>> launches;
+    int64_t shared_slots = 0;
+    auto plan = [&](Launch &l) {
+        PromptParams &p = l.p;
+        l.streams = prompt_streams(d.head_dim, l.most);
+        l.part_base = shared_slots;
+        shared_slots += plan_prompt(c, l.work, G, kPromptRows * l.streams, true, &p);
+        for (int32_t i = 0; i < p.n_seq; ++i)
+            for (int32_t k = p.first[i]; k < p.first[i + 1]; ++k) {
+                const int32_t b = p.member[k];
+                row_at[b] = l.part_base + p.part0[i] + (int64_t)(k - p.first[i]) * G;
+                row_rows[b] = (p.first[i + 1] - p.first[i]) * G;
+                row_splits[b] = p.splits[i];
+            }
+    };
+    for (const CommonPages &gr : groups) {
+        for (size_t r0 = 0; r0 < gr.rows.size();) {
+            if (launches.empty() || launches.back()->p.first[launches.back()->p.n_seq] == kMaxBatchPerLaunch) {
+                if (!launches.empty()) plan(*launches.back());
+                launches.push_back(std::make_unique<Launch>());
+                PromptParams &p = launches.back()->p;
+                prompt_params(c, q, n_q_heads, out, scale, &p);
+                p.q_rows = B;
+                p.shared = 1;
+                p.n_units = p.part_units = n_run * d.n_kv_heads;
+            }
+            Launch &l = *launches.back();
+            PromptParams &p = l.p;
+            const int32_t i = p.n_seq++, k0 = p.first[i];
+            const int32_t n = (int32_t)std::min<size_t>(gr.rows.size() - r0, kMaxBatchPerLaunch - k0);
+            p.seq[i] = seq_ids[gr.rows[0]];
+            p.row0[i] = k0;
+            p.slot0[i] = (int32_t)(gr.pages * P - 1);
+            p.first[i + 1] = k0 + n;
+            for (int32_t k = 0; k < n; ++k) {
+                const int32_t b = gr.rows[r0 + k];
+                p.member[k0 + k] = b;
+                row_begin[b] = gr.pages;
+            }
+            l.work.push_back({(int64_t)n * G, 0, 0, p.slot0[i]});
+            l.most = std::max<int64_t>(l.most, (int64_t)n * G);
+            r0 += n;
+        }
+    }
+    plan(*launches.back());
+    // ---- the rows' own pages
+    const int w_max = decode_max_warps(d.head_dim, G, fp8, d.page_size, c->n_sm);
+    if (w_max <= 0) return fail(KVG_ERR_CUDA, "decode kernel cannot be made resident");
+    std::vector<DecodeParams> decode;
+    if (kvg_status r = plan_decode(c, layer, seq_ids, B, G, w_max, &decode, 0, INT32_MAX, row_begin.data()); r != KVG_OK)
+        return r;
+    const int64_t own_slots = decode_slots(decode, w_max) * G;
+    KVG_CUDA(use_partials(c, st));
+    KVG_CUDA(c->part_o.ensure((size_t)(own_slots + shared_slots) * d.head_dim * sizeof(float)));
+    KVG_CUDA(c->part_ml.ensure((size_t)(own_slots + shared_slots) * sizeof(float2)));
+    float *const part_o = static_cast<float *>(c->part_o.ptr);
+    float2 *const part_ml = static_cast<float2 *>(c->part_ml.ptr);
+    SharedParts parts{};
+    parts.part_o = part_o + own_slots * d.head_dim;
+    parts.part_ml = part_ml + own_slots;
+    parts.units = n_run * d.n_kv_heads;
+    for (const WindowGroup &part : layer_parts(c, layer)) {
+        for (auto &l : launches) {
+            PromptParams &p = l->p;
+            prompt_layers(part, &p);
+            p.part_o = part_o + (own_slots + l->part_base) * d.head_dim;
+            p.part_ml = part_ml + own_slots + l->part_base;
+            for (int32_t i = 0; i < p.n_seq; ++i) {
+                p.begin[i] = part.window > 0 ? p.slot0[i] + 1 : 0;
+                for (int32_t k = p.first[i]; k < p.first[i + 1]; ++k) {
+                    p.lo[k] = 0;
+                    if (part.window > 0) {
+                        int32_t pg, in_page;
+                        window_start(c, seq_ids[p.member[k]], part.window, &pg, &in_page);
+                        p.lo[k] = (int32_t)(pg * P + in_page);
+                        p.begin[i] = std::min(p.begin[i], p.lo[k]);
+                    }
+                }
+            }
+            prompt_items(kPromptRows * l->streams, G, &p);
+            KVG_CUDA(launch_prompt(d.head_dim, fp8, l->streams, p, c->prompt_map, st));
+        }
+    }
+    for (DecodeParams &p : decode) {
+        decode_call(c, q, n_q_heads, out, scale, B, w_max, &p);
+        p.part_o = part_o;
+        p.part_ml = part_ml;
+        KVG_CUDA(launch_decode(d.head_dim, G, fp8, p, c->pool_map, st));
+        for (int32_t i = 0; i < p.B; ++i) {
+            parts.rows[i] = row_rows[p.b0 + i];
+            parts.splits[i] = row_splits[p.b0 + i];
+            parts.at[i] = row_at[p.b0 + i];
+        }
+        KVG_CUDA(launch_combine_shared(d.head_dim, p, parts, c->n_sm, st));
     }
     return used_partials(c, st);
 }

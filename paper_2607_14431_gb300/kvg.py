@@ -117,6 +117,7 @@ _SIGNATURES = {
                                    _i32),
     "kvg_decode_state_finish": ([_vp, _i64, _i32, _vp, _vp], _i32),
     "kvg_prompt_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
+    "kvg_decode_attention_shared": ([_vp, _i32, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_digest": ([_vp, _u64, _i32, _u64, _vp, _vp], _i32),
     "kvg_sync": ([_vp, _vp, ctypes.c_double, _P(kvg_graft_report)], _i32),
     "kvg_selftest_bounded_wait": ([_vp, _u64, _vp], _i32),
@@ -400,6 +401,14 @@ def kvg_prompt_attention(cache, layer: int, seq_ids, n_rows, q_ptr: int, n_q_hea
     rows = (ctypes.c_int32 * len(seq_ids))(*n_rows)
     _check(lib().kvg_prompt_attention(cache, layer, ids, rows, len(seq_ids), q_ptr, n_q_heads, out_ptr, float(scale),
                                       _stream(stream)))
+
+
+def kvg_decode_attention_shared(cache, layer: int, seq_ids, q_ptr: int, n_q_heads: int, out_ptr: int, scale: float,
+                                stream=None):
+    """kvg_decode_attention that reads the pages which rows of the batch have in common once."""
+    ids = (ctypes.c_int32 * len(seq_ids))(*seq_ids)
+    _check(lib().kvg_decode_attention_shared(cache, layer, ids, len(seq_ids), q_ptr, n_q_heads, out_ptr, float(scale),
+                                             _stream(stream)))
 
 
 def kvg_digest(ptr: int, n: int, mode: int, page_bytes: int, out_ptr: int, stream=None):
