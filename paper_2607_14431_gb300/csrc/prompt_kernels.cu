@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kTile = 128;       // query rows of a stream, columns of a key tile
 constexpr int kMaskSlots = 16;   // key tiles whose column masks are kept
-constexpr int kConvertWarps = 2;
+constexpr int kConvertWarps = 4;
 // The running maximum that the weights refer to is moved only when a row's
 // maximum passes it by more than this (in powers of two): weights then reach
 // at most 2^8, which costs no precision in bf16 or fp16, and the accumulator
@@ -50,11 +50,17 @@ struct Cfg {
     static constexpr int CHUNK = BOXES * BOX;
     static constexpr int RAW = FP8 ? kTile * DC : 0; // an fp8 chunk as it is in the cache
     static constexpr int Q_BYTES = STREAMS * kTile * D * 2;
-    static constexpr int STAGES = D == 64 ? 8 : FP8 ? (Q_BYTES > 32768 ? 3 : 4) : Q_BYTES > 32768 ? 5 : 6;
-    static constexpr int RAW_STAGES = FP8 ? 4 : 0;
+    static constexpr int STAGES = D == 64 ? 8 : FP8 ? (Q_BYTES > 32768 ? 4 : 5) : Q_BYTES > 32768 ? 5 : 6;
+    static constexpr int RAW_STAGES = FP8 ? 2 : 0;
     static constexpr int SOFTMAX_WARPS = 4 * STREAMS;
-    static constexpr int LOAD_WARP = SOFTMAX_WARPS, MMA_WARP = LOAD_WARP + 1, CONVERT_WARP = MMA_WARP + 1;
+    static constexpr int LOAD_WARP = SOFTMAX_WARPS, MMA_WARP = LOAD_WARP + 1, TIDY_WARP = LOAD_WARP + 2, CONVERT_WARP = LOAD_WARP + 4;
     static constexpr int THREADS = 32 * (CONVERT_WARP + (FP8 ? kConvertWarps : 0));
+    // Registers of a softmax thread and of the others, moved between the
+    // warpgroups where the launch's even share is too few for a row of scores:
+    // 3 groups of 168 (200 + 200 + 96 of 504, or 224 + 136 + 136), 4 of 128 (176
+    // + 176 + 80 + 80 of 512).  (A call in the kernel would void it.)
+    static constexpr int MORE_REGS = THREADS == 512 ? 176 : THREADS == 384 ? (STREAMS == 2 ? 200 : 224) : 0;
+    static constexpr int FEWER_REGS = THREADS == 512 ? 80 : STREAMS == 2 ? 96 : 136;
     static constexpr int SMEM = Q_BYTES + STAGES * CHUNK + RAW_STAGES * RAW + 1024;  // + alignment slack
     static_assert(D <= 128 || STREAMS == 1, "tensor memory");
     static_assert(SMEM <= 230 * 1024, "shared memory");
@@ -62,8 +68,10 @@ struct Cfg {
 constexpr int kScoreCols = 0, kOutCols = 256;  // tensor memory: scores (and weights), outputs
 
 struct Bars {
-    uint64_t full[8], empty[8], raw_full[4], raw_empty[4];
-    uint64_t scores[2], weights[2], out[2];  // a score tile is there; its weights are; their product is added
+    uint64_t landed[8], freed[4];            // copies: there; (fp8) converted, their place is free
+    uint64_t ready[8], empty[8];             // chunks of the ring: may be multiplied; have been
+    uint64_t scores[2], out[2];              // a score tile is there; its weights' product is added
+    uint64_t weights[2][2];                  // the halves of its weights are there
     uint64_t queries, drained;
     uint32_t mask[kMaskSlots][4];            // valid columns of key tile j % kMaskSlots
     uint32_t tmem;
@@ -71,7 +79,7 @@ struct Bars {
 };
 
 // Bounded wait that also ends when another warp gave up.
-__device__ __noinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, DevStatus *status) {
+__device__ __forceinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, DevStatus *status) {
     const uint64_t t0 = global_timer_ns();
     for (uint32_t it = 1;; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
@@ -116,7 +124,7 @@ __device__ __forceinline__ int first_slot(const PromptParams &p, int tile) {
 }
 
 // First slot that the row at `slot` attends to.
-__device__ int window_first(const PromptParams &p, int b, int slot) {
+__device__ __forceinline__ int window_first(const PromptParams &p, int b, int slot) {
     if (p.window <= 0) return 0;
     if (!p.holes[b]) return max(0, slot - p.window + 1);
     // pages that are not full lie in between: count valid rows back
@@ -227,7 +235,7 @@ __device__ __forceinline__ const uint8_t *row_at(const PromptParams &p, const It
 
 // A warp: attention of one query row over slots [first, last].
 template <int D, bool FP8>
-__device__ __noinline__ void attend_row(const PromptParams &p, const Item &it, int row, int first, int last,
+__device__ __forceinline__ void attend_row(const PromptParams &p, const Item &it, int row, int first, int last,
                                         float (&o)[D / 32], float &m, float &l) {
     constexpr int N = D / 32;
     const int lane = threadIdx.x & 31;
@@ -270,7 +278,7 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
 // output rows that one reached over again.  (A not finite output whose masked
 // values are all finite is as it should be.)
 template <int D, bool FP8>
-__device__ __noinline__ void repair(const PromptParams &p, const Item &it, int first_row, bool bad, int lo, int hi,
+__device__ __forceinline__ void repair(const PromptParams &p, const Item &it, int first_row, bool bad, int lo, int hi,
                                     bool partial) {
     constexpr int N = D / 32;
     const int lane = threadIdx.x & 31;
@@ -317,31 +325,39 @@ __device__ __noinline__ void repair(const PromptParams &p, const Item &it, int f
     }
 }
 
+// Tiles land as K0, then K(j + 1) and V(j) in turn, the last V alone: whether
+// the i-th is a value tile, and of which key tile.
+__device__ __forceinline__ bool value_tile(int i, int n, int &j) {
+    const bool last = i == 2 * n - 1;
+    j = last ? n - 1 : i / 2 - 1;
+    return last || (i > 0 && i % 2 == 0);
+}
+
 // ------------------------------------------------------------------ kernel --
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1)
     prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map) {
     constexpr int D = C::D, DC = C::DC, NCH = C::NCH, STREAMS = C::STREAMS, STAGES = C::STAGES;
     constexpr bool FP8 = C::FP8;
+    constexpr int LANDS = FP8 ? C::RAW_STAGES : STAGES;  // the ring that copies land in
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ Bars s;
     uint8_t *const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     uint8_t *const ring = smem + C::Q_BYTES;
     uint8_t *const raw = ring + STAGES * C::CHUNK;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;  // uniform in the warp
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
-            mbar_init(&s.full[i], FP8 ? 32 * kConvertWarps : 1);
+            mbar_init(&s.ready[i], FP8 ? 32 * kConvertWarps : 1);
             mbar_init(&s.empty[i], 1);
         }
-        for (int i = 0; i < C::RAW_STAGES; ++i) {
-            mbar_init(&s.raw_full[i], 1);
-            mbar_init(&s.raw_empty[i], 32 * kConvertWarps);
-        }
+        for (int i = 0; i < LANDS; ++i) mbar_init(&s.landed[i], 1);
+        for (int i = 0; i < C::RAW_STAGES; ++i) mbar_init(&s.freed[i], 32 * kConvertWarps);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.scores[i], 1);
-            mbar_init(&s.weights[i], 128);
+            mbar_init(&s.weights[i][0], 128);
+            mbar_init(&s.weights[i][1], 128);
             mbar_init(&s.out[i], 1);
         }
         mbar_init(&s.queries, 32 * C::SOFTMAX_WARPS);
@@ -359,235 +375,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     const Item it = item_of(p, blockIdx.x, STREAMS * kTile);
     const int n = it.k1 - it.k0;
     const bool partial = p.splits[it.b] > 1 || p.shared;
-
-    if (warp == C::LOAD_WARP) {
-        // ---- keys and values of tile j: K0, then K(j + 1) and V(j) in turn
-        struct Pages {
-            int rows;       // valid rows of the lane's page in the tile
-            int32_t at;     // its first row in the pool, of the layer's keys
-            uint32_t bytes; // of a chunk's copies, all lanes'
-        };
-        const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
-        const int last_page = it.last_slot / p.page_size;
-        auto find = [&](int j) {
-            const int kt = it.k0 + j;
-            Pages r{0, 0, 0};
-            int pg, sub = 0;
-            if (p.pages_per_tile) {
-                pg = lane < p.pages_per_tile ? kt * p.pages_per_tile + lane : last_page + 1;
-            } else {
-                pg = lane == 0 ? kt / p.tiles_per_page : last_page + 1;
-                sub = kt % p.tiles_per_page * kTile;
-            }
-            if (pg <= last_page) {
-                const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
-                const int pid = p.page_table[e];
-                r.rows = min(p.pages_per_tile ? p.page_size : kTile, p.page_fill[e] - sub);
-                if (r.rows < 0) r.rows = 0;
-                if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
-                    record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
-                    r.rows = 0;
-                }
-                r.at = (int32_t)((int64_t)p.layers[it.lr] * 2 * plane +
-                                 ((int64_t)pid * p.n_kv_heads + it.g) * p.page_size + sub);
-            }
-            return r;
-        };
-        int chunk = 0;  // of the ring that the copies land in
-        constexpr int LANDS = FP8 ? C::RAW_STAGES : STAGES;
-        uint64_t *const landed = FP8 ? s.raw_full : s.full;
-        uint64_t *const freed = FP8 ? s.raw_empty : s.empty;
-        const int box_bytes = p.box_rows * 128;
-        auto copy = [&](const Pages &r, bool values) {
-            const int n_pages = __popc(__ballot_sync(0xffffffffu, r.rows > 0));
-            for (int c = 0; c < NCH; ++c, ++chunk) {
-                const int st = chunk % LANDS;
-                if (chunk >= LANDS && !wait_bar(s, &freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
-                if (lane == 0) {
-                    if (n_pages)
-                        mbar_arrive_expect_tx(&landed[st], n_pages * box_bytes * (FP8 ? 1 : C::BOXES));
-                    else
-                        mbar_arrive(&landed[st]);
-                }
-                __syncwarp();
-                if (r.rows > 0) {
-                    const int32_t y = r.at + (values ? (int32_t)plane : 0);
-                    uint8_t *dst = (FP8 ? raw + st * C::RAW : ring + st * C::CHUNK) + lane * p.page_rows * 128;
-                    if constexpr (FP8) {
-                        tma_load_2d(dst, &map, c * DC, y, &landed[st]);
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < C::BOXES; ++x)
-                            tma_load_2d(dst + x * C::BOX, &map, c * DC + 64 * x, y, &landed[st]);
-                    }
-                }
-            }
-            return true;
-        };
-        auto note_mask = [&](const Pages &r, int j) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int a = lane * p.page_rows - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
-                uint32_t bits = 0;
-                if (r.rows > 0 && a < 32 && e > 0)
-                    bits = (e >= 32 ? ~0u : (1u << e) - 1) & ~(a > 0 ? (1u << a) - 1 : 0u);
-                bits = __reduce_or_sync(0xffffffffu, bits);
-                if (lane == 0) s.mask[j % kMaskSlots][w] = bits;
-            }
-            __syncwarp();
-        };
-        Pages now = find(0), next = now;
-        bool ok = n > 0;
-        if (ok) {
-            note_mask(now, 0);
-            ok = copy(now, false);
-        }
-        if (n > 1) next = find(1);
-        for (int j = 0; ok && j < n; ++j) {
-            if (j + 1 < n) {
-                note_mask(next, j + 1);
-                ok = copy(next, false);
-            }
-            if (ok) ok = copy(now, true);
-            now = next;
-            if (j + 2 < n) next = find(j + 2);
-        }
-        if (!ok && n > 0)  // gave up: no copy may still be landing when the CTA ends
-            for (int c = max(0, chunk - LANDS); c < chunk; ++c) (void)mbar_wait_bounded(&landed[c % LANDS], (c / LANDS) & 1);
-    } else if (warp == C::MMA_WARP) {
-        // ---- products: one lane issues; the warp clears value rows that are not valid
-        constexpr uint32_t QK = mma_desc(kTile, kTile, FP8, false), PV = mma_desc(kTile, DC, FP8, true);
-        const uint32_t qk = QK | (p.negate ? kMmaNegateA : 0u);
-        const uint32_t q_s = smem_addr(smem), ring_s = smem_addr(ring);
-        bool ok = n > 0 && wait_bar(s, &s.queries, 0, p.status);
-        tc_after_sync();
-        int chunk = 0;
-        auto arrived = [&](int c) { return wait_bar(s, &s.full[c % STAGES], (c / STAGES) & 1, p.status); };
-        // S = Q K^T of a stream into score columns `buf`, keys in chunks from c0
-        auto scores = [&](int stream, int buf, int c0) {
-            if (lane == 0) {
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t k_s = ring_s + (c0 + ks / (DC / 16)) % STAGES * C::CHUNK + ks % (DC / 16) / 4 * C::BOX;
-                    mma_ss(tmem + kScoreCols + buf * kTile,
-                           smem_desc(q_s + stream * (kTile * D * 2) + ks / 4 * C::BOX + ks % 4 * 32, 0, 1024),
-                           smem_desc(k_s + ks % 4 * 32, 0, 1024), qk, ks > 0);
-                }
-                mma_commit(&s.scores[buf]);
-            }
-        };
-        // O += P V of a stream, weights in score columns `buf`, chunk c of the values at ring chunk at
-        auto product = [&](int stream, int buf, int c, int at, bool add) {
-            if (lane == 0) {
-                const uint32_t v_s = ring_s + at % STAGES * C::CHUNK;
-#pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks)
-                    mma_ts(tmem + kOutCols + stream * kTile + c * DC, tmem + kScoreCols + buf * kTile + ks * 8,
-                           smem_desc(v_s + ks * 2048, C::BOX, 1024), PV, add || ks > 0);
-            }
-        };
-        auto release = [&](int c) {
-            if (lane == 0) mma_commit(&s.empty[c % STAGES]);
-        };
-        // the value rows of tile j that are not valid hold anything: zero weights must meet zeros
-        auto clear = [&](int j, int at) {
-            if constexpr (!FP8) {
-                const uint32_t *m = s.mask[j % kMaskSlots];
-                if ((m[0] & m[1] & m[2] & m[3]) == ~0u) return;
-                uint8_t *v = ring + at % STAGES * C::CHUNK;
-                for (int r = lane / 8; r < kTile; r += 4)
-                    if (!(m[r / 32] >> (r % 32) & 1))
-#pragma unroll
-                        for (int x = 0; x < C::BOXES; ++x)
-                            reinterpret_cast<uint4 *>(v + x * C::BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
-                fence_proxy_async_shared();
-                __syncwarp();
-            }
-        };
-        auto keys = [&]() {
-            for (int c = 0; ok && c < NCH; ++c) ok = arrived(chunk + c);
-        };
-        if (ok) keys();
-        if (ok) {
-            for (int st = 0; st < STREAMS; ++st) scores(st, st, chunk);
-            for (int c = 0; c < NCH; ++c) release(chunk + c);
-            chunk += NCH;
-        }
-        for (int j = 0; ok && j < n; ++j) {
-            const int k_at = chunk;
-            const bool more = j + 1 < n;
-            if (more) {
-                keys();
-                if (!ok) break;
-                chunk += NCH;
-                if (STREAMS == 1) {  // the next scores, beside this tile's weights
-                    // (their buffer's weights, of tile j - 1, were multiplied before)
-                    scores(0, (j + 1) & 1, k_at);
-                    for (int c = 0; c < NCH; ++c) release(k_at + c);
-                }
-            }
-            const int v_at = chunk;
-            for (int st = 0; ok && st < STREAMS; ++st) {
-                const int buf = STREAMS == 1 ? j & 1 : st;
-                for (int c = 0; ok && c < NCH; ++c) {
-                    if (st == 0) {
-                        ok = arrived(v_at + c);
-                        if (ok) clear(j, v_at + c);
-                    }
-                    if (ok && c == 0) {
-                        ok = wait_bar(s, &s.weights[buf], (STREAMS == 1 ? j >> 1 : j) & 1, p.status);
-                        tc_after_sync();
-                    }
-                    if (ok) product(st, buf, c, v_at + c, j > 0);
-                }
-                if (ok && lane == 0) mma_commit(&s.out[st]);
-                if (ok && STREAMS == 2 && more) scores(st, st, k_at);
-            }
-            if (!ok) break;
-            if (STREAMS == 2 && more) release(k_at);
-            for (int c = 0; c < NCH; ++c) release(v_at + c);
-            chunk += NCH;
-        }
-        // all products have completed before the tensor memory is given back
-        if (lane == 0) mma_commit(&s.drained);
-        __syncwarp();
-        (void)mbar_wait_bounded(&s.drained, 0);
-    } else if (FP8 && warp >= C::CONVERT_WARP) {
-        // ---- E4M3 codes to fp16 (exact), chunk by chunk
-        const int t = threadIdx.x - 32 * C::CONVERT_WARP, u = t % 8;
-        bool ok = true;
-        for (int i = 0; ok && i < 2 * n * NCH; ++i) {
-            const int rs = i % C::RAW_STAGES, st = i % STAGES;
-            // chunks come as K0, then K(j + 1) and V(j), the last V alone
-            const int tile2 = i / NCH;
-            const bool values = tile2 > 0 && ((tile2 & 1) == 0 || tile2 == 2 * n - 1);
-            const int j = tile2 == 2 * n - 1 ? n - 1 : tile2 / 2 - 1;
-            ok = wait_bar(s, &s.raw_full[rs], (i / C::RAW_STAGES) & 1, p.status);
-            if (ok && i >= STAGES) ok = wait_bar(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
-            if (!ok) break;
-            const uint8_t *src = raw + rs * C::RAW;
-            uint8_t *dst = ring + st * C::CHUNK + u / 4 * C::BOX;
-#pragma unroll 4
-            for (int r = t / 8; r < kTile; r += 4 * kConvertWarps) {
-                uint4 x = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
-                if (values && !(s.mask[j % kMaskSlots][r / 32] >> (r % 32) & 1)) x = make_uint4(0, 0, 0, 0);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                uint32_t y[8];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint16_t lo = (uint16_t)w[e], hi = (uint16_t)(w[e] >> 16);
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(lo));
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(hi));
-                }
-                const int u2 = u % 4 * 2;
-                *reinterpret_cast<uint4 *>(dst + r * 128 + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                *reinterpret_cast<uint4 *>(dst + r * 128 + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
-            }
-            fence_proxy_async_shared();
-            mbar_arrive(&s.full[st]);
-            mbar_arrive(&s.raw_empty[rs]);
-        }
-    } else if (warp < C::SOFTMAX_WARPS) {
+    if (warp < C::SOFTMAX_WARPS) {
+        if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
         // ---- queries to shared memory (rows past the item's as zeros)
         {
             constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR;
@@ -640,14 +429,15 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             float x[kTile];
 #pragma unroll
             for (int i = 0; i < kTile; i += 32) tmem_ld32(s_at + i, reinterpret_cast<uint32_t *>(x) + i);
-            tmem_wait_ld();
             // columns [from, to) of the tile are the row's
             const int kt = it.k0 + j;
             const int from = kt < tile_lo ? kTile : kt == tile_lo ? col_lo : 0;
             const int to = kt > tile_hi ? 0 : kt == tile_hi ? col_hi + 1 : kTile;
             const uint32_t *valid = s.mask[j % kMaskSlots];
             const bool whole = from == 0 && to == kTile && (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
-            if (!__all_sync(0xffffffffu, whole)) {
+            const bool all = __all_sync(0xffffffffu, whole);
+            tmem_wait_ld();
+            if (!all) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int a = from - 32 * w, e = to - 32 * w;
@@ -686,37 +476,49 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             if (move) m = top;
             const float base = m == -INFINITY ? 0.f : -m * c;
             const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
-            float2 part[4] = {};
+            // weights in the products' 16 bits, a half of the tile at a time so that
+            // its product starts while the other half is formed
+            uint32_t w[kTile / 2];
+            auto weigh = [&](int from_pair, int to_pair) {
 #pragma unroll
-            for (int i = 0; i < kTile; i += 64) {
-                uint32_t w[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    float2 y = fma2(make_float2(x[i + 2 * e], x[i + 2 * e + 1]), c2, b2);
-                    y.x = exp2_approx(y.x);
-                    y.y = exp2_approx(y.y);
-                    // weights in the products' 16 bits.  The sum adds the rounded
-                    // bf16 weights: where one is far above the others, its rounding
-                    // (2^-9) then divides out; fp16's (2^-12) stays below the output's.
+                for (int e = from_pair; e < to_pair; ++e) {
+                    const float2 y = fma2(make_float2(x[2 * e], x[2 * e + 1]), c2, b2);
                     if constexpr (FP8) {
-                        const __half2 h = __floats2half2_rn(y.x, y.y);
+                        const __half2 h = __floats2half2_rn(exp2_approx(y.x), exp2_approx(y.y));
                         w[e] = *reinterpret_cast<const uint32_t *>(&h);
                     } else {
-                        w[e] = pack_out(y.x, y.y);
-                        y = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                        w[e] = pack_out(exp2_approx(y.x), exp2_approx(y.y));
                     }
-                    part[e % 4] = add2(part[e % 4], y);
                 }
-                tmem_st32(s_at + i / 2, w);
-            }
-            sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
+            };
+            weigh(0, 32);
+            tmem_st32(s_at, w);
+            weigh(32, 48);
+            tmem_wait_st();
+            tc_before_sync();
+            mbar_arrive(&s.weights[buf][0]);
+            weigh(48, 64);
+            tmem_st32(s_at + 32, w + 32);
             tmem_wait_st();
             tc_before_sync();
             // the wait after the last tile tells its product from the one before
             // only if that one is known to be done
             if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
             if (!ok) break;
-            mbar_arrive(&s.weights[buf]);
+            mbar_arrive(&s.weights[buf][1]);
+            // The sum adds the rounded weights: where one is far above the others,
+            // its rounding then divides out.
+            float2 part[4] = {};
+#pragma unroll
+            for (int e = 0; e < kTile / 2; ++e) {
+                float2 y;
+                if constexpr (FP8)
+                    y = __half22float2(*reinterpret_cast<const __half2 *>(&w[e]));
+                else
+                    y = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                part[e % 4] = add2(part[e % 4], y);
+            }
+            sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
         }
         // ---- output
         if (ok && n > 0) ok = wait_bar(s, &s.out[stream], (n - 1) & 1, p.status);
@@ -762,6 +564,263 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             if (__any_sync(0xffffffffu, bad)) {
                 __syncwarp();
                 repair<D, FP8>(p, it, it.row0 + warp * 32, bad, lo, hi, partial);
+            }
+        }
+    } else {
+        if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER_REGS));
+        if (warp == C::LOAD_WARP) {
+            // ---- keys and values of tile j: K0, then K(j + 1) and V(j) in turn
+            struct Pages {
+                int rows;       // valid rows of the lane's page in the tile
+                int32_t at;     // its first row in the pool, of the layer's keys
+                uint32_t bytes; // of a chunk's copies, all lanes'
+            };
+            const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
+            const int last_page = it.last_slot / p.page_size;
+            auto find = [&](int j) {
+                const int kt = it.k0 + j;
+                Pages r{0, 0, 0};
+                int pg, sub = 0;
+                if (p.pages_per_tile) {
+                    pg = lane < p.pages_per_tile ? kt * p.pages_per_tile + lane : last_page + 1;
+                } else {
+                    pg = lane == 0 ? kt / p.tiles_per_page : last_page + 1;
+                    sub = kt % p.tiles_per_page * kTile;
+                }
+                if (pg <= last_page) {
+                    const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
+                    const int pid = p.page_table[e];
+                    r.rows = min(p.pages_per_tile ? p.page_size : kTile, p.page_fill[e] - sub);
+                    if (r.rows < 0) r.rows = 0;
+                    if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
+                        record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
+                        r.rows = 0;
+                    }
+                    r.at = (int32_t)((int64_t)p.layers[it.lr] * 2 * plane +
+                                     ((int64_t)pid * p.n_kv_heads + it.g) * p.page_size + sub);
+                }
+                return r;
+            };
+            int chunk = 0;
+            uint64_t *const landed = s.landed, *const freed = FP8 ? s.freed : s.empty;
+            const int box_bytes = p.box_rows * 128;
+            auto copy = [&](const Pages &r, bool values) {
+                const int n_pages = __popc(__ballot_sync(0xffffffffu, r.rows > 0));
+                for (int c = 0; c < NCH; ++c, ++chunk) {
+                    const int st = chunk % LANDS;
+                    if (chunk >= LANDS && !wait_bar(s, &freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
+                    if (lane == 0) {
+                        if (n_pages)
+                            mbar_arrive_expect_tx(&landed[st], n_pages * box_bytes * (FP8 ? 1 : C::BOXES));
+                        else
+                            mbar_arrive(&landed[st]);
+                    }
+                    __syncwarp();
+                    if (r.rows > 0) {
+                        const int32_t y = r.at + (values ? (int32_t)plane : 0);
+                        uint8_t *dst = (FP8 ? raw + st * C::RAW : ring + st * C::CHUNK) + lane * p.page_rows * 128;
+                        if constexpr (FP8) {
+                            tma_load_2d(dst, &map, c * DC, y, &landed[st]);
+                        } else {
+    #pragma unroll
+                            for (int x = 0; x < C::BOXES; ++x)
+                                tma_load_2d(dst + x * C::BOX, &map, c * DC + 64 * x, y, &landed[st]);
+                        }
+                    }
+                }
+                return true;
+            };
+            auto note_mask = [&](const Pages &r, int j) {
+    #pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int a = lane * p.page_rows - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
+                    uint32_t bits = 0;
+                    if (r.rows > 0 && a < 32 && e > 0)
+                        bits = (e >= 32 ? ~0u : (1u << e) - 1) & ~(a > 0 ? (1u << a) - 1 : 0u);
+                    bits = __reduce_or_sync(0xffffffffu, bits);
+                    if (lane == 0) s.mask[j % kMaskSlots][w] = bits;
+                }
+                __syncwarp();
+            };
+            Pages now = find(0), next = now;
+            bool ok = n > 0;
+            if (ok) {
+                note_mask(now, 0);
+                ok = copy(now, false);
+            }
+            if (n > 1) next = find(1);
+            for (int j = 0; ok && j < n; ++j) {
+                if (j + 1 < n) {
+                    note_mask(next, j + 1);
+                    ok = copy(next, false);
+                }
+                if (ok) ok = copy(now, true);
+                now = next;
+                if (j + 2 < n) next = find(j + 2);
+            }
+            if (!ok && n > 0)  // gave up: no copy may still be landing when the CTA ends
+                for (int c = max(0, chunk - LANDS); c < chunk; ++c) (void)mbar_wait_bounded(&landed[c % LANDS], (c / LANDS) & 1);
+        } else if (warp == C::MMA_WARP) {
+            // ---- products: one thread issues
+            constexpr uint32_t QK = mma_desc(kTile, kTile, FP8, false), PV = mma_desc(kTile, DC, FP8, true);
+            const uint32_t qk = QK | (p.negate ? kMmaNegateA : 0u);
+            const uint32_t q_d = smem_desc(smem_addr(smem), 0), k_d = smem_desc(smem_addr(ring), 0);
+            const uint32_t v_d = smem_desc(smem_addr(ring), C::BOX);
+            if (elect_one()) {
+                auto wait = [&](uint64_t *bar, uint32_t parity) {
+                    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, p.status);
+                };
+                int chunk = 0;
+                // the next tile's chunks are there
+                auto arrived = [&]() {
+                    bool ok = true;
+                    for (int c = chunk; ok && c < chunk + NCH; ++c) ok = wait(&s.ready[c % STAGES], (c / STAGES) & 1);
+                    return ok;
+                };
+                // S = Q K^T of a stream into score columns `buf`, keys in chunks from c0
+                auto scores = [&](int stream, int buf, int c0) {
+                    const uint32_t q = q_d + stream * (kTile * D * 2 / 16), to = tmem + kScoreCols + buf * kTile;
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c) {
+                        const uint32_t k = k_d + (c0 + c) % STAGES * (C::CHUNK / 16);
+#pragma unroll
+                        for (int i = 0; i < DC / 16; ++i) {
+                            const int ks = c * (DC / 16) + i;
+                            mma_ss(to, q + (ks / 4 * C::BOX + ks % 4 * 32) / 16, k + (i / 4 * C::BOX + i % 4 * 32) / 16, qk,
+                                   ks > 0);
+                        }
+                    }
+                    mma_commit(&s.scores[buf]);
+                };
+                // O += P V of a stream, half of the weights in score columns `buf`, values in chunks from c0
+                auto product = [&](int stream, int buf, int half, int c0, bool add) {
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c) {
+                        const uint32_t v = v_d + (c0 + c) % STAGES * (C::CHUNK / 16) + half * (kTile / 2 * 128 / 16);
+                        const uint32_t to = tmem + kOutCols + stream * kTile + c * DC;
+                        const uint32_t w = tmem + kScoreCols + buf * kTile + half * (kTile / 4);
+                        mma_ts(to, w, v, PV, add || half > 0);
+#pragma unroll
+                        for (int i = 1; i < kTile / 32; ++i) mma_ts(to, w + i * 8, v + i * (2048 / 16), PV, true);
+                    }
+                };
+                auto release = [&](int c0) {
+                    for (int c = c0; c < c0 + NCH; ++c) mma_commit(&s.empty[c % STAGES]);
+                };
+                bool ok = n > 0 && wait(&s.queries, 0) && arrived();
+                tc_after_sync();
+                if (ok) {
+                    for (int st = 0; st < STREAMS; ++st) scores(st, st, chunk);
+                    release(chunk);
+                    chunk += NCH;
+                }
+                for (int j = 0; ok && j < n; ++j) {
+                    const int k_at = chunk;
+                    const bool more = j + 1 < n;
+                    if (more) {
+                        ok = arrived();
+                        if (!ok) break;
+                        chunk += NCH;
+                        if (STREAMS == 1) {  // the next scores, beside this tile's weights
+                            // (their buffer's weights, of tile j - 1, were multiplied before)
+                            scores(0, (j + 1) & 1, k_at);
+                            release(k_at);
+                        }
+                    }
+                    ok = arrived();
+                    for (int st = 0; ok && st < STREAMS; ++st) {
+                        const int buf = STREAMS == 1 ? j & 1 : st;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            ok = wait(&s.weights[buf][half], (STREAMS == 1 ? j >> 1 : j) & 1);
+                            if (!ok) break;
+                            tc_after_sync();
+                            product(st, buf, half, chunk, j > 0);
+                        }
+                        if (!ok) break;
+                        mma_commit(&s.out[st]);
+                        if (STREAMS == 2 && more) scores(st, st, k_at);
+                    }
+                    if (!ok) break;
+                    if (STREAMS == 2 && more) release(k_at);
+                    release(chunk);
+                    chunk += NCH;
+                }
+                // all products have completed before the tensor memory is given back
+                mma_commit(&s.drained);
+                (void)mbar_wait_bounded(&s.drained, 0);
+            }
+            __syncwarp();
+        } else if (!FP8 && warp == C::TIDY_WARP) {
+            // ---- value rows that are not valid hold anything: zero weights must meet zeros
+            bool ok = true;
+            for (int i = 0; ok && i < 2 * n * NCH; ++i) {
+                const int st = i % STAGES;
+                ok = wait_bar(s, &s.landed[st], (i / STAGES) & 1, p.status);
+                if (!ok) break;
+                int j;
+                if (value_tile(i / NCH, n, j)) {
+                    const uint32_t *m = s.mask[j % kMaskSlots];
+                    if ((m[0] & m[1] & m[2] & m[3]) != ~0u) {
+                        uint8_t *v = ring + st * C::CHUNK;
+                        for (int r = lane / 8; r < kTile; r += 4)
+                            if (!(m[r / 32] >> (r % 32) & 1))
+#pragma unroll
+                                for (int x = 0; x < C::BOXES; ++x)
+                                    reinterpret_cast<uint4 *>(v + x * C::BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_shared();
+                        __syncwarp();
+                    }
+                }
+                if (lane == 0) mbar_arrive(&s.ready[st]);
+            }
+        } else if (FP8 && warp >= C::CONVERT_WARP) {
+            // ---- E4M3 codes to fp16 (exact), chunk by chunk
+            const int t = threadIdx.x - 32 * C::CONVERT_WARP, u = t % 8;
+            bool ok = true;
+            for (int i = 0; ok && i < 2 * n * NCH; ++i) {
+                const int rs = i % LANDS, st = i % STAGES;
+                int j;
+                const bool values = value_tile(i / NCH, n, j);
+                ok = wait_bar(s, &s.landed[rs], (i / LANDS) & 1, p.status);
+                if (ok && i >= STAGES) ok = wait_bar(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
+                if (!ok) break;
+                const uint8_t *src = raw + rs * C::RAW;
+                uint8_t *dst = ring + st * C::CHUNK + u / 4 * C::BOX;
+                constexpr int N = kTile / (4 * kConvertWarps);  // rows of a thread, those of a swizzle atom's place
+                uint4 x[N];
+    #pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int r = t / 8 + i * 4 * kConvertWarps;
+                    x[i] = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
+                }
+                if (values) {  // rows that are not valid hold anything: zero weights must meet zeros
+                    const uint32_t *m = s.mask[j % kMaskSlots];
+                    if ((m[0] & m[1] & m[2] & m[3]) != ~0u)
+    #pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int r = t / 8 + i * 4 * kConvertWarps;
+                            if (!(m[r / 32] >> (r % 32) & 1)) x[i] = make_uint4(0, 0, 0, 0);
+                        }
+                }
+    #pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int r = t / 8 + i * 4 * kConvertWarps;
+                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                    uint32_t y[8];
+    #pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint16_t lo = (uint16_t)w[e], hi = (uint16_t)(w[e] >> 16);
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(lo));
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(hi));
+                    }
+                    const int u2 = u % 4 * 2;
+                    *reinterpret_cast<uint4 *>(dst + r * 128 + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<uint4 *>(dst + r * 128 + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+                fence_proxy_async_shared();
+                mbar_arrive(&s.ready[st]);
+                mbar_arrive(&s.freed[rs]);
             }
         }
     }

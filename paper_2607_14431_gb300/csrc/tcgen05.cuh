@@ -49,14 +49,25 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *r) {
 }
 
 // --------------------------------------------------------------------- MMA --
-// Shared-memory operand in the 128-byte swizzle (atoms of 8 rows x 128 bytes,
-// base 1024-byte aligned).  K-major: rows of 128 bytes, `stride` between groups
-// of 8 rows, `lead` unused.  MN-major: `stride` between groups of 8 along k,
-// `lead` between groups of 64 16-bit elements along m or n.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 |
-           1ull << 46 | 2ull << 61;
+// True in one thread of the (converged) warp.  What it guards stays uniform for
+// the compiler: behind `lane == 0` the same 32 MMAs took 72 to 74 cycles each to
+// issue beside busy warps, behind this 64, the tensor cores' own time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
+
+// Shared-memory operand in the 128-byte swizzle (atoms of 8 rows x 128 bytes,
+// base 1024-byte aligned, 1024 bytes from one atom to the next along the rows:
+// along m or n for a K-major operand, along k for an MN-major one).  `lead`:
+// bytes between groups of 64 16-bit elements along m or n (MN-major).  Of the
+// descriptor only the low word varies; a step of x bytes adds x / 16 to it, so
+// that the issuing thread spends one addition per operand.
+__device__ __forceinline__ uint32_t smem_desc(uint32_t addr, uint32_t lead) {
+    return (addr & 0x3ffff) >> 4 | (lead >> 4) << 16;
+}
+constexpr uint32_t kDescHigh = (1024 >> 4) | 1u << 14 | 2u << 29;  // stride, version, swizzle
 
 // Instruction descriptor of kind::f16: bf16 (or f16) operands, fp32 accumulator,
 // A K-major; `negate` takes -A.
@@ -66,20 +77,20 @@ constexpr uint32_t mma_desc(int m, int n, bool f16, bool b_mn_major) {
 }
 constexpr uint32_t kMmaNegateA = 1u << 13;
 
-// One thread: D[tmem] (+)= A . B, k = 16.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+// One thread: D[tmem] (+)= A . B, k = 16; a, b: low words of the descriptors.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHigh)
         : "memory");
 }
 // A in tensor memory (two 16-bit elements a column).
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHigh)
         : "memory");
 }
 // One thread: `bar` gets an arrival once its MMAs so far have completed.
