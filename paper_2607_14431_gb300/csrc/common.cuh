@@ -358,8 +358,9 @@ struct PromptParams {
     const int32_t *page_table, *page_fill;
     int32_t max_pages, n_seq, window, shared;
     int32_t n_units;           // run layers x KV heads
-    int32_t pages_per_tile;    // key tiles: whole pages that one holds (0: a page takes several)
-    int32_t tiles_per_page, page_rows, box_rows;  // rows of a page in a tile, of a copy
+    int32_t unit;              // columns of a key tile that pages fill by themselves
+    int32_t pages_per_unit;    // whole pages that one holds (0: a page takes units_per_page)
+    int32_t units_per_page, page_rows, box_rows;  // rows of a page in a unit, of a copy
     float qscale, vscale;      // |softmax scale| * log2(e) (* k_scale), 1 or v_scale
     int32_t negate;            // the scale is negative
     const __nv_bfloat16 *q;    // [layers][q_rows][Hq][D]
@@ -504,7 +505,9 @@ bool sha256_parts_ok();
 // 128 rows each; then the join of the rows whose keys were split.  `map`: the
 // pool as boxes of 128 bytes x p.box_rows rows (make_pool_tensor_map).
 int prompt_streams(int head_dim, int64_t most_rows);
-void prompt_tiling(int page_size, PromptParams *p);
+int prompt_tile_rows(int head_dim, int streams);
+int prompt_ctas(int head_dim);
+void prompt_tiling(int page_size, int head_dim, PromptParams *p);
 cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
                           cudaStream_t s);
 cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t s);

@@ -11,9 +11,13 @@
 //
 // A work item is a KV head, a tile of query rows (tokens x the group's heads,
 // so that a KV head's queries share its keys) and a range of key tiles; a CTA
-// takes one.  Key tiles are 128 columns: the page's rows, or as many whole
-// pages as fit when pages are smaller, each at a multiple of 8 rows so that
-// its copy starts on a swizzle atom.
+// takes one, or for head_dim 256 a pair of CTAs (a cluster), each with half of
+// the query rows, of the keys' columns and of the values' dimensions: a single
+// CTA's shared memory held 2.5 key or value tiles there, which made it wait for
+// copies (8,191 rows of the 12B shape: 506 us; PAIR_TIME as pairs).
+// Key tiles are 128 columns, made of units of 128 (pairs: 64): a page's rows,
+// or as many whole pages as fit when pages are smaller, each at a multiple of 8
+// rows so that its copy starts on a swizzle atom.
 #include <math.h>
 
 #include <algorithm>
@@ -36,22 +40,28 @@ constexpr int kConvertWarps = 4;
 constexpr float kMaxSlack = 8.f;
 
 // STREAMS tiles of query rows share each key tile: with two, one's products
-// run while the other's weights are formed.  head_dim 256 has tensor memory
-// for one (256 columns of output); it keeps two score buffers instead, so that
-// the next tile's scores are formed ahead.
+// run while the other's weights are formed.  With one there are two score
+// buffers instead, so that the next tile's scores are formed ahead.
 template <int D_, bool FP8_, int STREAMS_>
 struct Cfg {
     static constexpr int D = D_, STREAMS = STREAMS_;
-    static constexpr bool FP8 = FP8_;
-    static constexpr int DC = D < 128 ? D : 128;     // dimensions of a chunk
-    static constexpr int NCH = D / DC;               // chunks of a key (or value) tile
-    static constexpr int BOXES = DC / 64;            // 128-byte wide boxes of a 16-bit chunk
-    static constexpr int BOX = kTile * 128;
-    static constexpr int CHUNK = BOXES * BOX;
-    static constexpr int RAW = FP8 ? kTile * DC : 0; // an fp8 chunk as it is in the cache
+    static constexpr bool FP8 = FP8_, PAIR = D == 256;
+    static constexpr int CTAS = PAIR ? 2 : 1;
+    static constexpr int DV = D / CTAS;              // dimensions of a CTA's values
+    static constexpr int UNIT = kTile / CTAS;        // columns of a CTA's keys
+    static constexpr int CHUNK = kTile * DV * 2;     // a CTA's keys or values of a tile, 16 bits
+    // boxes of 128 bytes x UNIT (keys) or 128 (values) rows
+    static constexpr int K_BOX = UNIT * 128, V_BOX = kTile * 128, K_BOXES = D / 64, V_BOXES = DV / 64;
+    static constexpr int RAW = FP8 ? CHUNK / 2 : 0;  // the same as fp8, as it is in the cache
     static constexpr int Q_BYTES = STREAMS * kTile * D * 2;
     static constexpr int STAGES = D == 64 ? 8 : FP8 ? (Q_BYTES > 32768 ? 4 : 5) : Q_BYTES > 32768 ? 5 : 6;
     static constexpr int RAW_STAGES = FP8 ? 2 : 0;
+    static constexpr int LANDS = FP8 ? RAW_STAGES : STAGES;  // the ring that copies land in
+    // Chunks come as K0, then K(j + 1) and V(j) in turn, the last V alone.  Two
+    // streams hand over and give back K(j + 1) and V(j) together (an MMA commit
+    // holds up the issuing thread): chunk c is of group (c + 1) / 2.
+    static constexpr bool GROUPED = STREAMS == 2;
+    static constexpr int GROUPS = GROUPED ? 4 : STAGES;
     static constexpr int SOFTMAX_WARPS = 4 * STREAMS;
     static constexpr int LOAD_WARP = SOFTMAX_WARPS, MMA_WARP = LOAD_WARP + 1, TIDY_WARP = LOAD_WARP + 2, CONVERT_WARP = LOAD_WARP + 4;
     static constexpr int THREADS = 32 * (CONVERT_WARP + (FP8 ? kConvertWarps : 0));
@@ -62,14 +72,15 @@ struct Cfg {
     static constexpr int MORE_REGS = THREADS == 512 ? 176 : THREADS == 384 ? (STREAMS == 2 ? 200 : 224) : 0;
     static constexpr int FEWER_REGS = THREADS == 512 ? 80 : STREAMS == 2 ? 96 : 136;
     static constexpr int SMEM = Q_BYTES + STAGES * CHUNK + RAW_STAGES * RAW + 1024;  // + alignment slack
-    static_assert(D <= 128 || STREAMS == 1, "tensor memory");
-    static_assert(SMEM <= 230 * 1024, "shared memory");
+    static_assert(!PAIR || STREAMS == 1, "tensor memory");
+    static_assert(SMEM <= 230400 + 1024, "shared memory");
+    static __device__ __forceinline__ int group(int chunk) { return GROUPED ? (chunk + 1) / 2 : chunk; }
 };
 constexpr int kScoreCols = 0, kOutCols = 256;  // tensor memory: scores (and weights), outputs
 
 struct Bars {
-    uint64_t landed[8], freed[4];            // copies: there; (fp8) converted, their place is free
-    uint64_t ready[8], empty[8];             // chunks of the ring: may be multiplied; have been
+    uint64_t landed[8], freed[2];            // copies: there; (fp8) converted, their place is free
+    uint64_t ready[8], empty[8];             // groups of chunks: may be multiplied; have been
     uint64_t scores[2], out[2];              // a score tile is there; its weights' product is added
     uint64_t weights[2][2];                  // the halves of its weights are there
     uint64_t queries, drained;
@@ -110,17 +121,22 @@ struct Item {
 // Key tile and column of a slot.
 __device__ __forceinline__ void tile_of(const PromptParams &p, int slot, int &tile, int &col) {
     const int pg = slot / p.page_size, r = slot - pg * p.page_size;
-    if (p.pages_per_tile) {
-        tile = pg / p.pages_per_tile;
-        col = (pg - tile * p.pages_per_tile) * p.page_rows + r;
+    int u;
+    if (p.pages_per_unit) {
+        u = pg / p.pages_per_unit;
+        col = (pg - u * p.pages_per_unit) * p.page_rows + r;
     } else {
-        tile = pg * p.tiles_per_page + r / kTile;
-        col = r % kTile;
+        u = pg * p.units_per_page + r / p.unit;
+        col = r % p.unit;
     }
+    const int per = kTile / p.unit;
+    tile = u / per;
+    col += (u - tile * per) * p.unit;
 }
 __device__ __forceinline__ int first_slot(const PromptParams &p, int tile) {
-    return p.pages_per_tile ? tile * p.pages_per_tile * p.page_size
-                            : tile / p.tiles_per_page * p.page_size + tile % p.tiles_per_page * kTile;
+    const int u = tile * (kTile / p.unit);
+    return p.pages_per_unit ? u * p.pages_per_unit * p.page_size
+                            : u / p.units_per_page * p.page_size + u % p.units_per_page * p.unit;
 }
 
 // First slot that the row at `slot` attends to.
@@ -337,44 +353,59 @@ __device__ __forceinline__ bool value_tile(int i, int n, int &j) {
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1)
     prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map) {
-    constexpr int D = C::D, DC = C::DC, NCH = C::NCH, STREAMS = C::STREAMS, STAGES = C::STAGES;
+    constexpr int D = C::D, STREAMS = C::STREAMS, STAGES = C::STAGES, LANDS = C::LANDS, CTAS = C::CTAS;
     constexpr bool FP8 = C::FP8;
-    constexpr int LANDS = FP8 ? C::RAW_STAGES : STAGES;  // the ring that copies land in
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ Bars s;
     uint8_t *const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     uint8_t *const ring = smem + C::Q_BYTES;
     uint8_t *const raw = ring + STAGES * C::CHUNK;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;  // uniform in the warp
+    const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
+    // a warp's arrival for the issuing thread (of a pair's first CTA), one for its lanes together
+    auto arrive_issuer = [&](uint64_t *bar, int times = 1) {
+        __syncwarp();
+        if (lane == 0)
+            for (int i = 0; i < times; ++i) {
+                if constexpr (CTAS == 2)
+                    mbar_arrive_first(bar);
+                else
+                    mbar_arrive(bar);
+            }
+    };
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < STAGES; ++i) {
-            mbar_init(&s.ready[i], FP8 ? 32 * kConvertWarps : 1);
+        for (int i = 0; i < C::GROUPS; ++i) {
+            mbar_init(&s.ready[i], CTAS * (C::GROUPED ? 2 : 1) * (FP8 ? kConvertWarps : 1));
             mbar_init(&s.empty[i], 1);
         }
         for (int i = 0; i < LANDS; ++i) mbar_init(&s.landed[i], 1);
-        for (int i = 0; i < C::RAW_STAGES; ++i) mbar_init(&s.freed[i], 32 * kConvertWarps);
+        for (int i = 0; i < C::RAW_STAGES; ++i) mbar_init(&s.freed[i], kConvertWarps);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.scores[i], 1);
-            mbar_init(&s.weights[i][0], 128);
-            mbar_init(&s.weights[i][1], 128);
+            mbar_init(&s.weights[i][0], CTAS * 4);
+            mbar_init(&s.weights[i][1], CTAS * 4);
             mbar_init(&s.out[i], 1);
         }
-        mbar_init(&s.queries, 32 * C::SOFTMAX_WARPS);
+        mbar_init(&s.queries, CTAS * C::SOFTMAX_WARPS);
         mbar_init(&s.drained, 1);
         s.abort = 0;
         fence_mbar_init();
     }
-    if (warp == C::MMA_WARP) tmem_alloc<512>(&s.tmem);
+    if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
     tc_before_sync();
-    __syncthreads();
+    if constexpr (CTAS == 2)
+        cluster_sync();
+    else
+        __syncthreads();
     tc_after_sync();
     const uint32_t tmem = s.tmem;
 
     after_previous();
-    const Item it = item_of(p, blockIdx.x, STREAMS * kTile);
+    const Item it = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
     const int n = it.k1 - it.k0;
     const bool partial = p.splits[it.b] > 1 || p.shared;
+    const int first = rank * kTile;  // of the item's rows
     if (warp < C::SOFTMAX_WARPS) {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
         // ---- queries to shared memory (rows past the item's as zeros)
@@ -385,8 +416,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             for (int i = 0; i < 32; i += RPI) {
                 const int r = warp * 32 + i + lane / LPR, rt = r % kTile;
                 uint4 x = make_uint4(0, 0, 0, 0);
-                if (r < it.rows) {
-                    x = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + r) * D)[u];
+                if (first + r < it.rows) {
+                    x = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + first + r) * D)[u];
                     if constexpr (FP8) {
                         uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -397,15 +428,15 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                         x = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
-                *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * C::BOX + rt * 128 +
+                *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * (kTile * 128) + rt * 128 +
                                            ((u % 8 ^ (rt & 7)) << 4)) = x;
             }
             fence_proxy_async_shared();
-            mbar_arrive(&s.queries);
+            arrive_issuer(&s.queries);
         }
         // ---- weights: a thread has a query row
         const int stream = warp / 4;
-        const int r = threadIdx.x, row = it.row0 + r;  // of the item, of the sequence
+        const int r = first + threadIdx.x, row = it.row0 + r;  // of the item, of the sequence
         const bool mine = r < it.rows;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // tensor memory lanes of the warp
         int lo = 0, hi = -1, tile_lo = 0, col_lo = 0, tile_hi = -1, col_hi = 0;
@@ -460,7 +491,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 const float a = rescale ? exp2_approx((m - top) * c) : 1.f;
                 sum.x *= a;
                 sum.y *= a;
-                ok = wait_bar(s, &s.out[stream], (j - 1) & 1, p.status);
+                // (two streams: the scores came after the previous product)
+                if (STREAMS == 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
                 if (!ok) break;
                 tc_after_sync();
 #pragma unroll 1
@@ -496,7 +528,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             weigh(32, 48);
             tmem_wait_st();
             tc_before_sync();
-            mbar_arrive(&s.weights[buf][0]);
+            arrive_issuer(&s.weights[buf][0]);
             weigh(48, 64);
             tmem_st32(s_at + 32, w + 32);
             tmem_wait_st();
@@ -505,7 +537,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             // only if that one is known to be done
             if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
             if (!ok) break;
-            mbar_arrive(&s.weights[buf][1]);
+            arrive_issuer(&s.weights[buf][1]);
             // The sum adds the rounded weights: where one is far above the others,
             // its rounding then divides out.
             float2 part[4] = {};
@@ -521,7 +553,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
         }
         // ---- output
-        if (ok && n > 0) ok = wait_bar(s, &s.out[stream], (n - 1) & 1, p.status);
+        if (ok && n > 0) ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (n - 1) & 1 : 0, p.status);
         if (ok) {
             tc_after_sync();
             const float l = sum.x + sum.y;
@@ -563,7 +595,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
             if (__any_sync(0xffffffffu, bad)) {
                 __syncwarp();
-                repair<D, FP8>(p, it, it.row0 + warp * 32, bad, lo, hi, partial);
+                repair<D, FP8>(p, it, it.row0 + first + warp * 32, bad, lo, hi, partial);
             }
         }
     } else {
@@ -571,27 +603,23 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         if (warp == C::LOAD_WARP) {
             // ---- keys and values of tile j: K0, then K(j + 1) and V(j) in turn
             struct Pages {
-                int rows;       // valid rows of the lane's page in the tile
-                int32_t at;     // its first row in the pool, of the layer's keys
-                uint32_t bytes; // of a chunk's copies, all lanes'
+                int rows;    // valid rows of the lane's page in the tile
+                int32_t at;  // its first row in the pool, of the layer's keys
             };
             const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
             const int last_page = it.last_slot / p.page_size;
+            // a lane has page `slot` of the tile's unit `unit`, at row `row` of the unit
+            const int unit = lane / 16, slot = lane % 16, row = slot * p.page_rows;
+            const bool has = unit < CTAS && (p.pages_per_unit ? slot < p.pages_per_unit : slot == 0);
             auto find = [&](int j) {
-                const int kt = it.k0 + j;
-                Pages r{0, 0, 0};
-                int pg, sub = 0;
-                if (p.pages_per_tile) {
-                    pg = lane < p.pages_per_tile ? kt * p.pages_per_tile + lane : last_page + 1;
-                } else {
-                    pg = lane == 0 ? kt / p.tiles_per_page : last_page + 1;
-                    sub = kt % p.tiles_per_page * kTile;
-                }
-                if (pg <= last_page) {
+                const int u = (it.k0 + j) * CTAS + unit;
+                Pages r{0, 0};
+                const int pg = p.pages_per_unit ? u * p.pages_per_unit + slot : u / p.units_per_page;
+                const int sub = p.pages_per_unit ? 0 : u % p.units_per_page * C::UNIT;
+                if (has && pg <= last_page) {
                     const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
                     const int pid = p.page_table[e];
-                    r.rows = min(p.pages_per_tile ? p.page_size : kTile, p.page_fill[e] - sub);
-                    if (r.rows < 0) r.rows = 0;
+                    r.rows = max(0, min(p.pages_per_unit ? p.page_size : C::UNIT, p.page_fill[e] - sub));
                     if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
                         record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
                         r.rows = 0;
@@ -602,38 +630,39 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 return r;
             };
             int chunk = 0;
-            uint64_t *const landed = s.landed, *const freed = FP8 ? s.freed : s.empty;
             const int box_bytes = p.box_rows * 128;
             auto copy = [&](const Pages &r, bool values) {
-                const int n_pages = __popc(__ballot_sync(0xffffffffu, r.rows > 0));
-                for (int c = 0; c < NCH; ++c, ++chunk) {
-                    const int st = chunk % LANDS;
-                    if (chunk >= LANDS && !wait_bar(s, &freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
-                    if (lane == 0) {
-                        if (n_pages)
-                            mbar_arrive_expect_tx(&landed[st], n_pages * box_bytes * (FP8 ? 1 : C::BOXES));
-                        else
-                            mbar_arrive(&landed[st]);
-                    }
-                    __syncwarp();
-                    if (r.rows > 0) {
-                        const int32_t y = r.at + (values ? (int32_t)plane : 0);
-                        uint8_t *dst = (FP8 ? raw + st * C::RAW : ring + st * C::CHUNK) + lane * p.page_rows * 128;
-                        if constexpr (FP8) {
-                            tma_load_2d(dst, &map, c * DC, y, &landed[st]);
-                        } else {
-    #pragma unroll
-                            for (int x = 0; x < C::BOXES; ++x)
-                                tma_load_2d(dst + x * C::BOX, &map, c * DC + 64 * x, y, &landed[st]);
-                        }
-                    }
+                const int st = chunk % LANDS;
+                if (chunk >= LANDS) {
+                    const int g = FP8 ? chunk - LANDS : C::group(chunk - LANDS);
+                    constexpr int NB = FP8 ? LANDS : C::GROUPS;
+                    if (!wait_bar(s, FP8 ? &s.freed[g % NB] : &s.empty[g % NB], (g / NB) & 1, p.status)) return false;
                 }
+                // a pair's keys are split by columns, its values by dimensions
+                const bool mine = r.rows > 0 && (values || CTAS == 1 || unit == rank);
+                const int boxes = (values ? C::V_BOXES : C::K_BOXES) / (FP8 ? 2 : 1);
+                const int n_pages = __popc(__ballot_sync(0xffffffffu, mine));
+                if (lane == 0) {
+                    if (n_pages)
+                        mbar_arrive_expect_tx(&s.landed[st], n_pages * box_bytes * boxes);
+                    else
+                        mbar_arrive(&s.landed[st]);
+                }
+                __syncwarp();
+                if (mine) {
+                    const int32_t y = r.at + (values ? (int32_t)plane : 0);
+                    uint8_t *dst = (FP8 ? raw + st * C::RAW : ring + st * C::CHUNK) + (values ? unit * C::UNIT + row : row) * 128;
+                    for (int x = 0; x < boxes; ++x)
+                        tma_load_2d(dst + x * (values ? C::V_BOX : C::K_BOX), &map,
+                                    (values ? rank * C::DV : 0) + x * (FP8 ? 128 : 64), y, &s.landed[st]);
+                }
+                ++chunk;
                 return true;
             };
             auto note_mask = [&](const Pages &r, int j) {
-    #pragma unroll
+#pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const int a = lane * p.page_rows - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
+                    const int a = unit * C::UNIT + row - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
                     uint32_t bits = 0;
                     if (r.rows > 0 && a < 32 && e > 0)
                         bits = (e >= 32 ? ~0u : (1u << e) - 1) & ~(a > 0 ? (1u << a) - 1 : 0u);
@@ -659,75 +688,69 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 if (j + 2 < n) next = find(j + 2);
             }
             if (!ok && n > 0)  // gave up: no copy may still be landing when the CTA ends
-                for (int c = max(0, chunk - LANDS); c < chunk; ++c) (void)mbar_wait_bounded(&landed[c % LANDS], (c / LANDS) & 1);
+                for (int c = max(0, chunk - LANDS); c < chunk; ++c)
+                    (void)mbar_wait_bounded(&s.landed[c % LANDS], (c / LANDS) & 1);
         } else if (warp == C::MMA_WARP) {
-            // ---- products: one thread issues
-            constexpr uint32_t QK = mma_desc(kTile, kTile, FP8, false), PV = mma_desc(kTile, DC, FP8, true);
+            // ---- products: one thread (of a pair's first CTA) issues
+            constexpr uint32_t QK = mma_desc(CTAS * kTile, kTile, FP8, false), PV = mma_desc(CTAS * kTile, D, FP8, true);
             const uint32_t qk = QK | (p.negate ? kMmaNegateA : 0u);
             const uint32_t q_d = smem_desc(smem_addr(smem), 0), k_d = smem_desc(smem_addr(ring), 0);
-            const uint32_t v_d = smem_desc(smem_addr(ring), C::BOX);
-            if (elect_one()) {
+            const uint32_t v_d = smem_desc(smem_addr(ring), C::V_BOX);
+            if (rank == 1) (void)mbar_wait_bounded(&s.drained, 0, 10000000000ull);  // while the first CTA issues
+            if (rank == 0 && elect_one()) {
                 auto wait = [&](uint64_t *bar, uint32_t parity) {
                     return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, p.status);
                 };
                 int chunk = 0;
-                // the next tile's chunks are there
-                auto arrived = [&]() {
-                    bool ok = true;
-                    for (int c = chunk; ok && c < chunk + NCH; ++c) ok = wait(&s.ready[c % STAGES], (c / STAGES) & 1);
-                    return ok;
+                // the group of chunk c is there
+                auto arrived = [&](int c) {
+                    const int g = C::group(c);
+                    return wait(&s.ready[g % C::GROUPS], (g / C::GROUPS) & 1);
                 };
-                // S = Q K^T of a stream into score columns `buf`, keys in chunks from c0
-                auto scores = [&](int stream, int buf, int c0) {
-                    const uint32_t q = q_d + stream * (kTile * D * 2 / 16), to = tmem + kScoreCols + buf * kTile;
-#pragma unroll
-                    for (int c = 0; c < NCH; ++c) {
-                        const uint32_t k = k_d + (c0 + c) % STAGES * (C::CHUNK / 16);
-#pragma unroll
-                        for (int i = 0; i < DC / 16; ++i) {
-                            const int ks = c * (DC / 16) + i;
-                            mma_ss(to, q + (ks / 4 * C::BOX + ks % 4 * 32) / 16, k + (i / 4 * C::BOX + i % 4 * 32) / 16, qk,
-                                   ks > 0);
-                        }
-                    }
-                    mma_commit(&s.scores[buf]);
+                // chunk c's place, and its group's, is free (where a later chunk takes it:
+                // every arrival of a commit has a waiter before the CTAs end)
+                auto release = [&](int c) {
+                    if (c - (C::GROUPED ? 1 : 0) + STAGES < 2 * n) mma_commit<CTAS>(&s.empty[C::group(c) % C::GROUPS]);
                 };
-                // O += P V of a stream, half of the weights in score columns `buf`, values in chunks from c0
-                auto product = [&](int stream, int buf, int half, int c0, bool add) {
+                // S = Q K^T of a stream into score columns `buf`, keys in chunk c
+                auto scores = [&](int stream, int buf, int c) {
+                    const uint32_t q = q_d + stream * (kTile * D * 2 / 16), k = k_d + c % STAGES * (C::CHUNK / 16);
+                    const uint32_t to = tmem + kScoreCols + buf * kTile;
 #pragma unroll
-                    for (int c = 0; c < NCH; ++c) {
-                        const uint32_t v = v_d + (c0 + c) % STAGES * (C::CHUNK / 16) + half * (kTile / 2 * 128 / 16);
-                        const uint32_t to = tmem + kOutCols + stream * kTile + c * DC;
-                        const uint32_t w = tmem + kScoreCols + buf * kTile + half * (kTile / 4);
-                        mma_ts(to, w, v, PV, add || half > 0);
+                    for (int i = 0; i < D / 16; ++i)
+                        mma_ss<CTAS>(to, q + (i / 4 * (kTile * 128) + i % 4 * 32) / 16, k + (i / 4 * C::K_BOX + i % 4 * 32) / 16,
+                                     qk, i > 0);
+                    mma_commit<CTAS>(&s.scores[buf]);
+                };
+                // O += P V of a stream, half of the weights in score columns `buf`, values in chunk c
+                auto product = [&](int stream, int buf, int half, int c, bool add) {
+                    const uint32_t v = v_d + c % STAGES * (C::CHUNK / 16) + half * (kTile / 2 * 128 / 16);
+                    const uint32_t to = tmem + kOutCols + stream * kTile;
+                    const uint32_t w = tmem + kScoreCols + buf * kTile + half * (kTile / 4);
+                    mma_ts<CTAS>(to, w, v, PV, add || half > 0);
 #pragma unroll
-                        for (int i = 1; i < kTile / 32; ++i) mma_ts(to, w + i * 8, v + i * (2048 / 16), PV, true);
-                    }
+                    for (int i = 1; i < kTile / 32; ++i) mma_ts<CTAS>(to, w + i * 8, v + i * (2048 / 16), PV, true);
                 };
-                auto release = [&](int c0) {
-                    for (int c = c0; c < c0 + NCH; ++c) mma_commit(&s.empty[c % STAGES]);
-                };
-                bool ok = n > 0 && wait(&s.queries, 0) && arrived();
+                bool ok = n > 0 && wait(&s.queries, 0) && arrived(0);
                 tc_after_sync();
                 if (ok) {
-                    for (int st = 0; st < STREAMS; ++st) scores(st, st, chunk);
-                    release(chunk);
-                    chunk += NCH;
+                    for (int st = 0; st < STREAMS; ++st) scores(st, st, 0);
+                    release(0);
+                    chunk = 1;
                 }
                 for (int j = 0; ok && j < n; ++j) {
                     const int k_at = chunk;
                     const bool more = j + 1 < n;
                     if (more) {
-                        ok = arrived();
+                        ok = arrived(chunk++);
                         if (!ok) break;
-                        chunk += NCH;
                         if (STREAMS == 1) {  // the next scores, beside this tile's weights
                             // (their buffer's weights, of tile j - 1, were multiplied before)
                             scores(0, (j + 1) & 1, k_at);
                             release(k_at);
                         }
                     }
-                    ok = arrived();
+                    if (!C::GROUPED || !more) ok = arrived(chunk);
                     for (int st = 0; ok && st < STREAMS; ++st) {
                         const int buf = STREAMS == 1 ? j & 1 : st;
 #pragma unroll
@@ -738,96 +761,104 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                             product(st, buf, half, chunk, j > 0);
                         }
                         if (!ok) break;
-                        mma_commit(&s.out[st]);
+                        if (STREAMS == 1 || !more) mma_commit<CTAS>(&s.out[st]);
                         if (STREAMS == 2 && more) scores(st, st, k_at);
                     }
                     if (!ok) break;
-                    if (STREAMS == 2 && more) release(k_at);
-                    release(chunk);
-                    chunk += NCH;
+                    release(chunk++);
                 }
                 // all products have completed before the tensor memory is given back
-                mma_commit(&s.drained);
+                mma_commit<CTAS>(&s.drained);
                 (void)mbar_wait_bounded(&s.drained, 0);
             }
             __syncwarp();
         } else if (!FP8 && warp == C::TIDY_WARP) {
             // ---- value rows that are not valid hold anything: zero weights must meet zeros
             bool ok = true;
-            for (int i = 0; ok && i < 2 * n * NCH; ++i) {
+            for (int i = 0; ok && i < 2 * n; ++i) {
                 const int st = i % STAGES;
                 ok = wait_bar(s, &s.landed[st], (i / STAGES) & 1, p.status);
                 if (!ok) break;
                 int j;
-                if (value_tile(i / NCH, n, j)) {
+                if (value_tile(i, n, j)) {
                     const uint32_t *m = s.mask[j % kMaskSlots];
                     if ((m[0] & m[1] & m[2] & m[3]) != ~0u) {
                         uint8_t *v = ring + st * C::CHUNK;
                         for (int r = lane / 8; r < kTile; r += 4)
                             if (!(m[r / 32] >> (r % 32) & 1))
 #pragma unroll
-                                for (int x = 0; x < C::BOXES; ++x)
-                                    reinterpret_cast<uint4 *>(v + x * C::BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
+                                for (int x = 0; x < C::V_BOXES; ++x)
+                                    reinterpret_cast<uint4 *>(v + x * C::V_BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
                         fence_proxy_async_shared();
-                        __syncwarp();
                     }
                 }
-                if (lane == 0) mbar_arrive(&s.ready[st]);
+                // (twice for a group of one)
+                arrive_issuer(&s.ready[C::group(i) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
             }
         } else if (FP8 && warp >= C::CONVERT_WARP) {
             // ---- E4M3 codes to fp16 (exact), chunk by chunk
             const int t = threadIdx.x - 32 * C::CONVERT_WARP, u = t % 8;
             bool ok = true;
-            for (int i = 0; ok && i < 2 * n * NCH; ++i) {
+            for (int i = 0; ok && i < 2 * n; ++i) {
                 const int rs = i % LANDS, st = i % STAGES;
                 int j;
-                const bool values = value_tile(i / NCH, n, j);
+                const bool values = value_tile(i, n, j);
                 ok = wait_bar(s, &s.landed[rs], (i / LANDS) & 1, p.status);
-                if (ok && i >= STAGES) ok = wait_bar(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
+                if (ok && i >= STAGES) {
+                    const int g = C::group(i - STAGES);
+                    ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
+                }
                 if (!ok) break;
                 const uint8_t *src = raw + rs * C::RAW;
-                uint8_t *dst = ring + st * C::CHUNK + u / 4 * C::BOX;
-                constexpr int N = kTile / (4 * kConvertWarps);  // rows of a thread, those of a swizzle atom's place
+                uint8_t *dst = ring + st * C::CHUNK;
+                constexpr int N = C::CHUNK / 2 / (128 * 4 * kConvertWarps);  // rows of 128 codes that a thread has
                 uint4 x[N];
-    #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int r = t / 8 + i * 4 * kConvertWarps;
-                    x[i] = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const int r = t / 8 + k * 4 * kConvertWarps;
+                    x[k] = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
                 }
                 if (values) {  // rows that are not valid hold anything: zero weights must meet zeros
                     const uint32_t *m = s.mask[j % kMaskSlots];
                     if ((m[0] & m[1] & m[2] & m[3]) != ~0u)
-    #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const int r = t / 8 + i * 4 * kConvertWarps;
-                            if (!(m[r / 32] >> (r % 32) & 1)) x[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) {
+                            const int r = t / 8 + k * 4 * kConvertWarps;
+                            if (!(m[r / 32] >> (r % 32) & 1)) x[k] = make_uint4(0, 0, 0, 0);
                         }
                 }
-    #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int r = t / 8 + i * 4 * kConvertWarps;
-                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                const int box = values ? C::V_BOX : C::K_BOX;
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const int r = t / 8 + k * 4 * kConvertWarps;
+                    const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
                     uint32_t y[8];
-    #pragma unroll
+#pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint16_t lo = (uint16_t)w[e], hi = (uint16_t)(w[e] >> 16);
                         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(lo));
                         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(hi));
                     }
-                    const int u2 = u % 4 * 2;
-                    *reinterpret_cast<uint4 *>(dst + r * 128 + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                    *reinterpret_cast<uint4 *>(dst + r * 128 + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+                    // a pair's keys: two boxes of codes, 64 rows each, become four
+                    const int half = values ? 0 : r / C::UNIT, rb = values ? r : r % C::UNIT, u2 = u % 4 * 2;
+                    uint8_t *to = dst + (half * 2 + u / 4) * box + rb * 128;
+                    *reinterpret_cast<uint4 *>(to + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<uint4 *>(to + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
                 }
                 fence_proxy_async_shared();
-                mbar_arrive(&s.ready[st]);
-                mbar_arrive(&s.freed[rs]);
+                arrive_issuer(&s.ready[C::group(i) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
+                if (lane == 0) mbar_arrive(&s.freed[rs]);
             }
         }
     }
+    // (a pair: the other CTA's arrivals and products reach into this one's memory)
     tc_before_sync();
-    __syncthreads();
+    if constexpr (CTAS == 2)
+        cluster_sync();
+    else
+        __syncthreads();
     tc_after_sync();
-    if (warp == C::MMA_WARP) tmem_free<512>(tmem);
+    if (warp == C::MMA_WARP) tmem_free<512, CTAS>(tmem);
 }
 
 // Joins the splits of each row: a warp per row of the sequences that were split.
@@ -876,7 +907,22 @@ struct PromptLaunch {
             if (e != cudaSuccess) return e;
             ready[dev].store(1);
         }
-        return launch_after(prompt_kernel<C>, p.item0[p.n_seq], C::THREADS, C::SMEM, s, p, map);
+        if (C::CTAS == 1) return launch_after(prompt_kernel<C>, p.item0[p.n_seq], C::THREADS, C::SMEM, s, p, map);
+        cudaLaunchAttribute attr[2]{};
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim = {C::CTAS, 1, 1};
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(p.item0[p.n_seq] * C::CTAS);
+        cfg.blockDim = dim3(C::THREADS);
+        cfg.dynamicSmemBytes = C::SMEM;
+        cfg.stream = s;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        e = cudaLaunchKernelEx(&cfg, prompt_kernel<C>, p, map);
+        count_launches(1);
+        return e != cudaSuccess ? e : cudaGetLastError();
     }
 };
 
@@ -885,13 +931,18 @@ struct PromptLaunch {
 // Two streams of query tiles unless no sequence has rows for the second.
 int prompt_streams(int head_dim, int64_t most_rows) { return head_dim <= 128 && most_rows > kTile ? 2 : 1; }
 
-// How pages fill the 128 columns of a key tile.
-void prompt_tiling(int page_size, PromptParams *p) {
+// Query rows of a work item, and the CTAs that share it.
+int prompt_tile_rows(int head_dim, int streams) { return kTile * (head_dim == 256 ? 2 : streams); }
+int prompt_ctas(int head_dim) { return head_dim == 256 ? 2 : 1; }
+
+// How pages fill the columns of a key tile.
+void prompt_tiling(int page_size, int head_dim, PromptParams *p) {
     const int rows = (page_size + 7) / 8 * 8;
+    p->unit = kTile / prompt_ctas(head_dim);
     p->page_rows = rows;
-    p->pages_per_tile = rows <= kTile ? kTile / rows : 0;
-    p->tiles_per_page = (page_size + kTile - 1) / kTile;
-    p->box_rows = std::min(rows, kTile);
+    p->pages_per_unit = rows <= p->unit ? p->unit / rows : 0;
+    p->units_per_page = (page_size + p->unit - 1) / p->unit;
+    p->box_rows = std::min(rows, p->unit);
 }
 
 cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,

@@ -987,7 +987,7 @@ extern "C" kvg_status kvg_cache_create(const kvg_dims *dims, int32_t n_pages, in
                             (unsigned long long)pool_rows));
     const bool fp8 = dims->kv_dtype == KVG_KV_E4M3;
     PromptParams tiling{};
-    prompt_tiling(dims->page_size, &tiling);
+    prompt_tiling(dims->page_size, dims->head_dim, &tiling);
     if (make_pool_tensor_map(&c->pool_map, c->pool, dims->head_dim, fp8,
                              decode_tile_tokens(dims->head_dim, fp8, dims->page_size), pool_rows) != cudaSuccess ||
         make_pool_tensor_map(&c->prompt_map, c->pool, dims->head_dim, fp8, tiling.box_rows, pool_rows) != cudaSuccess)
@@ -2507,7 +2507,7 @@ static void prompt_params(const kvg_cache *c, const void *q, int32_t n_q_heads, 
     p->page_table = c->page_table;
     p->page_fill = c->page_fill;
     p->max_pages = c->max_pages;
-    prompt_tiling(d.page_size, p);
+    prompt_tiling(d.page_size, d.head_dim, p);
     // a masked score is -inf times the scale: a scale of 0 becomes one that
     // keeps it (2^(1e-30 x) is 1)
     p->negate = scale < 0.f;
@@ -2534,7 +2534,7 @@ struct PromptWork {
     int64_t rows;
     int32_t tokens, begin, last;
 };
-constexpr int kPromptRows = 128;  // rows of a query tile, columns of a key tile
+constexpr int kPromptCols = 128;  // columns of a key tile
 
 // Work items of a launch: how many key ranges each sequence's query tiles are
 // split into.  An item costs its key tiles and kItemTiles more for its start,
@@ -2546,7 +2546,9 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
                            PromptParams *p) {
     constexpr double kItemTiles = 3.0;
     const int P = p->page_size;
-    const double slots_per_tile = p->pages_per_tile ? (double)p->pages_per_tile * P : (double)P / p->tiles_per_page;
+    const double slots_per_tile =
+        (p->pages_per_unit ? (double)p->pages_per_unit * P : (double)P / p->units_per_page) * (kPromptCols / p->unit);
+    const double at_once = (double)c->n_sm / prompt_ctas(c->dims.head_dim);
     struct Row {
         double longest, mean;
         int64_t tiles;
@@ -2571,7 +2573,7 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
             top = std::max(top, r.longest / s + kItemTiles);
         }
         const double mean = total / items;
-        const double est = std::max(top, std::ceil(items / c->n_sm) * mean) + (len < longest ? kItemTiles : 0.0);
+        const double est = std::max(top, std::ceil(items / at_once) * mean) + (len < longest ? kItemTiles : 0.0);
         if (est < best) {
             best = est;
             best_len = len;
@@ -2673,8 +2675,8 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
             }
             if (p.n_seq == 0) continue;
             const int streams = prompt_streams(d.head_dim, most);
-            const int64_t slots = plan_prompt(c, work, G, kPromptRows * streams, false, &p);
-            prompt_items(kPromptRows * streams, G, &p);
+            const int64_t slots = plan_prompt(c, work, G, prompt_tile_rows(d.head_dim, streams), false, &p);
+            prompt_items(prompt_tile_rows(d.head_dim, streams), G, &p);
             if (kvg_status r = prompt_partials(c, slots, &p); r != KVG_OK) return r;
             KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
             if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
@@ -2756,7 +2758,7 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
         PromptParams &p = l.p;
         l.streams = prompt_streams(d.head_dim, l.most);
         l.part_base = shared_slots;
-        shared_slots += plan_prompt(c, l.work, G, kPromptRows * l.streams, true, &p);
+        shared_slots += plan_prompt(c, l.work, G, prompt_tile_rows(d.head_dim, l.streams), true, &p);
         for (int32_t i = 0; i < p.n_seq; ++i)
             for (int32_t k = p.first[i]; k < p.first[i + 1]; ++k) {
                 const int32_t b = p.member[k];
@@ -2829,7 +2831,7 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
                     }
                 }
             }
-            prompt_items(kPromptRows * l->streams, G, &p);
+            prompt_items(prompt_tile_rows(d.head_dim, l->streams), G, &p);
             KVG_CUDA(launch_prompt(d.head_dim, fp8, l->streams, p, c->prompt_map, st));
         }
     }

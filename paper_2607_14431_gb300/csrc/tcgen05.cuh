@@ -6,18 +6,30 @@
 
 namespace kvg {
 
+// CTAS: 1, or 2 for the pair of CTAs of a cluster that work on one tile (all of
+// a kernel's tensor-core instructions name the same).
+
 // ------------------------------------------------------------ tensor memory --
-// Whole warps: columns (a power of two >= 32) of the SM's tensor memory; the
-// address is written to shared memory.
-template <int COLS>
+// Whole warps (of both CTAs): columns (a power of two >= 32) of the SM's tensor
+// memory; the address is written to shared memory.
+template <int COLS, int CTAS>
 __device__ __forceinline__ void tmem_alloc(uint32_t *dst) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "n"(COLS)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (CTAS == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "n"(COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "n"(COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
 }
-template <int COLS>
+template <int COLS, int CTAS>
 __device__ __forceinline__ void tmem_free(uint32_t addr) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
 }
 
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -77,26 +89,74 @@ constexpr uint32_t mma_desc(int m, int n, bool f16, bool b_mn_major) {
 }
 constexpr uint32_t kMmaNegateA = 1u << 13;
 
-// One thread: D[tmem] (+)= A . B, k = 16; a, b: low words of the descriptors.
+// One thread (of a pair's first CTA): D[tmem] (+)= A . B, k = 16; a, b: low
+// words of the descriptors.  A pair's A and D rows are split over the CTAs (half
+// of m each), its B over them along n; the addresses are the same in both.
+#define KVG_MMA_SS(GROUP)                                                                                          \
+    asm volatile(                                                                                                  \
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\t"                \
+        "mov.b64 y, {%2, %5};\n\ttcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),     \
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHigh)                                      \
+        : "memory")
+#define KVG_MMA_TS(GROUP)                                                                                          \
+    asm volatile(                                                                                                  \
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"                   \
+        "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),                          \
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHigh)                                      \
+        : "memory")
+template <int CTAS>
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHigh)
-        : "memory");
+    if constexpr (CTAS == 1)
+        KVG_MMA_SS("1");
+    else
+        KVG_MMA_SS("2");
 }
 // A in tensor memory (two 16-bit elements a column).
+template <int CTAS>
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "n"(kDescHigh)
-        : "memory");
+    if constexpr (CTAS == 1)
+        KVG_MMA_TS("1");
+    else
+        KVG_MMA_TS("2");
 }
-// One thread: `bar` gets an arrival once its MMAs so far have completed.
+#undef KVG_MMA_SS
+#undef KVG_MMA_TS
+// One thread: `bar` (of both CTAs of a pair) gets an arrival once its MMAs so
+// far have completed.
+template <int CTAS>
 __device__ __forceinline__ void mma_commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
-                 : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+                     : "memory");
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                smem_addr(bar)),
+            "h"((uint16_t)3)
+            : "memory");
+}
+
+// ----------------------------------------------------------------- cluster --
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// All threads of the cluster's CTAs; orders their shared-memory accesses.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// An arrival on the barrier at the same place in the cluster's first CTA.  What
+// it hands over lies in this SM's own memories, where the pair's products read
+// it: tensor-memory stores that have been waited for, shared-memory writes behind
+// fence.proxy.async, copies that have landed.  So it needs no fence of the
+// cluster's scope (with .release.cluster each arrival took 1,200 cycles, which
+// made it what a tile waited for).
+__device__ __forceinline__ void mbar_arrive_first(uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_addr(bar))
+        : "memory");
 }
 
 // ---------------------------------------------------- packed fp32 and exp2 --
