@@ -410,26 +410,32 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
         // ---- queries to shared memory (rows past the item's as zeros)
         {
-            constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR;
+            constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR, N = 32 / RPI, BATCH = N < 16 ? N : 16;
             const int u = lane % LPR;
-#pragma unroll 4
-            for (int i = 0; i < 32; i += RPI) {
-                const int r = warp * 32 + i + lane / LPR, rt = r % kTile;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (first + r < it.rows) {
-                    x = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + first + r) * D)[u];
+#pragma unroll 1
+            for (int i0 = 0; i0 < N; i0 += BATCH) {
+                uint4 x[BATCH];  // all on their way before the first is stored
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int r = first + warp * 32 + (i0 + i) * RPI + lane / LPR;
+                    x[i] = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + min(r, it.rows - 1)) * D)[u];
+                }
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int r = warp * 32 + (i0 + i) * RPI + lane / LPR, rt = r % kTile;
                     if constexpr (FP8) {
-                        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
                             w[e] = *reinterpret_cast<const uint32_t *>(&h);
                         }
-                        x = make_uint4(w[0], w[1], w[2], w[3]);
+                        x[i] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
+                    if (first + r >= it.rows) x[i] = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * (kTile * 128) + rt * 128 +
+                                               ((u % 8 ^ (rt & 7)) << 4)) = x[i];
                 }
-                *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * (kTile * 128) + rt * 128 +
-                                           ((u % 8 ^ (rt & 7)) << 4)) = x;
             }
             fence_proxy_async_shared();
             arrive_issuer(&s.queries);
