@@ -22,6 +22,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "tcgen05.cuh"
@@ -201,13 +202,16 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     it.row0 = t * tile_rows;
     it.rows = min(tile_rows, n - it.row0);
     it.last_slot = row_last(p, it, (it.row0 + it.rows - 1) >> it.gs);
-    const int from = p.shared || p.holes[b] ? p.begin[b] : window_first(p, b, p.slot0[b] + (it.row0 >> it.gs));
+    const int from = p.window <= 0               ? 0
+                     : p.shared || p.holes[b] ? p.begin[b]
+                                              : max(0, p.slot0[b] + (it.row0 >> it.gs) - p.window + 1);
     int ka, kb, col;
     tile_of(p, from, ka, col);
     tile_of(p, it.last_slot, kb, col);
     const int len = max(0, kb + 1 - ka);  // (a shared block may end before the rows' windows)
-    it.k0 = ka + (int)((int64_t)len * it.split / p.splits[b]);
-    it.k1 = ka + (int)((int64_t)len * (it.split + 1) / p.splits[b]);
+    const int part = len / p.splits[b], rest = len - part * p.splits[b];  // the first `rest` splits have one more
+    it.k0 = ka + part * it.split + min(it.split, rest);
+    it.k1 = it.k0 + part + (it.split < rest);
     return it;
 }
 
@@ -362,6 +366,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     uint8_t *const raw = ring + STAGES * C::CHUNK;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;  // uniform in the warp
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
+    // (from the launch's parameters alone, beside the set-up and the kernel before)
+    const Item it = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
+    const int n = it.k1 - it.k0;
+    const bool partial = p.splits[it.b] > 1 || p.shared;
+    const int first = rank * kTile;  // of the item's rows
     // a warp's arrival for the issuing thread (of a pair's first CTA), one for its lanes together
     auto arrive_issuer = [&](uint64_t *bar, int times = 1) {
         __syncwarp();
@@ -402,10 +411,6 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     const uint32_t tmem = s.tmem;
 
     after_previous();
-    const Item it = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
-    const int n = it.k1 - it.k0;
-    const bool partial = p.splits[it.b] > 1 || p.shared;
-    const int first = rank * kTile;  // of the item's rows
     if (warp < C::SOFTMAX_WARPS) {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
         // ---- queries to shared memory (rows past the item's as zeros)
@@ -452,6 +457,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             tile_of(p, lo, tile_lo, col_lo);
             tile_of(p, hi, tile_hi, col_hi);
         }
+        // where the row's result goes (now, beside the first copies)
+        const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
+        uint8_t *const to = partial ? reinterpret_cast<uint8_t *>(p.part_o) : reinterpret_cast<uint8_t *>(p.out);
+        float2 *const to_ml = p.part_ml;
+        const float vscale = p.vscale;
         const float c = p.qscale;
         float m = -INFINITY;               // what the weights refer to
         float2 sum = make_float2(0.f, 0.f);
@@ -565,38 +575,52 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             const float l = sum.x + sum.y;
             const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
             bool bad = false;
-            int64_t at = 0;
-            float inv = 1.f;
-            if (mine && partial) {
-                at = part_slot(p, it, it.split, row);
-                // (scores that are all NaN leave m at -inf, which would read as no column)
-                p.part_ml[at] = make_float2(l == l ? m * c : 0.f, l);
-            } else if (mine) {
-                at = q_row(p, it, row);
-                inv = __fdiv_rn(p.vscale, l);
-            }
+            // (scores that are all NaN leave m at -inf, which would read as no column)
+            if (mine && partial) to_ml[at] = make_float2(l == l ? m * c : 0.f, l);
+            const float inv = __fdiv_rn(vscale, l);
             if (n > 0) {
+                // 128 bytes of each row at a time, through shared memory (the queries'
+                // place, which no product reads any more), so that 8 lanes store a row's
+                uint8_t *const stage = smem + warp * (32 * 128);
+                const int bytes = partial ? 4 : 2, cols = 128 / bytes;
+                const bool stores = mine && !(partial && empty);
 #pragma unroll 1
-                for (int i = 0; i < D; i += 32) {
-                    float o[32];
-                    tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
-                    tmem_wait_ld();
-                    if (!mine || (partial && empty)) continue;
+                for (int i = 0; i < D; i += cols) {
+                    uint4 v[8];
                     float2 z = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) z = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), z);
-                    bad = bad || !(z.x + z.y == 0.f);
-                    if (partial) {
-                        float4 *to = reinterpret_cast<float4 *>(p.part_o + at * D + i);
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1 && partial) break;
+                        float o[32];
+                        tmem_ld32(o_at + i + 32 * h, reinterpret_cast<uint32_t *>(o));
+                        tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                    } else {
-                        uint4 *to = reinterpret_cast<uint4 *>(p.out + at * D + i);
+                        for (int e = 0; e < 32; e += 2) z = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), z);
+                        if (partial) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            to[e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                               pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                            for (int e = 0; e < 8; ++e)
+                                v[e] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                                                  __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                v[4 * h + e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                                          pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                        }
                     }
+                    bad = bad || (stores && !(z.x + z.y == 0.f));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4 *>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = v[e];
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        const int from = k + lane / 8, u = lane % 8;
+                        const int64_t row_at = __shfl_sync(0xffffffffu, at, from);
+                        const bool has = __shfl_sync(0xffffffffu, stores, from);
+                        const uint4 x = *reinterpret_cast<const uint4 *>(stage + from * 128 + ((u ^ (from & 7)) << 4));
+                        if (has) reinterpret_cast<uint4 *>(to + (row_at * D + i) * bytes)[u] = x;
+                    }
+                    __syncwarp();
                 }
             }
             if (__any_sync(0xffffffffu, bad)) {
@@ -848,8 +872,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     // a pair's keys: two boxes of codes, 64 rows each, become four
                     const int half = values ? 0 : r / C::UNIT, rb = values ? r : r % C::UNIT, u2 = u % 4 * 2;
                     uint8_t *to = dst + (half * 2 + u / 4) * box + rb * 128;
-                    *reinterpret_cast<uint4 *>(to + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                    *reinterpret_cast<uint4 *>(to + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+                    // (lanes of the second box take the other half first: 8 lanes, 8 bank groups)
+                    const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
+                    const int odd = u / 4;
+                    *reinterpret_cast<uint4 *>(to + (((u2 + odd) ^ (r & 7)) << 4)) = odd ? b : a;
+                    *reinterpret_cast<uint4 *>(to + (((u2 + 1 - odd) ^ (r & 7)) << 4)) = odd ? a : b;
                 }
                 fence_proxy_async_shared();
                 arrive_issuer(&s.ready[C::group(i) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
@@ -891,8 +918,14 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
         if (ml.y == 0.f) continue;
         const float a = exp2f(ml.x - M);
         L = __fmaf_rn(ml.y, a, L);
+        using Vec = std::conditional_t<N == 2, float2, float4>;
+        constexpr int W = sizeof(Vec) / 4;
+        float x[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) o[e] = __fmaf_rn(p.part_o[slot * D + lane * N + e], a, o[e]);
+        for (int e = 0; e < N / W; ++e)
+            reinterpret_cast<Vec *>(x)[e] = reinterpret_cast<const Vec *>(p.part_o + slot * D + lane * N)[e];
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] = __fmaf_rn(x[e], a, o[e]);
     }
     const float inv = __fdiv_rn(p.vscale, L);
     uint32_t *out = reinterpret_cast<uint32_t *>(p.out + q_row(p, it, row) * D + lane * N);
