@@ -196,7 +196,7 @@ struct AppendBatchParams {
 // New tokens' projections: queries rotated into q_out, keys and values into
 // the cache.  A launch takes up to kMaxBatchPerLaunch segments (consecutive
 // slots of a sequence) over up to kMaxQkvPages pages.
-constexpr int kMaxQkvPages = 4096;
+constexpr int kMaxQkvPages = 1024;
 struct QkvParams {
     const uint16_t *q, *k, *v;           // head h of a token at + h * head_dim
     int64_t q_token, k_token, v_token;   // elements between tokens
@@ -452,7 +452,7 @@ cudaError_t launch_graft_batch_pages(const GraftBatchParams &p, const uint32_t *
                                      uint32_t call, cudaStream_t s);
 cudaError_t launch_append(const AppendParams &p, int n_sm, cudaStream_t s);
 cudaError_t launch_append_batch(const AppendBatchParams &p, int n_sm, cudaStream_t s);
-cudaError_t launch_append_qkv(int head_dim, bool fp8, const QkvParams &p, cudaStream_t s);
+cudaError_t launch_append_qkv(int head_dim, bool fp8, const QkvParams &p, int n_sm, cudaStream_t s);
 cudaError_t launch_gather(const GatherParams &p, int n_sm, cudaStream_t s);
 cudaError_t launch_alias(const AliasParams &p, int n_sm, cudaStream_t s);
 // One 4-byte load per `stride` bytes of [base, base + bytes) (base 4-byte

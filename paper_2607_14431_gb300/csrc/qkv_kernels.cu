@@ -10,15 +10,20 @@
 //
 // Every value is read once and written once, so memory bounds it; for a
 // decode step's few rows the launch and one dependent load do.  A CTA takes a
-// token: the cos and sin of its position are the same for all its heads, so a
-// thread makes each pair's once, in shared memory, while the head rows' loads
-// are in flight.  A row is D / 8 lanes of 16 bytes each; a lane keeps the same
-// columns for all its rows, so its weights, cos and sin stay in registers, and
-// the other half of a pair comes from its lane by a shuffle.
+// run of tokens, one after the other, the next one's rows on their way while
+// the current one's are worked on; the cos and sin of a token's position, the
+// same for all its heads, are made once, in shared memory.  A head is D / 8
+// lanes of two 8-byte pieces: of a rotated half-pair head the same 4 columns of
+// both halves, so that no pair is split over lanes.  A lane keeps its columns
+// for all rows: weights, cos and sin stay in registers.
+// One layer of 8,191 rows of the 12B shape (268 MB): 95.6 us with a CTA per
+// token and the other half of a pair fetched by shuffles, APPEND_TIME this way.
 //
 // The angle: p f_i / (2 pi) turns as a 64-bit fixed-point product that wraps at
 // whole turns, so the fraction is good to 2^-33 turns at any position, where
 // an fp32 product would be off by 6e-3 radians at position 100,000.
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace kvg {
@@ -28,170 +33,246 @@ namespace {
 constexpr int kQkvThreads = 256;
 constexpr int kQkvUnroll = 4;  // rows of a lane in flight
 
-__device__ __forceinline__ void unpack_bf16x8(const uint4 &v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Eight columns of a row as they are handled: pairs (a[i], b[i]).  A lane's two
+// pieces hold a and b (half pairs), or pairs side by side.
+template <bool HALF>
+__device__ __forceinline__ void unpack(const uint2 &x, const uint2 &y, float (&a)[4], float (&b)[4]) {
+    const uint32_t w[4] = {x.x, x.y, y.x, y.y};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
+        if constexpr (HALF) {
+            (i < 2 ? a : b)[2 * i % 4] = lo;
+            (i < 2 ? a : b)[2 * i % 4 + 1] = hi;
+        } else {
+            a[i] = lo;
+            b[i] = hi;
+        }
     }
 }
 
-__device__ __forceinline__ uint4 pack_bf16x8(const float (&f)[8]) {
+// The eight values in the order of their columns.
+template <bool HALF>
+__device__ __forceinline__ float in_order(const float (&a)[4], const float (&b)[4], int i) {
+    return HALF ? (i < 4 ? a[i % 4] : b[i % 4]) : (i % 2 ? b[i / 2] : a[i / 2]);
+}
+
+template <bool HALF>
+__device__ __forceinline__ void pack_bf16(const float (&a)[4], const float (&b)[4], uint2 &x, uint2 &y) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        const __nv_bfloat162 t = __floats2bfloat162_rn(in_order<HALF>(a, b, 2 * i), in_order<HALF>(a, b, 2 * i + 1));
         w[i] = *reinterpret_cast<const uint32_t *>(&t);
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    x = make_uint2(w[0], w[1]);
+    y = make_uint2(w[2], w[3]);
 }
 
 // fp32 times the reciprocal scale (one rounding), to the E4M3 grid (nearest
 // even, saturating at +-448), as every append into an fp8 cache.
-__device__ __forceinline__ uint2 pack_e4m3x8(const float (&f)[8], float inv_scale) {
+template <bool HALF>
+__device__ __forceinline__ void pack_e4m3(const float (&a)[4], const float (&b)[4], float inv_scale, uint32_t &x, uint32_t &y) {
     uint32_t h[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float lo = __fmul_rn(f[2 * i], inv_scale), hi = __fmul_rn(f[2 * i + 1], inv_scale);
+        const float lo = __fmul_rn(in_order<HALF>(a, b, 2 * i), inv_scale);
+        const float hi = __fmul_rn(in_order<HALF>(a, b, 2 * i + 1), inv_scale);
         uint16_t c;
         asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
         h[i] = c;
     }
-    return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+    x = h[0] | (h[1] << 16);
+    y = h[2] | (h[3] << 16);
 }
 
-template <int D, bool FP8>
-__global__ void __launch_bounds__(kQkvThreads) append_qkv_kernel(const __grid_constant__ QkvParams p) {
+template <int D, bool FP8, bool HALF>
+__global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid_constant__ QkvParams p) {
     constexpr int LPR = D / 8;               // lanes of a row
     constexpr int RPP = kQkvThreads / LPR;   // rows that the CTA's threads hold at once
-    __shared__ float2 trig[D / 2];
-    const int t = blockIdx.x, lr = blockIdx.y;
+    constexpr int E = FP8 ? 1 : 2;           // bytes of a cached element
+    __shared__ float2 trig[2][D / 2];        // of the current and the next token
+    const int lr = blockIdx.y;
     const int lane = threadIdx.x % LPR, grp = threadIdx.x / LPR;
-    int b = 0;
-    for (int hi = p.n_seg - 1; b < hi;) {  // largest segment that starts at or before t
-        const int mid = (b + hi + 1) >> 1;
-        if (p.first[mid] <= t)
-            b = mid;
+    // the CTA's tokens [t0, end) of the launch
+    const int n_tokens = p.first[p.n_seg];
+    const int t0 = (int)((int64_t)n_tokens * blockIdx.x / gridDim.x);
+    const int end = (int)((int64_t)n_tokens * (blockIdx.x + 1) / gridDim.x);
+    int b0 = 0;
+    for (int hi = p.n_seg - 1; b0 < hi;) {  // largest segment that starts at or before t0
+        const int mid = (b0 + hi + 1) >> 1;
+        if (p.first[mid] <= t0)
+            b0 = mid;
         else
             hi = mid - 1;
     }
-    const int P = p.page_size;
-    const int slot = p.slot0[b] + (t - p.first[b]);
-    const int pg = slot / P, row = slot - pg * P;
-    const int pid = p.pids[p.pid0[b] + pg - p.slot0[b] / P];
-    const int64_t tok = p.tok0 + t;  // of the call's packed tokens
-    const int n_rows = p.n_q_heads + 2 * p.n_kv_heads;
-    const uint16_t *const q = p.q + lr * p.q_layer + tok * p.q_token + 8 * lane;
-    const uint16_t *const k = p.k + lr * p.k_layer + tok * p.k_token + 8 * lane;
-    const uint16_t *const v = p.v + lr * p.v_layer + tok * p.v_token + 8 * lane;
+    const int P = p.page_size, R = p.rotary_dim;
+    const bool turns = 8 * lane < R;  // the lane's columns are rotated
+    // its pieces: columns [c0, c0 + 4) and [c0 + c1, c0 + c1 + 4)
+    const int c0 = HALF && turns ? 4 * lane : 8 * lane, c1 = HALF && turns ? R / 2 : 4;
+    const int n_q = p.n_q_heads, n_qk = n_q + p.n_kv_heads, n_rows = n_qk + p.n_kv_heads;
+    const bool norms = p.q_norm || p.k_norm;
+    const float eps = p.eps, k_inv = p.k_inv_scale, v_inv = p.v_inv_scale;
+    const int64_t page_elems = (int64_t)p.n_kv_heads * P * D, out_token = (int64_t)n_q * D;
 
     after_previous();
-    const int pos = p.pos[tok];
-    if (p.write_meta && lr == 0 && threadIdx.x == 0) {
-        const int64_t seq = p.seq[b];
-        p.positions[seq * p.max_slots + slot] = pos;
-        // a page's last row of this launch knows its fill
-        if (row == P - 1 || t + 1 == p.first[b + 1]) {
-            p.page_table[seq * p.max_pages + pg] = pid;
-            p.page_fill[seq * p.max_pages + pg] = row + 1;
+    float wq[8], wk[8];  // weights and offset, a then b of the lane's pairs
+#pragma unroll
+    for (int i = 0; i < 8; ++i) wq[i] = wk[i] = 1.f;
+    auto weights = [&](const uint16_t *w, float (&to)[8]) {
+        w += (int64_t)lr * D + c0;
+        float a[4], d[4];
+        unpack<HALF>(*reinterpret_cast<const uint2 *>(w), *reinterpret_cast<const uint2 *>(w + c1), a, d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            to[i] = a[i] + p.norm_offset;
+            to[4 + i] = d[i] + p.norm_offset;
         }
-    }
+    };
+    if (p.q_norm) weights(p.q_norm, wq);
+    if (p.k_norm) weights(p.k_norm, wk);
+    auto turn = [&](int pos, int buf) {
+        for (int i = threadIdx.x; i < R / 2; i += kQkvThreads) {
+            const uint64_t frac = (uint64_t)(int64_t)pos * p.turn[i];  // of a turn, times 2^64
+            float sv, cv;
+            sincospif((float)(int32_t)(frac >> 32) * 0x1p-31f, &sv, &cv);
+            trig[buf][i] = make_float2(cv * p.attention_factor, sv * p.attention_factor);
+        }
+    };
 
-    const int R = p.rotary_dim;
-    const bool half = p.rotary_half;
-    const bool turns = 8 * lane < R;           // the lane's columns are rotated
-    const bool upper = half && 16 * lane >= R; // its columns are the second of their pairs
-    const int partner = (threadIdx.x & 31) + (!half || !turns ? 0 : upper ? -(R / 16) : R / 16);
-    float c[8], s[8];
-    uint4 wq = make_uint4(0, 0, 0, 0), wk = wq;
-    if (p.q_norm) wq = reinterpret_cast<const uint4 *>(p.q_norm + (int64_t)lr * D)[lane];
-    if (p.k_norm) wk = reinterpret_cast<const uint4 *>(p.k_norm + (int64_t)lr * D)[lane];
-
+    // head rows in batches of RPP * kQkvUnroll; most models have one
     for (int base = 0; base < n_rows; base += RPP * kQkvUnroll) {
-        uint4 x[kQkvUnroll];
+        // The lane's rows: where their first token is, how far the next one, and
+        // where they go (queries: from token to token; rows: from the page's slot)
+        const uint16_t *src[kQkvUnroll];
+        int64_t step[kQkvUnroll];
+        uint8_t *dst[kQkvUnroll];
+        int kind[kQkvUnroll];  // 0 query, 1 key, 2 value, 3 none
 #pragma unroll
         for (int u = 0; u < kQkvUnroll; ++u) {
             const int h = base + u * RPP + grp;
-            x[u] = make_uint4(0, 0, 0, 0);
-            if (h < n_rows) {
-                const int hk = h - p.n_q_heads, hv = hk - p.n_kv_heads;
-                x[u] = *reinterpret_cast<const uint4 *>(hk < 0 ? q + h * D : hv < 0 ? k + hk * D : v + hv * D);
-            }
+            kind[u] = h < n_q ? 0 : h < n_qk ? 1 : h < n_rows ? 2 : 3;
+            const int head = h - (kind[u] == 0 ? 0 : kind[u] == 1 ? n_q : n_qk);
+            const uint16_t *x = kind[u] == 0 ? p.q + lr * p.q_layer : kind[u] == 1 ? p.k + lr * p.k_layer : p.v + lr * p.v_layer;
+            step[u] = kind[u] == 0 ? p.q_token : kind[u] == 1 ? p.k_token : p.v_token;
+            src[u] = x + (p.tok0 + t0) * step[u] + (kind[u] == 3 ? 0 : head * D) + c0;
+            dst[u] = kind[u] == 0
+                         ? reinterpret_cast<uint8_t *>(p.q_out + (lr * p.n_tokens + p.tok0 + t0) * out_token + head * D + c0)
+                         : p.pool + ((((int64_t)(p.layer0 + lr) * 2 + (kind[u] == 2)) * p.pool_pages * p.n_kv_heads + head) * P * D + c0) * E;
         }
-        if (base == 0) {
-            for (int i = threadIdx.x; i < R / 2; i += kQkvThreads) {
-                const uint64_t frac = (uint64_t)(int64_t)pos * p.turn[i];  // of a turn, times 2^64
-                float sv, cv;
-                sincospif((float)(int32_t)(frac >> 32) * 0x1p-31f, &sv, &cv);
-                trig[i] = make_float2(cv * p.attention_factor, sv * p.attention_factor);
-            }
-            __syncthreads();
+        uint2 x[kQkvUnroll][2];
+        auto load = [&]() {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                c[j] = 1.f;
-                s[j] = 0.f;
-                if (turns) {
-                    const float2 cs = trig[half ? 8 * lane + j - (upper ? R / 2 : 0) : 4 * lane + j / 2];
-                    c[j] = cs.x;
-                    s[j] = (half ? upper : j & 1) ? cs.y : -cs.y;
+            for (int u = 0; u < kQkvUnroll; ++u) {
+                x[u][0] = x[u][1] = make_uint2(0, 0);
+                if (kind[u] < 3) {
+                    x[u][0] = *reinterpret_cast<const uint2 *>(src[u]);
+                    x[u][1] = *reinterpret_cast<const uint2 *>(src[u] + c1);
+                }
+                src[u] += step[u];
+            }
+        };
+        int pos = p.pos[p.tok0 + t0], b = b0;
+        load();
+        __syncthreads();  // (a batch before is done with the angles)
+        turn(pos, 0);
+        __syncthreads();
+        for (int t = t0, buf = 0; t < end; ++t, buf ^= 1) {
+            while (t >= p.first[b + 1]) ++b;
+            const int slot = p.slot0[b] + (t - p.first[b]);
+            const int pg = slot / P, row = slot - pg * P;
+            const int pid = p.pids[p.pid0[b] + pg - p.slot0[b] / P];
+            if (p.write_meta && base == 0 && lr == 0 && threadIdx.x == 0) {
+                const int64_t seq = p.seq[b];
+                p.positions[seq * p.max_slots + slot] = pos;
+                // a page's last row of this launch knows its fill
+                if (row == P - 1 || t + 1 == p.first[b + 1]) {
+                    p.page_table[seq * p.max_pages + pg] = pid;
+                    p.page_fill[seq * p.max_pages + pg] = row + 1;
                 }
             }
-        }
+            const int64_t at_slot = (pid * page_elems + (int64_t)row * D) * E, at_query = (t - t0) * out_token * 2;
+            float c[4], s[4];
 #pragma unroll
-        for (int u = 0; u < kQkvUnroll; ++u) {
-            const int h = base + u * RPP + grp;
-            const int hk = h - p.n_q_heads, hv = hk - p.n_kv_heads;
-            float f[8], y[8];
-            unpack_bf16x8(x[u], f);
-            if (p.q_norm || p.k_norm) {
-                float ss = 0.f;
+            for (int i = 0; i < 4; ++i) {
+                const float2 cs = turns ? trig[buf][4 * lane + i] : make_float2(1.f, 0.f);
+                c[i] = cs.x;
+                s[i] = cs.y;
+            }
+            uint2 now[kQkvUnroll][2];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss = __fmaf_rn(f[j], f[j], ss);
+            for (int u = 0; u < kQkvUnroll; ++u) {
+                now[u][0] = x[u][0];
+                now[u][1] = x[u][1];
+            }
+            const bool more = t + 1 < end;
+            if (more) {  // the next token's, while this one's are worked on
+                pos = p.pos[p.tok0 + t + 1];
+                load();
+            }
 #pragma unroll
-                for (int o = LPR / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                if (hv < 0 && (hk < 0 ? p.q_norm : p.k_norm)) {
-                    const float rms = rsqrtf(ss * (1.f / D) + p.eps);
-                    float w[8];
-                    unpack_bf16x8(hk < 0 ? wq : wk, w);
+            for (int u = 0; u < kQkvUnroll; ++u) {
+                float f[4], g[4];
+                unpack<HALF>(now[u][0], now[u][1], f, g);
+                if (norms) {
+                    float ss = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] *= rms * (w[j] + p.norm_offset);
+                    for (int i = 0; i < 4; ++i) ss = __fmaf_rn(f[i], f[i], __fmaf_rn(g[i], g[i], ss));
+#pragma unroll
+                    for (int o = LPR / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                    if (kind[u] == 0 ? p.q_norm : kind[u] == 1 ? p.k_norm : nullptr) {
+                        const float rms = rsqrtf(ss * (1.f / D) + eps);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            f[i] *= rms * (kind[u] ? wk[i] : wq[i]);
+                            g[i] *= rms * (kind[u] ? wk[4 + i] : wq[4 + i]);
+                        }
+                    }
+                }
+                if (kind[u] == 3) continue;
+                if (turns && kind[u] < 2) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float a = f[i], d = g[i];
+                        f[i] = __fmaf_rn(-d, s[i], a * c[i]);
+                        g[i] = __fmaf_rn(a, s[i], d * c[i]);
+                    }
+                }
+                uint8_t *const to = dst[u] + (kind[u] ? at_slot : at_query);
+                if (FP8 && kind[u]) {
+                    uint32_t y0, y1;
+                    pack_e4m3<HALF>(f, g, kind[u] == 2 ? v_inv : k_inv, y0, y1);
+                    *reinterpret_cast<uint32_t *>(to) = y0;
+                    *reinterpret_cast<uint32_t *>(to + c1) = y1;
+                } else {
+                    uint2 y0, y1;
+                    pack_bf16<HALF>(f, g, y0, y1);
+                    *reinterpret_cast<uint2 *>(to) = kind[u] == 2 ? now[u][0] : y0;
+                    *reinterpret_cast<uint2 *>(to + 2 * c1) = kind[u] == 2 ? now[u][1] : y1;
                 }
             }
-            if (R) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = half ? __shfl_sync(0xffffffffu, f[j], partner) : f[j ^ 1];
-                if (turns && hv < 0) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = __fmaf_rn(y[j], s[j], f[j] * c[j]);
-                }
+            if (more) {
+                turn(pos, buf ^ 1);
+                __syncthreads();
             }
-            if (h >= n_rows) continue;
-            if (hk < 0) {
-                uint16_t *const out = p.q_out + ((lr * p.n_tokens + tok) * p.n_q_heads + h) * D;
-                reinterpret_cast<uint4 *>(out)[lane] = pack_bf16x8(f);
-                continue;
-            }
-            const int kv = hv >= 0, head = kv ? hv : hk;
-            const int64_t page = ((int64_t)(p.layer0 + lr) * 2 + kv) * p.pool_pages + pid;
-            const int64_t at = ((page * p.n_kv_heads + head) * P + row) * D;  // element of the pool
-            if constexpr (FP8)
-                reinterpret_cast<uint2 *>(p.pool + at)[lane] = pack_e4m3x8(f, kv ? p.v_inv_scale : p.k_inv_scale);
-            else
-                reinterpret_cast<uint4 *>(p.pool + 2 * at)[lane] = kv ? x[u] : pack_bf16x8(f);
         }
     }
-    let_next_start();
+}
+
+template <int D, bool FP8>
+cudaError_t run_qkv(const QkvParams &p, int n_sm, cudaStream_t s) {
+    const dim3 grid(std::min(p.first[p.n_seg], std::max(1, 3 * n_sm / p.n_layers_run)), p.n_layers_run);
+    return launch_after(p.rotary_half ? append_qkv_kernel<D, FP8, true> : append_qkv_kernel<D, FP8, false>, grid,
+                        kQkvThreads, 0, s, p);
 }
 
 }  // namespace
 
-cudaError_t launch_append_qkv(int head_dim, bool fp8, const QkvParams &p, cudaStream_t s) {
-    const dim3 grid(p.first[p.n_seg], p.n_layers_run);
+cudaError_t launch_append_qkv(int head_dim, bool fp8, const QkvParams &p, int n_sm, cudaStream_t s) {
     switch (head_dim) {
-        case 64: return launch_after(fp8 ? append_qkv_kernel<64, true> : append_qkv_kernel<64, false>, grid, kQkvThreads, 0, s, p);
-        case 128: return launch_after(fp8 ? append_qkv_kernel<128, true> : append_qkv_kernel<128, false>, grid, kQkvThreads, 0, s, p);
-        case 256: return launch_after(fp8 ? append_qkv_kernel<256, true> : append_qkv_kernel<256, false>, grid, kQkvThreads, 0, s, p);
+        case 64: return fp8 ? run_qkv<64, true>(p, n_sm, s) : run_qkv<64, false>(p, n_sm, s);
+        case 128: return fp8 ? run_qkv<128, true>(p, n_sm, s) : run_qkv<128, false>(p, n_sm, s);
+        case 256: return fp8 ? run_qkv<256, true>(p, n_sm, s) : run_qkv<256, false>(p, n_sm, s);
     }
     return cudaErrorInvalidValue;
 }

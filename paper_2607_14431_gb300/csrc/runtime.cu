@@ -1311,7 +1311,7 @@ extern "C" kvg_status kvg_cache_append_qkv(kvg_cache *c, int32_t layer, const in
     if (total > 0x7fffffff) return fail(KVG_ERR_ARG, "more than 2^31 - 1 rows");
     if (total == 0) return KVG_OK;
     DeviceGuard g(c->device);
-    QkvParams p{};
+    QkvParams p;  // every field is set, of the arrays what the launch reads
     p.q = static_cast<const uint16_t *>(in->q);
     p.k = static_cast<const uint16_t *>(in->k);
     p.v = static_cast<const uint16_t *>(in->v);
@@ -1337,12 +1337,16 @@ extern "C" kvg_status kvg_cache_append_qkv(kvg_cache *c, int32_t layer, const in
     p.page_fill = c->page_fill;
     p.positions = c->positions;
     p.write_meta = opens;
+    p.tok0 = 0;
+    p.n_seg = 0;
+    p.rotary_dim = p.rotary_half = 0;
     p.attention_factor = 1.f;
+    p.k_inv_scale = p.v_inv_scale = 1.f;
     if (rotary) {
         p.rotary_dim = rotary->desc.rotary_dim;
         p.rotary_half = rotary->desc.style == KVG_ROPE_HALF;
         p.attention_factor = rotary->desc.attention_factor;
-        memcpy(p.turn, rotary->turn, sizeof p.turn);
+        memcpy(p.turn, rotary->turn, rotary->desc.rotary_dim / 2 * sizeof p.turn[0]);
     }
     if (d.kv_dtype == KVG_KV_E4M3) {
         p.k_inv_scale = 1.0f / d.k_scale;
@@ -1351,7 +1355,8 @@ extern "C" kvg_status kvg_cache_append_qkv(kvg_cache *c, int32_t layer, const in
     int32_t n_pids = 0;
     auto launch = [&]() {
         if (p.n_seg == 0) return cudaSuccess;
-        const cudaError_t e = launch_append_qkv(d.head_dim, d.kv_dtype == KVG_KV_E4M3, p, static_cast<cudaStream_t>(stream));
+        const cudaError_t e = launch_append_qkv(d.head_dim, d.kv_dtype == KVG_KV_E4M3, p, c->n_sm,
+                                                static_cast<cudaStream_t>(stream));
         p.tok0 += p.first[p.n_seg];
         p.n_seg = n_pids = 0;
         return e;

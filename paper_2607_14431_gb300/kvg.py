@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+from array import array
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "_build", "libkvg.so")
@@ -158,10 +159,24 @@ def _check(status: int):
         raise KvgError(status, msg or lib().kvg_status_string(status).decode())
 
 
+def _current_stream() -> int:
+    """The current stream's handle.  torch's public accessor makes a Stream object (3 us a call); what it reads
+    the handle with is called instead where it is there and agrees."""
+    global _current_stream
+    import torch
+    raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+    public = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    handle = public()  # initializes CUDA
+    if raw is not None and device is not None and raw(device()) == handle:
+        _current_stream = lambda: raw(device())  # noqa: E731
+    else:
+        _current_stream = public
+    return handle
+
+
 def _stream(stream) -> int:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     return int(getattr(stream, "cuda_stream", stream))
 
 
@@ -304,10 +319,9 @@ def kvg_cache_append_qkv(cache, layer: int, seq_ids, n_rows, qkv: kvg_qkv, rotar
     """rotary: a handle (Rotary.h) or None; q_out_ptr: None when qkv has no queries."""
     if len(n_rows) != len(seq_ids):
         raise ValueError("seq_ids and n_rows differ in length")
-    ids = (ctypes.c_int32 * len(seq_ids))(*seq_ids)
-    rows = (ctypes.c_int32 * len(seq_ids))(*n_rows)
-    _check(lib().kvg_cache_append_qkv(cache, layer, ids, rows, len(seq_ids), ctypes.byref(qkv), rotary, pos_ptr,
-                                      q_out_ptr, _stream(stream)))
+    ids, rows = array("i", seq_ids), array("i", n_rows)
+    _check(lib().kvg_cache_append_qkv(cache, layer, ids.buffer_info()[0], rows.buffer_info()[0], len(ids),
+                                      ctypes.byref(qkv), rotary, pos_ptr, q_out_ptr, _stream(stream)))
 
 
 def kvg_cache_release(cache, seq: int, stream=None):
@@ -397,18 +411,17 @@ def kvg_prompt_attention(cache, layer: int, seq_ids, n_rows, q_ptr: int, n_q_hea
     """Causal attention of each sequence's last n_rows[b] slots, packed; q and out [Lrun][sum n_rows][Hq][D] bf16."""
     if len(n_rows) != len(seq_ids):
         raise ValueError("seq_ids and n_rows differ in length")
-    ids = (ctypes.c_int32 * len(seq_ids))(*seq_ids)
-    rows = (ctypes.c_int32 * len(seq_ids))(*n_rows)
-    _check(lib().kvg_prompt_attention(cache, layer, ids, rows, len(seq_ids), q_ptr, n_q_heads, out_ptr, float(scale),
-                                      _stream(stream)))
+    ids, rows = array("i", seq_ids), array("i", n_rows)
+    _check(lib().kvg_prompt_attention(cache, layer, ids.buffer_info()[0], rows.buffer_info()[0], len(ids), q_ptr,
+                                      n_q_heads, out_ptr, scale, _stream(stream)))
 
 
 def kvg_decode_attention_shared(cache, layer: int, seq_ids, q_ptr: int, n_q_heads: int, out_ptr: int, scale: float,
                                 stream=None):
     """kvg_decode_attention that reads the pages which rows of the batch have in common once."""
-    ids = (ctypes.c_int32 * len(seq_ids))(*seq_ids)
-    _check(lib().kvg_decode_attention_shared(cache, layer, ids, len(seq_ids), q_ptr, n_q_heads, out_ptr, float(scale),
-                                             _stream(stream)))
+    ids = array("i", seq_ids)
+    _check(lib().kvg_decode_attention_shared(cache, layer, ids.buffer_info()[0], len(ids), q_ptr, n_q_heads, out_ptr,
+                                             scale, _stream(stream)))
 
 
 def kvg_digest(ptr: int, n: int, mode: int, page_bytes: int, out_ptr: int, stream=None):

@@ -229,7 +229,7 @@ def test_without_norm_and_rotation_it_is_the_append(kvg, fp8):
 
 
 def test_many_sequences_and_more_pages_than_a_launch_takes(kvg):
-    """300 sequences (a launch takes 256) and 4,500 pages of one row (a launch takes 4,096)."""
+    """300 sequences (a launch takes 256) and 4,500 pages of one row (a launch takes 1,024)."""
     rows = [1 + 4200 * (b == 7) for b in range(300)]
     case = (1, 2, 1, 64, 1, rows, False, 64, 0, "none", True, True, 11)
     q, k, v, w, pos, m, rotary, f, qkv, qo = build(kvg, case)
