@@ -32,6 +32,7 @@ namespace {
 
 constexpr int kQkvThreads = 256;
 constexpr int kQkvUnroll = 4;  // rows of a lane in flight
+constexpr int kQkvTurns = 8;   // tokens whose angles are made together
 
 // Eight columns of a row as they are handled: pairs (a[i], b[i]).  A lane's two
 // pieces hold a and b (half pairs), or pairs side by side.
@@ -87,11 +88,12 @@ __device__ __forceinline__ void pack_e4m3(const float (&a)[4], const float (&b)[
 }
 
 template <int D, bool FP8, bool HALF>
-__global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid_constant__ QkvParams p) {
+__global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid_constant__ QkvParams p) {
     constexpr int LPR = D / 8;               // lanes of a row
     constexpr int RPP = kQkvThreads / LPR;   // rows that the CTA's threads hold at once
     constexpr int E = FP8 ? 1 : 2;           // bytes of a cached element
-    __shared__ float2 trig[2][D / 2];        // of the current and the next token
+    __shared__ float2 trig[kQkvTurns][D / 2];  // of some tokens
+    __shared__ int places[2][kQkvTurns];     // positions of them and of the next
     const int lr = blockIdx.y;
     const int lane = threadIdx.x % LPR, grp = threadIdx.x / LPR;
     // the CTA's tokens [t0, end) of the launch
@@ -131,13 +133,24 @@ __global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid
     };
     if (p.q_norm) weights(p.q_norm, wq);
     if (p.k_norm) weights(p.k_norm, wk);
-    auto turn = [&](int pos, int buf) {
-        for (int i = threadIdx.x; i < R / 2; i += kQkvThreads) {
-            const uint64_t frac = (uint64_t)(int64_t)pos * p.turn[i];  // of a turn, times 2^64
+    // Cos and sin of the tokens [t, t + kQkvTurns): all threads for all of them,
+    // so that two barriers serve eight tokens and no warp waits for another's
+    // few pairs (with a barrier per token half of the stalls were there).
+    const int pairs = R / 2;
+    auto fetch = [&](int t, int buf) {
+        if (threadIdx.x < kQkvTurns && t + (int)threadIdx.x < end) places[buf][threadIdx.x] = p.pos[p.tok0 + t + threadIdx.x];
+    };
+    auto turn = [&](int t, int buf) {
+        __syncthreads();  // the angles before are used, the positions are there
+        const int n = min(kQkvTurns, end - t) * pairs;
+        for (int i = threadIdx.x; i < n; i += kQkvThreads) {
+            const int k = i / pairs, pair = i - k * pairs;
+            const uint64_t frac = (uint64_t)(int64_t)places[buf][k] * p.turn[pair];  // of a turn, times 2^64
             float sv, cv;
             sincospif((float)(int32_t)(frac >> 32) * 0x1p-31f, &sv, &cv);
-            trig[buf][i] = make_float2(cv * p.attention_factor, sv * p.attention_factor);
+            trig[k][pair] = make_float2(cv * p.attention_factor, sv * p.attention_factor);
         }
+        __syncthreads();
     };
 
     // head rows in batches of RPP * kQkvUnroll; most models have one
@@ -160,11 +173,9 @@ __global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid
                          ? reinterpret_cast<uint8_t *>(p.q_out + (lr * p.n_tokens + p.tok0 + t0) * out_token + head * D + c0)
                          : p.pool + ((((int64_t)(p.layer0 + lr) * 2 + (kind[u] == 2)) * p.pool_pages * p.n_kv_heads + head) * P * D + c0) * E;
         }
-        uint2 x[kQkvUnroll][2];
-        auto load = [&]() {
+        auto load = [&](uint2 (&x)[kQkvUnroll][2]) {
 #pragma unroll
             for (int u = 0; u < kQkvUnroll; ++u) {
-                x[u][0] = x[u][1] = make_uint2(0, 0);
                 if (kind[u] < 3) {
                     x[u][0] = *reinterpret_cast<const uint2 *>(src[u]);
                     x[u][1] = *reinterpret_cast<const uint2 *>(src[u] + c1);
@@ -172,62 +183,71 @@ __global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid
                 src[u] += step[u];
             }
         };
-        int pos = p.pos[p.tok0 + t0], b = b0;
-        load();
-        __syncthreads();  // (a batch before is done with the angles)
-        turn(pos, 0);
-        __syncthreads();
-        for (int t = t0, buf = 0; t < end; ++t, buf ^= 1) {
-            while (t >= p.first[b + 1]) ++b;
-            const int slot = p.slot0[b] + (t - p.first[b]);
-            const int pg = slot / P, row = slot - pg * P;
-            const int pid = p.pids[p.pid0[b] + pg - p.slot0[b] / P];
+        // where token t goes: kept from token to token, looked up at a page's or a segment's end
+        int b = b0 - 1, seg_end = t0, pg = 0, row = P - 1, buf = 0, k = kQkvTurns;
+        int64_t at_slot = 0, at_query = 0;
+        uint2 xa[kQkvUnroll][2] = {}, xb[kQkvUnroll][2] = {};
+        __syncthreads();  // (a batch before is done with the positions)
+        fetch(t0, 0);
+        load(xa);
+        auto token = [&](int t, const uint2 (&x)[kQkvUnroll][2], uint2 (&ahead)[kQkvUnroll][2]) {
+            if (k == kQkvTurns) {
+                turn(t, buf);
+                fetch(t + kQkvTurns, buf ^= 1);
+                k = 0;
+            }
+            const bool new_segment = t == seg_end, new_page = !new_segment && ++row == P;
+            if (new_segment) {
+                ++b;
+                seg_end = p.first[b + 1];
+                const int slot = p.slot0[b] + (t - p.first[b]);
+                pg = slot / P;
+                row = slot - pg * P;
+            } else if (new_page) {
+                ++pg;
+                row = 0;
+            }
+            at_slot += D * E;
+            if (new_segment || new_page)
+                at_slot = (p.pids[p.pid0[b] + pg - p.slot0[b] / P] * page_elems + (int64_t)row * D) * E;
             if (p.write_meta && base == 0 && lr == 0 && threadIdx.x == 0) {
                 const int64_t seq = p.seq[b];
-                p.positions[seq * p.max_slots + slot] = pos;
+                p.positions[seq * p.max_slots + (int64_t)pg * P + row] = places[buf ^ 1][k];
                 // a page's last row of this launch knows its fill
-                if (row == P - 1 || t + 1 == p.first[b + 1]) {
-                    p.page_table[seq * p.max_pages + pg] = pid;
+                if (row == P - 1 || t + 1 == seg_end) {
+                    p.page_table[seq * p.max_pages + pg] = p.pids[p.pid0[b] + pg - p.slot0[b] / P];
                     p.page_fill[seq * p.max_pages + pg] = row + 1;
                 }
             }
-            const int64_t at_slot = (pid * page_elems + (int64_t)row * D) * E, at_query = (t - t0) * out_token * 2;
             float c[4], s[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 cs = turns ? trig[buf][4 * lane + i] : make_float2(1.f, 0.f);
+                const float2 cs = turns ? trig[k][4 * lane + i] : make_float2(1.f, 0.f);
                 c[i] = cs.x;
                 s[i] = cs.y;
             }
-            uint2 now[kQkvUnroll][2];
-#pragma unroll
-            for (int u = 0; u < kQkvUnroll; ++u) {
-                now[u][0] = x[u][0];
-                now[u][1] = x[u][1];
-            }
-            const bool more = t + 1 < end;
-            if (more) {  // the next token's, while this one's are worked on
-                pos = p.pos[p.tok0 + t + 1];
-                load();
-            }
+            ++k;
+            if (t + 1 < end) load(ahead);  // the next token's, while this one's are worked on
 #pragma unroll
             for (int u = 0; u < kQkvUnroll; ++u) {
                 float f[4], g[4];
-                unpack<HALF>(now[u][0], now[u][1], f, g);
-                if (norms) {
+                unpack<HALF>(x[u][0], x[u][1], f, g);
+                if (norms && __any_sync(0xffffffffu, kind[u] < 2)) {
                     float ss = 0.f;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) ss = __fmaf_rn(f[i], f[i], __fmaf_rn(g[i], g[i], ss));
 #pragma unroll
                     for (int o = LPR / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                    if (kind[u] == 0 ? p.q_norm : kind[u] == 1 ? p.k_norm : nullptr) {
-                        const float rms = rsqrtf(ss * (1.f / D) + eps);
+                    const float rms = rsqrtf(ss * (1.f / D) + eps);
+                    auto scale = [&](const float (&w)[8]) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            f[i] *= rms * (kind[u] ? wk[i] : wq[i]);
-                            g[i] *= rms * (kind[u] ? wk[4 + i] : wq[4 + i]);
+                            f[i] *= rms * w[i];
+                            g[i] *= rms * w[4 + i];
                         }
-                    }
+                    };
+                    if (kind[u] == 0 && p.q_norm) scale(wq);
+                    if (kind[u] == 1 && p.k_norm) scale(wk);
                 }
                 if (kind[u] == 3) continue;
                 if (turns && kind[u] < 2) {
@@ -239,7 +259,10 @@ __global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid
                     }
                 }
                 uint8_t *const to = dst[u] + (kind[u] ? at_slot : at_query);
-                if (FP8 && kind[u]) {
+                if (!FP8 && kind[u] == 2) {
+                    *reinterpret_cast<uint2 *>(to) = x[u][0];
+                    *reinterpret_cast<uint2 *>(to + 2 * c1) = x[u][1];
+                } else if (FP8 && kind[u]) {
                     uint32_t y0, y1;
                     pack_e4m3<HALF>(f, g, kind[u] == 2 ? v_inv : k_inv, y0, y1);
                     *reinterpret_cast<uint32_t *>(to) = y0;
@@ -247,21 +270,22 @@ __global__ void __launch_bounds__(kQkvThreads, 3) append_qkv_kernel(const __grid
                 } else {
                     uint2 y0, y1;
                     pack_bf16<HALF>(f, g, y0, y1);
-                    *reinterpret_cast<uint2 *>(to) = kind[u] == 2 ? now[u][0] : y0;
-                    *reinterpret_cast<uint2 *>(to + 2 * c1) = kind[u] == 2 ? now[u][1] : y1;
+                    *reinterpret_cast<uint2 *>(to) = y0;
+                    *reinterpret_cast<uint2 *>(to + 2 * c1) = y1;
                 }
             }
-            if (more) {
-                turn(pos, buf ^ 1);
-                __syncthreads();
-            }
+            at_query += out_token * 2;
+        };
+        for (int t = t0; t < end; t += 2) {
+            token(t, xa, xb);
+            if (t + 1 < end) token(t + 1, xb, xa);
         }
     }
 }
 
 template <int D, bool FP8>
 cudaError_t run_qkv(const QkvParams &p, int n_sm, cudaStream_t s) {
-    const dim3 grid(std::min(p.first[p.n_seg], std::max(1, 3 * n_sm / p.n_layers_run)), p.n_layers_run);
+    const dim3 grid(std::min(p.first[p.n_seg], std::max(1, 2 * n_sm / p.n_layers_run)), p.n_layers_run);
     return launch_after(p.rotary_half ? append_qkv_kernel<D, FP8, true> : append_qkv_kernel<D, FP8, false>, grid,
                         kQkvThreads, 0, s, p);
 }
