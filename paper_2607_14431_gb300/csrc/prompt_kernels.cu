@@ -527,15 +527,18 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             // weights in the products' 16 bits, a half of the tile at a time so that
             // its product starts while the other half is formed
             uint32_t w[kTile / 2];
+            float2 part[4] = {};
             auto weigh = [&](int from_pair, int to_pair) {
 #pragma unroll
                 for (int e = from_pair; e < to_pair; ++e) {
-                    const float2 y = fma2(make_float2(x[2 * e], x[2 * e + 1]), c2, b2);
-                    if constexpr (FP8) {
-                        const __half2 h = __floats2half2_rn(exp2_approx(y.x), exp2_approx(y.y));
+                    float2 y = fma2(make_float2(x[2 * e], x[2 * e + 1]), c2, b2);
+                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                    if constexpr (FP8) {  // fp16's rounding (2^-12) stays below the output's: summed as they are
+                        const __half2 h = __floats2half2_rn(y.x, y.y);
                         w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                        part[e % 4] = add2(part[e % 4], y);
                     } else {
-                        w[e] = pack_out(exp2_approx(y.x), exp2_approx(y.y));
+                        w[e] = pack_out(y.x, y.y);
                     }
                 }
             };
@@ -554,17 +557,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
             if (!ok) break;
             arrive_issuer(&s.weights[buf][1]);
-            // The sum adds the rounded weights: where one is far above the others,
-            // its rounding then divides out.
-            float2 part[4] = {};
+            // The sum adds the rounded bf16 weights: where one is far above the
+            // others, its rounding then divides out.  (Beside the products.)
+            if constexpr (!FP8) {
 #pragma unroll
-            for (int e = 0; e < kTile / 2; ++e) {
-                float2 y;
-                if constexpr (FP8)
-                    y = __half22float2(*reinterpret_cast<const __half2 *>(&w[e]));
-                else
-                    y = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
-                part[e % 4] = add2(part[e % 4], y);
+                for (int e = 0; e < kTile / 2; ++e)
+                    part[e % 4] = add2(part[e % 4], make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)));
             }
             sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
         }
