@@ -79,12 +79,27 @@ struct Cfg {
 };
 constexpr int kScoreCols = 0, kOutCols = 256;  // tensor memory: scores (and weights), outputs
 
+// ------------------------------------------------------------ a work item --
+struct Item {
+    int b, split, lr, g;
+    int gs;         // log2 of the group
+    int row0, rows; // of the sequence's rows (token x head of the group), those of the item
+    int k0, k1;     // key tiles
+    int last_slot;  // of the sequence's pages that the item reads
+};
+
+// Items that a CTA knows of at once: the load warp is at most two ahead.
+constexpr int kItems = 4;
+
 struct Bars {
     uint64_t landed[8], freed[2];            // copies: there; (fp8) converted, their place is free
     uint64_t ready[8], empty[8];             // groups of chunks: may be multiplied; have been
     uint64_t scores[2], out[2];              // a score tile is there; its weights' product is added
     uint64_t weights[2][2];                  // the halves of its weights are there
-    uint64_t queries, drained;
+    uint64_t queries, taken[2], drained;     // an item's queries are there, its outputs have been read
+    uint64_t next[kItems], known[kItems];    // of item k (k % kItems): the answer is there, what it is
+    uint4 answer[kItems];
+    Item item[kItems];                       // b < 0: no more
     uint32_t mask[kMaskSlots][4];            // valid columns of key tile j % kMaskSlots
     uint32_t tmem;
     int abort;
@@ -111,13 +126,6 @@ __device__ __forceinline__ bool wait_bar(Bars &s, uint64_t *bar, uint32_t parity
 }
 
 // ------------------------------------------------------------ a work item --
-struct Item {
-    int b, split, lr, g;
-    int gs;         // log2 of the group
-    int row0, rows; // of the sequence's rows (token x head of the group), those of the item
-    int k0, k1;     // key tiles
-    int last_slot;  // of the sequence's pages that the item reads
-};
 
 // Key tile and column of a slot.
 __device__ __forceinline__ void tile_of(const PromptParams &p, int slot, int &tile, int &col) {
@@ -211,7 +219,7 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     const int len = max(0, kb + 1 - ka);  // (a shared block may end before the rows' windows)
     const int part = len / p.splits[b], rest = len - part * p.splits[b];  // the first `rest` splits have one more
     it.k0 = ka + part * it.split + min(it.split, rest);
-    it.k1 = it.k0 + part + (it.split < rest);
+    it.k1 = it.k0 + max(1, part + (it.split < rest));  // (one tile past the last: no valid column)
     return it;
 }
 
@@ -287,6 +295,13 @@ __device__ __forceinline__ void attend_row(const PromptParams &p, const Item &it
     }
 }
 
+__device__ __forceinline__ bool finite(const float (&o)[32]) {
+    float2 z[2] = {};
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) z[e / 2 % 2] = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), z[e / 2 % 2]);
+    return z[0].x + z[0].y + z[1].x + z[1].y == 0.f;
+}
+
 __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
@@ -353,6 +368,21 @@ __device__ __forceinline__ bool value_tile(int i, int n, int &j) {
     return last || (i > 0 && i % 2 == 0);
 }
 
+// Which group's commit frees each place of the ring: a lane remembers the group
+// of the chunk that its place holds.
+template <class C>
+struct Groups {
+    int held = 0, before = 0;  // the lane's place; groups of the items before
+    // place st is for the item's i-th chunk: the group of the chunk it held
+    __device__ __forceinline__ int take(int st, int lane, int i) {
+        const int g = of(st);
+        if (lane == st) held = before + C::group(i);
+        return g;
+    }
+    __device__ __forceinline__ int of(int st) const { return __shfl_sync(0xffffffffu, held, st); }
+    __device__ __forceinline__ void end(int n) { before += C::group(2 * n - 1) + 1; }
+};
+
 // ------------------------------------------------------------------ kernel --
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1)
@@ -366,11 +396,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     uint8_t *const raw = ring + STAGES * C::CHUNK;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;  // uniform in the warp
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
-    // (from the launch's parameters alone, beside the set-up and the kernel before)
-    const Item it = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
-    const int n = it.k1 - it.k0;
-    const bool partial = p.splits[it.b] > 1 || p.shared;
-    const int first = rank * kTile;  // of the item's rows
+    const int first = rank * kTile;  // of an item's rows
     // a warp's arrival for the issuing thread (of a pair's first CTA), one for its lanes together
     auto arrive_issuer = [&](uint64_t *bar, int times = 1) {
         __syncwarp();
@@ -397,10 +423,18 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             mbar_init(&s.out[i], 1);
         }
         mbar_init(&s.queries, CTAS * C::SOFTMAX_WARPS);
+        mbar_init(&s.taken[0], CTAS * 4);
+        mbar_init(&s.taken[1], CTAS * 4);
+        for (int i = 0; i < kItems; ++i) {
+            mbar_init(&s.next[i], 1);
+            mbar_init(&s.known[i], 1);
+        }
         mbar_init(&s.drained, 1);
         s.abort = 0;
         fence_mbar_init();
     }
+    // (from the launch's parameters alone: beside the set-up and the kernel before)
+    if (threadIdx.x == 32 * C::LOAD_WARP) s.item[0] = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
     if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
     tc_before_sync();
     if constexpr (CTAS == 2)
@@ -410,77 +444,87 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     tc_after_sync();
     const uint32_t tmem = s.tmem;
 
-    after_previous();
+    // The CTA's items: its own, then those of CTAs that have not started, so that
+    // copies run ahead into the next item while an item's outputs are stored.
+    // The issuing thread asks for item k + 2 when every warp is in item k (so the
+    // answer for item k - 2 and what it meant are read); the load warp, which is
+    // ahead, works out what an answer means for all.  The CTA's item k >= 1, for a warp:
+    auto has_item = [&](int k) {
+        return wait_bar(s, &s.known[k % kItems], ((k - 1) / kItems) & 1, p.status) && s.item[k % kItems].b >= 0;
+    };
+
     if (warp < C::SOFTMAX_WARPS) {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
-        // ---- queries to shared memory (rows past the item's as zeros)
-        {
-            constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR, N = 32 / RPI, BATCH = N < 16 ? N : 16;
+        const int stream = warp / 4;
+        // an item's queries to shared memory (rows past the item's as zeros): a batch
+        // of loads all on their way before the first is stored
+        constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR, N = 32 / RPI, BATCH = N < 16 ? N : 16;
+        auto fetch_queries = [&](const Item &it) {
             const int u = lane % LPR;
 #pragma unroll 1
             for (int i0 = 0; i0 < N; i0 += BATCH) {
-                uint4 x[BATCH];  // all on their way before the first is stored
+            uint4 qx[BATCH];
 #pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int r = first + warp * 32 + (i0 + i) * RPI + lane / LPR;
-                    x[i] = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + min(r, it.rows - 1)) * D)[u];
-                }
+            for (int i = 0; i < BATCH; ++i) {
+                const int r = first + warp * 32 + (i0 + i) * RPI + lane / LPR;
+                qx[i] = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + min(r, it.rows - 1)) * D)[u];
+            }
 #pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int r = warp * 32 + (i0 + i) * RPI + lane / LPR, rt = r % kTile;
-                    if constexpr (FP8) {
-                        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            for (int i = 0; i < BATCH; ++i) {
+                const int r = warp * 32 + (i0 + i) * RPI + lane / LPR, rt = r % kTile;
+                uint4 x = qx[i];
+                if constexpr (FP8) {
+                    uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
-                            w[e] = *reinterpret_cast<const uint32_t *>(&h);
-                        }
-                        x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int e = 0; e < 4; ++e) {
+                        const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                        w[e] = *reinterpret_cast<const uint32_t *>(&h);
                     }
-                    if (first + r >= it.rows) x[i] = make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * (kTile * 128) + rt * 128 +
-                                               ((u % 8 ^ (rt & 7)) << 4)) = x[i];
+                    x = make_uint4(w[0], w[1], w[2], w[3]);
                 }
+                if (first + r >= it.rows) x = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * (kTile * 128) + rt * 128 +
+                                           ((u % 8 ^ (rt & 7)) << 4)) = x;
+            }
             }
             fence_proxy_async_shared();
             arrive_issuer(&s.queries);
-        }
+        };
+        after_previous();
+        fetch_queries(s.item[0]);
+        bool ok = true;
+        int tiles = 0;  // of the items before
+        for (int k = 0; ok; ++k) {
+        const Item &it = s.item[k % kItems];  // (there until item k + 4 is known)
+        const int k0 = it.k0, n = it.k1 - k0;
         // ---- weights: a thread has a query row
-        const int stream = warp / 4;
-        const int r = first + threadIdx.x, row = it.row0 + r;  // of the item, of the sequence
-        const bool mine = r < it.rows;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // tensor memory lanes of the warp
-        int lo = 0, hi = -1, tile_lo = 0, col_lo = 0, tile_hi = -1, col_hi = 0;
+        const int r = first + threadIdx.x;                   // the thread's row of the item
+        const bool mine = r < it.rows;
+        int tile_lo = 0, col_lo = 0, tile_hi = -1, col_hi = 0;
         if (mine) {
-            lo = row_first(p, it, row >> it.gs);
-            hi = row_last(p, it, row >> it.gs);
-            tile_of(p, lo, tile_lo, col_lo);
-            tile_of(p, hi, tile_hi, col_hi);
+            const int token = (it.row0 + r) >> it.gs;
+            tile_of(p, row_first(p, it, token), tile_lo, col_lo);
+            tile_of(p, row_last(p, it, token), tile_hi, col_hi);
         }
-        // where the row's result goes (now, beside the first copies)
-        const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
-        uint8_t *const to = partial ? reinterpret_cast<uint8_t *>(p.part_o) : reinterpret_cast<uint8_t *>(p.out);
-        float2 *const to_ml = p.part_ml;
-        const float vscale = p.vscale;
         const float c = p.qscale;
         float m = -INFINITY;               // what the weights refer to
         float2 sum = make_float2(0.f, 0.f);
         const uint32_t o_at = tmem + lanes + kOutCols + stream * kTile;
-        bool ok = true;
         for (int j = 0; j < n; ++j) {
-            const int buf = STREAMS == 1 ? j & 1 : stream;
+            const int J = tiles + j, buf = STREAMS == 1 ? J & 1 : stream;
             const uint32_t s_at = tmem + lanes + kScoreCols + buf * kTile;
-            ok = wait_bar(s, &s.scores[buf], (STREAMS == 1 ? j >> 1 : j) & 1, p.status);
+            ok = wait_bar(s, &s.scores[buf], (STREAMS == 1 ? J >> 1 : J) & 1, p.status);
             if (!ok) break;
             tc_after_sync();
             float x[kTile];
 #pragma unroll
             for (int i = 0; i < kTile; i += 32) tmem_ld32(s_at + i, reinterpret_cast<uint32_t *>(x) + i);
             // columns [from, to) of the tile are the row's
-            const int kt = it.k0 + j;
+            const int kt = k0 + j;
             const int from = kt < tile_lo ? kTile : kt == tile_lo ? col_lo : 0;
             const int to = kt > tile_hi ? 0 : kt == tile_hi ? col_hi + 1 : kTile;
-            const uint32_t *valid = s.mask[j % kMaskSlots];
+            const uint32_t *valid = s.mask[J % kMaskSlots];
             const bool whole = from == 0 && to == kTile && (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
             const bool all = __all_sync(0xffffffffu, whole);
             tmem_wait_ld();
@@ -508,7 +552,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 sum.x *= a;
                 sum.y *= a;
                 // (two streams: the scores came after the previous product)
-                if (STREAMS == 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
+                if (STREAMS == 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
                 if (!ok) break;
                 tc_after_sync();
 #pragma unroll 1
@@ -554,7 +598,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             tc_before_sync();
             // the wait after the last tile tells its product from the one before
             // only if that one is known to be done
-            if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (j - 1) & 1, p.status);
+            if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
             if (!ok) break;
             arrive_issuer(&s.weights[buf][1]);
             // The sum adds the rounded bf16 weights: where one is far above the
@@ -566,65 +610,64 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
             sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
         }
+        tiles += n;
+        if (!ok) break;
+        // ---- the next item's queries (this one's scores are all there, so nothing
+        // reads their place any more): its first products run beside the output
+        const bool more = has_item(k + 1);
+        if (more) fetch_queries(s.item[(k + 1) % kItems]);
         // ---- output
-        if (ok && n > 0) ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (n - 1) & 1 : 0, p.status);
+        ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (tiles - 1) & 1 : k & 1, p.status);
         if (ok) {
             tc_after_sync();
             const float l = sum.x + sum.y;
             const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
             bool bad = false;
+            const int row = it.row0 + r;
+            const bool partial = p.splits[it.b] > 1 || p.shared;
+            const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
             // (scores that are all NaN leave m at -inf, which would read as no column)
-            if (mine && partial) to_ml[at] = make_float2(l == l ? m * c : 0.f, l);
-            const float inv = __fdiv_rn(vscale, l);
-            if (n > 0) {
-                // 128 bytes of each row at a time, through shared memory (the queries'
-                // place, which no product reads any more), so that 8 lanes store a row's
-                uint8_t *const stage = smem + warp * (32 * 128);
-                const int bytes = partial ? 4 : 2, cols = 128 / bytes;
-                const bool stores = mine && !(partial && empty);
+            if (mine && partial) p.part_ml[at] = make_float2(l == l ? m * c : 0.f, l);
+            const float inv = __fdiv_rn(p.vscale, l);
+            if (partial) {
+                float4 *const to = reinterpret_cast<float4 *>(p.part_o + at * D);
 #pragma unroll 1
-                for (int i = 0; i < D; i += cols) {
-                    uint4 v[8];
-                    float2 z = make_float2(0.f, 0.f);
+                for (int i = 0; i < D; i += 32) {
+                    float o[32];
+                    tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
+                    tmem_wait_ld();
+                    bad = bad || !finite(o);
+                    if (mine && !empty)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (h == 1 && partial) break;
-                        float o[32];
-                        tmem_ld32(o_at + i + 32 * h, reinterpret_cast<uint32_t *>(o));
-                        tmem_wait_ld();
+                        for (int e = 0; e < 8; ++e) to[i / 4 + e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                }
+            } else {
+                uint4 *const to = reinterpret_cast<uint4 *>(p.out + at * D);
+#pragma unroll 1
+                for (int i = 0; i < D; i += 32) {
+                    float o[32];
+                    tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
+                    tmem_wait_ld();
+                    bad = bad || !finite(o);
+                    if (mine)
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) z = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), z);
-                        if (partial) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                v[e] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
-                                                  __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                v[4 * h + e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                                          pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
-                        }
-                    }
-                    bad = bad || (stores && !(z.x + z.y == 0.f));
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4 *>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = v[e];
-                    __syncwarp();
-#pragma unroll
-                    for (int k = 0; k < 32; k += 4) {
-                        const int from = k + lane / 8, u = lane % 8;
-                        const int64_t row_at = __shfl_sync(0xffffffffu, at, from);
-                        const bool has = __shfl_sync(0xffffffffu, stores, from);
-                        const uint4 x = *reinterpret_cast<const uint4 *>(stage + from * 128 + ((u ^ (from & 7)) << 4));
-                        if (has) reinterpret_cast<uint4 *>(to + (row_at * D + i) * bytes)[u] = x;
-                    }
-                    __syncwarp();
+                        for (int e = 0; e < 4; ++e)
+                            to[i / 8 + e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                                       pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
                 }
             }
+            bad = bad && mine && !(partial && empty);
+            // (read: the next item's products may be added there)
+            tc_before_sync();
+            arrive_issuer(&s.taken[stream]);
             if (__any_sync(0xffffffffu, bad)) {
                 __syncwarp();
-                repair<D, FP8>(p, it, it.row0 + first + warp * 32, bad, lo, hi, partial);
+                const int token = row >> it.gs;
+                repair<D, FP8>(p, it, it.row0 + first + warp * 32, bad, mine ? row_first(p, it, token) : 0,
+                               mine ? row_last(p, it, token) : -1, partial);
             }
+        }
+        if (!more) break;
         }
     } else {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER_REGS));
@@ -635,14 +678,16 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 int32_t at;  // its first row in the pool, of the layer's keys
             };
             const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
-            const int last_page = it.last_slot / p.page_size;
-            // a lane has page `slot` of the tile's unit `unit`, at row `row` of the unit
-            const int unit = lane / 16, slot = lane % 16, row = slot * p.page_rows;
-            const bool has = unit < CTAS && (p.pages_per_unit ? slot < p.pages_per_unit : slot == 0);
+            // a lane has page `place` of the tile's unit `unit`, at row `row` of the unit
+            const int unit = lane / 16, place = lane % 16, row = place * p.page_rows;
+            const bool has = unit < CTAS && (p.pages_per_unit ? place < p.pages_per_unit : place == 0);
+            Item it = s.item[0];
+            after_previous();
+            int last_page = 0;
             auto find = [&](int j) {
                 const int u = (it.k0 + j) * CTAS + unit;
                 Pages r{0, 0};
-                const int pg = p.pages_per_unit ? u * p.pages_per_unit + slot : u / p.units_per_page;
+                const int pg = p.pages_per_unit ? u * p.pages_per_unit + place : u / p.units_per_page;
                 const int sub = p.pages_per_unit ? 0 : u % p.units_per_page * C::UNIT;
                 if (has && pg <= last_page) {
                     const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
@@ -658,13 +703,16 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 return r;
             };
             int chunk = 0;
+            Groups<C> groups;
             const int box_bytes = p.box_rows * 128;
-            auto copy = [&](const Pages &r, bool values) {
+            // the i-th copy of the item
+            auto copy = [&](const Pages &r, bool values, int i) {
                 const int st = chunk % LANDS;
-                if (chunk >= LANDS) {
-                    const int g = FP8 ? chunk - LANDS : C::group(chunk - LANDS);
-                    constexpr int NB = FP8 ? LANDS : C::GROUPS;
-                    if (!wait_bar(s, FP8 ? &s.freed[g % NB] : &s.empty[g % NB], (g / NB) & 1, p.status)) return false;
+                if constexpr (FP8) {
+                    if (chunk >= LANDS && !wait_bar(s, &s.freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
+                } else {
+                    const int g = groups.take(st, lane, i);
+                    if (chunk >= LANDS && !wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status)) return false;
                 }
                 // a pair's keys are split by columns, its values by dimensions
                 const bool mine = r.rows > 0 && (values || CTAS == 1 || unit == rank);
@@ -699,23 +747,46 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 }
                 __syncwarp();
             };
-            Pages now = find(0), next = now;
-            bool ok = n > 0;
-            if (ok) {
-                note_mask(now, 0);
-                ok = copy(now, false);
-            }
-            if (n > 1) next = find(1);
-            for (int j = 0; ok && j < n; ++j) {
-                if (j + 1 < n) {
-                    note_mask(next, j + 1);
-                    ok = copy(next, false);
+            bool ok = true;
+            for (int k = 0, tiles = 0; ok; ++k) {
+                const int n = it.k1 - it.k0;
+                last_page = it.last_slot / p.page_size;
+                Pages now = find(0), next = now;
+                note_mask(now, tiles);
+                ok = copy(now, false, 0);
+                if (n > 1) next = find(1);
+                for (int j = 0; ok && j < n; ++j) {
+                    if (j + 1 < n) {
+                        note_mask(next, tiles + j + 1);
+                        ok = copy(next, false, 2 * j + 1);
+                    }
+                    if (ok) ok = copy(now, true, j + 1 < n ? 2 * j + 2 : 2 * j + 1);
+                    now = next;
+                    if (j + 2 < n) next = find(j + 2);
                 }
-                if (ok) ok = copy(now, true);
-                now = next;
-                if (j + 2 < n) next = find(j + 2);
+                tiles += n;
+                groups.end(n);
+                if (!ok) break;
+                // the next item, for all
+                const int slot = (k + 1) % kItems;
+                if (!wait_bar(s, &s.next[slot], (k / kItems) & 1, p.status)) break;
+                const int x = answered_cta(&s.answer[slot]);
+                fence_proxy_async_shared();  // read before another answer lands there
+                it = item_of(p, max(x, 0) / CTAS, STREAMS * CTAS * kTile);
+                if (x < 0) it.b = -1;
+                if (lane == 0) {
+                    s.item[slot] = it;
+                    mbar_arrive(&s.known[slot]);
+                }
+                if (x < 0) break;
             }
-            if (!ok && n > 0)  // gave up: no copy may still be landing when the CTA ends
+            // every commit's arrival is awaited before the CTA ends
+            if constexpr (!FP8)
+                for (int c = max(0, chunk - LANDS); ok && c < chunk; ++c) {
+                    const int g = groups.of(c % LANDS);
+                    ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
+                }
+            if (!ok)  // gave up: no copy may still be landing when the CTA ends
                 for (int c = max(0, chunk - LANDS); c < chunk; ++c)
                     (void)mbar_wait_bounded(&s.landed[c % LANDS], (c / LANDS) & 1);
         } else if (warp == C::MMA_WARP) {
@@ -724,22 +795,26 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             const uint32_t qk = QK | (p.negate ? kMmaNegateA : 0u);
             const uint32_t q_d = smem_desc(smem_addr(smem), 0), k_d = smem_desc(smem_addr(ring), 0);
             const uint32_t v_d = smem_desc(smem_addr(ring), C::V_BOX);
-            if (rank == 1) (void)mbar_wait_bounded(&s.drained, 0, 10000000000ull);  // while the first CTA issues
+            if (rank == 1) {  // its part in the questions, while the first CTA issues
+                for (int k = 1;; ++k) {
+                    if (lane == 0) mbar_arrive_expect_tx(&s.next[k % kItems], sizeof(uint4));
+                    __syncwarp();
+                    if (!wait_bar(s, &s.next[k % kItems], ((k - 1) / kItems) & 1, p.status)) break;
+                    if (answered_cta(&s.answer[k % kItems]) < 0) break;
+                }
+                (void)mbar_wait_bounded(&s.drained, 0);
+            }
             if (rank == 0 && elect_one()) {
                 auto wait = [&](uint64_t *bar, uint32_t parity) {
                     return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, p.status);
                 };
-                int chunk = 0;
-                // the group of chunk c is there
-                auto arrived = [&](int c) {
-                    const int g = C::group(c);
+                int chunk = 0, group = 0;  // of the next chunk; groups of the items before
+                // the group of the item's i-th chunk is there; its place is free
+                auto arrived = [&](int i) {
+                    const int g = group + C::group(i);
                     return wait(&s.ready[g % C::GROUPS], (g / C::GROUPS) & 1);
                 };
-                // chunk c's place, and its group's, is free (where a later chunk takes it:
-                // every arrival of a commit has a waiter before the CTAs end)
-                auto release = [&](int c) {
-                    if (c - (C::GROUPED ? 1 : 0) + STAGES < 2 * n) mma_commit<CTAS>(&s.empty[C::group(c) % C::GROUPS]);
-                };
+                auto release = [&](int i) { mma_commit<CTAS>(&s.empty[(group + C::group(i)) % C::GROUPS]); };
                 // S = Q K^T of a stream into score columns `buf`, keys in chunk c
                 auto scores = [&](int stream, int buf, int c) {
                     const uint32_t q = q_d + stream * (kTile * D * 2 / 16), k = k_d + c % STAGES * (C::CHUNK / 16);
@@ -759,41 +834,64 @@ __global__ void __launch_bounds__(C::THREADS, 1)
 #pragma unroll
                     for (int i = 1; i < kTile / 32; ++i) mma_ts<CTAS>(to, w + i * 8, v + i * (2048 / 16), PV, true);
                 };
-                bool ok = n > 0 && wait(&s.queries, 0) && arrived(0);
-                tc_after_sync();
-                if (ok) {
-                    for (int st = 0; st < STREAMS; ++st) scores(st, st, 0);
+                auto ask = [&](int k) {
+                    mbar_arrive_expect_tx(&s.next[k % kItems], sizeof(uint4));
+                    ask_for_cta<CTAS>(&s.answer[k % kItems], &s.next[k % kItems]);
+                };
+                ask(1);
+                bool ok = true;
+                int n = s.item[0].k1 - s.item[0].k0;
+                for (int k = 0, tiles = 0; ok; ++k) {
+                    ok = wait(&s.queries, k & 1) && arrived(0);
+                    if (!ok) break;
+                    tc_after_sync();
+                    // every warp is in this item; no further question after a no
+                    ok = wait(&s.next[(k + 1) % kItems], (k / kItems) & 1);
+                    if (!ok) break;
+                    if (answered_cta(&s.answer[(k + 1) % kItems]) >= 0) ask(k + 2);
+                    for (int st = 0; st < STREAMS; ++st) scores(st, STREAMS == 1 ? tiles & 1 : st, chunk);
                     release(0);
-                    chunk = 1;
-                }
-                for (int j = 0; ok && j < n; ++j) {
-                    const int k_at = chunk;
-                    const bool more = j + 1 < n;
-                    if (more) {
-                        ok = arrived(chunk++);
-                        if (!ok) break;
-                        if (STREAMS == 1) {  // the next scores, beside this tile's weights
-                            // (their buffer's weights, of tile j - 1, were multiplied before)
-                            scores(0, (j + 1) & 1, k_at);
-                            release(k_at);
-                        }
-                    }
-                    if (!C::GROUPED || !more) ok = arrived(chunk);
-                    for (int st = 0; ok && st < STREAMS; ++st) {
-                        const int buf = STREAMS == 1 ? j & 1 : st;
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            ok = wait(&s.weights[buf][half], (STREAMS == 1 ? j >> 1 : j) & 1);
+                    ++chunk;
+                    int i = 1;  // chunk of the item
+                    for (int j = 0; ok && j < n; ++j) {
+                        const int J = tiles + j, k_at = chunk;
+                        const bool more = j + 1 < n;
+                        if (more) {
+                            ok = arrived(i);
                             if (!ok) break;
-                            tc_after_sync();
-                            product(st, buf, half, chunk, j > 0);
+                            if (STREAMS == 1) {  // the next scores, beside this tile's weights
+                                // (their buffer's weights, of tile j - 1, were multiplied before)
+                                scores(0, (J + 1) & 1, k_at);
+                                release(i);
+                            }
+                            ++i, ++chunk;
+                        }
+                        if (!C::GROUPED || !more) ok = arrived(i);
+                        for (int st = 0; ok && st < STREAMS; ++st) {
+                            const int buf = STREAMS == 1 ? J & 1 : st;
+                            // (the first product of an item takes the place of the outputs before)
+                            if (j == 0 && k > 0) ok = wait(&s.taken[st], (k - 1) & 1);
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                ok = ok && wait(&s.weights[buf][half], (STREAMS == 1 ? J >> 1 : J) & 1);
+                                if (!ok) break;
+                                tc_after_sync();
+                                product(st, buf, half, chunk, j > 0);
+                            }
+                            if (!ok) break;
+                            if (STREAMS == 1 || !more) mma_commit<CTAS>(&s.out[st]);
+                            if (STREAMS == 2 && more) scores(st, st, k_at);
                         }
                         if (!ok) break;
-                        if (STREAMS == 1 || !more) mma_commit<CTAS>(&s.out[st]);
-                        if (STREAMS == 2 && more) scores(st, st, k_at);
+                        release(i);
+                        ++i, ++chunk;
                     }
                     if (!ok) break;
-                    release(chunk++);
+                    tiles += n;
+                    group += C::group(2 * n - 1) + 1;
+                    ok = wait(&s.known[(k + 1) % kItems], (k / kItems) & 1);
+                    if (!ok || s.item[(k + 1) % kItems].b < 0) break;
+                    n = s.item[(k + 1) % kItems].k1 - s.item[(k + 1) % kItems].k0;
                 }
                 // all products have completed before the tensor memory is given back
                 mma_commit<CTAS>(&s.drained);
@@ -803,39 +901,48 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         } else if (!FP8 && warp == C::TIDY_WARP) {
             // ---- value rows that are not valid hold anything: zero weights must meet zeros
             bool ok = true;
-            for (int i = 0; ok && i < 2 * n; ++i) {
-                const int st = i % STAGES;
-                ok = wait_bar(s, &s.landed[st], (i / STAGES) & 1, p.status);
-                if (!ok) break;
-                int j;
-                if (value_tile(i, n, j)) {
-                    const uint32_t *m = s.mask[j % kMaskSlots];
-                    if ((m[0] & m[1] & m[2] & m[3]) != ~0u) {
-                        uint8_t *v = ring + st * C::CHUNK;
-                        for (int r = lane / 8; r < kTile; r += 4)
-                            if (!(m[r / 32] >> (r % 32) & 1))
+            for (int k = 0, tiles = 0, chunk = 0, group = 0; ok; ++k) {
+                const int n = s.item[k % kItems].k1 - s.item[k % kItems].k0;
+                for (int i = 0; ok && i < 2 * n; ++i, ++chunk) {
+                    const int st = chunk % STAGES;
+                    ok = wait_bar(s, &s.landed[st], (chunk / STAGES) & 1, p.status);
+                    if (!ok) break;
+                    int j;
+                    if (value_tile(i, n, j)) {
+                        const uint32_t *m = s.mask[(tiles + j) % kMaskSlots];
+                        if ((m[0] & m[1] & m[2] & m[3]) != ~0u) {
+                            uint8_t *v = ring + st * C::CHUNK;
+                            for (int r = lane / 8; r < kTile; r += 4)
+                                if (!(m[r / 32] >> (r % 32) & 1))
 #pragma unroll
-                                for (int x = 0; x < C::V_BOXES; ++x)
-                                    reinterpret_cast<uint4 *>(v + x * C::V_BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
-                        fence_proxy_async_shared();
+                                    for (int x = 0; x < C::V_BOXES; ++x)
+                                        reinterpret_cast<uint4 *>(v + x * C::V_BOX + r * 128)[lane % 8] = make_uint4(0, 0, 0, 0);
+                            fence_proxy_async_shared();
+                        }
                     }
+                    // (twice for a group of one)
+                    arrive_issuer(&s.ready[(group + C::group(i)) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
                 }
-                // (twice for a group of one)
-                arrive_issuer(&s.ready[C::group(i) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
+                tiles += n;
+                group += C::group(2 * n - 1) + 1;
+                ok = ok && has_item(k + 1);
             }
         } else if (FP8 && warp >= C::CONVERT_WARP) {
             // ---- E4M3 codes to fp16 (exact), chunk by chunk
             const int t = threadIdx.x - 32 * C::CONVERT_WARP, u = t % 8;
             bool ok = true;
-            for (int i = 0; ok && i < 2 * n; ++i) {
-                const int rs = i % LANDS, st = i % STAGES;
+            Groups<C> groups;
+            int chunk = 0;
+            for (int k = 0, tiles = 0, group = 0; ok; ++k) {
+            const int n = s.item[k % kItems].k1 - s.item[k % kItems].k0;
+            for (int i = 0; ok && i < 2 * n; ++i, ++chunk) {
+                const int rs = chunk % LANDS, st = chunk % STAGES;
                 int j;
                 const bool values = value_tile(i, n, j);
-                ok = wait_bar(s, &s.landed[rs], (i / LANDS) & 1, p.status);
-                if (ok && i >= STAGES) {
-                    const int g = C::group(i - STAGES);
-                    ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
-                }
+                j += tiles;
+                ok = wait_bar(s, &s.landed[rs], (chunk / LANDS) & 1, p.status);
+                const int g = groups.take(st, lane, i);
+                if (ok && chunk >= STAGES) ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
                 if (!ok) break;
                 const uint8_t *src = raw + rs * C::RAW;
                 uint8_t *dst = ring + st * C::CHUNK;
@@ -877,8 +984,18 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     *reinterpret_cast<uint4 *>(to + (((u2 + 1 - odd) ^ (r & 7)) << 4)) = odd ? a : b;
                 }
                 fence_proxy_async_shared();
-                arrive_issuer(&s.ready[C::group(i) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
+                arrive_issuer(&s.ready[(group + C::group(i)) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
                 if (lane == 0) mbar_arrive(&s.freed[rs]);
+            }
+            tiles += n;
+            group += C::group(2 * n - 1) + 1;
+            groups.end(n);
+            if (!ok || !has_item(k + 1)) break;
+            }
+            // every commit's arrival is awaited before the CTA ends
+            for (int c = max(0, chunk - STAGES); ok && c < chunk; ++c) {
+                const int g = groups.of(c % STAGES);
+                ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
             }
         }
     }

@@ -159,6 +159,37 @@ __device__ __forceinline__ void mbar_arrive_first(uint64_t *bar) {
         : "memory");
 }
 
+// ------------------------------------------------------- work of other CTAs --
+// One thread: asks for a CTA (a cluster) of the grid that has not started, to do
+// its work instead; the answer, 16 bytes, lands at `answer` and completes 16
+// bytes on `bar` (of every CTA of a cluster).  Not to be asked again after a no.
+template <int CTAS>
+__device__ __forceinline__ void ask_for_cta(uint4 *answer, uint64_t *bar) {
+    if constexpr (CTAS == 1)
+        asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                         smem_addr(answer)),
+                     "r"(smem_addr(bar))
+                     : "memory");
+    else
+        asm volatile(
+            "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.multicast::cluster::all.b128 "
+            "[%0], [%1];" ::"r"(smem_addr(answer)),
+            "r"(smem_addr(bar))
+            : "memory");
+}
+// The x index of that CTA (the cluster's first), or -1.
+__device__ __forceinline__ int answered_cta(const uint4 *answer) {
+    uint32_t x = 0, yes;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\tld.shared.b128 a, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\tselp.u32 %1, 1, 0, p;\n\tmov.u32 %0, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
+        : "=r"(x), "=r"(yes)
+        : "r"(smem_addr(answer))
+        : "memory");
+    return yes ? (int)x : -1;
+}
+
 // ---------------------------------------------------- packed fp32 and exp2 --
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
