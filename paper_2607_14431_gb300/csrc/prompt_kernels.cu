@@ -538,11 +538,13 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     for (int i = 0; i < 32; ++i) x[32 * w + i] = bits >> i & 1 ? x[32 * w + i] : -INFINITY;
                 }
             }
-            float t[4] = {x[0], x[1], x[2], x[3]};
+            float t[4];
 #pragma unroll
-            for (int i = 4; i < kTile; i += 4)
+            for (int e = 0; e < 4; ++e) t[e] = fmaxf(x[e], x[4 + e]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] = fmaxf(t[e], x[i + e]);
+            for (int i = 8; i < kTile; i += 8)  // (three operands to an instruction)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = fmaxf(fmaxf(t[e], x[i + e]), x[i + 4 + e]);
             const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
             // move the reference?  (-inf: no column so far, nothing to rescale)
             const bool move = top > m && (m == -INFINITY || (top - m) * c > kMaxSlack);
