@@ -38,6 +38,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -656,10 +657,8 @@ struct Merged {
 };
 constexpr int kCombineMaxThreads = 512;
 
-// SHARED: the row's partials over shared pages follow the decode's own.
-template <int D, int COLS, bool SHARED = false>
-__device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, int col0, int b, int lr,
-                                                 const SharedParts *sp = nullptr) {
+template <int D, int COLS>
+__device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, int col0, int b, int lr) {
     constexpr int LANES = COLS / 4;
     __shared__ float4 sum_o[kCombineMaxThreads];
     __shared__ float sum_l[kCombineMaxThreads / LANES];
@@ -670,8 +669,7 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     const int grp = lr >= p.layer1;
     const int32_t *pref = p.rows[grp].pref_tiles;
     const int64_t Tb = pref[b + 1] - pref[b];
-    const int n_shared = SHARED ? sp->splits[b] : 0;
-    if (Tb + n_shared <= 0) {  // the whole block
+    if (Tb <= 0) {  // the whole block
         after_previous();
         return res;
     }
@@ -679,29 +677,15 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     const int64_t unit = ((int64_t)lr * p.B + b) * p.n_kv_heads + g;
     const int64_t first = (int64_t)g * Tb +  // of the group's tiles
                           (int64_t)p.n_kv_heads * ((int64_t)(lr - (grp ? p.layer1 : 0)) * pref[p.B] + pref[b]);
-    const int64_t wa = Tb > 0 ? warp_of(first, T, W) : 0;
-    const int n_own = Tb > 0 ? (int)(warp_of(first + Tb - 1, T, W) - wa) + 1 : 0, n = n_own + n_shared;
+    const int64_t wa = warp_of(first, T, W);
+    const int n = (int)(warp_of(first + Tb - 1, T, W) - wa) + 1;
     const int64_t slot = unit + wa + (grp ? p.n_warps[0] : 0);
     const float2 *ml = p.part_ml + slot * G + hh;
     const float4 *po = reinterpret_cast<const float4 *>(p.part_o + (slot * G + hh) * D + col0) + d4;
     const int64_t step = (int64_t)G * (D / 4);  // float4 between consecutive partials
-    auto shared_slot = [&](int i) {
-        const int64_t u = (int64_t)(i - n_own) * sp->units + p.qlayers[lr] * p.n_kv_heads + g;
-        return sp->at[b] + u * sp->rows[b] + hh;
-    };
-    auto ml_at = [&](int i) {
-        if constexpr (SHARED)
-            if (i >= n_own) return sp->part_ml[shared_slot(i)];
-        return ml[(int64_t)i * G];
-    };
-    auto o_at = [&](int i) {
-        if constexpr (SHARED)
-            if (i >= n_own) return reinterpret_cast<const float4 *>(sp->part_o + shared_slot(i) * D + col0)[d4];
-        return po[i * step];
-    };
     after_previous();
     float M = -INFINITY;
-    for (int i = threadIdx.x & 31; i < n; i += 32) M = fmaxf(M, ml_at(i).x);
+    for (int i = threadIdx.x & 31; i < n; i += 32) M = fmaxf(M, ml[(int64_t)i * G].x);
 #pragma unroll
     for (int x = 16; x; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
     res.M = M;
@@ -714,8 +698,8 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * R;
                 if (i < n) {
-                    x[u] = ml_at(i);
-                    v[u] = o_at(i);
+                    x[u] = ml[(int64_t)i * G];
+                    v[u] = po[i * step];
                 }
             }
 #pragma unroll
@@ -749,33 +733,91 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     return res;
 }
 
-// (o / l) vscale of a head's columns as bf16 (SHARED: a sum that is NaN gives NaN).
-template <int D, int COLS, bool SHARED = false>
-__device__ __forceinline__ void store_merged(const DecodeParams &p, const Merged &m, int h, int col0, int b, int lr) {
+template <int D, int COLS>
+__global__ void __launch_bounds__(kCombineMaxThreads) combine_kernel(const DecodeParams p) {
+    constexpr int PARTS = D / COLS;
+    const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
+    const Merged m = merge_partials<D, COLS>(p, h, col0, b, lr);
     if (threadIdx.x >= COLS / 4) return;
     float r[4] = {m.o.x, m.o.y, m.o.z, m.o.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = (SHARED ? m.L != 0.f : m.L > 0.f) ? __fdiv_rn(r[e], m.L) * p.vscale : 0.f;
+    for (int e = 0; e < 4; ++e) r[e] = m.L > 0.f ? __fdiv_rn(r[e], m.L) * p.vscale : 0.f;
     const __nv_bfloat162 lo = __floats2bfloat162_rn(r[0], r[1]), hi = __floats2bfloat162_rn(r[2], r[3]);
     uint2 *out = reinterpret_cast<uint2 *>(
         p.out + ((int64_t)(p.qlayers[lr] * p.q_row_stride_b + p.b0 + b) * p.n_q_heads + h) * D + col0);
     out[threadIdx.x] = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
 }
 
-template <int D, int COLS>
-__global__ void __launch_bounds__(kCombineMaxThreads) combine_kernel(const DecodeParams p) {
-    constexpr int PARTS = D / COLS;
-    const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
-    store_merged<D, COLS>(p, merge_partials<D, COLS>(p, h, col0, b, lr), h, col0, b, lr);
-}
-
-// The same for rows that read some of their pages together (kvg_decode_attention_shared).
-template <int D, int COLS>
-__global__ void __launch_bounds__(kCombineMaxThreads)
+// Merge of a decode whose rows read some of their pages together
+// (kvg_decode_attention_shared): the row's partials over the shared pages, then
+// its own.  Few of each (an SM has a key range of the shared pages, a short tail
+// is a warp or two), so a warp takes a row, a lane D / 32 of its columns, four
+// partials in flight: 3,072 rows of the 31B shape over 9 ranges COMBINE_NOW,
+// with a block per row as above COMBINE_BEFORE.
+constexpr int kCombineRows = 8;  // of a block
+template <int D>
+__global__ void __launch_bounds__(32 * kCombineRows)
     combine_shared_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ SharedParts sp) {
-    constexpr int PARTS = D / COLS;
-    const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
-    store_merged<D, COLS, true>(p, merge_partials<D, COLS, true>(p, h, col0, b, lr, &sp), h, col0, b, lr);
+    constexpr int N = D / 32, U = 4;
+    using Vec = std::conditional_t<N == 2, float2, float4>;
+    constexpr int W = sizeof(Vec) / 4;
+    const int lane = threadIdx.x & 31, G = p.n_q_heads / p.n_kv_heads;
+    const int at = blockIdx.x * kCombineRows + threadIdx.x / 32;
+    if (at >= p.n_q_heads * p.B * p.n_layers_run) return;
+    const int h = at % p.n_q_heads, b = at / p.n_q_heads % p.B, lr = at / p.n_q_heads / p.B;
+    const int g = h / G, hh = h - g * G, grp = lr >= p.layer1;
+    // the row's own partials: of the decode's warps wa, wa + 1, ...
+    const int32_t *pref = p.rows[grp].pref_tiles;
+    const int64_t Tb = pref[b + 1] - pref[b], T = p.group_tiles(grp), WN = p.n_warps[grp];
+    const int64_t unit = ((int64_t)lr * p.B + b) * p.n_kv_heads + g;
+    int n_own = 0;
+    int64_t own = 0;
+    if (Tb > 0) {
+        const int64_t first = (int64_t)g * Tb +  // of the group's tiles
+                              (int64_t)p.n_kv_heads * ((int64_t)(lr - (grp ? p.layer1 : 0)) * pref[p.B] + pref[b]);
+        const int64_t wa = warp_of(first, T, WN);
+        n_own = (int)(warp_of(first + Tb - 1, T, WN) - wa) + 1;
+        own = (unit + wa + (grp ? p.n_warps[0] : 0)) * G + hh;
+    }
+    const int n_shared = sp.splits[b], n = n_shared + n_own;
+    const int64_t part = sp.at[b] + (int64_t)(p.qlayers[lr] * p.n_kv_heads + g) * sp.rows[b] + hh;
+    const int64_t part_step = (int64_t)sp.units * sp.rows[b];
+    after_previous();
+    auto ml_at = [&](int i) { return i < n_shared ? sp.part_ml[part + i * part_step] : p.part_ml[own + (int64_t)(i - n_shared) * G]; };
+    float M = -INFINITY;
+    for (int i = lane; i < n; i += 32) M = fmaxf(M, ml_at(i).x);
+#pragma unroll
+    for (int x = 16; x; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+    float o[N] = {}, L = 0.f;
+    for (int i0 = 0; i0 < n; i0 += U) {
+        Vec v[U][N / W];
+        float2 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u;
+            if (i >= n) continue;
+            x[u] = ml_at(i);
+            const float *src = i < n_shared ? sp.part_o + (part + i * part_step) * D : p.part_o + (own + (int64_t)(i - n_shared) * G) * D;
+#pragma unroll
+            for (int e = 0; e < N / W; ++e) v[u][e] = reinterpret_cast<const Vec *>(src + lane * N)[e];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u >= n || x[u].y == 0.f) continue;  // (no rows: not even written)
+            const float sc = exp2f(x[u].x - M);
+            L = __fmaf_rn(x[u].y, sc, L);
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = __fmaf_rn(reinterpret_cast<const float *>(v[u])[e], sc, o[e]);
+        }
+    }
+    uint32_t *out = reinterpret_cast<uint32_t *>(
+        p.out + ((int64_t)(p.qlayers[lr] * p.q_row_stride_b + p.b0 + b) * p.n_q_heads + h) * D + lane * N);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {  // (a sum that is NaN gives NaN)
+        const float y0 = L != 0.f ? __fdiv_rn(o[e], L) * p.vscale : 0.f, y1 = L != 0.f ? __fdiv_rn(o[e + 1], L) * p.vscale : 0.f;
+        const __nv_bfloat162 y = __floats2bfloat162_rn(y0, y1);
+        out[e / 2] = *reinterpret_cast<const uint32_t *>(&y);
+    }
 }
 
 // The same merge for a split decode: the unit's partials give (M, L, O) for
@@ -965,7 +1007,7 @@ cudaError_t launch_decode(int head_dim, int group, bool fp8, const DecodeParams 
 // Threads of a combine block over `cols` columns of a head: a group of cols / 4
 // lanes per up to four partials of the row with the most of them (the loads
 // one thread keeps in flight).
-static int combine_threads(int cols, const DecodeParams &p, int n_shared = 0) {
+static int combine_threads(int cols, const DecodeParams &p) {
     int64_t most = 1;
     for (int g = 0; g < kMaxWindowGroups; ++g) {
         if (p.group_tiles(g) <= 0) continue;
@@ -974,7 +1016,6 @@ static int combine_threads(int cols, const DecodeParams &p, int n_shared = 0) {
             tb = std::max<int64_t>(tb, p.rows[g].pref_tiles[b + 1] - p.rows[g].pref_tiles[b]);
         most = std::max(most, tb * p.n_warps[g] / p.group_tiles(g) + 2);
     }
-    most += n_shared;
     const int lanes = cols / 4;
     int threads = std::max(lanes, 32);
     while (threads < kCombineMaxThreads && (int64_t)(threads / lanes) * 4 < most) threads *= 2;
@@ -998,18 +1039,13 @@ cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaSt
     return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, int n_sm,
-                                  cudaStream_t s) {
-    const bool narrow = (int64_t)p.n_q_heads * p.B * p.n_layers_run <= n_sm;
-    const int cols = narrow ? 64 : head_dim;
-    const dim3 grid(p.n_q_heads * (head_dim / cols), p.B, p.n_layers_run);
-    const int n = combine_threads(cols, p, *std::max_element(parts.splits, parts.splits + p.B));
+cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s) {
+    const int64_t rows = (int64_t)p.n_q_heads * p.B * p.n_layers_run;
+    const unsigned grid = (unsigned)((rows + kCombineRows - 1) / kCombineRows);
     switch (head_dim) {
-        case 64: return launch_after(combine_shared_kernel<64, 64>, grid, n, 0, s, p, parts);
-        case 128:
-            return launch_after(narrow ? combine_shared_kernel<128, 64> : combine_shared_kernel<128, 128>, grid, n, 0, s, p, parts);
-        case 256:
-            return launch_after(narrow ? combine_shared_kernel<256, 64> : combine_shared_kernel<256, 256>, grid, n, 0, s, p, parts);
+        case 64: return launch_after(combine_shared_kernel<64>, grid, 32 * kCombineRows, 0, s, p, parts);
+        case 128: return launch_after(combine_shared_kernel<128>, grid, 32 * kCombineRows, 0, s, p, parts);
+        case 256: return launch_after(combine_shared_kernel<256>, grid, 32 * kCombineRows, 0, s, p, parts);
     }
     return cudaErrorInvalidValue;
 }

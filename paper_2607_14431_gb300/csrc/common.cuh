@@ -526,8 +526,7 @@ cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuui
                               const cuuint64_t *strides, const cuuint32_t *box);
 cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaStream_t s);
 // The combine with the partials of the rows' shared pages beside the decode's.
-cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, int n_sm,
-                                  cudaStream_t s);
+cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
 bool decode_supported(int head_dim, int group, bool fp8 = false);
 int decode_tile_tokens(int head_dim, bool fp8, int page_size);
 int decode_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);

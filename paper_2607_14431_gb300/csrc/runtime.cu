@@ -2850,7 +2850,7 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
             parts.splits[i] = row_splits[p.b0 + i];
             parts.at[i] = row_at[p.b0 + i];
         }
-        KVG_CUDA(launch_combine_shared(d.head_dim, p, parts, c->n_sm, st));
+        KVG_CUDA(launch_combine_shared(d.head_dim, p, parts, st));
     }
     return used_partials(c, st);
 }
