@@ -783,6 +783,7 @@ __global__ void __launch_bounds__(32 * kCombineRows)
     const int64_t part = sp.at[b] + (int64_t)(p.qlayers[lr] * p.n_kv_heads + g) * sp.rows[b] + hh;
     const int64_t part_step = (int64_t)sp.units * sp.rows[b];
     after_previous();
+    let_next_start();  // a few microseconds to its end, and room for the next beside it
     auto ml_at = [&](int i) { return i < n_shared ? sp.part_ml[part + i * part_step] : p.part_ml[own + (int64_t)(i - n_shared) * G]; };
     float M = -INFINITY;
     for (int i = lane; i < n; i += 32) M = fmaxf(M, ml_at(i).x);

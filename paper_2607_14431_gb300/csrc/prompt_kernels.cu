@@ -368,6 +368,68 @@ __device__ __forceinline__ bool value_tile(int i, int n, int &j) {
     return last || (i > 0 && i % 2 == 0);
 }
 
+// A lane's page of a key tile: lane i has page i % 16 of the tile's unit i / 16.
+struct Page {
+    int rows;    // valid rows of it in the tile
+    int32_t at;  // its first row in the pool, of the layer's keys
+};
+template <class C>
+__device__ __forceinline__ Page find_page(const PromptParams &p, const Item &it, int kt, int lane) {
+    const int unit = lane / 16, place = lane % 16, u = kt * C::CTAS + unit;
+    const bool has = unit < C::CTAS && (p.pages_per_unit ? place < p.pages_per_unit : place == 0);
+    const int pg = p.pages_per_unit ? u * p.pages_per_unit + place : u / p.units_per_page;
+    const int sub = p.pages_per_unit ? 0 : u % p.units_per_page * C::UNIT;
+    Page r{0, 0};
+    if (has && pg <= it.last_slot / p.page_size) {
+        const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
+        const int pid = p.page_table[e];
+        r.rows = max(0, min(p.pages_per_unit ? p.page_size : C::UNIT, p.page_fill[e] - sub));
+        if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
+            record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
+            r.rows = 0;
+        }
+        r.at = (int32_t)((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads * p.page_size +
+                         ((int64_t)pid * p.n_kv_heads + it.g) * p.page_size + sub);
+    }
+    return r;
+}
+
+// Queries of a tile's rows on their way to shared memory: a warp's 32 rows, in
+// batches whose loads are all under way before the first is stored.
+template <class C>
+struct Queries {
+    static constexpr int D = C::D, LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR, N = 32 / RPI, BATCH = N < 16 ? N : 16;
+    uint4 x[BATCH];
+    // rows from first + i0 * RPI of the item (the last again past its end)
+    __device__ __forceinline__ void load(const PromptParams &p, const Item &it, int first, int i0, int lane) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int r = first + (i0 + i) * RPI + lane / LPR;
+            x[i] = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + min(r, it.rows - 1)) * D)[lane % LPR];
+        }
+    }
+    // to the swizzled rows of the tile at `to` (zeros past the item's end)
+    __device__ __forceinline__ void store(const Item &it, int first, int i0, int lane, uint8_t *to) const {
+        const int u = lane % LPR;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int r = first + (i0 + i) * RPI + lane / LPR, rt = r % kTile;
+            uint4 y = x[i];
+            if constexpr (C::FP8) {
+                uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                    w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                }
+                y = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (r >= it.rows) y = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(to + u / 8 * (kTile * 128) + rt * 128 + ((u % 8 ^ (rt & 7)) << 4)) = y;
+        }
+    }
+};
+
 // Which group's commit frees each place of the ring: a lane remembers the group
 // of the chunk that its place holds.
 template <class C>
@@ -433,9 +495,24 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         s.abort = 0;
         fence_mbar_init();
     }
-    // (from the launch's parameters alone: beside the set-up and the kernel before)
-    if (threadIdx.x == 32 * C::LOAD_WARP) s.item[0] = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
     if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
+    // The first item (from the launch's parameters alone), its first pages and its
+    // queries, all beside the set-up.
+    const int q_first = first + warp * 32;  // the warp's first row of the item
+    Queries<C> queries;
+    Item it;
+    Page now{0, 0}, next{0, 0};
+    if (warp <= C::LOAD_WARP) {
+        it = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
+        after_previous();
+        if (warp < C::LOAD_WARP) {
+            queries.load(p, it, q_first, 0, lane);
+        } else {
+            now = find_page<C>(p, it, it.k0, lane);
+            if (it.k1 - it.k0 > 1) next = find_page<C>(p, it, it.k0 + 1, lane);
+            if (lane == 0) s.item[0] = it;
+        }
+    }
     tc_before_sync();
     if constexpr (CTAS == 2)
         cluster_sync();
@@ -456,42 +533,19 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     if (warp < C::SOFTMAX_WARPS) {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
         const int stream = warp / 4;
-        // an item's queries to shared memory (rows past the item's as zeros): a batch
-        // of loads all on their way before the first is stored
-        constexpr int LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR, N = 32 / RPI, BATCH = N < 16 ? N : 16;
-        auto fetch_queries = [&](const Item &it) {
-            const int u = lane % LPR;
+        uint8_t *const q_tile = smem + stream * (kTile * D * 2);
+        // the batches after the first, which has been loaded
+        auto finish_queries = [&](const Item &it, Queries<C> &q) {
+            q.store(it, q_first, 0, lane, q_tile);
 #pragma unroll 1
-            for (int i0 = 0; i0 < N; i0 += BATCH) {
-            uint4 qx[BATCH];
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {
-                const int r = first + warp * 32 + (i0 + i) * RPI + lane / LPR;
-                qx[i] = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + min(r, it.rows - 1)) * D)[u];
-            }
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {
-                const int r = warp * 32 + (i0 + i) * RPI + lane / LPR, rt = r % kTile;
-                uint4 x = qx[i];
-                if constexpr (FP8) {
-                    uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
-                        w[e] = *reinterpret_cast<const uint32_t *>(&h);
-                    }
-                    x = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                if (first + r >= it.rows) x = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(smem + r / kTile * (kTile * D * 2) + u / 8 * (kTile * 128) + rt * 128 +
-                                           ((u % 8 ^ (rt & 7)) << 4)) = x;
-            }
+            for (int i0 = Queries<C>::BATCH; i0 < Queries<C>::N; i0 += Queries<C>::BATCH) {
+                q.load(p, it, q_first, i0, lane);
+                q.store(it, q_first, i0, lane, q_tile);
             }
             fence_proxy_async_shared();
             arrive_issuer(&s.queries);
         };
-        after_previous();
-        fetch_queries(s.item[0]);
+        finish_queries(it, queries);
         bool ok = true;
         int tiles = 0;  // of the items before
         for (int k = 0; ok; ++k) {
@@ -617,7 +671,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         // ---- the next item's queries (this one's scores are all there, so nothing
         // reads their place any more): its first products run beside the output
         const bool more = has_item(k + 1);
-        if (more) fetch_queries(s.item[(k + 1) % kItems]);
+        if (more) {
+            const Item &after = s.item[(k + 1) % kItems];
+            Queries<C> q;
+            q.load(p, after, q_first, 0, lane);
+            finish_queries(after, q);
+        }
         // ---- output
         ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (tiles - 1) & 1 : k & 1, p.status);
         if (ok) {
@@ -675,40 +734,14 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER_REGS));
         if (warp == C::LOAD_WARP) {
             // ---- keys and values of tile j: K0, then K(j + 1) and V(j) in turn
-            struct Pages {
-                int rows;    // valid rows of the lane's page in the tile
-                int32_t at;  // its first row in the pool, of the layer's keys
-            };
             const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
-            // a lane has page `place` of the tile's unit `unit`, at row `row` of the unit
-            const int unit = lane / 16, place = lane % 16, row = place * p.page_rows;
-            const bool has = unit < CTAS && (p.pages_per_unit ? place < p.pages_per_unit : place == 0);
-            Item it = s.item[0];
-            after_previous();
-            int last_page = 0;
-            auto find = [&](int j) {
-                const int u = (it.k0 + j) * CTAS + unit;
-                Pages r{0, 0};
-                const int pg = p.pages_per_unit ? u * p.pages_per_unit + place : u / p.units_per_page;
-                const int sub = p.pages_per_unit ? 0 : u % p.units_per_page * C::UNIT;
-                if (has && pg <= last_page) {
-                    const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
-                    const int pid = p.page_table[e];
-                    r.rows = max(0, min(p.pages_per_unit ? p.page_size : C::UNIT, p.page_fill[e] - sub));
-                    if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
-                        record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
-                        r.rows = 0;
-                    }
-                    r.at = (int32_t)((int64_t)p.layers[it.lr] * 2 * plane +
-                                     ((int64_t)pid * p.n_kv_heads + it.g) * p.page_size + sub);
-                }
-                return r;
-            };
+            const int unit = lane / 16, row = lane % 16 * p.page_rows;         // of the lane's page
+            auto find = [&](int j) { return find_page<C>(p, it, it.k0 + j, lane); };
             int chunk = 0;
             Groups<C> groups;
             const int box_bytes = p.box_rows * 128;
             // the i-th copy of the item
-            auto copy = [&](const Pages &r, bool values, int i) {
+            auto copy = [&](const Page &r, bool values, int i) {
                 const int st = chunk % LANDS;
                 if constexpr (FP8) {
                     if (chunk >= LANDS && !wait_bar(s, &s.freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
@@ -737,7 +770,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 ++chunk;
                 return true;
             };
-            auto note_mask = [&](const Pages &r, int j) {
+            auto note_mask = [&](const Page &r, int j) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int a = unit * C::UNIT + row - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
@@ -752,11 +785,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             bool ok = true;
             for (int k = 0, tiles = 0; ok; ++k) {
                 const int n = it.k1 - it.k0;
-                last_page = it.last_slot / p.page_size;
-                Pages now = find(0), next = now;
+                if (k > 0) {
+                    now = find(0);
+                    if (n > 1) next = find(1);
+                }
                 note_mask(now, tiles);
                 ok = copy(now, false, 0);
-                if (n > 1) next = find(1);
                 for (int j = 0; ok && j < n; ++j) {
                     if (j + 1 < n) {
                         note_mask(next, tiles + j + 1);
@@ -1016,6 +1050,7 @@ template <int D>
 __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant__ PromptParams p) {
     constexpr int N = D / 32;
     after_previous();
+    let_next_start();  // a few microseconds to its end, and room for the next beside it
     const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
     const int lane = threadIdx.x & 31, gs = 31 - __clz(p.n_q_heads / p.n_kv_heads);
     if (at >= ((int64_t)p.first[p.n_seq] << gs) * p.n_units) return;
