@@ -801,6 +801,13 @@ struct kvg_cache {
     cudaEvent_t batch_ev = nullptr, batch_done = nullptr;
     std::vector<uint8_t> pinned;  // per page: owned by a pool-resident store block
     std::vector<int32_t> alias;   // per pinned page: sequences whose page tables point at it
+    // per sequence: the runs of a block's full pages that its page table points
+    // at.  A page is of one block, so equal runs are the same pages.
+    struct AliasRun {
+        int32_t page0, first_pid, n;  // from the sequence's page page0
+        bool operator==(const AliasRun &o) const { return page0 == o.page0 && first_pid == o.first_pid && n == o.n; }
+    };
+    std::vector<std::vector<AliasRun>> seq_alias;
     // cos/sin tables of the deltas grafts have used (cos[D/2] then sin[D/2]),
     // so a batch that re-bases many grafts does not recompute them each call
     std::unordered_map<int64_t, std::vector<float>> rope_memo;
@@ -1000,6 +1007,7 @@ extern "C" kvg_status kvg_cache_create(const kvg_dims *dims, int32_t n_pages, in
     c->pinned.assign(n_pages, 0);
     c->alias.assign(n_pages, 0);
     c->seq_pages.assign(max_seqs, {});
+    c->seq_alias.assign(max_seqs, {});
     c->n_slots.assign(max_seqs, 0);
     c->open_slot.assign(max_seqs, 0);
     c->open_rows.assign(max_seqs, 0);
@@ -1404,6 +1412,7 @@ extern "C" kvg_status kvg_cache_release(kvg_cache *c, int32_t seq, void *stream)
             c->free_list.push_back(pid);
     }
     c->seq_pages[seq].clear();
+    c->seq_alias[seq].clear();
     c->seq_fill[seq].clear();
     c->n_slots[seq] = 0;
     c->open_rows[seq] = 0;
@@ -1743,6 +1752,7 @@ static kvg_status pool_graft(kvg_store *s, const kvg_store::Blk &blk, kvg_cache 
     auto &sp = c->seq_pages[seq];
     const int64_t jdst = dst / P;
     sp.insert(sp.end(), pages.begin(), pages.end());
+    if (npb > partial) c->seq_alias[seq].push_back({(int32_t)jdst, pages[0], (int32_t)npb - partial});
     c->n_slots[seq] = (int32_t)(dst + n);
     note_fills(c, seq, dst, dst + n);
     if (partial) {
@@ -2695,34 +2705,47 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
 // Batch rows whose sequences begin with the same pages.
 struct CommonPages {
     std::vector<int32_t> rows;
-    int32_t pages;  // leading pages that all of them have, equally filled
+    int32_t pages;  // leading pages that all of them have, full ones of pool-resident blocks
+    size_t runs;
 };
 
 static std::vector<CommonPages> common_pages(const kvg_cache *c, const int32_t *seq_ids, int32_t B) {
     std::vector<CommonPages> groups;
     std::unordered_map<int32_t, size_t> by_page;  // first page -> group
     for (int32_t b = 0; b < B; ++b) {
-        const auto &sp = c->seq_pages[seq_ids[b]];
-        if (sp.empty()) continue;
-        const auto it = by_page.emplace(sp[0], groups.size());
+        const auto &runs = c->seq_alias[seq_ids[b]];
+        if (runs.empty() || runs[0].page0 != 0) continue;
+        const auto it = by_page.emplace(runs[0].first_pid, groups.size());
         if (it.second) {
-            groups.push_back({{b}, (int32_t)sp.size()});
+            // runs that follow one another without a page of the sequence's own
+            CommonPages g{{b}, 0, 0};
+            while (g.runs < runs.size() && runs[g.runs].page0 == g.pages) g.pages += runs[g.runs++].n;
+            groups.push_back(std::move(g));
             continue;
         }
         CommonPages &g = groups[it.first->second];
-        const int32_t first = seq_ids[g.rows[0]];
-        const auto &fp = c->seq_pages[first];
-        const int32_t most = std::min<int32_t>(g.pages, (int32_t)sp.size());
-        int32_t n = 0;
-        while (n < most && sp[n] == fp[n] && c->seq_fill[seq_ids[b]][n] == c->seq_fill[first][n]) ++n;
+        const auto &first = c->seq_alias[seq_ids[g.rows[0]]];
         g.rows.push_back(b);
-        g.pages = n;
+        size_t k = 0;
+        int32_t pages = 0;
+        while (k < g.runs && k < runs.size() && runs[k] == first[k]) pages += runs[k++].n;
+        g.runs = k;
+        g.pages = pages;
     }
     return groups;
 }
 
-// Bytes of keys and values not read again from which a group is worth it.
-constexpr double kSharedMinBytes = 1.0;
+// From how many kilobytes of keys and values not read again the common pages
+// get launches of their own.  Those cost 10 us more than the decode's on the
+// smallest batches, and the pages that rows read again come from L2 as long as
+// they fit: 4 rows on 4,096 tokens of the 12B shape (101 MB saved) 24.7 us by the
+// decode and 25.5 shared, 2 rows on 16,384 (134 MB) 44.0 and 41.9, 64 rows on 256
+// (132 MB) 31.7 and 29.5; of the 31B shape 4 on 4,096 20.2 and 22.6, 2 on 16,384
+// 38.5 and 38.2; 64 rows of the tiny shape on 4,096 (132 MB) 24.8 and 22.4.
+static double shared_min_bytes() {
+    static const int kb = env_knob("KVG_SHARED_MIN_KB", 120000);
+    return 1000.0 * kb;
+}
 
 extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B,
                                                   const void *q, int32_t n_q_heads, void *out, float scale,
@@ -2737,12 +2760,12 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
     const int64_t P = d.page_size;
     const int32_t n_run = layer < 0 ? d.n_layers : 1;
     std::vector<CommonPages> groups = common_pages(c, seq_ids, B);
-    // a group's pages are read once instead of once per row where that saves enough
-    const double page_bytes = 2.0 * n_run * (double)c->page_bytes;
-    groups.erase(std::remove_if(groups.begin(), groups.end(), [&](const CommonPages &g) {
-        return (double)(g.rows.size() - 1) * g.pages * page_bytes < kSharedMinBytes;
+    double saved = 0;
+    groups.erase(std::remove_if(groups.begin(), groups.end(), [](const CommonPages &g) {
+        return g.rows.size() < 2 || g.pages == 0;
     }), groups.end());
-    if (groups.empty())
+    for (const CommonPages &g : groups) saved += (double)(g.rows.size() - 1) * g.pages * 2.0 * n_run * (double)c->page_bytes;
+    if (groups.empty() || saved < shared_min_bytes())
         return decode_impl("kvg_decode_attention_shared", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0,
                            INT32_MAX, nullptr, 0);
     DeviceGuard g(c->device);

@@ -2,6 +2,7 @@
 sequence's rows (bounds: the decode gate's), for batches whose sequences were
 given the same pool-resident block."""
 import math
+import os
 
 import pytest
 import torch
@@ -10,6 +11,7 @@ from kvg_testlib import need_gpu
 from test_gpu_prompt_attention import Bed, check, normal, reference
 
 pytestmark = pytest.mark.gpu
+os.environ.setdefault("KVG_SHARED_MIN_KB", "1")  # the launches for common pages also where they do not pay
 
 
 @pytest.fixture(scope="module")
