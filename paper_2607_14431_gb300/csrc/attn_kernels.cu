@@ -752,8 +752,8 @@ __global__ void __launch_bounds__(kCombineMaxThreads) combine_kernel(const Decod
 // (kvg_decode_attention_shared): the row's partials over the shared pages, then
 // its own.  Few of each (an SM has a key range of the shared pages, a short tail
 // is a warp or two), so a warp takes a row, a lane D / 32 of its columns, four
-// partials in flight: 3,072 rows of the 31B shape over 9 ranges COMBINE_NOW,
-// with a block per row as above COMBINE_BEFORE.
+// partials in flight: 96 sequences of the 31B shape over 9 ranges 8.3 us, with
+// a block per row as above 12.1 us.
 constexpr int kCombineRows = 8;  // of a block
 template <int D>
 __global__ void __launch_bounds__(32 * kCombineRows)

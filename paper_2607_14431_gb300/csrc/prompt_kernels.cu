@@ -14,7 +14,7 @@
 // takes one, or for head_dim 256 a pair of CTAs (a cluster), each with half of
 // the query rows, of the keys' columns and of the values' dimensions: a single
 // CTA's shared memory held 2.5 key or value tiles there, which made it wait for
-// copies (8,191 rows of the 12B shape: 506 us; PAIR_TIME as pairs).
+// copies (8,191 rows of the 12B shape: 506 us; 392 us as pairs, all else the same).
 // Key tiles are 128 columns, made of units of 128 (pairs: 64): a page's rows,
 // or as many whole pages as fit when pages are smaller, each at a multiple of 8
 // rows so that its copy starts on a swizzle atom.
@@ -464,11 +464,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         __syncwarp();
         if (lane == 0)
             for (int i = 0; i < times; ++i) {
-                if constexpr (CTAS == 2)
-                    mbar_arrive_first(bar);
-                else
-                    mbar_arrive(bar);
-            }
+            if constexpr (CTAS == 2)
+                mbar_arrive_first(bar);
+            else
+                mbar_arrive(bar);
+        }
     };
 
     if (threadIdx.x == 0) {
@@ -549,186 +549,186 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         bool ok = true;
         int tiles = 0;  // of the items before
         for (int k = 0; ok; ++k) {
-        const Item &it = s.item[k % kItems];  // (there until item k + 4 is known)
-        const int k0 = it.k0, n = it.k1 - k0;
-        // ---- weights: a thread has a query row
-        const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // tensor memory lanes of the warp
-        const int r = first + threadIdx.x;                   // the thread's row of the item
-        const bool mine = r < it.rows;
-        int tile_lo = 0, col_lo = 0, tile_hi = -1, col_hi = 0;
-        if (mine) {
-            const int token = (it.row0 + r) >> it.gs;
-            tile_of(p, row_first(p, it, token), tile_lo, col_lo);
-            tile_of(p, row_last(p, it, token), tile_hi, col_hi);
-        }
-        const float c = p.qscale;
-        float m = -INFINITY;               // what the weights refer to
-        float2 sum = make_float2(0.f, 0.f);
-        const uint32_t o_at = tmem + lanes + kOutCols + stream * kTile;
-        for (int j = 0; j < n; ++j) {
-            const int J = tiles + j, buf = STREAMS == 1 ? J & 1 : stream;
-            const uint32_t s_at = tmem + lanes + kScoreCols + buf * kTile;
-            ok = wait_bar(s, &s.scores[buf], (STREAMS == 1 ? J >> 1 : J) & 1, p.status);
-            if (!ok) break;
-            tc_after_sync();
-            float x[kTile];
-#pragma unroll
-            for (int i = 0; i < kTile; i += 32) tmem_ld32(s_at + i, reinterpret_cast<uint32_t *>(x) + i);
-            // columns [from, to) of the tile are the row's
-            const int kt = k0 + j;
-            const int from = kt < tile_lo ? kTile : kt == tile_lo ? col_lo : 0;
-            const int to = kt > tile_hi ? 0 : kt == tile_hi ? col_hi + 1 : kTile;
-            const uint32_t *valid = s.mask[J % kMaskSlots];
-            const bool whole = from == 0 && to == kTile && (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
-            const bool all = __all_sync(0xffffffffu, whole);
-            tmem_wait_ld();
-            if (!all) {
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int a = from - 32 * w, e = to - 32 * w;
-                    const uint32_t bits = valid[w] & (e >= 32 ? ~0u : e <= 0 ? 0u : (1u << e) - 1) &
-                                          (a >= 32 ? 0u : a <= 0 ? ~0u : ~((1u << a) - 1));
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) x[32 * w + i] = bits >> i & 1 ? x[32 * w + i] : -INFINITY;
-                }
+            const Item &it = s.item[k % kItems];  // (there until item k + 4 is known)
+            const int k0 = it.k0, n = it.k1 - k0;
+            // ---- weights: a thread has a query row
+            const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // tensor memory lanes of the warp
+            const int r = first + threadIdx.x;                   // the thread's row of the item
+            const bool mine = r < it.rows;
+            int tile_lo = 0, col_lo = 0, tile_hi = -1, col_hi = 0;
+            if (mine) {
+                const int token = (it.row0 + r) >> it.gs;
+                tile_of(p, row_first(p, it, token), tile_lo, col_lo);
+                tile_of(p, row_last(p, it, token), tile_hi, col_hi);
             }
-            float t[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = fmaxf(x[e], x[4 + e]);
-#pragma unroll
-            for (int i = 8; i < kTile; i += 8)  // (three operands to an instruction)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] = fmaxf(fmaxf(t[e], x[i + e]), x[i + 4 + e]);
-            const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-            // move the reference?  (-inf: no column so far, nothing to rescale)
-            const bool move = top > m && (m == -INFINITY || (top - m) * c > kMaxSlack);
-            const bool rescale = move && m != -INFINITY;
-            if (__any_sync(0xffffffffu, rescale)) {
-                const float a = rescale ? exp2_approx((m - top) * c) : 1.f;
-                sum.x *= a;
-                sum.y *= a;
-                // (two streams: the scores came after the previous product)
-                if (STREAMS == 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
+            const float c = p.qscale;
+            float m = -INFINITY;               // what the weights refer to
+            float2 sum = make_float2(0.f, 0.f);
+            const uint32_t o_at = tmem + lanes + kOutCols + stream * kTile;
+            for (int j = 0; j < n; ++j) {
+                const int J = tiles + j, buf = STREAMS == 1 ? J & 1 : stream;
+                const uint32_t s_at = tmem + lanes + kScoreCols + buf * kTile;
+                ok = wait_bar(s, &s.scores[buf], (STREAMS == 1 ? J >> 1 : J) & 1, p.status);
                 if (!ok) break;
                 tc_after_sync();
-#pragma unroll 1
-                for (int i = 0; i < D; i += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(o_at + i, o);
-                    tmem_wait_ld();
+                float x[kTile];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
-                    tmem_st32(o_at + i, o);
-                }
-            }
-            if (move) m = top;
-            const float base = m == -INFINITY ? 0.f : -m * c;
-            const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
-            // weights in the products' 16 bits, a half of the tile at a time so that
-            // its product starts while the other half is formed
-            uint32_t w[kTile / 2];
-            float2 part[4] = {};
-            auto weigh = [&](int from_pair, int to_pair) {
+                for (int i = 0; i < kTile; i += 32) tmem_ld32(s_at + i, reinterpret_cast<uint32_t *>(x) + i);
+                // columns [from, to) of the tile are the row's
+                const int kt = k0 + j;
+                const int from = kt < tile_lo ? kTile : kt == tile_lo ? col_lo : 0;
+                const int to = kt > tile_hi ? 0 : kt == tile_hi ? col_hi + 1 : kTile;
+                const uint32_t *valid = s.mask[J % kMaskSlots];
+                const bool whole = from == 0 && to == kTile && (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
+                const bool all = __all_sync(0xffffffffu, whole);
+                tmem_wait_ld();
+                if (!all) {
 #pragma unroll
-                for (int e = from_pair; e < to_pair; ++e) {
-                    float2 y = fma2(make_float2(x[2 * e], x[2 * e + 1]), c2, b2);
-                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
-                    if constexpr (FP8) {  // fp16's rounding (2^-12) stays below the output's: summed as they are
-                        const __half2 h = __floats2half2_rn(y.x, y.y);
-                        w[e] = *reinterpret_cast<const uint32_t *>(&h);
-                        part[e % 4] = add2(part[e % 4], y);
-                    } else {
-                        w[e] = pack_out(y.x, y.y);
+                    for (int w = 0; w < 4; ++w) {
+                        const int a = from - 32 * w, e = to - 32 * w;
+                        const uint32_t bits = valid[w] & (e >= 32 ? ~0u : e <= 0 ? 0u : (1u << e) - 1) &
+                                              (a >= 32 ? 0u : a <= 0 ? ~0u : ~((1u << a) - 1));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[32 * w + i] = bits >> i & 1 ? x[32 * w + i] : -INFINITY;
                     }
                 }
-            };
-            weigh(0, 32);
-            tmem_st32(s_at, w);
-            weigh(32, 48);
-            tmem_wait_st();
-            tc_before_sync();
-            arrive_issuer(&s.weights[buf][0]);
-            weigh(48, 64);
-            tmem_st32(s_at + 32, w + 32);
-            tmem_wait_st();
-            tc_before_sync();
-            // the wait after the last tile tells its product from the one before
-            // only if that one is known to be done
-            if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
+                float t[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = fmaxf(x[e], x[4 + e]);
+#pragma unroll
+                for (int i = 8; i < kTile; i += 8)  // (three operands to an instruction)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = fmaxf(fmaxf(t[e], x[i + e]), x[i + 4 + e]);
+                const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                // move the reference?  (-inf: no column so far, nothing to rescale)
+                const bool move = top > m && (m == -INFINITY || (top - m) * c > kMaxSlack);
+                const bool rescale = move && m != -INFINITY;
+                if (__any_sync(0xffffffffu, rescale)) {
+                    const float a = rescale ? exp2_approx((m - top) * c) : 1.f;
+                    sum.x *= a;
+                    sum.y *= a;
+                    // (two streams: the scores came after the previous product)
+                    if (STREAMS == 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
+                    if (!ok) break;
+                    tc_after_sync();
+#pragma unroll 1
+                    for (int i = 0; i < D; i += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_at + i, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+                        tmem_st32(o_at + i, o);
+                    }
+                }
+                if (move) m = top;
+                const float base = m == -INFINITY ? 0.f : -m * c;
+                const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
+                // weights in the products' 16 bits, a half of the tile at a time so that
+                // its product starts while the other half is formed
+                uint32_t w[kTile / 2];
+                float2 part[4] = {};
+                auto weigh = [&](int from_pair, int to_pair) {
+#pragma unroll
+                    for (int e = from_pair; e < to_pair; ++e) {
+                        float2 y = fma2(make_float2(x[2 * e], x[2 * e + 1]), c2, b2);
+                        y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                        if constexpr (FP8) {  // fp16's rounding (2^-12) stays below the output's: summed as they are
+                            const __half2 h = __floats2half2_rn(y.x, y.y);
+                            w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                            part[e % 4] = add2(part[e % 4], y);
+                        } else {
+                            w[e] = pack_out(y.x, y.y);
+                        }
+                    }
+                };
+                weigh(0, 32);
+                tmem_st32(s_at, w);
+                weigh(32, 48);
+                tmem_wait_st();
+                tc_before_sync();
+                arrive_issuer(&s.weights[buf][0]);
+                weigh(48, 64);
+                tmem_st32(s_at + 32, w + 32);
+                tmem_wait_st();
+                tc_before_sync();
+                // the wait after the last tile tells its product from the one before
+                // only if that one is known to be done
+                if (STREAMS == 1 && j > 0 && j == n - 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
+                if (!ok) break;
+                arrive_issuer(&s.weights[buf][1]);
+                // The sum adds the rounded bf16 weights: where one is far above the
+                // others, its rounding then divides out.  (Beside the products.)
+                if constexpr (!FP8) {
+#pragma unroll
+                    for (int e = 0; e < kTile / 2; ++e)
+                        part[e % 4] = add2(part[e % 4], make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)));
+                }
+                sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
+            }
+            tiles += n;
             if (!ok) break;
-            arrive_issuer(&s.weights[buf][1]);
-            // The sum adds the rounded bf16 weights: where one is far above the
-            // others, its rounding then divides out.  (Beside the products.)
-            if constexpr (!FP8) {
-#pragma unroll
-                for (int e = 0; e < kTile / 2; ++e)
-                    part[e % 4] = add2(part[e % 4], make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)));
+            // ---- the next item's queries (this one's scores are all there, so nothing
+            // reads their place any more): its first products run beside the output
+            const bool more = has_item(k + 1);
+            if (more) {
+                const Item &after = s.item[(k + 1) % kItems];
+                Queries<C> q;
+                q.load(p, after, q_first, 0, lane);
+                finish_queries(after, q);
             }
-            sum = add2(sum, add2(add2(part[0], part[1]), add2(part[2], part[3])));
-        }
-        tiles += n;
-        if (!ok) break;
-        // ---- the next item's queries (this one's scores are all there, so nothing
-        // reads their place any more): its first products run beside the output
-        const bool more = has_item(k + 1);
-        if (more) {
-            const Item &after = s.item[(k + 1) % kItems];
-            Queries<C> q;
-            q.load(p, after, q_first, 0, lane);
-            finish_queries(after, q);
-        }
-        // ---- output
-        ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (tiles - 1) & 1 : k & 1, p.status);
-        if (ok) {
-            tc_after_sync();
-            const float l = sum.x + sum.y;
-            const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
-            bool bad = false;
-            const int row = it.row0 + r;
-            const bool partial = p.splits[it.b] > 1 || p.shared;
-            const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
-            // (scores that are all NaN leave m at -inf, which would read as no column)
-            if (mine && partial) p.part_ml[at] = make_float2(l == l ? m * c : 0.f, l);
-            const float inv = __fdiv_rn(p.vscale, l);
-            if (partial) {
-                float4 *const to = reinterpret_cast<float4 *>(p.part_o + at * D);
+            // ---- output
+            ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (tiles - 1) & 1 : k & 1, p.status);
+            if (ok) {
+                tc_after_sync();
+                const float l = sum.x + sum.y;
+                const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
+                bool bad = false;
+                const int row = it.row0 + r;
+                const bool partial = p.splits[it.b] > 1 || p.shared;
+                const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
+                // (scores that are all NaN leave m at -inf, which would read as no column)
+                if (mine && partial) p.part_ml[at] = make_float2(l == l ? m * c : 0.f, l);
+                const float inv = __fdiv_rn(p.vscale, l);
+                if (partial) {
+                    float4 *const to = reinterpret_cast<float4 *>(p.part_o + at * D);
 #pragma unroll 1
-                for (int i = 0; i < D; i += 32) {
-                    float o[32];
-                    tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
-                    tmem_wait_ld();
-                    bad = bad || !finite(o);
-                    if (mine && !empty)
+                    for (int i = 0; i < D; i += 32) {
+                        float o[32];
+                        tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
+                        tmem_wait_ld();
+                        bad = bad || !finite(o);
+                        if (mine && !empty)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) to[i / 4 + e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                }
-            } else {
-                uint4 *const to = reinterpret_cast<uint4 *>(p.out + at * D);
+                            for (int e = 0; e < 8; ++e) to[i / 4 + e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                } else {
+                    uint4 *const to = reinterpret_cast<uint4 *>(p.out + at * D);
 #pragma unroll 1
-                for (int i = 0; i < D; i += 32) {
-                    float o[32];
-                    tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
-                    tmem_wait_ld();
-                    bad = bad || !finite(o);
-                    if (mine)
+                    for (int i = 0; i < D; i += 32) {
+                        float o[32];
+                        tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
+                        tmem_wait_ld();
+                        bad = bad || !finite(o);
+                        if (mine)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            to[i / 8 + e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                                       pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                            for (int e = 0; e < 4; ++e)
+                                to[i / 8 + e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                                           pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                    }
+                }
+                bad = bad && mine && !(partial && empty);
+                // (read: the next item's products may be added there)
+                tc_before_sync();
+                arrive_issuer(&s.taken[stream]);
+                if (__any_sync(0xffffffffu, bad)) {
+                    __syncwarp();
+                    const int token = row >> it.gs;
+                    repair<D, FP8>(p, it, it.row0 + first + warp * 32, bad, mine ? row_first(p, it, token) : 0,
+                                   mine ? row_last(p, it, token) : -1, partial);
                 }
             }
-            bad = bad && mine && !(partial && empty);
-            // (read: the next item's products may be added there)
-            tc_before_sync();
-            arrive_issuer(&s.taken[stream]);
-            if (__any_sync(0xffffffffu, bad)) {
-                __syncwarp();
-                const int token = row >> it.gs;
-                repair<D, FP8>(p, it, it.row0 + first + warp * 32, bad, mine ? row_first(p, it, token) : 0,
-                               mine ? row_last(p, it, token) : -1, partial);
-            }
-        }
-        if (!more) break;
+            if (!more) break;
         }
     } else {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER_REGS));
@@ -970,63 +970,63 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             Groups<C> groups;
             int chunk = 0;
             for (int k = 0, tiles = 0, group = 0; ok; ++k) {
-            const int n = s.item[k % kItems].k1 - s.item[k % kItems].k0;
-            for (int i = 0; ok && i < 2 * n; ++i, ++chunk) {
-                const int rs = chunk % LANDS, st = chunk % STAGES;
-                int j;
-                const bool values = value_tile(i, n, j);
-                j += tiles;
-                ok = wait_bar(s, &s.landed[rs], (chunk / LANDS) & 1, p.status);
-                const int g = groups.take(st, lane, i);
-                if (ok && chunk >= STAGES) ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
-                if (!ok) break;
-                const uint8_t *src = raw + rs * C::RAW;
-                uint8_t *dst = ring + st * C::CHUNK;
-                constexpr int N = C::CHUNK / 2 / (128 * 4 * kConvertWarps);  // rows of 128 codes that a thread has
-                uint4 x[N];
+                const int n = s.item[k % kItems].k1 - s.item[k % kItems].k0;
+                for (int i = 0; ok && i < 2 * n; ++i, ++chunk) {
+                    const int rs = chunk % LANDS, st = chunk % STAGES;
+                    int j;
+                    const bool values = value_tile(i, n, j);
+                    j += tiles;
+                    ok = wait_bar(s, &s.landed[rs], (chunk / LANDS) & 1, p.status);
+                    const int g = groups.take(st, lane, i);
+                    if (ok && chunk >= STAGES) ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
+                    if (!ok) break;
+                    const uint8_t *src = raw + rs * C::RAW;
+                    uint8_t *dst = ring + st * C::CHUNK;
+                    constexpr int N = C::CHUNK / 2 / (128 * 4 * kConvertWarps);  // rows of 128 codes that a thread has
+                    uint4 x[N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const int r = t / 8 + k * 4 * kConvertWarps;
-                    x[k] = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
-                }
-                if (values) {  // rows that are not valid hold anything: zero weights must meet zeros
-                    const uint32_t *m = s.mask[j % kMaskSlots];
-                    if ((m[0] & m[1] & m[2] & m[3]) != ~0u)
-#pragma unroll
-                        for (int k = 0; k < N; ++k) {
-                            const int r = t / 8 + k * 4 * kConvertWarps;
-                            if (!(m[r / 32] >> (r % 32) & 1)) x[k] = make_uint4(0, 0, 0, 0);
-                        }
-                }
-                const int box = values ? C::V_BOX : C::K_BOX;
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const int r = t / 8 + k * 4 * kConvertWarps;
-                    const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-                    uint32_t y[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint16_t lo = (uint16_t)w[e], hi = (uint16_t)(w[e] >> 16);
-                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(lo));
-                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(hi));
+                    for (int k = 0; k < N; ++k) {
+                        const int r = t / 8 + k * 4 * kConvertWarps;
+                        x[k] = *reinterpret_cast<const uint4 *>(src + r * 128 + ((u ^ (r & 7)) << 4));
                     }
-                    // a pair's keys: two boxes of codes, 64 rows each, become four
-                    const int half = values ? 0 : r / C::UNIT, rb = values ? r : r % C::UNIT, u2 = u % 4 * 2;
-                    uint8_t *to = dst + (half * 2 + u / 4) * box + rb * 128;
-                    // (lanes of the second box take the other half first: 8 lanes, 8 bank groups)
-                    const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
-                    const int odd = u / 4;
-                    *reinterpret_cast<uint4 *>(to + (((u2 + odd) ^ (r & 7)) << 4)) = odd ? b : a;
-                    *reinterpret_cast<uint4 *>(to + (((u2 + 1 - odd) ^ (r & 7)) << 4)) = odd ? a : b;
+                    if (values) {  // rows that are not valid hold anything: zero weights must meet zeros
+                        const uint32_t *m = s.mask[j % kMaskSlots];
+                        if ((m[0] & m[1] & m[2] & m[3]) != ~0u)
+#pragma unroll
+                            for (int k = 0; k < N; ++k) {
+                                const int r = t / 8 + k * 4 * kConvertWarps;
+                                if (!(m[r / 32] >> (r % 32) & 1)) x[k] = make_uint4(0, 0, 0, 0);
+                            }
+                    }
+                    const int box = values ? C::V_BOX : C::K_BOX;
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const int r = t / 8 + k * 4 * kConvertWarps;
+                        const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+                        uint32_t y[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint16_t lo = (uint16_t)w[e], hi = (uint16_t)(w[e] >> 16);
+                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(lo));
+                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(hi));
+                        }
+                        // a pair's keys: two boxes of codes, 64 rows each, become four
+                        const int half = values ? 0 : r / C::UNIT, rb = values ? r : r % C::UNIT, u2 = u % 4 * 2;
+                        uint8_t *to = dst + (half * 2 + u / 4) * box + rb * 128;
+                        // (lanes of the second box take the other half first: 8 lanes, 8 bank groups)
+                        const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
+                        const int odd = u / 4;
+                        *reinterpret_cast<uint4 *>(to + (((u2 + odd) ^ (r & 7)) << 4)) = odd ? b : a;
+                        *reinterpret_cast<uint4 *>(to + (((u2 + 1 - odd) ^ (r & 7)) << 4)) = odd ? a : b;
+                    }
+                    fence_proxy_async_shared();
+                    arrive_issuer(&s.ready[(group + C::group(i)) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
+                    if (lane == 0) mbar_arrive(&s.freed[rs]);
                 }
-                fence_proxy_async_shared();
-                arrive_issuer(&s.ready[(group + C::group(i)) % C::GROUPS], C::GROUPED && (i == 0 || i == 2 * n - 1) ? 2 : 1);
-                if (lane == 0) mbar_arrive(&s.freed[rs]);
-            }
-            tiles += n;
-            group += C::group(2 * n - 1) + 1;
-            groups.end(n);
-            if (!ok || !has_item(k + 1)) break;
+                tiles += n;
+                group += C::group(2 * n - 1) + 1;
+                groups.end(n);
+                if (!ok || !has_item(k + 1)) break;
             }
             // every commit's arrival is awaited before the CTA ends
             for (int c = max(0, chunk - STAGES); ok && c < chunk; ++c) {
