@@ -18,6 +18,7 @@
 // Key tiles are 128 columns, made of units of 128 (pairs: 64): a page's rows,
 // or as many whole pages as fit when pages are smaller, each at a multiple of 8
 // rows so that its copy starts on a swizzle atom.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -65,6 +66,8 @@ struct Cfg {
     static constexpr int GROUPS = GROUPED ? 4 : STAGES;
     static constexpr int SOFTMAX_WARPS = 4 * STREAMS;
     static constexpr int LOAD_WARP = SOFTMAX_WARPS, MMA_WARP = LOAD_WARP + 1, TIDY_WARP = LOAD_WARP + 2, CONVERT_WARP = LOAD_WARP + 4;
+    // (for an fp8 cache the converting warps tidy and fetch queries)
+    static constexpr int NEXT_WARP = LOAD_WARP + 3;
     static constexpr int THREADS = 32 * (CONVERT_WARP + (FP8 ? kConvertWarps : 0));
     // Registers of a softmax thread and of the others, moved between the
     // warpgroups where the launch's even share is too few for a row of scores:
@@ -96,7 +99,8 @@ struct Bars {
     uint64_t ready[8], empty[8];             // groups of chunks: may be multiplied; have been
     uint64_t scores[2], out[2];              // a score tile is there; its weights' product is added
     uint64_t weights[2][2];                  // the halves of its weights are there
-    uint64_t queries, taken[2], drained;     // an item's queries are there, its outputs have been read
+    uint64_t queries, scored;                // an item's queries are there, have been multiplied
+    uint64_t taken[2], drained;              // its outputs have been read
     uint64_t next[kItems], known[kItems];    // of item k (k % kItems): the answer is there, what it is
     uint4 answer[kItems];
     Item item[kItems];                       // b < 0: no more
@@ -295,13 +299,6 @@ __device__ __forceinline__ void attend_row(const PromptParams &p, const Item &it
     }
 }
 
-__device__ __forceinline__ bool finite(const float (&o)[32]) {
-    float2 z[2] = {};
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) z[e / 2 % 2] = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), z[e / 2 % 2]);
-    return z[0].x + z[0].y + z[1].x + z[1].y == 0.f;
-}
-
 __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
@@ -361,11 +358,11 @@ __device__ __forceinline__ void repair(const PromptParams &p, const Item &it, in
 }
 
 // Tiles land as K0, then K(j + 1) and V(j) in turn, the last V alone: whether
-// the i-th is a value tile, and of which key tile.
+// the i-th is a value tile, and of which key tile the keys or values are.
 __device__ __forceinline__ bool value_tile(int i, int n, int &j) {
-    const bool last = i == 2 * n - 1;
-    j = last ? n - 1 : i / 2 - 1;
-    return last || (i > 0 && i % 2 == 0);
+    const bool last = i == 2 * n - 1, values = last || (i > 0 && i % 2 == 0);
+    j = last ? n - 1 : values ? i / 2 - 1 : (i + 1) / 2;
+    return values;
 }
 
 // A lane's page of a key tile: lane i has page i % 16 of the tile's unit i / 16.
@@ -373,62 +370,133 @@ struct Page {
     int rows;    // valid rows of it in the tile
     int32_t at;  // its first row in the pool, of the layer's keys
 };
+struct Entry {  // the same as it is in the tables, on its way
+    int pid, fill, sub;  // sub: first row in the page
+};
 template <class C>
-__device__ __forceinline__ Page find_page(const PromptParams &p, const Item &it, int kt, int lane) {
-    const int unit = lane / 16, place = lane % 16, u = kt * C::CTAS + unit;
-    const bool has = unit < C::CTAS && (p.pages_per_unit ? place < p.pages_per_unit : place == 0);
-    const int pg = p.pages_per_unit ? u * p.pages_per_unit + place : u / p.units_per_page;
-    const int sub = p.pages_per_unit ? 0 : u % p.units_per_page * C::UNIT;
-    Page r{0, 0};
-    if (has && pg <= it.last_slot / p.page_size) {
-        const int64_t e = (int64_t)p.seq[it.b] * p.max_pages + pg;
-        const int pid = p.page_table[e];
-        r.rows = max(0, min(p.pages_per_unit ? p.page_size : C::UNIT, p.page_fill[e] - sub));
-        if (r.rows && (pid < 0 || pid >= p.pool_pages)) {
+struct Pages {
+    const int32_t *table, *fill;  // of the item's sequence
+    int32_t base;                 // the pool's row where page 0 would start
+    int last;                     // the item's last page
+    __device__ __forceinline__ void of(const PromptParams &p, const Item &it) {
+        const int64_t e = (int64_t)p.seq[it.b] * p.max_pages;
+        table = p.page_table + e;
+        fill = p.page_fill + e;
+        base = (int32_t)(((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads + it.g) * p.page_size);
+        last = it.last_slot / p.page_size;
+    }
+    // of key tile kt (none from k1 on)
+    __device__ __forceinline__ Entry load(const PromptParams &p, int kt, int k1, int lane) const {
+        const int unit = lane / 16, place = lane % 16, u = kt * C::CTAS + unit;
+        int pg = u * p.pages_per_unit + place;
+        bool has = unit < C::CTAS && place < p.pages_per_unit;
+        Entry e{0, 0, 0};
+        if (!p.pages_per_unit) {
+            pg = u / p.units_per_page;
+            e.sub = (u - pg * p.units_per_page) * C::UNIT;
+            has = unit < C::CTAS && place == 0;
+        }
+        if (has && pg <= last && kt < k1) {
+            e.pid = table[pg];
+            e.fill = fill[pg];
+        }
+        return e;
+    }
+    __device__ __forceinline__ Page page(const PromptParams &p, const Entry &e) const {
+        Page r;
+        r.rows = max(0, min(p.pages_per_unit ? p.page_size : C::UNIT, e.fill - e.sub));
+        if (r.rows && (e.pid < 0 || e.pid >= p.pool_pages)) {
             record_error(p.status, KVG_ERR_DEVICE_CHECK, 21);
             r.rows = 0;
         }
-        r.at = (int32_t)((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads * p.page_size +
-                         ((int64_t)pid * p.n_kv_heads + it.g) * p.page_size + sub);
-    }
-    return r;
-}
-
-// Queries of a tile's rows on their way to shared memory: a warp's 32 rows, in
-// batches whose loads are all under way before the first is stored.
-template <class C>
-struct Queries {
-    static constexpr int D = C::D, LPR = D / 8 < 32 ? D / 8 : 32, RPI = 32 / LPR, N = 32 / RPI, BATCH = N < 16 ? N : 16;
-    uint4 x[BATCH];
-    // rows from first + i0 * RPI of the item (the last again past its end)
-    __device__ __forceinline__ void load(const PromptParams &p, const Item &it, int first, int i0, int lane) {
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int r = first + (i0 + i) * RPI + lane / LPR;
-            x[i] = reinterpret_cast<const uint4 *>(p.q + q_row(p, it, it.row0 + min(r, it.rows - 1)) * D)[lane % LPR];
-        }
-    }
-    // to the swizzled rows of the tile at `to` (zeros past the item's end)
-    __device__ __forceinline__ void store(const Item &it, int first, int i0, int lane, uint8_t *to) const {
-        const int u = lane % LPR;
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int r = first + (i0 + i) * RPI + lane / LPR, rt = r % kTile;
-            uint4 y = x[i];
-            if constexpr (C::FP8) {
-                uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __half2 h = __floats2half2_rn(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
-                    w[e] = *reinterpret_cast<const uint32_t *>(&h);
-                }
-                y = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            if (r >= it.rows) y = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4 *>(to + u / 8 * (kTile * 128) + rt * 128 + ((u % 8 ^ (rt & 7)) << 4)) = y;
-        }
+        r.at = base + e.pid * (p.n_kv_heads * p.page_size) + e.sub;
+        return r;
     }
 };
+
+// Query rows of an item on their way to the swizzled rows of their tiles, by
+// warps that each have CHUNKS times 32 of a CTA's rows: rows 32 w, w = from,
+// from + step, ...  (What runs once per item is kept to short loops here and for
+// the outputs: unrolled, it waited for its instructions.)
+template <class C, int CHUNKS>
+struct Queries {
+    static constexpr int D = C::D, LPR = D / 8, RPI = 32 / LPR, N = 32 / RPI;  // lanes of a row, rows of a copy
+    const __nv_bfloat16 *src;  // the lane's piece of the item's first row
+    int off[CHUNKS];           // the lane's row of each 32, in rows from there; INT_MIN: past the item's end
+
+    __device__ __forceinline__ void find(const PromptParams &p, const Item &it, int first, int from, int step, int lane,
+                                         bool prefetch) {
+        const int64_t base = q_row(p, it, it.row0);
+        src = p.q + base * D + lane % LPR * 8;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int r = first + (from + c * step) * 32 + lane;
+            off[c] = r < it.rows ? (int)(q_row(p, it, it.row0 + r) - base) : INT_MIN;  // (a tile's rows: less than 2^31 apart)
+            if (prefetch && r < it.rows)
+#pragma unroll 1
+                for (int x = 0; x < D; x += 64) prefetch_l2(p.q + (base + off[c]) * D + x);
+        }
+    }
+    // the lane's piece of copy i of rows 32 w
+    static __device__ __forceinline__ uint8_t *at(uint8_t *q_tiles, int w, int i, int lane) {
+        const int u = lane % LPR, h = lane / LPR;
+        return q_tiles + w / 4 * (kTile * D * 2) + w % 4 * (32 * 128) + u / 8 * (kTile * 128) + h * 128 + i * RPI * 128 +
+               (((u % 8 ^ h) << 4) ^ (i * RPI % 8 << 4));
+    }
+    __device__ __forceinline__ void copy(int from, int step, int lane, uint8_t *q_tiles) const {
+#pragma unroll 1
+        for (int c = 0; c < CHUNKS; ++c) {
+            int mine = off[0];
+#pragma unroll
+            for (int x = 1; x < CHUNKS; ++x) mine = c == x ? off[x] : mine;
+#pragma unroll 1
+            for (int i0 = 0; i0 < N; i0 += 8) {
+                int o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = __shfl_sync(0xffffffffu, mine, (i0 + i) * RPI + lane / LPR);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    async_copy16(at(q_tiles, from + c * step, i0 + i, lane), src + (int64_t)(o[i] == INT_MIN ? 0 : o[i]) * D,
+                                 o[i] != INT_MIN);
+            }
+        }
+    }
+    // After the lane's copies, for an fp8 cache's products: bf16 to fp16, in place.
+    static __device__ __forceinline__ void convert(int from, int step, int lane, uint8_t *q_tiles) {
+        constexpr int BATCH = 4;
+#pragma unroll 1
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll 1
+            for (int i0 = 0; i0 < N; i0 += BATCH) {
+                uint4 x[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) x[i] = *reinterpret_cast<const uint4 *>(at(q_tiles, from + c * step, i0 + i, lane));
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const __half2 h = __floats2half2_rn(__uint_as_float(y[e] << 16), __uint_as_float(y[e] & 0xffff0000u));
+                        y[e] = *reinterpret_cast<const uint32_t *>(&h);
+                    }
+                    *reinterpret_cast<uint4 *>(at(q_tiles, from + c * step, i0 + i, lane)) = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+            }
+    }
+};
+
+// Lane q of four has row q of a 4 x 4 block: column q of it, for each.
+__device__ __forceinline__ void transpose4(uint32_t (&v)[4], int q) {
+#pragma unroll
+    for (int d = 1; d <= 2; d *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (!(i & d)) {
+                const bool odd = q & d;
+                const uint32_t x = __shfl_xor_sync(0xffffffffu, odd ? v[i] : v[i | d], d);
+                (odd ? v[i] : v[i | d]) = x;
+            }
+}
 
 // Which group's commit frees each place of the ring: a lane remembers the group
 // of the chunk that its place holds.
@@ -464,11 +532,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         __syncwarp();
         if (lane == 0)
             for (int i = 0; i < times; ++i) {
-            if constexpr (CTAS == 2)
-                mbar_arrive_first(bar);
-            else
-                mbar_arrive(bar);
-        }
+                if constexpr (CTAS == 2)
+                    mbar_arrive_first(bar);
+                else
+                    mbar_arrive(bar);
+            }
     };
 
     if (threadIdx.x == 0) {
@@ -485,6 +553,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             mbar_init(&s.out[i], 1);
         }
         mbar_init(&s.queries, CTAS * C::SOFTMAX_WARPS);
+        mbar_init(&s.scored, 1);
         mbar_init(&s.taken[0], CTAS * 4);
         mbar_init(&s.taken[1], CTAS * 4);
         for (int i = 0; i < kItems; ++i) {
@@ -498,18 +567,19 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
     // The first item (from the launch's parameters alone), its first pages and its
     // queries, all beside the set-up.
-    const int q_first = first + warp * 32;  // the warp's first row of the item
-    Queries<C> queries;
     Item it;
-    Page now{0, 0}, next{0, 0};
+    Pages<C> pages;
+    Entry coming{0, 0, 0}, after{0, 0, 0};
+    Queries<C, 1> first_queries;
     if (warp <= C::LOAD_WARP) {
         it = item_of(p, blockIdx.x / CTAS, STREAMS * CTAS * kTile);
         after_previous();
         if (warp < C::LOAD_WARP) {
-            queries.load(p, it, q_first, 0, lane);
+            first_queries.find(p, it, first, warp, 0, lane, false);
         } else {
-            now = find_page<C>(p, it, it.k0, lane);
-            if (it.k1 - it.k0 > 1) next = find_page<C>(p, it, it.k0 + 1, lane);
+            pages.of(p, it);
+            coming = pages.load(p, it.k0, it.k1, lane);
+            after = pages.load(p, it.k0 + 1, it.k1, lane);
             if (lane == 0) s.item[0] = it;
         }
     }
@@ -524,8 +594,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     // The CTA's items: its own, then those of CTAs that have not started, so that
     // copies run ahead into the next item while an item's outputs are stored.
     // The issuing thread asks for item k + 2 when every warp is in item k (so the
-    // answer for item k - 2 and what it meant are read); the load warp, which is
-    // ahead, works out what an answer means for all.  The CTA's item k >= 1, for a warp:
+    // answer for item k - 2 and what it meant are read); one warp works out what an
+    // answer means for all.  The CTA's item k >= 1, for a warp:
     auto has_item = [&](int k) {
         return wait_bar(s, &s.known[k % kItems], ((k - 1) / kItems) & 1, p.status) && s.item[k % kItems].b >= 0;
     };
@@ -533,19 +603,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     if (warp < C::SOFTMAX_WARPS) {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::MORE_REGS));
         const int stream = warp / 4;
-        uint8_t *const q_tile = smem + stream * (kTile * D * 2);
-        // the batches after the first, which has been loaded
-        auto finish_queries = [&](const Item &it, Queries<C> &q) {
-            q.store(it, q_first, 0, lane, q_tile);
-#pragma unroll 1
-            for (int i0 = Queries<C>::BATCH; i0 < Queries<C>::N; i0 += Queries<C>::BATCH) {
-                q.load(p, it, q_first, i0, lane);
-                q.store(it, q_first, i0, lane, q_tile);
-            }
-            fence_proxy_async_shared();
-            arrive_issuer(&s.queries);
-        };
-        finish_queries(it, queries);
+        first_queries.copy(warp, 0, lane, smem);
+        async_wait_all();
+        if constexpr (FP8) first_queries.convert(warp, 0, lane, smem);
+        fence_proxy_async_shared();
+        arrive_issuer(&s.queries);
         bool ok = true;
         int tiles = 0;  // of the items before
         for (int k = 0; ok; ++k) {
@@ -668,56 +730,73 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
             tiles += n;
             if (!ok) break;
-            // ---- the next item's queries (this one's scores are all there, so nothing
-            // reads their place any more): its first products run beside the output
-            const bool more = has_item(k + 1);
-            if (more) {
-                const Item &after = s.item[(k + 1) % kItems];
-                Queries<C> q;
-                q.load(p, after, q_first, 0, lane);
-                finish_queries(after, q);
-            }
             // ---- output
+            const float l = sum.x + sum.y;
+            const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
+            const int row = it.row0 + r;
+            const bool partial = p.splits[it.b] > 1 || p.shared;
+            const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
+            const float inv = __fdiv_rn(p.vscale, l);
+            const bool put = mine && !(partial && empty);
             ok = wait_bar(s, &s.out[stream], STREAMS == 1 ? (tiles - 1) & 1 : k & 1, p.status);
             if (ok) {
                 tc_after_sync();
-                const float l = sum.x + sum.y;
-                const bool empty = m == -INFINITY && l == 0.f;  // no column of the item's is the row's
-                bool bad = false;
-                const int row = it.row0 + r;
-                const bool partial = p.splits[it.b] > 1 || p.shared;
-                const int64_t at = !mine ? 0 : partial ? part_slot(p, it, it.split, row) : q_row(p, it, row);
                 // (scores that are all NaN leave m at -inf, which would read as no column)
                 if (mine && partial) p.part_ml[at] = make_float2(l == l ? m * c : 0.f, l);
-                const float inv = __fdiv_rn(p.vscale, l);
-                if (partial) {
-                    float4 *const to = reinterpret_cast<float4 *>(p.part_o + at * D);
+                bool bad = false;
+                // 16 of the warp's rows at a time: a lane has two columns of every eight of
+                // rows lane / 4 and lane / 4 + 8, so that a store has 32 bytes (partials) or,
+                // with blocks of 4 x 4 lanes transposed, 64 bytes (outputs) of 8 rows each
 #pragma unroll 1
-                    for (int i = 0; i < D; i += 32) {
-                        float o[32];
-                        tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
-                        tmem_wait_ld();
-                        bad = bad || !finite(o);
-                        if (mine && !empty)
+                for (int h = 0; h < 2; ++h) {
+                    int64_t to[2];
+                    float f[2], z[2] = {};
+                    bool puts[2];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) to[i / 4 + e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    for (int e = 0; e < 2; ++e) {
+                        const int from = h * 16 + e * 8 + lane / 4;
+                        to[e] = __shfl_sync(0xffffffffu, at, from) * D;
+                        f[e] = __shfl_sync(0xffffffffu, inv, from);
+                        puts[e] = __shfl_sync(0xffffffffu, put, from);
                     }
-                } else {
-                    uint4 *const to = reinterpret_cast<uint4 *>(p.out + at * D);
-#pragma unroll 1
+                    float o[16], next_o[16];
+                    tmem_ld16(o_at + (h << 20), reinterpret_cast<uint32_t *>(next_o));
+#pragma unroll 2
                     for (int i = 0; i < D; i += 32) {
-                        float o[32];
-                        tmem_ld32(o_at + i, reinterpret_cast<uint32_t *>(o));
                         tmem_wait_ld();
-                        bad = bad || !finite(o);
-                        if (mine)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                to[i / 8 + e] = make_uint4(pack_out(o[8 * e] * inv, o[8 * e + 1] * inv), pack_out(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                                           pack_out(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_out(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                        for (int x = 0; x < 16; ++x) o[x] = next_o[x];
+                        if (i + 32 < D) tmem_ld16(o_at + (h << 20) + i + 32, reinterpret_cast<uint32_t *>(next_o));
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float2 y[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                y[x] = make_float2(o[4 * x + 2 * e], o[4 * x + 2 * e + 1]);
+                                z[e] = __fmaf_rn(y[x].x, 0.f, __fmaf_rn(y[x].y, 0.f, z[e]));
+                            }
+                            if (partial) {
+                                float2 *const out = reinterpret_cast<float2 *>(p.part_o + to[e] + i) + lane % 4;
+                                if (puts[e])
+#pragma unroll
+                                    for (int x = 0; x < 4; ++x) out[4 * x] = y[x];
+                            } else {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) v[x] = pack_out(y[x].x * f[e], y[x].y * f[e]);
+                                transpose4(v, lane % 4);
+                                if (puts[e])
+                                    reinterpret_cast<uint4 *>(p.out + to[e] + i)[lane % 4] = make_uint4(v[0], v[1], v[2], v[3]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t not_finite = __ballot_sync(0xffffffffu, !(z[e] == 0.f));
+                        if (lane / 8 == 2 * h + e) bad = not_finite >> lane % 8 * 4 & 15;
                     }
                 }
-                bad = bad && mine && !(partial && empty);
+                bad = bad && put;
                 // (read: the next item's products may be added there)
                 tc_before_sync();
                 arrive_issuer(&s.taken[stream]);
@@ -728,7 +807,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                                    mine ? row_last(p, it, token) : -1, partial);
                 }
             }
-            if (!more) break;
+            if (!has_item(k + 1)) break;
         }
     } else {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER_REGS));
@@ -736,41 +815,56 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             // ---- keys and values of tile j: K0, then K(j + 1) and V(j) in turn
             const int64_t plane = p.pool_pages * p.n_kv_heads * p.page_size;  // rows of a layer's keys
             const int unit = lane / 16, row = lane % 16 * p.page_rows;         // of the lane's page
-            auto find = [&](int j) { return find_page<C>(p, it, it.k0 + j, lane); };
-            int chunk = 0;
+            int chunk = 0, st = 0, round = 0;  // the next chunk, its place, how often that was filled
             Groups<C> groups;
             const int box_bytes = p.box_rows * 128;
+            // the lane's rows of a tile without invalid columns (-1: there is none)
+            const int whole = p.pages_per_unit && p.pages_per_unit * p.page_size != C::UNIT ? -1
+                              : unit >= C::CTAS || lane % 16 >= max(1, p.pages_per_unit)    ? 0
+                                                                                            : min(p.page_size, C::UNIT);
             // the i-th copy of the item
             auto copy = [&](const Page &r, bool values, int i) {
-                const int st = chunk % LANDS;
                 if constexpr (FP8) {
-                    if (chunk >= LANDS && !wait_bar(s, &s.freed[st], (chunk / LANDS - 1) & 1, p.status)) return false;
+                    if (round && !wait_bar(s, &s.freed[st], (round - 1) & 1, p.status)) return false;
                 } else {
                     const int g = groups.take(st, lane, i);
-                    if (chunk >= LANDS && !wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status)) return false;
+                    if (round && !wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status)) return false;
                 }
                 // a pair's keys are split by columns, its values by dimensions
                 const bool mine = r.rows > 0 && (values || CTAS == 1 || unit == rank);
                 const int boxes = (values ? C::V_BOXES : C::K_BOXES) / (FP8 ? 2 : 1);
-                const int n_pages = __popc(__ballot_sync(0xffffffffu, mine));
-                if (lane == 0) {
-                    if (n_pages)
-                        mbar_arrive_expect_tx(&s.landed[st], n_pages * box_bytes * boxes);
+                const uint32_t pages = __ballot_sync(0xffffffffu, mine);
+                if (elect_one()) {
+                    if (pages)
+                        mbar_arrive_expect_tx(&s.landed[st], __popc(pages) * box_bytes * boxes);
                     else
                         mbar_arrive(&s.landed[st]);
                 }
                 __syncwarp();
-                if (mine) {
-                    const int32_t y = r.at + (values ? (int32_t)plane : 0);
-                    uint8_t *dst = (FP8 ? raw + st * C::RAW : ring + st * C::CHUNK) + (values ? unit * C::UNIT + row : row) * 128;
-                    for (int x = 0; x < boxes; ++x)
-                        tma_load_2d(dst + x * (values ? C::V_BOX : C::K_BOX), &map,
-                                    (values ? rank * C::DV : 0) + x * (FP8 ? 128 : 64), y, &s.landed[st]);
+                // (one elected thread issues: a copy that any lane might make took over 100 cycles)
+                uint8_t *const to = FP8 ? raw + st * C::RAW : ring + st * C::CHUNK;
+                for (uint32_t left = pages; left; left &= left - 1) {
+                    const int from = __ffs(left) - 1;
+                    const int32_t y = __shfl_sync(0xffffffffu, r.at, from) + (values ? (int32_t)plane : 0);
+                    uint8_t *const dst = to + ((values ? from / 16 * C::UNIT : 0) + from % 16 * p.page_rows) * 128;
+                    if (elect_one())
+#pragma unroll
+                        for (int x = 0; x < C::K_BOXES; ++x)
+                            if (x < boxes)
+                                tma_load_2d(dst + x * (values ? C::V_BOX : C::K_BOX), &map,
+                                            (values ? rank * C::DV : 0) + x * (FP8 ? 128 : 64), y, &s.landed[st]);
                 }
                 ++chunk;
+                if (++st == LANDS) st = 0, ++round;
                 return true;
             };
             auto note_mask = [&](const Page &r, int j) {
+                // (a tile of whole pages without padding rows)
+                if (__all_sync(0xffffffffu, r.rows == whole)) {
+                    if (lane < 4) s.mask[j % kMaskSlots][lane] = ~0u;
+                    __syncwarp();
+                    return;
+                }
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int a = unit * C::UNIT + row - 32 * w, e = a + r.rows;  // the lane's columns [a, e) of the word
@@ -783,38 +877,38 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 __syncwarp();
             };
             bool ok = true;
+            Page now{0, 0}, before{0, 0};  // of the last key tile, of the one before; `coming` and `after` are of the next two
             for (int k = 0, tiles = 0; ok; ++k) {
                 const int n = it.k1 - it.k0;
-                if (k > 0) {
-                    now = find(0);
-                    if (n > 1) next = find(1);
-                }
-                note_mask(now, tiles);
-                ok = copy(now, false, 0);
-                for (int j = 0; ok && j < n; ++j) {
-                    if (j + 1 < n) {
-                        note_mask(next, tiles + j + 1);
-                        ok = copy(next, false, 2 * j + 1);
+                bool more = true;
+                for (int i = 0; ok && i < 2 * n; ++i) {
+                    int j;
+                    const bool values = value_tile(i, n, j);
+                    if (!values) {
+                        before = now;
+                        now = pages.page(p, coming);
+                        note_mask(now, tiles + j);
                     }
-                    if (ok) ok = copy(now, true, j + 1 < n ? 2 * j + 2 : 2 * j + 1);
-                    now = next;
-                    if (j + 2 < n) next = find(j + 2);
+                    ok = copy(values && j + 1 < n ? before : now, values, i);
+                    if (!ok) break;
+                    // the pages of another key tile, or of the next item's first two
+                    int kt = it.k0 + j + 2, loads = !values;
+                    if (i == 2 * n - 1) {
+                        more = has_item(k + 1);
+                        if (!more) break;
+                        it = s.item[(k + 1) % kItems];
+                        pages.of(p, it);
+                        kt = it.k0;
+                        loads = 2;
+                    }
+                    for (; loads > 0; --loads, ++kt) {
+                        coming = after;
+                        after = pages.load(p, kt, it.k1, lane);
+                    }
                 }
                 tiles += n;
                 groups.end(n);
-                if (!ok) break;
-                // the next item, for all
-                const int slot = (k + 1) % kItems;
-                if (!wait_bar(s, &s.next[slot], (k / kItems) & 1, p.status)) break;
-                const int x = answered_cta(&s.answer[slot]);
-                fence_proxy_async_shared();  // read before another answer lands there
-                it = item_of(p, max(x, 0) / CTAS, STREAMS * CTAS * kTile);
-                if (x < 0) it.b = -1;
-                if (lane == 0) {
-                    s.item[slot] = it;
-                    mbar_arrive(&s.known[slot]);
-                }
-                if (x < 0) break;
+                if (!more) break;
             }
             // every commit's arrival is awaited before the CTA ends
             if constexpr (!FP8)
@@ -881,11 +975,13 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     ok = wait(&s.queries, k & 1) && arrived(0);
                     if (!ok) break;
                     tc_after_sync();
-                    // every warp is in this item; no further question after a no
+                    // every warp has left item k - 2, whose places item k + 2 takes (the products of
+                    // item k - 1 came after its outputs were read); no further question after a no
                     ok = wait(&s.next[(k + 1) % kItems], (k / kItems) & 1);
                     if (!ok) break;
                     if (answered_cta(&s.answer[(k + 1) % kItems]) >= 0) ask(k + 2);
                     for (int st = 0; st < STREAMS; ++st) scores(st, STREAMS == 1 ? tiles & 1 : st, chunk);
+                    if (n == 1) mma_commit<CTAS>(&s.scored);
                     release(0);
                     ++chunk;
                     int i = 1;  // chunk of the item
@@ -898,6 +994,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                             if (STREAMS == 1) {  // the next scores, beside this tile's weights
                                 // (their buffer's weights, of tile j - 1, were multiplied before)
                                 scores(0, (J + 1) & 1, k_at);
+                                if (j + 2 == n) mma_commit<CTAS>(&s.scored);
                                 release(i);
                             }
                             ++i, ++chunk;
@@ -919,6 +1016,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                             if (STREAMS == 2 && more) scores(st, st, k_at);
                         }
                         if (!ok) break;
+                        if (STREAMS == 2 && j + 2 == n) mma_commit<CTAS>(&s.scored);
                         release(i);
                         ++i, ++chunk;
                     }
@@ -934,6 +1032,33 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 (void)mbar_wait_bounded(&s.drained, 0);
             }
             __syncwarp();
+        } else if (warp == C::NEXT_WARP) {
+            // ---- the next item, for all, and its queries as soon as nothing reads this
+            // one's: its first products run beside the output
+            for (int k = 0;; ++k) {
+                const int slot = (k + 1) % kItems;
+                if (!wait_bar(s, &s.next[slot], (k / kItems) & 1, p.status)) break;
+                const int x = answered_cta(&s.answer[slot]);
+                fence_proxy_async_shared();  // read before another answer lands there
+                Item after = item_of(p, max(x, 0) / CTAS, STREAMS * CTAS * kTile);
+                if (x < 0) after.b = -1;
+                if (lane == 0) {
+                    s.item[slot] = after;
+                    mbar_arrive(&s.known[slot]);
+                }
+                __syncwarp();
+                if constexpr (!FP8) {
+                    Queries<C, C::SOFTMAX_WARPS> q;
+                    if (x >= 0) q.find(p, after, first, 0, 1, lane, true);
+                    if (!wait_bar(s, &s.scored, k & 1, p.status)) break;
+                    if (x < 0) break;
+                    q.copy(0, 1, lane, smem);
+                    async_wait_all();
+                    fence_proxy_async_shared();
+                    arrive_issuer(&s.queries, C::SOFTMAX_WARPS);
+                }
+                if (x < 0) break;
+            }
         } else if (!FP8 && warp == C::TIDY_WARP) {
             // ---- value rows that are not valid hold anything: zero weights must meet zeros
             bool ok = true;
@@ -968,10 +1093,24 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             const int t = threadIdx.x - 32 * C::CONVERT_WARP, u = t % 8;
             bool ok = true;
             Groups<C> groups;
-            int chunk = 0;
-            for (int k = 0, tiles = 0, group = 0; ok; ++k) {
+            // the queries of the items after the first, as soon as nothing reads the item's
+            // before: its first products run beside the output
+            const int from = warp - C::CONVERT_WARP;
+            int chunk = 0, k = 0;
+            for (int tiles = 0, group = 0; ok; ++k) {
                 const int n = s.item[k % kItems].k1 - s.item[k % kItems].k0;
                 for (int i = 0; ok && i < 2 * n; ++i, ++chunk) {
+                    if (i == 0 && k > 0) {
+                        Queries<C, C::SOFTMAX_WARPS / kConvertWarps> q;
+                        q.find(p, s.item[k % kItems], first, from, kConvertWarps, lane, true);
+                        ok = wait_bar(s, &s.scored, (k - 1) & 1, p.status);
+                        if (!ok) break;
+                        q.copy(from, kConvertWarps, lane, smem);
+                        async_wait_all();
+                        q.convert(from, kConvertWarps, lane, smem);
+                        fence_proxy_async_shared();
+                        arrive_issuer(&s.queries, C::SOFTMAX_WARPS / kConvertWarps);
+                    }
                     const int rs = chunk % LANDS, st = chunk % STAGES;
                     int j;
                     const bool values = value_tile(i, n, j);
@@ -1029,6 +1168,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 if (!ok || !has_item(k + 1)) break;
             }
             // every commit's arrival is awaited before the CTA ends
+            if (ok) ok = wait_bar(s, &s.scored, k & 1, p.status);
             for (int c = max(0, chunk - STAGES); ok && c < chunk; ++c) {
                 const int g = groups.of(c % STAGES);
                 ok = wait_bar(s, &s.empty[g % C::GROUPS], (g / C::GROUPS) & 1, p.status);
