@@ -351,6 +351,26 @@ inline int64_t decode_slots(const std::vector<DecodeParams> &plan, int64_t w_max
 // Query rows of up to kMaxBatchPerLaunch sequences over layers of one window.
 // shared: "sequences" are groups of batch rows whose sequences have the same
 // first pages; a group's rows are its members, seq is one of them.
+// Division of 0 <= n < 2^31 by a number that the host knows, as a product
+// (Granlund and Montgomery, "Division by invariant integers using
+// multiplication", 1994): with l = ceil(log2 d), n / d is the product of n and
+// floor(2^(31 + l) / d) + 1, shifted by 31 + l.
+struct Divisor {
+    int32_t d;
+    uint32_t mul, shift;
+    Divisor() = default;
+    explicit Divisor(int32_t by) : d(by), mul(0), shift(0) {
+        if (d <= 1) return;
+        uint32_t l = 1;
+        while (((int64_t)1 << l) < d) ++l;
+        mul = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint32_t)d + 1);
+        shift = l - 1;
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift); }
+#endif
+};
+
 struct PromptParams {
     const uint8_t *pool;
     int64_t pool_pages;
@@ -358,6 +378,8 @@ struct PromptParams {
     const int32_t *page_table, *page_fill;
     int32_t max_pages, n_seq, window, shared;
     int32_t n_units;           // run layers x KV heads
+    int32_t log2_group;        // of the query heads to a KV head
+    Divisor by_units, by_kv_heads, by_page, by_pages;  // n_units, n_kv_heads, page_size, pages_per_unit or units_per_page
     int32_t unit;              // columns of a key tile that pages fill by themselves
     int32_t pages_per_unit;    // whole pages that one holds (0: a page takes units_per_page)
     int32_t units_per_page, page_rows, box_rows;  // rows of a page in a unit, of a copy

@@ -18,6 +18,20 @@
 // Key tiles are 128 columns, made of units of 128 (pairs: 64): a page's rows,
 // or as many whole pages as fit when pages are smaller, each at a multiple of 8
 // rows so that its copy starts on a swizzle atom.
+//
+// Warps: four per stream of 128 query rows form weights (a thread has a row);
+// one loads pages, one thread issues products, one zeroes the value rows that
+// hold nothing (four convert E4M3 codes to fp16 instead, exact, for an fp8
+// cache), one works out the next item and fetches its queries.
+//
+// What bounds it: the tensor cores and, with two streams, the softmax between
+// them.  A tile of 256 x 128 is 2,150 cycles of products; it takes 2,400 for
+// head_dim 256 (1.68 PFLOP/s over 8,191 rows of the 12B shape, 327 us) and
+// 2,650 for 128 (1.55, 8,192 rows of the 31B shape on 16,384 in 1,770 us): each
+// stream's scores, weights and products follow one another, and the weights of
+// one take longer (1,350 cycles) than the products of the other.  Packed fp8
+// prompts of 1 .. 1,501 rows with windows of 1,024 (168 us) spend 6,000 of
+// 36,000 cycles an item between items.
 #include <limits.h>
 #include <math.h>
 
@@ -133,10 +147,10 @@ __device__ __forceinline__ bool wait_bar(Bars &s, uint64_t *bar, uint32_t parity
 
 // Key tile and column of a slot.
 __device__ __forceinline__ void tile_of(const PromptParams &p, int slot, int &tile, int &col) {
-    const int pg = slot / p.page_size, r = slot - pg * p.page_size;
+    const int pg = p.by_page.div(slot), r = slot - pg * p.page_size;
     int u;
     if (p.pages_per_unit) {
-        u = pg / p.pages_per_unit;
+        u = p.by_pages.div(pg);
         col = (pg - u * p.pages_per_unit) * p.page_rows + r;
     } else {
         u = pg * p.units_per_page + r / p.unit;
@@ -149,7 +163,7 @@ __device__ __forceinline__ void tile_of(const PromptParams &p, int slot, int &ti
 __device__ __forceinline__ int first_slot(const PromptParams &p, int tile) {
     const int u = tile * (kTile / p.unit);
     return p.pages_per_unit ? u * p.pages_per_unit * p.page_size
-                            : u / p.units_per_page * p.page_size + u % p.units_per_page * p.unit;
+                            : p.by_pages.div(u) * p.page_size + (u - p.by_pages.div(u) * p.units_per_page) * p.unit;
 }
 
 // First slot that the row at `slot` attends to.
@@ -201,16 +215,14 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     Item it;
     const int b = search(p.item0, p.n_seq, at);
     it.b = b;
-    it.gs = 31 - __clz(p.n_q_heads / p.n_kv_heads);
+    it.gs = p.log2_group;
     const int n = (p.first[b + 1] - p.first[b]) << it.gs, nt = (n + tile_rows - 1) / tile_rows;
-    int rem = at - p.item0[b];
-    const int per_tile = p.splits[b] * p.n_units;
-    const int t = nt - 1 - rem / per_tile;
-    rem %= per_tile;
-    it.split = rem / p.n_units;
-    rem %= p.n_units;
-    it.lr = rem / p.n_kv_heads;
-    it.g = rem % p.n_kv_heads;
+    const int splits = p.splits[b], of_unit = at - p.item0[b];
+    const int rem = p.by_units.div(of_unit), unit = of_unit - rem * p.n_units;
+    const int tile = splits == 1 ? rem : rem / splits, t = nt - 1 - tile;
+    it.split = rem - tile * splits;
+    it.lr = p.by_kv_heads.div(unit);
+    it.g = unit - it.lr * p.n_kv_heads;
     it.row0 = t * tile_rows;
     it.rows = min(tile_rows, n - it.row0);
     it.last_slot = row_last(p, it, (it.row0 + it.rows - 1) >> it.gs);
@@ -221,7 +233,7 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     tile_of(p, from, ka, col);
     tile_of(p, it.last_slot, kb, col);
     const int len = max(0, kb + 1 - ka);  // (a shared block may end before the rows' windows)
-    const int part = len / p.splits[b], rest = len - part * p.splits[b];  // the first `rest` splits have one more
+    const int part = splits == 1 ? len : len / splits, rest = len - part * splits;  // the first `rest` splits have one more
     it.k0 = ka + part * it.split + min(it.split, rest);
     it.k1 = it.k0 + max(1, part + (it.split < rest));  // (one tile past the last: no valid column)
     return it;
@@ -383,7 +395,7 @@ struct Pages {
         table = p.page_table + e;
         fill = p.page_fill + e;
         base = (int32_t)(((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads + it.g) * p.page_size);
-        last = it.last_slot / p.page_size;
+        last = p.by_page.div(it.last_slot);
     }
     // of key tile kt (none from k1 on)
     __device__ __forceinline__ Entry load(const PromptParams &p, int kt, int k1, int lane) const {
@@ -392,7 +404,7 @@ struct Pages {
         bool has = unit < C::CTAS && place < p.pages_per_unit;
         Entry e{0, 0, 0};
         if (!p.pages_per_unit) {
-            pg = u / p.units_per_page;
+            pg = p.by_pages.div(u);
             e.sub = (u - pg * p.units_per_page) * C::UNIT;
             has = unit < C::CTAS && place == 0;
         }
@@ -539,6 +551,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
     };
 
+    if (warp == C::LOAD_WARP && lane == 0)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::GROUPS; ++i) {
             mbar_init(&s.ready[i], CTAS * (C::GROUPED ? 2 : 1) * (FP8 ? kConvertWarps : 1));
@@ -1191,17 +1205,17 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
     constexpr int N = D / 32;
     after_previous();
     let_next_start();  // a few microseconds to its end, and room for the next beside it
-    const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    const int lane = threadIdx.x & 31, gs = 31 - __clz(p.n_q_heads / p.n_kv_heads);
-    if (at >= ((int64_t)p.first[p.n_seq] << gs) * p.n_units) return;
+    const int rows4 = p.by_units.div(blockIdx.x), unit = blockIdx.x - rows4 * p.n_units;
+    const int lane = threadIdx.x & 31, gs = p.log2_group;
+    const int64_t row_of_all = (int64_t)rows4 * 4 + threadIdx.x / 32;
+    if (row_of_all >= (int64_t)p.first[p.n_seq] << gs) return;
     Item it{};
     it.gs = gs;
-    const int64_t row_of_all = at / p.n_units;
     it.b = search(p.first, p.n_seq, row_of_all >> gs);
     if (p.splits[it.b] == 1) return;
-    const int unit = (int)(at - row_of_all * p.n_units), row = (int)(row_of_all - ((int64_t)p.first[it.b] << gs));
-    it.lr = unit / p.n_kv_heads;
-    it.g = unit % p.n_kv_heads;
+    const int row = (int)(row_of_all - ((int64_t)p.first[it.b] << gs));
+    it.lr = p.by_kv_heads.div(unit);
+    it.g = unit - it.lr * p.n_kv_heads;
     float M = -INFINITY, L = 0.f, o[N] = {};
     for (int i = 0; i < p.splits[it.b]; ++i) M = fmaxf(M, p.part_ml[part_slot(p, it, i, row)].x);
     for (int i = 0; i < p.splits[it.b]; ++i) {
@@ -1259,7 +1273,11 @@ struct PromptLaunch {
 
 }  // namespace
 
-// Two streams of query tiles unless no sequence has rows for the second.
+// Two streams of query tiles unless no sequence has rows for the second (single
+// calls on an idle GPU): 8,192
+// rows of the 31B shape on 16,384 1,617 us (one stream 2,331), packed fp8 prompts
+// of 1 .. 1,501 rows 176 (240); 7 x 40 .. 60 rows, a tile or less, on 3,000 ..
+// 5,000 77.5 (one stream 67.8).  (head_dim 256 fills the tensor memory with one.)
 int prompt_streams(int head_dim, int64_t most_rows) { return head_dim <= 128 && most_rows > kTile ? 2 : 1; }
 
 // Query rows of a work item, and the CTAs that share it.
@@ -1290,8 +1308,7 @@ cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParam
 }
 
 cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t s) {
-    const int64_t rows = (int64_t)p.first[p.n_seq] * (p.n_q_heads / p.n_kv_heads) * p.n_units;
-    const int64_t grid = (rows + 3) / 4;
+    const int64_t grid = ((((int64_t)p.first[p.n_seq] << p.log2_group) + 3) / 4) * p.n_units;
     switch (head_dim) {
         case 64: return launch_after(prompt_join_kernel<64>, (unsigned)grid, 128, 0, s, p);
         case 128: return launch_after(prompt_join_kernel<128>, (unsigned)grid, 128, 0, s, p);
