@@ -105,8 +105,13 @@ struct Item {
     int last_slot;  // of the sequence's pages that the item reads
 };
 
-// Items that a CTA knows of at once: the load warp is at most two ahead.
+// Items that a CTA knows of at once.
 constexpr int kItems = 4;
+// The next item is asked for kAskTiles key tiles before an item's end (the
+// answer, the first pages and the queries take some 8,000 cycles), so that CTAs
+// end close together: 20 us apart instead of 35 in packed fp8 prompts of up to 9
+// tiles an item (161 us; 167 to 171 asked for at its start).
+constexpr int kAskTiles = 5;
 
 struct Bars {
     uint64_t landed[8], freed[2];            // copies: there; (fp8) converted, their place is free
@@ -607,9 +612,9 @@ __global__ void __launch_bounds__(C::THREADS, 1)
 
     // The CTA's items: its own, then those of CTAs that have not started, so that
     // copies run ahead into the next item while an item's outputs are stored.
-    // The issuing thread asks for item k + 2 when every warp is in item k (so the
-    // answer for item k - 2 and what it meant are read); one warp works out what an
-    // answer means for all.  The CTA's item k >= 1, for a warp:
+    // The issuing thread asks for item k + 1 while it is in item k (every warp has
+    // left item k - 3, whose places it takes), one warp works out what the answer
+    // means for all.  The CTA's item k >= 1, for a warp:
     auto has_item = [&](int k) {
         return wait_bar(s, &s.known[k % kItems], ((k - 1) / kItems) & 1, p.status) && s.item[k % kItems].b >= 0;
     };
@@ -982,57 +987,58 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     mbar_arrive_expect_tx(&s.next[k % kItems], sizeof(uint4));
                     ask_for_cta<CTAS>(&s.answer[k % kItems], &s.next[k % kItems]);
                 };
-                ask(1);
                 bool ok = true;
                 int n = s.item[0].k1 - s.item[0].k0;
                 for (int k = 0, tiles = 0; ok; ++k) {
                     ok = wait(&s.queries, k & 1) && arrived(0);
                     if (!ok) break;
                     tc_after_sync();
-                    // every warp has left item k - 2, whose places item k + 2 takes (the products of
-                    // item k - 1 came after its outputs were read); no further question after a no
-                    ok = wait(&s.next[(k + 1) % kItems], (k / kItems) & 1);
-                    if (!ok) break;
-                    if (answered_cta(&s.answer[(k + 1) % kItems]) >= 0) ask(k + 2);
                     for (int st = 0; st < STREAMS; ++st) scores(st, STREAMS == 1 ? tiles & 1 : st, chunk);
                     if (n == 1) mma_commit<CTAS>(&s.scored);
                     release(0);
                     ++chunk;
                     int i = 1;  // chunk of the item
-                    for (int j = 0; ok && j < n; ++j) {
-                        const int J = tiles + j, k_at = chunk;
-                        const bool more = j + 1 < n;
-                        if (more) {
-                            ok = arrived(i);
-                            if (!ok) break;
-                            if (STREAMS == 1) {  // the next scores, beside this tile's weights
-                                // (their buffer's weights, of tile j - 1, were multiplied before)
-                                scores(0, (J + 1) & 1, k_at);
-                                if (j + 2 == n) mma_commit<CTAS>(&s.scored);
-                                release(i);
+                    // (asked between two runs of tiles: within the loop, 8,192 rows of the 31B shape
+                    // on 16,384 took 1,645 us for 1,629)
+#pragma unroll 1
+                    for (int part = 0, j = 0; ok && part < 2; ++part) {
+                        const int end = part ? n : max(0, n - kAskTiles);
+                        if (part) ask(k + 1);
+                        for (; ok && j < end; ++j) {
+                            const int J = tiles + j, k_at = chunk;
+                            const bool more = j + 1 < n;
+                            if (more) {
+                                ok = arrived(i);
+                                if (!ok) break;
+                                if (STREAMS == 1) {  // the next scores, beside this tile's weights
+                                    // (their buffer's weights, of tile j - 1, were multiplied before)
+                                    scores(0, (J + 1) & 1, k_at);
+                                    if (j + 2 == n) mma_commit<CTAS>(&s.scored);
+                                    release(i);
+                                }
+                                ++i, ++chunk;
                             }
+                            if (!C::GROUPED || !more) ok = arrived(i);
+                            for (int st = 0; ok && st < STREAMS; ++st) {
+                                const int buf = STREAMS == 1 ? J & 1 : st;
+                                // (the first product of an item takes the place of the outputs before)
+                                if (j == 0 && k > 0) ok = wait(&s.taken[st], (k - 1) & 1);
+#pragma unroll
+                                for (int half = 0; half < 2; ++half) {
+                                    ok = ok && wait(&s.weights[buf][half], (STREAMS == 1 ? J >> 1 : J) & 1);
+                                    if (!ok) break;
+                                    tc_after_sync();
+                                    product(st, buf, half, chunk, j > 0);
+                                }
+                                if (!ok) break;
+                                if (STREAMS == 1 || !more) mma_commit<CTAS>(&s.out[st]);
+                                if (STREAMS == 2 && more) scores(st, st, k_at);
+                            }
+                            if (!ok) break;
+                            if (STREAMS == 2 && j + 2 == n) mma_commit<CTAS>(&s.scored);
+                            release(i);
                             ++i, ++chunk;
                         }
-                        if (!C::GROUPED || !more) ok = arrived(i);
-                        for (int st = 0; ok && st < STREAMS; ++st) {
-                            const int buf = STREAMS == 1 ? J & 1 : st;
-                            // (the first product of an item takes the place of the outputs before)
-                            if (j == 0 && k > 0) ok = wait(&s.taken[st], (k - 1) & 1);
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                ok = ok && wait(&s.weights[buf][half], (STREAMS == 1 ? J >> 1 : J) & 1);
-                                if (!ok) break;
-                                tc_after_sync();
-                                product(st, buf, half, chunk, j > 0);
-                            }
-                            if (!ok) break;
-                            if (STREAMS == 1 || !more) mma_commit<CTAS>(&s.out[st]);
-                            if (STREAMS == 2 && more) scores(st, st, k_at);
-                        }
-                        if (!ok) break;
-                        if (STREAMS == 2 && j + 2 == n) mma_commit<CTAS>(&s.scored);
-                        release(i);
-                        ++i, ++chunk;
                     }
                     if (!ok) break;
                     tiles += n;

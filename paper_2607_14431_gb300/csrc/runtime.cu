@@ -2644,6 +2644,7 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
     const int64_t P = d.page_size;
     int64_t total = 0;
     bool single = true;
+    std::vector<int32_t> order, row0(B);  // sequences with rows; first packed row
     for (int32_t b = 0; b < B; ++b) {
         const int32_t sq = seq_ids[b];
         if (n_rows[b] < 0 || n_rows[b] > c->n_slots[sq])
@@ -2652,15 +2653,20 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
         const auto &f = c->seq_fill[sq];
         for (int64_t pg = (c->n_slots[sq] - n_rows[b]) / P; n_rows[b] && pg + 1 < (int64_t)f.size(); ++pg)
             if (f[pg] < P) return fail(KVG_ERR_ARG, "seq %d: unfilled slots among its last %d", sq, n_rows[b]);
+        row0[b] = (int32_t)total;
+        if (n_rows[b]) order.push_back(b);
         total += n_rows[b];
+        if (total > 0x7fffffff / n_q_heads) return fail(KVG_ERR_ARG, "more than 2^31 - 1 query rows x heads");
         single = single && n_rows[b] == 1;
     }
-    if (total > 0x7fffffff / n_q_heads) return fail(KVG_ERR_ARG, "more than 2^31 - 1 query rows x heads");
     if (total == 0) return KVG_OK;
     // prompts of one token are a decode step
     if (single)
         return decode_impl("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0, INT32_MAX,
                            nullptr, 0);
+    // the longest work items first, so that the SMs end close together
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int32_t a, int32_t b) { return c->n_slots[seq_ids[a]] > c->n_slots[seq_ids[b]]; });
     DeviceGuard g(c->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     PromptParams p{};
@@ -2670,17 +2676,15 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
     KVG_CUDA(use_partials(c, st));
     for (const WindowGroup &part : layer_parts(c, layer)) {
         prompt_layers(part, &p);
-        int32_t row = 0;
-        for (int32_t b = 0; b < B;) {
+        for (size_t at = 0; at < order.size();) {
             p.n_seq = 0;
             std::vector<PromptWork> work;
             int64_t most = 0;
-            for (; b < B && p.n_seq < kMaxBatchPerLaunch; ++b) {
-                if (n_rows[b] == 0) continue;
-                const int32_t i = p.n_seq++, sq = seq_ids[b];
+            for (; at < order.size() && p.n_seq < kMaxBatchPerLaunch; ++at) {
+                const int32_t b = order[at], i = p.n_seq++, sq = seq_ids[b];
                 const auto &f = c->seq_fill[sq];
                 p.seq[i] = sq;
-                p.row0[i] = row;
+                p.row0[i] = row0[b];
                 p.slot0[i] = c->n_slots[sq] - n_rows[b];
                 p.holes[i] = std::any_of(f.begin(), f.end() - 1, [P](int32_t x) { return x < P; });
                 p.begin[i] = 0;
@@ -2693,11 +2697,9 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
                     }
                 }
                 p.first[i + 1] = p.first[i] + n_rows[b];
-                row += n_rows[b];
                 most = std::max<int64_t>(most, (int64_t)n_rows[b] * G);
                 work.push_back({(int64_t)n_rows[b] * G, n_rows[b], p.begin[i], p.slot0[i]});
             }
-            if (p.n_seq == 0) continue;
             const int streams = prompt_streams(d.head_dim, most);
             const int64_t slots = plan_prompt(c, work, G, prompt_tile_rows(d.head_dim, streams), false, &p);
             prompt_items(prompt_tile_rows(d.head_dim, streams), G, &p);
