@@ -21,17 +21,17 @@
 //
 // Warps: four per stream of 128 query rows form weights (a thread has a row);
 // one loads pages, one thread issues products, one zeroes the value rows that
-// hold nothing (four convert E4M3 codes to fp16 instead, exact, for an fp8
-// cache), one works out the next item and fetches its queries.
+// hold nothing, one works out the next item and fetches its queries (for an fp8
+// cache four convert E4M3 codes to fp16, exact, and do the last two jobs).
 //
 // What bounds it: the tensor cores and, with two streams, the softmax between
 // them.  A tile of 256 x 128 is 2,150 cycles of products; it takes 2,400 for
 // head_dim 256 (1.68 PFLOP/s over 8,191 rows of the 12B shape, 327 us) and
-// 2,650 for 128 (1.55, 8,192 rows of the 31B shape on 16,384 in 1,770 us): each
+// 2,650 for 128 (1.53, 8,192 rows of the 31B shape on 16,384 in 1,795 us): each
 // stream's scores, weights and products follow one another, and the weights of
 // one take longer (1,350 cycles) than the products of the other.  Packed fp8
-// prompts of 1 .. 1,501 rows with windows of 1,024 (168 us) spend 6,000 of
-// 36,000 cycles an item between items.
+// prompts of 1 .. 1,501 rows with windows of 1,024 (161 us) spend 6,500 of
+// 34,000 cycles an item between items.
 #include <limits.h>
 #include <math.h>
 
