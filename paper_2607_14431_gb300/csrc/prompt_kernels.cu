@@ -22,7 +22,8 @@
 // Warps: four per stream of 128 query rows form weights (a thread has a row);
 // one loads pages, one thread issues products, one zeroes the value rows that
 // hold nothing, one works out the next item and fetches its queries (for an fp8
-// cache four convert E4M3 codes to fp16, exact, and do the last two jobs).
+// cache four convert E4M3 codes to fp16, exact, zero those rows and fetch the
+// queries).
 //
 // What bounds it: the tensor cores and, with two streams, the softmax between
 // them.  A tile of 256 x 128 is 2,150 cycles of products; it takes 2,400 for
@@ -77,7 +78,10 @@ struct Cfg {
     // streams hand over and give back K(j + 1) and V(j) together (an MMA commit
     // holds up the issuing thread): chunk c is of group (c + 1) / 2.
     static constexpr bool GROUPED = STREAMS == 2;
-    static constexpr int GROUPS = GROUPED ? 4 : STAGES;
+    // (As many barriers as a ring may hold groups: items of one tile have a chunk to
+    // each, and two groups that land on one barrier would be one phase ahead.)
+    static constexpr int GROUPS = GROUPED ? 8 : STAGES;
+    static_assert(GROUPS >= STAGES && GROUPS <= 8, "groups in flight");
     static constexpr int SOFTMAX_WARPS = 4 * STREAMS;
     static constexpr int LOAD_WARP = SOFTMAX_WARPS, MMA_WARP = LOAD_WARP + 1, TIDY_WARP = LOAD_WARP + 2, CONVERT_WARP = LOAD_WARP + 4;
     // (for an fp8 cache the converting warps tidy and fetch queries)

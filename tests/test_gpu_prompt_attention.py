@@ -209,6 +209,21 @@ def test_many_sequences(kvg):
     run(bed, 2, list(range(n)), rows)
 
 
+@pytest.mark.parametrize("d,fp8", [(64, False), (128, False), (256, False), (128, True), (256, True)])
+@pytest.mark.parametrize("most", [4, 200])
+def test_an_sm_takes_many_items_of_few_tiles(kvg, d, fp8, most):
+    """Six work items and more for each SM, of one to three key tiles (rows above 128 / G: two streams)."""
+    rng = np.random.default_rng(d + most)
+    batch = 120 if most == 4 else 40
+    rows, past = rng.integers(1, most, batch), rng.integers(0, 190, batch)
+    rows[0] = 2  # (not all of one row)
+    need = int(sum(-(-(r + p) // 32) for r, p in zip(rows, past)))
+    bed = Bed(kvg, 1, 8 if most == 4 else 16, d, 32, need, batch, 400, fp8=fp8)
+    for b in range(batch):
+        bed.append(b, int(rows[b] + past[b]), 10 * b)
+    run(bed, 2 * bed.hkv, list(range(batch)), [int(x) for x in rows])
+
+
 @pytest.mark.parametrize("window", [0, 70])
 def test_unfilled_page_tails_between_grafted_blocks(kvg, window):
     bed = Bed(kvg, 1, 2, 128, 64, 40, 3, 1024)
