@@ -403,6 +403,7 @@ struct PromptParams {
     int32_t part_units;                    // layers of q x KV heads
     float *part_o;                         // [slots][D]
     float2 *part_ml;                       // [slots] (m, l)
+    int2 *redo;                            // [items][8] (rows, entry before): rows to be computed over
     int32_t member[kMaxBatchPerLaunch];    // shared: batch row of each member
     int32_t lo[kMaxBatchPerLaunch];        // shared: first slot that it attends to
 };
@@ -529,6 +530,7 @@ bool sha256_parts_ok();
 int prompt_streams(int head_dim, int64_t most_rows);
 int prompt_tile_rows(int head_dim, int streams);
 int prompt_ctas(int head_dim);
+uint64_t prompt_redo_bytes(int64_t items);
 void prompt_tiling(int page_size, int head_dim, PromptParams *p);
 cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
                           cudaStream_t s);

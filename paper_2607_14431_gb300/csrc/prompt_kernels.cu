@@ -50,6 +50,7 @@ namespace {
 constexpr int kTile = 128;       // query rows of a stream, columns of a key tile
 constexpr int kMaskSlots = 16;   // key tiles whose column masks are kept
 constexpr int kConvertWarps = 4;
+constexpr int kRowWarps = 8;     // 32 rows of an item each, at most
 // The running maximum that the weights refer to is moved only when a row's
 // maximum passes it by more than this (in powers of two): weights then reach
 // at most 2^8, which costs no precision in bf16 or fp16, and the accumulator
@@ -107,6 +108,7 @@ struct Item {
     int row0, rows; // of the sequence's rows (token x head of the group), those of the item
     int k0, k1;     // key tiles
     int last_slot;  // of the sequence's pages that the item reads
+    int at;         // of the launch's items
 };
 
 // Items that a CTA knows of at once.
@@ -130,6 +132,7 @@ struct Bars {
     uint32_t mask[kMaskSlots][4];            // valid columns of key tile j % kMaskSlots
     uint32_t tmem;
     int abort;
+    int redo;                                // last entry of p.redo that the CTA made, or -1
 };
 
 // Bounded wait that also ends when another warp gave up.
@@ -222,6 +225,7 @@ __device__ __forceinline__ int search(const int32_t *first, int n, int64_t at) {
 // The longest tiles of a sequence (its last rows) come first.
 __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_rows) {
     Item it;
+    it.at = at;
     const int b = search(p.item0, p.n_seq, at);
     it.b = b;
     it.gs = p.log2_group;
@@ -286,11 +290,14 @@ __device__ __forceinline__ const uint8_t *row_at(const PromptParams &p, const It
     return p.pool + (((page * p.n_kv_heads + it.g) * p.page_size) + r) * D * E;
 }
 
-// A warp: attention of one query row over slots [first, last].
+// A warp: attention of one query row over slots [first, last], from the last one
+// back, some slots' loads in flight together.  (Of an fp8 cache one: with four,
+// although nothing is computed over, 4,096 rows of the 31B shape on 8,192 took
+// 570 us for 562, packed prompts of 1 .. 1,501 rows 170 for 169.)
 template <int D, bool FP8>
 __device__ __forceinline__ void attend_row(const PromptParams &p, const Item &it, int row, int first, int last,
                                         float (&o)[D / 32], float &m, float &l) {
-    constexpr int N = D / 32;
+    constexpr int N = D / 32, U = FP8 ? 1 : 4;
     const int lane = threadIdx.x & 31;
     float q[N];
     load_row<D, false>(reinterpret_cast<const uint8_t *>(p.q + q_row(p, it, row) * D), lane, q);
@@ -298,25 +305,42 @@ __device__ __forceinline__ void attend_row(const PromptParams &p, const Item &it
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = 0.f;
-    for (int slot = first; slot <= last; ++slot) {
+    for (int slot = last; slot >= first; slot -= U) {
+        const uint8_t *k[U];
         int64_t v_off;
-        const uint8_t *k = row_at<D, FP8>(p, it, slot, v_off);
-        if (!k) continue;
-        float x[N], s = 0.f;
-        load_row<D, FP8>(k, lane, x);
+        float s[U];
 #pragma unroll
-        for (int i = 0; i < N; ++i) s = __fmaf_rn(q[i], x[i], s);
+        for (int u = 0; u < U; ++u) {
+            k[u] = slot - u >= first ? row_at<D, FP8>(p, it, slot - u, v_off) : nullptr;
+            s[u] = 0.f;
+            if (!k[u]) continue;
+            float x[N];
+            load_row<D, FP8>(k[u], lane, x);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        s *= p.negate ? -p.qscale : p.qscale;
-        const float mn = fmaxf(m, s);
-        const float base = mn == -INFINITY ? 0.f : mn;
-        const float a = exp2f(m - base), w = exp2f(s - base);
-        m = mn;
-        l = __fmaf_rn(l, a, w);
-        load_row<D, FP8>(k + v_off, lane, x);
+            for (int i = 0; i < N; ++i) s[u] = __fmaf_rn(q[i], x[i], s[u]);
+        }
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = __fmaf_rn(o[i], a, w * x[i]);
+        for (int d = 16; d; d >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], d);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!k[u]) continue;
+            s[u] *= p.negate ? -p.qscale : p.qscale;
+            const float mn = fmaxf(m, s[u]);
+            const float base = mn == -INFINITY ? 0.f : mn;
+            const float a = exp2f(m - base), w = exp2f(s[u] - base);
+            m = mn;
+            l = __fmaf_rn(l, a, w);
+            float x[N];
+            load_row<D, FP8>(k[u] + v_off, lane, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = __fmaf_rn(o[i], a, w * x[i]);
+        }
+        bool nan = true;
+#pragma unroll
+        for (int i = 0; i < N; ++i) nan = nan && o[i] != o[i];
+        if (__all_sync(0xffffffffu, nan)) break;  // (stays so)
     }
 }
 
@@ -326,19 +350,23 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
 }
 
 // A value row that is not finite reaches, as 0 x inf, the outputs of rows of
-// its tile that do not attend to it.  The warp whose outputs are not finite
-// looks for such rows among the columns that its tiles masked, and computes the
-// output rows that one reached over again.  (A not finite output whose masked
-// values are all finite is as it should be.)
+// its tile that do not attend to it.  So a warp whose outputs are not finite
+// notes its 32 rows, and when the CTA has done all its items (nothing waits for
+// it then, however long it takes) its warps compute those that such a row reached
+// over from the definition, each a row at a time.
+
+// A warp: of 32 rows from first_row on, those that a value row which is not
+// finite reached without being attended to, among the columns that their tiles
+// masked.  (Other outputs that are not finite are as they should be.)
 template <int D, bool FP8>
-__device__ __forceinline__ void repair(const PromptParams &p, const Item &it, int first_row, bool bad, int lo, int hi,
-                                    bool partial) {
+__device__ __forceinline__ uint32_t reached(const PromptParams &p, const Item &it, int first_row) {
     constexpr int N = D / 32;
-    const int lane = threadIdx.x & 31;
-    int tile_lo, tile_hi, col;
+    const int lane = threadIdx.x & 31, row = first_row + lane;
+    const bool mine = row < it.row0 + it.rows;
+    const int lo = mine ? row_first(p, it, row >> it.gs) : 0, hi = mine ? row_last(p, it, row >> it.gs) : -1;
+    int tile_lo, tile_hi = 0x7fffffff, col;
     tile_of(p, lo, tile_lo, col);
-    tile_of(p, hi, tile_hi, col);
-    if (hi < lo) tile_hi = 0x7fffffff;  // not a row of the item's
+    if (mine) tile_of(p, hi, tile_hi, col);
     const int from = __reduce_min_sync(0xffffffffu, tile_hi), to = __reduce_max_sync(0xffffffffu, tile_lo);
     bool redo = false;
     for (int kt = it.k0; kt < it.k1; ++kt) {
@@ -356,25 +384,40 @@ __device__ __forceinline__ void repair(const PromptParams &p, const Item &it, in
             if (__any_sync(0xffffffffu, !fine)) redo = redo || slot < lo || slot > hi;
         }
     }
-    const uint32_t todo = __ballot_sync(0xffffffffu, bad && redo);
-    for (int i = 0; i < 32; ++i) {
-        if (!(todo >> i & 1)) continue;
-        const int row = first_row + i;
-        const int f = max(__shfl_sync(0xffffffffu, lo, i), first_slot(p, it.k0));
-        const int l_ = min(__shfl_sync(0xffffffffu, hi, i), first_slot(p, it.k1) - 1);
-        float o[N], m, l;
-        attend_row<D, FP8>(p, it, row, f, l_, o, m, l);
-        if (partial) {
-            const int64_t at = part_slot(p, it, it.split, row);
+    return __ballot_sync(0xffffffffu, mine && redo);
+}
+
+// The CTA's warps, of the entries up to `last`.
+template <int D, bool FP8>
+__device__ __forceinline__ void compute_over(const PromptParams &p, int last, int tile_rows, int warp, int warps) {
+    constexpr int N = D / 32;
+    const int lane = threadIdx.x & 31;
+    int n = 0;  // rows so far
+    for (int id = last; id >= 0;) {
+        const int2 entry = p.redo[id];
+        const Item it = item_of(p, id / kRowWarps, tile_rows);
+        const int first_row = it.row0 + id % kRowWarps * 32;
+        const bool partial = p.splits[it.b] > 1 || p.shared;
+        for (uint32_t left = entry.x & reached<D, FP8>(p, it, first_row); left; left &= left - 1, ++n) {
+            if (n % warps != warp) continue;
+            const int row = first_row + __ffs(left) - 1, token = row >> it.gs;
+            const int from = max(row_first(p, it, token), first_slot(p, it.k0));
+            const int to = min(row_last(p, it, token), first_slot(p, it.k1) - 1);
+            float o[N], m, l;
+            attend_row<D, FP8>(p, it, row, from, to, o, m, l);
+            if (partial) {
+                const int64_t at = part_slot(p, it, it.split, row);
 #pragma unroll
-            for (int e = 0; e < N; ++e) p.part_o[at * D + lane * N + e] = o[e];
-            if (lane == 0) p.part_ml[at] = make_float2(l == l ? m : 0.f, l);
-        } else {
-            const float inv = p.vscale / l;
-            uint32_t *out = reinterpret_cast<uint32_t *>(p.out + q_row(p, it, row) * D + lane * N);
+                for (int e = 0; e < N; ++e) p.part_o[at * D + lane * N + e] = o[e];
+                if (lane == 0) p.part_ml[at] = make_float2(l == l ? m : 0.f, l);
+            } else {
+                const float inv = p.vscale / l;
+                uint32_t *out = reinterpret_cast<uint32_t *>(p.out + q_row(p, it, row) * D + lane * N);
 #pragma unroll
-            for (int e = 0; e < N / 2; ++e) out[e] = pack_out(o[2 * e] * inv, o[2 * e + 1] * inv);
+                for (int e = 0; e < N / 2; ++e) out[e] = pack_out(o[2 * e] * inv, o[2 * e + 1] * inv);
+            }
         }
+        id = entry.y;
     }
 }
 
@@ -585,6 +628,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         }
         mbar_init(&s.drained, 1);
         s.abort = 0;
+        s.redo = -1;
         fence_mbar_init();
     }
     if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
@@ -823,11 +867,10 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 // (read: the next item's products may be added there)
                 tc_before_sync();
                 arrive_issuer(&s.taken[stream]);
-                if (__any_sync(0xffffffffu, bad)) {
-                    __syncwarp();
-                    const int token = row >> it.gs;
-                    repair<D, FP8>(p, it, it.row0 + first + warp * 32, bad, mine ? row_first(p, it, token) : 0,
-                                   mine ? row_last(p, it, token) : -1, partial);
+                const uint32_t rows = __ballot_sync(0xffffffffu, bad);
+                if (rows && lane == 0) {
+                    const int id = it.at * kRowWarps + rank * 4 + warp;
+                    p.redo[id] = make_int2((int)rows, atomicExch(&s.redo, id));
                 }
             }
             if (!has_item(k + 1)) break;
@@ -1207,6 +1250,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         __syncthreads();
     tc_after_sync();
     if (warp == C::MMA_WARP) tmem_free<512, CTAS>(tmem);
+    if (s.redo >= 0 && !s.abort) compute_over<D, FP8>(p, s.redo, STREAMS * CTAS * kTile, warp, C::THREADS / 32);
 }
 
 // Joins the splits of each row: a warp per row of the sequences that were split.
@@ -1293,6 +1337,7 @@ int prompt_streams(int head_dim, int64_t most_rows) { return head_dim <= 128 && 
 // Query rows of a work item, and the CTAs that share it.
 int prompt_tile_rows(int head_dim, int streams) { return kTile * (head_dim == 256 ? 2 : streams); }
 int prompt_ctas(int head_dim) { return head_dim == 256 ? 2 : 1; }
+uint64_t prompt_redo_bytes(int64_t items) { return (uint64_t)items * kRowWarps * sizeof(int2); }
 
 // How pages fill the columns of a key tile.
 void prompt_tiling(int page_size, int head_dim, PromptParams *p) {

@@ -778,7 +778,7 @@ struct kvg_cache {
     // sequence, for the calls of the other layers
     std::vector<int32_t> open_slot, open_rows;
     std::vector<int32_t> layer_window;  // per layer: 0 = global attention, W > 0 = last W tokens
-    Scratch leaf, part_o, part_ml;
+    Scratch leaf, part_o, part_ml, redo;
     // the split-K partials are shared by every decode of the cache: a decode
     // on another stream than the previous one waits for that one's last
     // kernel (part_ev, recorded after each decode) instead of racing on them
@@ -1039,6 +1039,7 @@ extern "C" void kvg_cache_destroy(kvg_cache *c) {
     c->leaf.release();
     c->part_o.release();
     c->part_ml.release();
+    c->redo.release();
     delete c;
 }
 
@@ -2607,8 +2608,10 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
     return slots;
 }
 
-// Prefix sums of the items of a launch over p->n_units, and what the kernels divide by.
-static void prompt_items(int64_t tile_rows, int G, PromptParams *p) {
+// Prefix sums of the items of a launch over p->n_units, what the kernels divide
+// by, and the scratch in which CTAs note rows (ordered between streams as the
+// partials are).
+static kvg_status prompt_items(kvg_cache *c, int64_t tile_rows, int G, PromptParams *p) {
     p->log2_group = 0;
     while (1 << p->log2_group < G) ++p->log2_group;
     p->by_units = Divisor(p->n_units);
@@ -2620,6 +2623,9 @@ static void prompt_items(int64_t tile_rows, int G, PromptParams *p) {
         const int64_t rows = (int64_t)(p->first[i + 1] - p->first[i]) * G;
         p->item0[i + 1] = p->item0[i] + (int32_t)((rows + tile_rows - 1) / tile_rows * p->splits[i] * p->n_units);
     }
+    KVG_CUDA(c->redo.ensure(prompt_redo_bytes(p->item0[p->n_seq])));
+    p->redo = static_cast<int2 *>(c->redo.ptr);
+    return KVG_OK;
 }
 
 static kvg_status prompt_partials(kvg_cache *c, int64_t slots, PromptParams *p) {
@@ -2702,7 +2708,7 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
             }
             const int streams = prompt_streams(d.head_dim, most);
             const int64_t slots = plan_prompt(c, work, G, prompt_tile_rows(d.head_dim, streams), false, &p);
-            prompt_items(prompt_tile_rows(d.head_dim, streams), G, &p);
+            if (kvg_status r = prompt_items(c, prompt_tile_rows(d.head_dim, streams), G, &p); r != KVG_OK) return r;
             if (kvg_status r = prompt_partials(c, slots, &p); r != KVG_OK) return r;
             KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
             if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
@@ -2870,7 +2876,7 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
                     }
                 }
             }
-            prompt_items(prompt_tile_rows(d.head_dim, l->streams), G, &p);
+            if (kvg_status r = prompt_items(c, prompt_tile_rows(d.head_dim, l->streams), G, &p); r != KVG_OK) return r;
             KVG_CUDA(launch_prompt(d.head_dim, fp8, l->streams, p, c->prompt_map, st));
         }
     }
