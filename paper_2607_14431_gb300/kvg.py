@@ -294,21 +294,31 @@ def make_qkv(q, k, v, q_norm=None, k_norm=None, eps: float = 1e-6, norm_offset: 
     """kvg_qkv of tensors [tokens][heads][head_dim] or [layers][tokens][heads][head_dim] (q None: keys and
     values only), which may be slices of one buffer as long as a token's heads are adjacent.  The tensors must
     stay alive as long as the struct is used."""
+    def bf16(x):  # or its bits in an integer tensor
+        return x.dtype is k.dtype or (x.element_size() == 2 and str(x.dtype) != "torch.float16")
+
     def strides(x):
         if x is None:
             return 0, 0
-        if x.element_size() != 2 or x.dim() not in (3, 4):
+        shape, step = x.shape, x.stride()
+        if not bf16(x) or len(shape) not in (3, 4):
             raise ValueError("q, k and v are bf16 [tokens][heads][head_dim] or [layers][tokens][heads][head_dim]")
-        if (x.shape[-1] > 1 and x.stride(-1) != 1) or (x.shape[-2] > 1 and x.stride(-2) != x.shape[-1]):
+        if (shape[-1] > 1 and step[-1] != 1) or (shape[-2] > 1 and step[-2] != shape[-1]):
             raise ValueError("a token's heads must be adjacent")
-        return x.stride(-3), x.stride(0) if x.dim() == 4 else 0
+        if (shape[-1] != width or shape[-3] != tokens or (x is v and shape[-2] != heads)
+                or (layers and len(shape) == 4 and shape[0] != layers)):
+            raise ValueError("q, k and v have the same layers, tokens and head_dim, k and v the same heads")
+        return step[-3], step[0] if len(shape) == 4 else 0
 
     def ptr(x):
         return None if x is None else x.data_ptr()
 
+    if k.element_size() != 2 or str(k.dtype) == "torch.float16" or k.dim() not in (3, 4):
+        raise ValueError("q, k and v are bf16 [tokens][heads][head_dim] or [layers][tokens][heads][head_dim]")
+    layers, (tokens, heads, width) = k.shape[0] if k.dim() == 4 else 0, k.shape[-3:]
     for w in (q_norm, k_norm):
-        if w is not None and not (w.is_contiguous() and w.element_size() == 2):
-            raise ValueError("norm weights are contiguous bf16")
+        if w is not None and not (w.is_contiguous() and bf16(w) and w.shape[-1] == width):
+            raise ValueError("norm weights are contiguous bf16 [head_dim] or [layers][head_dim]")
     (qt, ql), (kt, kl), (vt, vl) = strides(q), strides(k), strides(v)
     return kvg_qkv(ptr(q), ptr(k), ptr(v), qt, kt, vt, ql, kl, vl, ptr(q_norm), ptr(k_norm), float(eps),
                    float(norm_offset), 0 if q is None else q.shape[-2], 0)
