@@ -308,7 +308,8 @@ def make_qkv(q, k, v, q_norm=None, k_norm=None, eps: float = 1e-6, norm_offset: 
         if (shape[-1] != width or shape[-3] != tokens or (x is v and shape[-2] != heads)
                 or (layers and len(shape) == 4 and shape[0] != layers)):
             raise ValueError("q, k and v have the same layers, tokens and head_dim, k and v the same heads")
-        return step[-3], step[0] if len(shape) == 4 else 0
+        # (the distance between tokens, or layers, of which there is one is never used, and may be anything)
+        return step[-3] if tokens > 1 else 0, step[0] if len(shape) == 4 and shape[0] > 1 else 0
 
     def ptr(x):
         return None if x is None else x.data_ptr()

@@ -1,5 +1,6 @@
 """make_qkv: tensors that are not what kvg_qkv describes are refused before
-their memory is read as if they were."""
+their memory is read as if they were; a stride that nothing uses does not
+matter."""
 import pytest
 import torch
 
@@ -35,3 +36,10 @@ def test_weights_of_another_head_dim_are_refused():
     qkv(k_norm=torch.ones(64, dtype=BF16))
     qkv((2, 5, 4, 64), (2, 5, 2, 64), (2, 5, 2, 64), q_norm=torch.ones(2, 64, dtype=BF16))
     qkv((1, 5, 4, 64))  # one layer, named or not
+
+
+def test_one_token_of_a_wide_buffer():
+    """Rows of 8 x 64 + 3 elements: a token's stride is no multiple of 8, but there is one token."""
+    x = torch.zeros(1, 8 * 64 + 3, dtype=BF16)[:, :512].view(1, 8, 64)
+    c = kvg.make_qkv(*x.split([4, 2, 2], dim=1))
+    assert (c.q_token, c.k_token, c.v_token) == (0, 0, 0) and (c.k - c.q, c.v - c.k) == (512, 256)
