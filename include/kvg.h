@@ -616,7 +616,8 @@ kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *
  * as by kvg_decode_attention.  Rows are grouped by their first page; a group's
  * common pages are the leading ones that all its sequences have.  Nothing has
  * to be declared, and a batch without common pages, or with so few that
- * reading them again costs less, is kvg_decode_attention.
+ * reading them again costs less, is kvg_decode_attention; a windowed layer
+ * counts what its rows' windows reach of them, each window by itself.
  * Arguments, results (within the rounding of the merge; bitwise reproducible
  * for the same batch) and errors as for kvg_decode_attention. */
 kvg_status kvg_decode_attention_shared(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, int32_t B,

@@ -779,9 +779,9 @@ __global__ void __launch_bounds__(32 * kCombineRows)
         n_own = (int)(warp_of(first + Tb - 1, T, WN) - wa) + 1;
         own = (unit + wa + (grp ? p.n_warps[0] : 0)) * G + hh;
     }
-    const int n_shared = sp.splits[b], n = n_shared + n_own;
-    const int64_t part = sp.at[b] + (int64_t)(p.qlayers[lr] * p.n_kv_heads + g) * sp.rows[b] + hh;
-    const int64_t part_step = (int64_t)sp.units * sp.rows[b];
+    const int n_shared = sp.splits[grp][b], n = n_shared + n_own;
+    const int64_t part = sp.at[grp][b] + (int64_t)((lr - (grp ? p.layer1 : 0)) * p.n_kv_heads + g) * sp.rows[grp][b] + hh;
+    const int64_t part_step = (int64_t)sp.units[grp] * sp.rows[grp][b];
     after_previous();
     let_next_start();  // a few microseconds to its end, and room for the next beside it
     auto ml_at = [&](int i) { return i < n_shared ? sp.part_ml[part + i * part_step] : p.part_ml[own + (int64_t)(i - n_shared) * G]; };

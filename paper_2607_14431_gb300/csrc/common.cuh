@@ -400,7 +400,6 @@ struct PromptParams {
     int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
     int32_t splits[kMaxBatchPerLaunch];    // key ranges that a query tile's items divide
     int64_t part0[kMaxBatchPerLaunch];     // first partial result
-    int32_t part_units;                    // layers of q x KV heads
     float *part_o;                         // [slots][D]
     float2 *part_ml;                       // [slots] (m, l)
     int2 *redo;                            // [items][8] (rows, entry before): rows to be computed over
@@ -409,15 +408,15 @@ struct PromptParams {
 };
 
 // Where the combine of a decode finds its rows' partials over the pages that
-// they share with other rows: of batch row b (of the launch), query head h of
-// layer ql and key range i < splits[b] at slot at[b] + (i * units + ql * Hkv +
-// h / G) * rows[b] + h % G.
+// they share with other rows: of the launch's window group w, batch row b, the
+// group's layer l, query head h and key range i < splits[w][b] at slot at[w][b] +
+// (i * units[w] + l * Hkv + h / G) * rows[w][b] + h % G.
 struct SharedParts {
     const float *part_o;   // [slots][D]
     const float2 *part_ml; // [slots]
-    int32_t units;         // layers of q x KV heads
-    int32_t rows[kMaxBatchPerLaunch], splits[kMaxBatchPerLaunch];
-    int64_t at[kMaxBatchPerLaunch];
+    int32_t units[kMaxWindowGroups];  // the group's layers x KV heads
+    int32_t rows[kMaxWindowGroups][kMaxBatchPerLaunch], splits[kMaxWindowGroups][kMaxBatchPerLaunch];
+    int64_t at[kMaxWindowGroups][kMaxBatchPerLaunch];
 };
 
 // -------------------------------------------------------------- launchers --

@@ -206,8 +206,8 @@ __device__ __forceinline__ int64_t q_row(const PromptParams &p, const Item &it, 
 // Slot of a row's partial result.
 __device__ __forceinline__ int64_t part_slot(const PromptParams &p, const Item &it, int split, int row) {
     const int64_t n = (int64_t)(p.first[it.b + 1] - p.first[it.b]) << it.gs;
-    const int unit = p.qlayers[it.lr] * p.n_kv_heads + it.g;
-    return p.part0[it.b] + ((int64_t)split * p.part_units + unit) * n + row;
+    const int unit = it.lr * p.n_kv_heads + it.g;
+    return p.part0[it.b] + ((int64_t)split * p.n_units + unit) * n + row;
 }
 
 __device__ __forceinline__ int search(const int32_t *first, int n, int64_t at) {

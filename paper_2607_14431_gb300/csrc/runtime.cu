@@ -2300,10 +2300,11 @@ static std::vector<WindowGroup> layer_parts(const kvg_cache *c, int32_t layer) {
 // workers).
 // page_begin / page_end: only the sequence's pages [page_begin, page_end)
 // are read (a split decode over a slot range); the defaults read them all.
-// row_begin: the first page of each batch row instead.
+// part_begin: instead, per part of layer_parts, the first page of each batch row
+// (null: 0).
 static kvg_status plan_decode(const kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B, int G, int w_max,
                               std::vector<DecodeParams> *plan, int32_t page_begin = 0,
-                              int32_t page_end = INT32_MAX, const int32_t *row_begin = nullptr) {
+                              int32_t page_end = INT32_MAX, const std::vector<const int32_t *> *part_begin = nullptr) {
     const kvg_dims &d = c->dims;
     const int TOK = decode_tile_tokens(d.head_dim, d.kv_dtype == KVG_KV_E4M3, d.page_size);
     const int tpp = (d.page_size + TOK - 1) / TOK;
@@ -2330,6 +2331,7 @@ static kvg_status plan_decode(const kvg_cache *c, int32_t layer, const int32_t *
             int64_t tiles[2] = {};
             for (size_t k = 0; k < n_parts; ++k) {
                 const WindowGroup &part = parts[i0 + k];
+                const int32_t *rows_begin = part_begin ? (*part_begin)[i0 + k] : nullptr;
                 GroupRows &rows = p.rows[k];
                 int32_t acc = 0;
                 for (int32_t i = 0; i < nb; ++i) {
@@ -2338,7 +2340,7 @@ static kvg_status plan_decode(const kvg_cache *c, int32_t layer, const int32_t *
                     int32_t pg = 0, row = 0;
                     if (part.window > 0) window_start(c, sq, part.window, &pg, &row);
                     int32_t t0 = pg * tpp + row / TOK, lo = row % TOK;
-                    const int32_t begin = row_begin ? row_begin[b0 + i] : page_begin;
+                    const int32_t begin = rows_begin ? rows_begin[b0 + i] : page_begin;
                     if (begin > 0 && (int64_t)begin * tpp > t0) {
                         t0 = begin * tpp;
                         lo = 0;
@@ -2603,7 +2605,7 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
         const int32_t s = (int32_t)std::max(1.0, std::ceil(rows[i].longest / best_len - 1e-9));
         p->splits[i] = s;
         p->part0[i] = slots;
-        if (s > 1 || always) slots += work[i].rows * p->part_units * s;
+        if (s > 1 || always) slots += work[i].rows * p->n_units * s;
     }
     return slots;
 }
@@ -2678,7 +2680,6 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
     PromptParams p{};
     prompt_params(c, q, n_q_heads, out, scale, &p);
     p.q_rows = total;
-    p.part_units = (layer < 0 ? d.n_layers : 1) * d.n_kv_heads;
     KVG_CUDA(use_partials(c, st));
     for (const WindowGroup &part : layer_parts(c, layer)) {
         prompt_layers(part, &p);
@@ -2758,10 +2759,56 @@ static std::vector<CommonPages> common_pages(const kvg_cache *c, const int32_t *
 // they fit: 4 rows on 4,096 tokens of the 12B shape (101 MB saved) 24.7 us by the
 // decode and 25.5 shared, 2 rows on 16,384 (134 MB) 44.0 and 41.9, 64 rows on 256
 // (132 MB) 31.7 and 29.5; of the 31B shape 4 on 4,096 20.2 and 22.6, 2 on 16,384
-// 38.5 and 38.2; 64 rows of the tiny shape on 4,096 (132 MB) 24.8 and 22.4.
+// 38.5 and 38.2; 64 rows of the tiny shape on 4,096 (132 MB) 24.8 and 22.4.  On a
+// windowed layer the window's part of the block counts: 32 rows with tails of 600
+// and windows of 1,100, 1,400 and 1,800 (127, 203, 305 MB) of the 12B shape 56.3,
+// 62.5, 76.8 and 59.6, 60.9, 63.7, of the 31B shape 50.2, 54.3, 60.4 and 57.5,
+// 59.6, 61.6 (long tails hide the second reading best).
 static double shared_min_bytes() {
     static const int kb = env_knob("KVG_SHARED_MIN_KB", 120000);
     return 1000.0 * kb;
+}
+
+// The common pages as the layers of one window see them: the groups whose pages
+// get launches of their own, and of each batch row where its decode begins then
+// (page; 0: its window's start), the first common slot that it attends to, and
+// its partials (SharedParts).
+struct SharedPart {
+    std::vector<const CommonPages *> groups;
+    std::vector<int32_t> begin, lo, rows, splits;
+    std::vector<int64_t> at;
+};
+
+static SharedPart shared_part(const kvg_cache *c, const WindowGroup &layers, const std::vector<CommonPages> &groups,
+                              const int32_t *seq_ids, int32_t B) {
+    const int64_t P = c->dims.page_size;
+    SharedPart part;
+    part.begin.assign(B, 0);
+    part.lo.assign(B, 0);
+    part.rows.assign(B, 0);
+    part.splits.assign(B, 0);
+    part.at.assign(B, 0);
+    double saved = 0;  // slots that are not read again: what the rows' windows reach, but for the one that reaches most
+    for (const CommonPages &g : groups) {
+        int64_t all = 0, most = 0;
+        for (int32_t b : g.rows) {
+            const int64_t end = g.pages * P;
+            if (layers.window > 0) {
+                int32_t pg, in_page;
+                window_start(c, seq_ids[b], layers.window, &pg, &in_page);
+                part.lo[b] = (int32_t)std::min(end, pg * P + in_page);
+            }
+            all += end - part.lo[b];
+            most = std::max(most, end - part.lo[b]);
+        }
+        if (all == most) continue;
+        saved += (double)(all - most);
+        part.groups.push_back(&g);
+    }
+    if (saved * 2.0 * layers.layers.size() * (double)c->page_bytes / P < shared_min_bytes()) part.groups.clear();
+    for (const CommonPages *g : part.groups)
+        for (int32_t b : g->rows) part.begin[b] = g->pages;
+    return part;
 }
 
 extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, const int32_t *seq_ids, int32_t B,
@@ -2775,14 +2822,18 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
     const kvg_dims &d = c->dims;
     const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
     const int64_t P = d.page_size;
-    const int32_t n_run = layer < 0 ? d.n_layers : 1;
     std::vector<CommonPages> groups = common_pages(c, seq_ids, B);
-    double saved = 0;
     groups.erase(std::remove_if(groups.begin(), groups.end(), [](const CommonPages &g) {
         return g.rows.size() < 2 || g.pages == 0;
     }), groups.end());
-    for (const CommonPages &g : groups) saved += (double)(g.rows.size() - 1) * g.pages * 2.0 * n_run * (double)c->page_bytes;
-    if (groups.empty() || saved < shared_min_bytes())
+    const std::vector<WindowGroup> windows = groups.empty() ? std::vector<WindowGroup>() : layer_parts(c, layer);
+    std::vector<SharedPart> parts;  // of the layers of each window
+    bool any = false;
+    for (const WindowGroup &w : windows) {
+        parts.push_back(shared_part(c, w, groups, seq_ids, B));
+        any = any || !parts.back().groups.empty();
+    }
+    if (!any)
         return decode_impl("kvg_decode_attention_shared", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0,
                            INT32_MAX, nullptr, 0);
     DeviceGuard g(c->device);
@@ -2794,103 +2845,95 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
         int64_t part_base, most;
         int streams;
     };
-    std::vector<int32_t> row_begin(B, 0);
-    std::vector<int32_t> row_rows(B, 0), row_splits(B, 0);
-    std::vector<int64_t> row_at(B, 0);
     std::vector<std::unique_ptr<Launch>> launches;
     int64_t shared_slots = 0;
-    auto plan = [&](Launch &l) {
-        PromptParams &p = l.p;
-        l.streams = prompt_streams(d.head_dim, l.most);
-        l.part_base = shared_slots;
-        shared_slots += plan_prompt(c, l.work, G, prompt_tile_rows(d.head_dim, l.streams), true, &p);
-        for (int32_t i = 0; i < p.n_seq; ++i)
-            for (int32_t k = p.first[i]; k < p.first[i + 1]; ++k) {
-                const int32_t b = p.member[k];
-                row_at[b] = l.part_base + p.part0[i] + (int64_t)(k - p.first[i]) * G;
-                row_rows[b] = (p.first[i + 1] - p.first[i]) * G;
-                row_splits[b] = p.splits[i];
-            }
-    };
-    for (const CommonPages &gr : groups) {
-        for (size_t r0 = 0; r0 < gr.rows.size();) {
-            if (launches.empty() || launches.back()->p.first[launches.back()->p.n_seq] == kMaxBatchPerLaunch) {
-                if (!launches.empty()) plan(*launches.back());
-                launches.push_back(std::make_unique<Launch>());
-                PromptParams &p = launches.back()->p;
-                prompt_params(c, q, n_q_heads, out, scale, &p);
-                p.q_rows = B;
-                p.shared = 1;
-                p.n_units = p.part_units = n_run * d.n_kv_heads;
-            }
-            Launch &l = *launches.back();
+    std::vector<const int32_t *> part_begin;
+    std::vector<int32_t> part_of(d.n_layers, 0);
+    for (size_t w = 0; w < windows.size(); ++w) {
+        SharedPart &part = parts[w];
+        for (const auto &l : windows[w].layers) part_of[l.first] = (int32_t)w;
+        part_begin.push_back(part.begin.data());
+        auto plan = [&](Launch &l) {
             PromptParams &p = l.p;
-            const int32_t i = p.n_seq++, k0 = p.first[i];
-            const int32_t n = (int32_t)std::min<size_t>(gr.rows.size() - r0, kMaxBatchPerLaunch - k0);
-            p.seq[i] = seq_ids[gr.rows[0]];
-            p.row0[i] = k0;
-            p.slot0[i] = (int32_t)(gr.pages * P - 1);
-            p.first[i + 1] = k0 + n;
-            for (int32_t k = 0; k < n; ++k) {
-                const int32_t b = gr.rows[r0 + k];
-                p.member[k0 + k] = b;
-                row_begin[b] = gr.pages;
+            l.streams = prompt_streams(d.head_dim, l.most);
+            l.part_base = shared_slots;
+            shared_slots += plan_prompt(c, l.work, G, prompt_tile_rows(d.head_dim, l.streams), true, &p);
+            for (int32_t i = 0; i < p.n_seq; ++i)
+                for (int32_t k = p.first[i]; k < p.first[i + 1]; ++k) {
+                    const int32_t b = p.member[k];
+                    part.at[b] = l.part_base + p.part0[i] + (int64_t)(k - p.first[i]) * G;
+                    part.rows[b] = (p.first[i + 1] - p.first[i]) * G;
+                    part.splits[b] = p.splits[i];
+                }
+        };
+        Launch *last = nullptr;  // of the part
+        for (const CommonPages *gr : part.groups) {
+            for (size_t r0 = 0; r0 < gr->rows.size();) {
+                if (!last || last->p.first[last->p.n_seq] == kMaxBatchPerLaunch) {
+                    if (last) plan(*last);
+                    launches.push_back(std::make_unique<Launch>());
+                    last = launches.back().get();
+                    prompt_params(c, q, n_q_heads, out, scale, &last->p);
+                    prompt_layers(windows[w], &last->p);
+                    last->p.q_rows = B;
+                    last->p.shared = 1;
+                }
+                PromptParams &p = last->p;
+                const int32_t i = p.n_seq++, k0 = p.first[i];
+                const int32_t n = (int32_t)std::min<size_t>(gr->rows.size() - r0, kMaxBatchPerLaunch - k0);
+                p.seq[i] = seq_ids[gr->rows[0]];
+                p.row0[i] = k0;
+                p.slot0[i] = (int32_t)(gr->pages * P - 1);
+                p.begin[i] = p.slot0[i] + 1;
+                p.first[i + 1] = k0 + n;
+                for (int32_t k = k0; k < k0 + n; ++k) {
+                    p.member[k] = gr->rows[r0 + k - k0];
+                    p.lo[k] = part.lo[p.member[k]];
+                    p.begin[i] = std::min(p.begin[i], p.lo[k]);
+                }
+                last->work.push_back({(int64_t)n * G, 0, p.begin[i], p.slot0[i]});
+                last->most = std::max<int64_t>(last->most, (int64_t)n * G);
+                r0 += n;
             }
-            l.work.push_back({(int64_t)n * G, 0, 0, p.slot0[i]});
-            l.most = std::max<int64_t>(l.most, (int64_t)n * G);
-            r0 += n;
         }
+        if (last) plan(*last);
     }
-    plan(*launches.back());
     // ---- the rows' own pages
     const int w_max = decode_max_warps(d.head_dim, G, fp8, d.page_size, c->n_sm);
     if (w_max <= 0) return fail(KVG_ERR_CUDA, "decode kernel cannot be made resident");
     std::vector<DecodeParams> decode;
-    if (kvg_status r = plan_decode(c, layer, seq_ids, B, G, w_max, &decode, 0, INT32_MAX, row_begin.data()); r != KVG_OK)
-        return r;
+    if (kvg_status r = plan_decode(c, layer, seq_ids, B, G, w_max, &decode, 0, INT32_MAX, &part_begin); r != KVG_OK) return r;
     const int64_t own_slots = decode_slots(decode, w_max) * G;
     KVG_CUDA(use_partials(c, st));
     KVG_CUDA(c->part_o.ensure((size_t)(own_slots + shared_slots) * d.head_dim * sizeof(float)));
     KVG_CUDA(c->part_ml.ensure((size_t)(own_slots + shared_slots) * sizeof(float2)));
     float *const part_o = static_cast<float *>(c->part_o.ptr);
     float2 *const part_ml = static_cast<float2 *>(c->part_ml.ptr);
-    SharedParts parts{};
-    parts.part_o = part_o + own_slots * d.head_dim;
-    parts.part_ml = part_ml + own_slots;
-    parts.units = n_run * d.n_kv_heads;
-    for (const WindowGroup &part : layer_parts(c, layer)) {
-        for (auto &l : launches) {
-            PromptParams &p = l->p;
-            prompt_layers(part, &p);
-            p.part_o = part_o + (own_slots + l->part_base) * d.head_dim;
-            p.part_ml = part_ml + own_slots + l->part_base;
-            for (int32_t i = 0; i < p.n_seq; ++i) {
-                p.begin[i] = part.window > 0 ? p.slot0[i] + 1 : 0;
-                for (int32_t k = p.first[i]; k < p.first[i + 1]; ++k) {
-                    p.lo[k] = 0;
-                    if (part.window > 0) {
-                        int32_t pg, in_page;
-                        window_start(c, seq_ids[p.member[k]], part.window, &pg, &in_page);
-                        p.lo[k] = (int32_t)(pg * P + in_page);
-                        p.begin[i] = std::min(p.begin[i], p.lo[k]);
-                    }
-                }
-            }
-            if (kvg_status r = prompt_items(c, prompt_tile_rows(d.head_dim, l->streams), G, &p); r != KVG_OK) return r;
-            KVG_CUDA(launch_prompt(d.head_dim, fp8, l->streams, p, c->prompt_map, st));
-        }
+    for (auto &l : launches) {
+        PromptParams &p = l->p;
+        p.part_o = part_o + (own_slots + l->part_base) * d.head_dim;
+        p.part_ml = part_ml + own_slots + l->part_base;
+        if (kvg_status r = prompt_items(c, prompt_tile_rows(d.head_dim, l->streams), G, &p); r != KVG_OK) return r;
+        KVG_CUDA(launch_prompt(d.head_dim, fp8, l->streams, p, c->prompt_map, st));
     }
+    SharedParts at{};
+    at.part_o = part_o + own_slots * d.head_dim;
+    at.part_ml = part_ml + own_slots;
     for (DecodeParams &p : decode) {
         decode_call(c, q, n_q_heads, out, scale, B, w_max, &p);
         p.part_o = part_o;
         p.part_ml = part_ml;
         KVG_CUDA(launch_decode(d.head_dim, G, fp8, p, c->pool_map, st));
-        for (int32_t i = 0; i < p.B; ++i) {
-            parts.rows[i] = row_rows[p.b0 + i];
-            parts.splits[i] = row_splits[p.b0 + i];
-            parts.at[i] = row_at[p.b0 + i];
+        for (int w = 0; w < (p.layer1 < p.n_layers_run ? 2 : 1); ++w) {
+            const SharedPart &part = parts[part_of[p.layers[w ? p.layer1 : 0]]];
+            at.units[w] = (w ? p.n_layers_run - p.layer1 : p.layer1) * d.n_kv_heads;
+            for (int32_t i = 0; i < p.B; ++i) {
+                at.rows[w][i] = part.rows[p.b0 + i];
+                at.splits[w][i] = part.splits[p.b0 + i];
+                at.at[w][i] = part.at[p.b0 + i];
+            }
         }
-        KVG_CUDA(launch_combine_shared(d.head_dim, p, parts, st));
+        KVG_CUDA(launch_combine_shared(d.head_dim, p, at, st));
     }
     return used_partials(c, st);
 }
