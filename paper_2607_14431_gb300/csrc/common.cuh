@@ -395,8 +395,8 @@ struct PromptParams {
     int32_t first[kMaxBatchPerLaunch + 1]; // prefix sums of the query rows
     int32_t row0[kMaxBatchPerLaunch];      // first packed row
     int32_t slot0[kMaxBatchPerLaunch];     // its slot (shared: the last slot of the common pages)
-    int32_t begin[kMaxBatchPerLaunch];     // no row attends to an earlier slot (with holes, or shared)
-    uint8_t holes[kMaxBatchPerLaunch];     // a page before the last is not full
+    int32_t begin[kMaxBatchPerLaunch];     // no row attends to an earlier slot (windowed, or shared)
+    int32_t solid[kMaxBatchPerLaunch];     // every slot from here on is valid (pages may end early before)
     int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
     int32_t splits[kMaxBatchPerLaunch];    // key ranges that a query tile's items divide
     int64_t part0[kMaxBatchPerLaunch];     // first partial result

@@ -181,7 +181,8 @@ __device__ __forceinline__ int first_slot(const PromptParams &p, int tile) {
 // First slot that the row at `slot` attends to.
 __device__ __forceinline__ int window_first(const PromptParams &p, int b, int slot) {
     if (p.window <= 0) return 0;
-    if (!p.holes[b]) return max(0, slot - p.window + 1);
+    const int from = max(0, slot - p.window + 1);
+    if (from >= p.solid[b]) return from;
     // pages that are not full lie in between: count valid rows back
     const int32_t *fill = p.page_fill + (int64_t)p.seq[b] * p.max_pages;
     int pg = slot / p.page_size, n = slot % p.page_size + 1, left = p.window;
@@ -239,9 +240,11 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     it.row0 = t * tile_rows;
     it.rows = min(tile_rows, n - it.row0);
     it.last_slot = row_last(p, it, (it.row0 + it.rows - 1) >> it.gs);
-    const int from = p.window <= 0               ? 0
-                     : p.shared || p.holes[b] ? p.begin[b]
-                                              : max(0, p.slot0[b] + (it.row0 >> it.gs) - p.window + 1);
+    int from = p.window <= 0 ? 0 : p.begin[b];
+    if (p.window > 0 && !p.shared) {
+        const int reach = max(0, p.slot0[b] + (it.row0 >> it.gs) - p.window + 1);
+        if (reach >= p.solid[b]) from = reach;
+    }
     int ka, kb, col;
     tile_of(p, from, ka, col);
     tile_of(p, it.last_slot, kb, col);

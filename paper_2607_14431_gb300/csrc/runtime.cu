@@ -2693,11 +2693,14 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
                 p.seq[i] = sq;
                 p.row0[i] = row0[b];
                 p.slot0[i] = c->n_slots[sq] - n_rows[b];
-                p.holes[i] = std::any_of(f.begin(), f.end() - 1, [P](int32_t x) { return x < P; });
-                p.begin[i] = 0;
+                // (the query rows' own pages are full: looked at above)
+                int64_t full = p.slot0[i] / P;  // from this page on all but the last are
+                while (p.window > 0 && full > 0 && f[full - 1] == P && full * P > p.slot0[i] - p.window + 1) --full;
+                p.begin[i] = p.solid[i] = 0;
                 if (p.window > 0) {  // what the first row's window reaches back to
                     p.begin[i] = std::max(0, p.slot0[i] - p.window + 1);
-                    if (p.holes[i]) {
+                    if (full * P > p.begin[i]) {
+                        p.solid[i] = (int32_t)(full * P);
                         int32_t pg, in_page;
                         window_start(c, sq, (int64_t)p.window + n_rows[b] - 1, &pg, &in_page);
                         p.begin[i] = pg * d.page_size + in_page;
