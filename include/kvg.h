@@ -299,9 +299,15 @@ kvg_status kvg_cache_append_batch(kvg_cache *cache, const int32_t *seq_ids, int3
  * by factor; KVG_ROPE_SCALING_YARN: a pair that turns r times over
  * original_positions keeps f_i for r >= beta_fast, has it divided by factor
  * for r <= beta_slow, and takes the blend linear in r in between ("YaRN",
- * Peng et al. 2023, whose attention factor is 0.1 ln(factor) + 1).
- * The angle is formed from a 64-bit fixed-point fraction of a turn, so it is
- * good to fp32 at every int32 position.
+ * Peng et al. 2023, whose attention factor is 0.1 ln(factor) + 1).  That is
+ * the paper's equation.  A blend linear in the pair's index i between the two
+ * bounds, as models of that name may have been made with, gives the same outer
+ * pairs and others between (head_dim 128, theta 1e4, factor 8 over 4,096,
+ * bounds 32 and 1: pair 36 turns 2.3 times as fast): these calls do not make
+ * that table.
+ * The angle is formed from a 64-bit fixed-point fraction of a turn, f_i in
+ * fp64: it is off by at most 2^-26 turns (the fraction in fp32) and
+ * |position| f_i / (2 pi) 2^-50, which is as much from position 2^26 on.
  * A block's relocation (kvg_graft with delta != 0) rotates whole heads by
  * kvg_dims.rope_theta / rope_style: it fits rows appended with rotary_dim =
  * head_dim, the same base and style, and no scaling.
@@ -601,9 +607,11 @@ kvg_status kvg_decode_attention_noalloc(kvg_cache *cache, int32_t layer, const i
  * there: o = sum softmax(scale * q . k) v per query head, its KV head being
  * h / (n_q_heads / n_kv_heads), accumulated in fp32 and rounded to bf16.
  * q, out: device bf16 [n_layers_run][T][n_q_heads][head_dim], 16-byte
- * aligned; layer as for kvg_decode_attention.  A value row that a query does
- * not attend to does not reach its output, whatever bits it holds.  Where
- * every n_rows[b] is 1 this is kvg_decode_attention.
+ * aligned; layer and group sizes as for kvg_decode_attention.  A value row
+ * that a query does not attend to does not reach its output, whatever bits it
+ * holds.  Products with an fp8 cache take q as fp16, as the decode's do: past
+ * 65,504 an element is infinite.  Where every n_rows[b] is 1 this is
+ * kvg_decode_attention.
  * Errors: KVG_ERR_ARG as for kvg_decode_attention, for more query rows than
  * slots, and where a graft left unfilled slots among a sequence's query rows. */
 kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,

@@ -348,9 +348,6 @@ inline int64_t decode_slots(const std::vector<DecodeParams> &plan, int64_t w_max
 }
 
 // ---------------------------------------------------- prompt attention --
-// Query rows of up to kMaxBatchPerLaunch sequences over layers of one window.
-// shared: "sequences" are groups of batch rows whose sequences have the same
-// first pages; a group's rows are its members, seq is one of them.
 // Division of 0 <= n < 2^31 by a number that the host knows, as a product
 // (Granlund and Montgomery, "Division by invariant integers using
 // multiplication", 1994): with l = ceil(log2 d), n / d is the product of n and
@@ -371,6 +368,9 @@ struct Divisor {
 #endif
 };
 
+// Query rows of up to kMaxBatchPerLaunch sequences over layers of one window.
+// shared: "sequences" are groups of batch rows whose sequences have the same
+// first pages; a group's rows are its members, seq is one of them.
 struct PromptParams {
     const uint8_t *pool;
     int64_t pool_pages;
@@ -514,14 +514,6 @@ cudaError_t launch_sha256_serial_part(const uint8_t *seg0, uint64_t n0, const ui
 // Whether the hashing in parts is there (the two-warp forms are not turned off).
 bool sha256_parts_ok();
 
-// Persistent decode: p.n_warps one-warp CTAs per group, then the
-// combine over every (layer, row, query head).  decode_tile_tokens() is the
-// tile height TOK of the kernel for that element type and page size (tiles per page =
-// ceil(P / TOK); the host plan and the tensor map's box must use the same
-// one as the kernel); decode_max_warps() the
-// number of co-resident warps the decode kernel can keep on the device.
-// Split-decode state -> bf16 output: out[r][d] = o / l (0 where l = 0), for
-// n_rows rows of D + 4 floats.
 // Many query rows over the same pages, on the tensor cores: p.item0[n_seq]
 // work items (query tile x KV head x layer x key range), streams query tiles of
 // 128 rows each; then the join of the rows whose keys were split.  `map`: the
@@ -534,8 +526,16 @@ void prompt_tiling(int page_size, int head_dim, PromptParams *p);
 cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
                           cudaStream_t s);
 cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t s);
+// Split-decode state -> bf16 output: out[r][d] = o / l (0 where l = 0), for
+// n_rows rows of D + 4 floats.
 cudaError_t launch_state_finish(const float *state, int64_t n_rows, int head_dim, __nv_bfloat16 *out,
                                 cudaStream_t s);
+// Persistent decode: p.n_warps one-warp CTAs per group, then the
+// combine over every (layer, row, query head).  decode_tile_tokens() is the
+// tile height TOK of the kernel for that element type and page size (tiles per page =
+// ceil(P / TOK); the host plan and the tensor map's box must use the same
+// one as the kernel); decode_max_warps() the
+// number of co-resident warps the decode kernel can keep on the device.
 cudaError_t launch_decode(int head_dim, int group, bool fp8, const DecodeParams &p, const CUtensorMap &pool_map,
                           cudaStream_t s);
 // Tensor map of a cache pool: a 2-D bf16 (or fp8) tensor of head_dim columns

@@ -21,8 +21,9 @@
 // TB/s; the rest of the time is instruction issue: some 60 a piece of a row).
 //
 // The angle: p f_i / (2 pi) turns as a 64-bit fixed-point product that wraps at
-// whole turns, so the fraction is good to 2^-33 turns at any position, where
-// an fp32 product would be off by 6e-3 radians at position 100,000.
+// whole turns.  What it is off by: the fraction in fp32 2^-26 turns, and p f_i /
+// (2 pi) times 2^-50 of the host's fp64 f_i, as much at position 2^26; an fp32
+// product would be off by 6e-3 radians (10^-3 turns) at position 100,000.
 #include <algorithm>
 
 #include "common.cuh"
