@@ -607,7 +607,8 @@ kvg_status kvg_decode_attention_noalloc(kvg_cache *cache, int32_t layer, const i
  * there: o = sum softmax(scale * q . k) v per query head, its KV head being
  * h / (n_q_heads / n_kv_heads), accumulated in fp32 and rounded to bf16.
  * q, out: device bf16 [n_layers_run][T][n_q_heads][head_dim], 16-byte
- * aligned; layer and group sizes as for kvg_decode_attention.  A value row
+ * aligned, not overlapping (rows may be computed over from q); layer and
+ * group sizes as for kvg_decode_attention.  A value row
  * that a query does not attend to does not reach its output, whatever bits it
  * holds.  Products with an fp8 cache take q as fp16, as the decode's do: past
  * 65,504 an element is infinite.  Where every n_rows[b] is 1 this is
