@@ -2829,7 +2829,12 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
     groups.erase(std::remove_if(groups.begin(), groups.end(), [](const CommonPages &g) {
         return g.rows.size() < 2 || g.pages == 0;
     }), groups.end());
-    const std::vector<WindowGroup> windows = groups.empty() ? std::vector<WindowGroup>() : layer_parts(c, layer);
+    // (what all layers would read again without windows: a batch of little is planned no further)
+    double most = 0;
+    for (const CommonPages &g : groups)
+        most += (double)(g.rows.size() - 1) * g.pages * 2.0 * (layer < 0 ? d.n_layers : 1) * (double)c->page_bytes;
+    std::vector<WindowGroup> windows;
+    if (most > 0 && most >= shared_min_bytes()) windows = layer_parts(c, layer);
     std::vector<SharedPart> parts;  // of the layers of each window
     bool any = false;
     for (const WindowGroup &w : windows) {
