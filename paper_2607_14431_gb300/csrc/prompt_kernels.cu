@@ -294,13 +294,11 @@ __device__ __forceinline__ const uint8_t *row_at(const PromptParams &p, const It
 }
 
 // A warp: attention of one query row over slots [first, last], from the last one
-// back, some slots' loads in flight together.  (Of an fp8 cache one: with four,
-// although nothing is computed over, 4,096 rows of the 31B shape on 8,192 took
-// 570 us for 562, packed prompts of 1 .. 1,501 rows 170 for 169.)
+// back, some slots' loads in flight together.
 template <int D, bool FP8>
 __device__ __forceinline__ void attend_row(const PromptParams &p, const Item &it, int row, int first, int last,
                                         float (&o)[D / 32], float &m, float &l) {
-    constexpr int N = D / 32, U = FP8 ? 1 : 4;
+    constexpr int N = D / 32, U = 4;
     const int lane = threadIdx.x & 31;
     float q[N];
     load_row<D, false>(reinterpret_cast<const uint8_t *>(p.q + q_row(p, it, row) * D), lane, q);
@@ -353,10 +351,13 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
 }
 
 // A value row that is not finite reaches, as 0 x inf, the outputs of rows of
-// its tile that do not attend to it.  So a warp whose outputs are not finite
-// notes its 32 rows, and when the CTA has done all its items (nothing waits for
-// it then, however long it takes) its warps compute those that such a row reached
-// over from the definition, each a row at a time.
+// its tile that do not attend to it.  So a softmax warp whose outputs are not
+// finite notes its 32 rows, and when the CTA has done all its items (nothing
+// waits for those warps then, however long it takes) they compute the ones that
+// such a row reached over from the definition, each a row at a time.
+
+// Of some of the CTA's warps, always the same.
+__device__ __forceinline__ void sync_warps(int warps) { asm volatile("bar.sync 1, %0;" ::"r"(32 * warps) : "memory"); }
 
 // A warp: of 32 rows from first_row on, those that a value row which is not
 // finite reached without being attended to, among the columns that their tiles
@@ -390,18 +391,29 @@ __device__ __forceinline__ uint32_t reached(const PromptParams &p, const Item &i
     return __ballot_sync(0xffffffffu, mine && redo);
 }
 
-// The CTA's warps, of the entries up to `last`.
+// The CTA's softmax warps (all of them), of the entries up to `last`: first each
+// takes entries and keeps the rows that are to be computed, then rows.  8,192
+// rows of the 31B shape on 4,096 whose queries are all NaN take 1.25 ms (finite
+// ones 0.69), with all values NaN 1.7.
 template <int D, bool FP8>
 __device__ __forceinline__ void compute_over(const PromptParams &p, int last, int tile_rows, int warp, int warps) {
     constexpr int N = D / 32;
     const int lane = threadIdx.x & 31;
-    int n = 0;  // rows so far
+    int n = 0;  // entries, then rows so far
+    for (int id = last; id >= 0; id = p.redo[id].y, ++n) {
+        if (n % warps != warp) continue;
+        const Item it = item_of(p, id / kRowWarps, tile_rows);
+        const uint32_t rows = reached<D, FP8>(p, it, it.row0 + id % kRowWarps * 32);
+        if (lane == 0) p.redo[id].x &= (int)rows;
+    }
+    sync_warps(warps);
+    n = 0;
     for (int id = last; id >= 0;) {
         const int2 entry = p.redo[id];
         const Item it = item_of(p, id / kRowWarps, tile_rows);
         const int first_row = it.row0 + id % kRowWarps * 32;
         const bool partial = p.splits[it.b] > 1 || p.shared;
-        for (uint32_t left = entry.x & reached<D, FP8>(p, it, first_row); left; left &= left - 1, ++n) {
+        for (uint32_t left = entry.x; left; left &= left - 1, ++n) {
             if (n % warps != warp) continue;
             const int row = first_row + __ffs(left) - 1, token = row >> it.gs;
             const int from = max(row_first(p, it, token), first_slot(p, it.k0));
@@ -878,6 +890,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
             if (!has_item(k + 1)) break;
         }
+        // Nothing waits for these warps any more.  (Here and not after the last barrier,
+        // where all warps would be left with the few registers of the others: packed fp8
+        // prompts of 1 .. 1,501 rows 166 us and 170, although nothing is computed over.)
+        sync_warps(C::SOFTMAX_WARPS);
+        if (s.redo >= 0 && !s.abort) compute_over<D, FP8>(p, s.redo, STREAMS * CTAS * kTile, warp, C::SOFTMAX_WARPS);
     } else {
         if constexpr (C::MORE_REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::FEWER_REGS));
         if (warp == C::LOAD_WARP) {
@@ -1253,7 +1270,6 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         __syncthreads();
     tc_after_sync();
     if (warp == C::MMA_WARP) tmem_free<512, CTAS>(tmem);
-    if (s.redo >= 0 && !s.abort) compute_over<D, FP8>(p, s.redo, STREAMS * CTAS * kTile, warp, C::THREADS / 32);
 }
 
 // Joins the splits of each row: a warp per row of the sequences that were split.
