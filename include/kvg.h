@@ -34,6 +34,11 @@
  *     caller and must stay valid until the enqueued work completes.
  *   - Threads: a store or cache must not be used from two host threads at
  *     once.  Different caches are independent.
+ *   - CUDA graphs: the attention calls may be captured, once a call of the same
+ *     sizes has grown the cache's scratch (KVG_ERR_CUDA otherwise).  What the
+ *     host knows (pages, row counts) is as it was at the capture.  Replays
+ *     share the scratch with each other and with the cache's other attention:
+ *     the caller orders them (one stream, or events).
  */
 #ifndef KVG_H
 #define KVG_H
@@ -63,6 +68,9 @@ enum { KVG_RESIDENCY_HBM = 0, KVG_RESIDENCY_PINNED_HOST = 1, KVG_RESIDENCY_CACHE
 enum { KVG_ROPE_HALF = 0, KVG_ROPE_INTERLEAVED = 1 };
 /* Scaling of the rotation frequencies for long contexts (kvg_rotary_desc). */
 enum { KVG_ROPE_SCALING_NONE = 0, KVG_ROPE_SCALING_LINEAR = 1, KVG_ROPE_SCALING_YARN = 2 };
+/* How the pairs of a head are shared out among axes (kvg_rotary_create_axes). */
+enum { KVG_ROPE_AXES_SECTIONS = 0, KVG_ROPE_AXES_TURNS = 1, KVG_ROPE_AXES_OWN = 2 };
+#define KVG_ROPE_MAX_AXES 4
 enum { KVG_GRAFT_VERIFY = 1u, KVG_GRAFT_SYNC = 2u };
 enum { KVG_SHA256_PLAIN = 0, KVG_SHA256_PAGED = 1 };
 enum { KVG_DECODE_MERGE = 1u };
@@ -324,6 +332,26 @@ typedef struct kvg_rotary kvg_rotary;
 kvg_status kvg_rotary_create(const kvg_rotary_desc *desc, kvg_rotary **out);
 void kvg_rotary_destroy(kvg_rotary *rotary);
 
+/* Rotary positions on several axes, for rows of images and video beside text
+ * (the restored context's rows keep the positions they were computed at, Sec.
+ * 3.2): a token has a position on each of n_axes axes (time, height, width) and
+ * pair i turns by position[axis of i] * f_i.  sections[a] (host array of n_axes
+ * numbers >= 0, their sum rotary_dim / 2) pairs belong to axis a:
+ *   KVG_ROPE_AXES_SECTIONS: the first sections[0] pairs to axis 0, the next
+ *     sections[1] to axis 1, and so on, f_i as for one axis;
+ *   KVG_ROPE_AXES_TURNS: pair i to axis i % n_axes while that axis has had fewer
+ *     than its sections[a] pairs, to axis 0 from then on, f_i as for one axis
+ *     (the pairs of axis a > 0 end below rotary_dim / 2);
+ *   KVG_ROPE_AXES_OWN: sections as above, a ladder of frequencies to each: pair j
+ *     of axis a has f = theta^(-j / sections[a]).
+ * Scaling applies to each pair's f.  One axis is kvg_rotary_create.
+ * A call that is given such a rotary takes positions [n_axes][T]; the position
+ * tags of the rows are those of axis 0, and a relocated graft (delta != 0),
+ * which turns whole heads by one position, does not fit them.
+ * n_axes in [1, KVG_ROPE_MAX_AXES]; KVG_ERR_ARG otherwise. */
+kvg_status kvg_rotary_create_axes(const kvg_rotary_desc *desc, const int32_t *sections, int32_t n_axes,
+                                  int32_t layout, kvg_rotary **out);
+
 /* Projections of T packed tokens (device, bf16): head h of token t (and run
  * layer l) starts at + t * x_token + l * x_layer + h * head_dim elements, so
  * slices of one projection's output are taken as they are (the x_layer are
@@ -348,7 +376,8 @@ typedef struct kvg_qkv {
  * kvg_cache_append quantizes).
  * Packed rows: sequence seq_ids[b] (host array, distinct ids, B <= 4096) gets
  * the next n_rows[b] (host array, >= 0) of the T = sum n_rows tokens at its
- * end.  A decode step is n_rows of 1 throughout.  positions: device int32 [T].
+ * end.  A decode step is n_rows of 1 throughout.  positions: device int32 [T]
+ * ([n_axes][T] for a rotary of several axes).
  * q_out: device bf16 [layers run][T][n_q_heads][head_dim]; it may be q itself
  * where that has the same layout, and overlaps nothing else.
  * rotary: null for no rotation.
@@ -617,6 +646,19 @@ kvg_status kvg_decode_attention_noalloc(kvg_cache *cache, int32_t layer, const i
  * slots, and where a graft left unfilled slots among a sequence's query rows. */
 kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
                                 int32_t B, const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
+
+/* Attention of decoder rows to an encoder's states of another length, whose
+ * keys and values are a sequence's rows (kvg_cache_append, or kvg_cache_append_qkv
+ * without queries; a stored block once for many requests, Sec. 3.3): n_rows[b]
+ * packed query rows (host array, >= 0, B <= 4096, T = sum n_rows) each attend to
+ * every valid row of sequence seq_ids[b], on a windowed layer to its last W, as
+ * kvg_decode_attention does.  A sequence may be named more than once; rows of a
+ * sequence without rows get 0.  q, out, sums, layers, group sizes, fp8 queries
+ * and values that are not attended to as for kvg_prompt_attention.  Where every
+ * n_rows[b] is 1 this is kvg_decode_attention.  Errors: as for
+ * kvg_decode_attention, and KVG_ERR_ARG for a negative n_rows[b]. */
+kvg_status kvg_cross_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                               int32_t B, const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
 
 /* kvg_decode_attention for a batch whose sequences were given the same stored
  * block (a pool-resident block grafted into each, Sec. 4.4: their page tables

@@ -197,22 +197,25 @@ struct AppendBatchParams {
 // the cache.  A launch takes up to kMaxBatchPerLaunch segments (consecutive
 // slots of a sequence) over up to kMaxQkvPages pages.
 constexpr int kMaxQkvPages = 1024;
+constexpr int kMaxAxes = KVG_ROPE_MAX_AXES;
+constexpr int kAxisShift = 62;           // of a pair's turns (below 2^62, as no frequency is above 1): its axis
+static_assert(kMaxAxes <= 1 << (64 - kAxisShift), "axes in two bits");
 struct QkvParams {
     const uint16_t *q, *k, *v;           // head h of a token at + h * head_dim
     int64_t q_token, k_token, v_token;   // elements between tokens
     int64_t q_layer, k_layer, v_layer;   // elements between run layers
     const uint16_t *q_norm, *k_norm;     // [n_layers_run][D] or null
     float eps, norm_offset;
-    const int32_t *pos;                  // [n_tokens]
+    const int32_t *pos;                  // [n_axes][n_tokens]; the first axis's are the position tags
     uint16_t *q_out;                     // [n_layers_run][n_tokens][Hq][D]
     uint8_t *pool;
     int64_t pool_pages, n_tokens, tok0;  // tokens of the call, first of this launch
     int32_t n_layers_run, layer0, n_q_heads, n_kv_heads, page_size, max_pages, max_slots, n_seg;
     int32_t *page_table, *page_fill, *positions;
     int32_t write_meta;                  // page table, fills and position tags too
-    int32_t rotary_dim, rotary_half;
+    int32_t rotary_dim, rotary_half, n_axes;
     float attention_factor, k_inv_scale, v_inv_scale;
-    uint64_t turn[kMaxHalfDim];          // 2^64 turns per position of each pair
+    uint64_t turn[kMaxHalfDim];          // 2^64 turns per position of each pair, its axis above them
     int32_t seq[kMaxBatchPerLaunch];
     int32_t first[kMaxBatchPerLaunch + 1];  // first token of each segment, from tok0
     int32_t slot0[kMaxBatchPerLaunch];
@@ -377,6 +380,7 @@ struct PromptParams {
     int32_t n_kv_heads, page_size, n_q_heads, n_layers_run;
     const int32_t *page_table, *page_fill;
     int32_t max_pages, n_seq, window, shared;
+    int32_t span;              // every row of a sequence attends to the slots [begin, slot0] (shared: [lo, slot0])
     int32_t n_units;           // run layers x KV heads
     int32_t log2_group;        // of the query heads to a KV head
     Divisor by_units, by_kv_heads, by_page, by_pages;  // n_units, n_kv_heads, page_size, pages_per_unit or units_per_page
@@ -394,8 +398,8 @@ struct PromptParams {
     int32_t seq[kMaxBatchPerLaunch];
     int32_t first[kMaxBatchPerLaunch + 1]; // prefix sums of the query rows
     int32_t row0[kMaxBatchPerLaunch];      // first packed row
-    int32_t slot0[kMaxBatchPerLaunch];     // its slot (shared: the last slot of the common pages)
-    int32_t begin[kMaxBatchPerLaunch];     // no row attends to an earlier slot (windowed, or shared)
+    int32_t slot0[kMaxBatchPerLaunch];     // its slot (span: the last slot that the rows attend to)
+    int32_t begin[kMaxBatchPerLaunch];     // no row attends to an earlier slot (windowed, or span)
     int32_t solid[kMaxBatchPerLaunch];     // every slot from here on is valid (pages may end early before)
     int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
     int32_t splits[kMaxBatchPerLaunch];    // key ranges that a query tile's items divide

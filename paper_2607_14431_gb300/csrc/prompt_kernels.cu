@@ -1,13 +1,15 @@
 // prompt_kernels.cu — attention of many query rows over the same pages of a
 // paged cache, on the 5th-generation tensor cores.
 //
-// Two calls use it: a prompt's rows over its sequence (Sec. 3.2: new queries
-// are computed on top of a restored block), and the rows of a batch over the
-// pages of a block that its sequences share.  Query row i attends to the valid
-// rows (below their page's fill) in slots [lo_i, hi_i]:
+// Three calls use it: a prompt's rows over its sequence (Sec. 3.2: new queries
+// are computed on top of a restored block), the rows of a batch over the
+// pages of a block that its sequences share, and a decoder's rows over an
+// encoder's states.  Query row i attends to the valid rows (below their page's
+// fill) in slots [lo_i, hi_i]:
 //   o_i = sum_j softmax_j(scale q_i . k_j) v_j
 // For a prompt hi_i is the row's own slot and lo_i 0 or the slot of the last
-// `window` valid rows up to it; for a shared block hi_i is its last slot.
+// `window` valid rows up to it; for a shared block hi_i is its last slot, for
+// states the last one of the sequence.
 //
 // A work item is a KV head, a tile of query rows (tokens x the group's heads,
 // so that a KV head's queries share its keys) and a range of key tiles; a CTA
@@ -193,10 +195,10 @@ __device__ __forceinline__ int window_first(const PromptParams &p, int b, int sl
     return pg * p.page_size + max(0, n - left);
 }
 __device__ __forceinline__ int row_first(const PromptParams &p, const Item &it, int tok) {
-    return p.shared ? p.lo[p.row0[it.b] + tok] : window_first(p, it.b, p.slot0[it.b] + tok);
+    return p.shared ? p.lo[p.row0[it.b] + tok] : p.span ? p.begin[it.b] : window_first(p, it.b, p.slot0[it.b] + tok);
 }
 __device__ __forceinline__ int row_last(const PromptParams &p, const Item &it, int tok) {
-    return p.slot0[it.b] + (p.shared ? 0 : tok);
+    return p.slot0[it.b] + (p.span ? 0 : tok);
 }
 // Row of q and out.
 __device__ __forceinline__ int64_t q_row(const PromptParams &p, const Item &it, int row) {
@@ -241,7 +243,7 @@ __device__ __forceinline__ Item item_of(const PromptParams &p, int at, int tile_
     it.rows = min(tile_rows, n - it.row0);
     it.last_slot = row_last(p, it, (it.row0 + it.rows - 1) >> it.gs);
     int from = p.window <= 0 ? 0 : p.begin[b];
-    if (p.window > 0 && !p.shared) {
+    if (p.window > 0 && !p.span) {
         const int reach = max(0, p.slot0[b] + (it.row0 >> it.gs) - p.window + 1);
         if (reach >= p.solid[b]) from = reach;
     }

@@ -24,6 +24,12 @@
 // whole turns.  What it is off by: the fraction in fp32 2^-26 turns, and p f_i /
 // (2 pi) times 2^-50 of the host's fp64 f_i, as much at position 2^26; an fp32
 // product would be off by 6e-3 radians (10^-3 turns) at position 100,000.
+//
+// Positions on several axes (images and video: time, height, width): pair i
+// turns by the token's position on the pair's axis.  Only the angles differ, and
+// they are made once a token, so a row costs what it does with one axis; the
+// axis is in the top two bits of the pair's turns, which leaves the loop over
+// the pairs without a second table.
 #include <algorithm>
 
 #include "common.cuh"
@@ -95,7 +101,7 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
     constexpr int RPP = kQkvThreads / LPR;   // rows that the CTA's threads hold at once
     constexpr int E = FP8 ? 1 : 2;           // bytes of a cached element
     __shared__ float2 trig[kQkvTurns][D / 2];  // of some tokens
-    __shared__ int places[2][kQkvTurns];     // positions of them and of the next
+    __shared__ int places[2][kMaxAxes][kQkvTurns];  // positions of them and of the next
     const int lr = blockIdx.y;
     const int lane = threadIdx.x % LPR, grp = threadIdx.x / LPR;
     // the CTA's tokens [t0, end) of the launch
@@ -140,14 +146,17 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
     // few pairs (with a barrier per token half of the stalls were there).
     const int pairs = R / 2;
     auto fetch = [&](int t, int buf) {
-        if (threadIdx.x < kQkvTurns && t + (int)threadIdx.x < end) places[buf][threadIdx.x] = p.pos[p.tok0 + t + threadIdx.x];
+        const int axis = threadIdx.x / kQkvTurns, k = threadIdx.x % kQkvTurns;
+        if (axis < p.n_axes && t + k < end) places[buf][axis][k] = p.pos[axis * p.n_tokens + p.tok0 + t + k];
     };
     auto turn = [&](int t, int buf) {
         __syncthreads();  // the angles before are used, the positions are there
         const int n = min(kQkvTurns, end - t) * pairs;
         for (int i = threadIdx.x; i < n; i += kQkvThreads) {
             const int k = i / pairs, pair = i - k * pairs;
-            const uint64_t frac = (uint64_t)(int64_t)places[buf][k] * p.turn[pair];  // of a turn, times 2^64
+            const uint64_t turn = p.turn[pair];
+            // of a turn, times 2^64
+            const uint64_t frac = (uint64_t)(int64_t)places[buf][turn >> kAxisShift][k] * (turn & (((uint64_t)1 << kAxisShift) - 1));
             float sv, cv;
             sincospif((float)(int32_t)(frac >> 32) * 0x1p-31f, &sv, &cv);
             trig[k][pair] = make_float2(cv * p.attention_factor, sv * p.attention_factor);
@@ -214,7 +223,7 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
                 at_slot = (p.pids[p.pid0[b] + pg - p.slot0[b] / P] * page_elems + (int64_t)row * D) * E;
             if (p.write_meta && base == 0 && lr == 0 && threadIdx.x == 0) {
                 const int64_t seq = p.seq[b];
-                p.positions[seq * p.max_slots + (int64_t)pg * P + row] = places[buf ^ 1][k];
+                p.positions[seq * p.max_slots + (int64_t)pg * P + row] = places[buf ^ 1][0][k];
                 // a page's last row of this launch knows its fill
                 if (row == P - 1 || t + 1 == seg_end) {
                     p.page_table[seq * p.max_pages + pg] = p.pids[p.pid0[b] + pg - p.slot0[b] / P];

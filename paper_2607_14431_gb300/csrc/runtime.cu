@@ -176,13 +176,23 @@ int32_t copy_chunk_bytes(const kvg_dims &d) {
 }
 
 // Growable device scratch.  Growing frees the old buffer (cudaFree waits for
-// the device), so work still using it has finished.
+// the device), so work still using it has finished.  A buffer that a captured
+// graph names is kept for its replays instead.
 struct Scratch {
     void *ptr = nullptr;
     size_t cap = 0;
-    cudaError_t ensure(size_t bytes) {
+    bool captured = false;
+    std::vector<void *> kept;
+    // capturing: the call is being captured, where nothing can be allocated
+    cudaError_t ensure(size_t bytes, bool capturing = false) {
+        if (bytes > cap && capturing) return cudaErrorStreamCaptureUnsupported;
+        captured = captured || capturing;
         if (bytes <= cap) return cudaSuccess;
-        if (ptr) cudaFree(ptr);
+        if (ptr && captured)
+            kept.push_back(ptr);
+        else if (ptr)
+            cudaFree(ptr);
+        captured = false;
         ptr = nullptr;
         cap = 0;
         size_t want = std::max(bytes, (size_t)1 << 20);
@@ -193,6 +203,8 @@ struct Scratch {
     }
     void release() {
         if (ptr) cudaFree(ptr);
+        for (void *p : kept) cudaFree(p);
+        kept.clear();
         ptr = nullptr;
         cap = 0;
     }
@@ -785,6 +797,7 @@ struct kvg_cache {
     cudaEvent_t part_ev = nullptr;
     cudaStream_t part_stream = nullptr;
     bool part_used = false;
+    bool capturing = false;  // the call at hand is being captured into a graph
     CUtensorMap pool_map;  // decode kernel's 2-D view of the pool
     CUtensorMap prompt_map;  // prompt kernel's
     // library streams and events for hashing a host-store graft's pages while
@@ -1229,11 +1242,19 @@ extern "C" kvg_status kvg_cache_append_batch(kvg_cache *c, const int32_t *seq_id
 // with the position is the fraction of a turn.
 struct kvg_rotary {
     kvg_rotary_desc desc;
-    uint64_t turn[kMaxHalfDim];
+    int32_t n_axes;
+    uint64_t turn[kMaxHalfDim];  // (and the pair's axis, from bit kAxisShift on)
 };
 
 extern "C" kvg_status kvg_rotary_create(const kvg_rotary_desc *d, kvg_rotary **out) {
     if (!d || !out) return fail(KVG_ERR_ARG, "null argument");
+    const int32_t all = d->rotary_dim / 2;
+    return kvg_rotary_create_axes(d, &all, 1, KVG_ROPE_AXES_SECTIONS, out);
+}
+
+extern "C" kvg_status kvg_rotary_create_axes(const kvg_rotary_desc *d, const int32_t *sections, int32_t n_axes,
+                                             int32_t layout, kvg_rotary **out) {
+    if (!d || !sections || !out) return fail(KVG_ERR_ARG, "null argument");
     *out = nullptr;
     if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256)
         return fail(KVG_ERR_ARG, "head_dim must be 64, 128 or 256");
@@ -1251,19 +1272,40 @@ extern "C" kvg_status kvg_rotary_create(const kvg_rotary_desc *d, kvg_rotary **o
         !(d->original_positions > 0 && std::isfinite(d->beta_fast) && std::isfinite(d->beta_slow) &&
           d->beta_fast > d->beta_slow))
         return fail(KVG_ERR_ARG, "blended scaling needs original_positions > 0 and beta_fast > beta_slow");
+    if (n_axes < 1 || n_axes > kMaxAxes) return fail(KVG_ERR_ARG, "n_axes must be in [1, %d]", kMaxAxes);
+    if (layout != KVG_ROPE_AXES_SECTIONS && layout != KVG_ROPE_AXES_TURNS && layout != KVG_ROPE_AXES_OWN)
+        return fail(KVG_ERR_ARG, "bad layout %d of the axes", layout);
+    const int n_pairs = d->rotary_dim / 2;
+    int64_t sum = 0;
+    for (int a = 0; a < n_axes; ++a) {
+        if (sections[a] < 0) return fail(KVG_ERR_ARG, "axis %d: negative section", a);
+        sum += sections[a];
+        if (layout == KVG_ROPE_AXES_TURNS && a > 0 && a + (int64_t)n_axes * (sections[a] - 1) >= n_pairs)
+            return fail(KVG_ERR_ARG, "axis %d: %d pairs in turn among %d pairs of %d axes", a, sections[a], n_pairs, n_axes);
+    }
+    if (sum != n_pairs)
+        return fail(KVG_ERR_ARG, "sections of %lld pairs, rotary_dim has %d", (long long)sum, n_pairs);
     const double two_pi = 6.283185307179586476925286766559;
     kvg_rotary *r = new (std::nothrow) kvg_rotary();
     if (!r) return fail(KVG_ERR_OOM, "rotary table");
     r->desc = *d;
-    for (int i = 0; i < d->rotary_dim / 2; ++i) {
-        double f = std::pow(d->theta, -2.0 * i / d->rotary_dim);
+    r->n_axes = n_axes;
+    for (int i = 0, a = 0, first = 0; i < n_pairs; ++i) {  // first: pair of axis a's section
+        while (layout != KVG_ROPE_AXES_TURNS && i - first == sections[a]) first += sections[a++];
+        if (layout == KVG_ROPE_AXES_TURNS) {
+            a = i % n_axes;
+            if (i / n_axes >= sections[a]) a = 0;
+        }
+        double f = layout == KVG_ROPE_AXES_OWN ? std::pow(d->theta, -(double)(i - first) / sections[a])
+                                               : std::pow(d->theta, -2.0 * i / d->rotary_dim);
         if (d->scaling == KVG_ROPE_SCALING_LINEAR) f /= d->factor;
         if (d->scaling == KVG_ROPE_SCALING_YARN) {
             const double turns = d->original_positions * f / two_pi;
             const double keep = std::min(1.0, std::max(0.0, (turns - d->beta_slow) / (d->beta_fast - d->beta_slow)));
             f = f * keep + f / d->factor * (1.0 - keep);
         }
-        r->turn[i] = (uint64_t)(f / two_pi * 18446744073709551616.0);  // f <= 1: below 2^62
+        r->turn[i] = (uint64_t)(f / two_pi * 18446744073709551616.0)  // f <= 1: below 2^62
+                     | (uint64_t)a << kAxisShift;
     }
     *out = r;
     return KVG_OK;
@@ -1349,10 +1391,12 @@ extern "C" kvg_status kvg_cache_append_qkv(kvg_cache *c, int32_t layer, const in
     p.tok0 = 0;
     p.n_seg = 0;
     p.rotary_dim = p.rotary_half = 0;
+    p.n_axes = 1;
     p.attention_factor = 1.f;
     p.k_inv_scale = p.v_inv_scale = 1.f;
     if (rotary) {
         p.rotary_dim = rotary->desc.rotary_dim;
+        p.n_axes = rotary->n_axes;
         p.rotary_half = rotary->desc.style == KVG_ROPE_HALF;
         p.attention_factor = rotary->desc.attention_factor;
         memcpy(p.turn, rotary->turn, rotary->desc.rotary_dim / 2 * sizeof p.turn[0]);
@@ -2397,13 +2441,19 @@ extern "C" kvg_status kvg_cache_set_layer_windows(kvg_cache *c, const int32_t *w
 }
 
 // The split partials are shared by every attention of the cache: a call on
-// another stream than the previous one waits for that one's last kernel.
+// another stream than the previous one waits for that one's last kernel.  A call
+// that is being captured does not (its replays are the caller's to order).
 static cudaError_t use_partials(kvg_cache *c, cudaStream_t st) {
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaError_t e = cudaStreamIsCapturing(st, &capture); e != cudaSuccess) return e;
+    c->capturing = capture != cudaStreamCaptureStatusNone;
+    if (c->capturing) return cudaSuccess;
     if (!c->part_ev)
         if (cudaError_t e = cudaEventCreateWithFlags(&c->part_ev, cudaEventDisableTiming); e != cudaSuccess) return e;
     return c->part_used && st != c->part_stream ? cudaStreamWaitEvent(st, c->part_ev, 0) : cudaSuccess;
 }
 static kvg_status used_partials(kvg_cache *c, cudaStream_t st) {
+    if (c->capturing) return KVG_OK;
     KVG_CUDA(cudaEventRecord(c->part_ev, st));
     c->part_stream = st;
     c->part_used = true;
@@ -2460,8 +2510,8 @@ static kvg_status decode_impl(const char *what, kvg_cache *c, int32_t layer, con
     if (r != KVG_OK) return r;
     const size_t slots = (size_t)decode_slots(plan, w_max);
     KVG_CUDA(use_partials(c, st));
-    KVG_CUDA(c->part_o.ensure(slots * G * d.head_dim * sizeof(float)));
-    KVG_CUDA(c->part_ml.ensure(slots * G * sizeof(float2)));
+    KVG_CUDA(c->part_o.ensure(slots * G * d.head_dim * sizeof(float), c->capturing));
+    KVG_CUDA(c->part_ml.ensure(slots * G * sizeof(float2), c->capturing));
     for (DecodeParams &p : plan) {
         decode_call(c, q, n_q_heads, out, scale, B, w_max, &p);
         p.part_o = static_cast<float *>(c->part_o.ptr);
@@ -2625,15 +2675,15 @@ static kvg_status prompt_items(kvg_cache *c, int64_t tile_rows, int G, PromptPar
         const int64_t rows = (int64_t)(p->first[i + 1] - p->first[i]) * G;
         p->item0[i + 1] = p->item0[i] + (int32_t)((rows + tile_rows - 1) / tile_rows * p->splits[i] * p->n_units);
     }
-    KVG_CUDA(c->redo.ensure(prompt_redo_bytes(p->item0[p->n_seq])));
+    KVG_CUDA(c->redo.ensure(prompt_redo_bytes(p->item0[p->n_seq]), c->capturing));
     p->redo = static_cast<int2 *>(c->redo.ptr);
     return KVG_OK;
 }
 
 static kvg_status prompt_partials(kvg_cache *c, int64_t slots, PromptParams *p) {
     if (slots) {
-        KVG_CUDA(c->part_o.ensure((size_t)slots * c->dims.head_dim * sizeof(float)));
-        KVG_CUDA(c->part_ml.ensure((size_t)slots * sizeof(float2)));
+        KVG_CUDA(c->part_o.ensure((size_t)slots * c->dims.head_dim * sizeof(float), c->capturing));
+        KVG_CUDA(c->part_ml.ensure((size_t)slots * sizeof(float2), c->capturing));
     }
     p->part_o = static_cast<float *>(c->part_o.ptr);
     p->part_ml = static_cast<float2 *>(c->part_ml.ptr);
@@ -2709,6 +2759,79 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
                 p.first[i + 1] = p.first[i] + n_rows[b];
                 most = std::max<int64_t>(most, (int64_t)n_rows[b] * G);
                 work.push_back({(int64_t)n_rows[b] * G, n_rows[b], p.begin[i], p.slot0[i]});
+            }
+            const int streams = prompt_streams(d.head_dim, most);
+            const int64_t slots = plan_prompt(c, work, G, prompt_tile_rows(d.head_dim, streams), false, &p);
+            if (kvg_status r = prompt_items(c, prompt_tile_rows(d.head_dim, streams), G, &p); r != KVG_OK) return r;
+            if (kvg_status r = prompt_partials(c, slots, &p); r != KVG_OK) return r;
+            KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
+            if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
+        }
+    }
+    return used_partials(c, st);
+}
+
+// ----------------------------------------------------------- cross attention --
+
+extern "C" kvg_status kvg_cross_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                          int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
+                                          void *stream) {
+    Trace trace_("kvg_cross_attention");
+    if (!n_rows) return fail(KVG_ERR_ARG, "kvg_cross_attention: null argument");
+    int G = 0;
+    if (kvg_status r = check_decode("kvg_cross_attention", c, layer, seq_ids, B, q, n_q_heads, out, &G); r != KVG_OK) return r;
+    const kvg_dims &d = c->dims;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    int64_t total = 0;
+    bool single = true;
+    std::vector<int32_t> order, none, row0(B);  // with rows and states, with rows alone; first packed row
+    for (int32_t b = 0; b < B; ++b) {
+        if (n_rows[b] < 0) return fail(KVG_ERR_ARG, "negative n_rows");
+        row0[b] = (int32_t)total;
+        if (n_rows[b]) (c->n_slots[seq_ids[b]] ? order : none).push_back(b);
+        total += n_rows[b];
+        if (total > 0x7fffffff / n_q_heads) return fail(KVG_ERR_ARG, "more than 2^31 - 1 query rows x heads");
+        single = single && n_rows[b] == 1;
+    }
+    if (total == 0) return KVG_OK;
+    // one row each is a decode step
+    if (single)
+        return decode_impl("kvg_cross_attention", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0, INT32_MAX,
+                           nullptr, 0);
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int32_t a, int32_t b) { return c->n_slots[seq_ids[a]] > c->n_slots[seq_ids[b]]; });
+    DeviceGuard g(c->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const size_t row_bytes = (size_t)n_q_heads * d.head_dim * sizeof(__nv_bfloat16);
+    for (int32_t b : none)
+        KVG_CUDA(cudaMemset2DAsync(static_cast<uint8_t *>(out) + row0[b] * row_bytes, total * row_bytes, 0,
+                                   n_rows[b] * row_bytes, layer < 0 ? d.n_layers : 1, st));
+    if (order.empty()) return KVG_OK;
+    PromptParams p{};
+    prompt_params(c, q, n_q_heads, out, scale, &p);
+    p.q_rows = total;
+    p.span = 1;
+    KVG_CUDA(use_partials(c, st));
+    for (const WindowGroup &part : layer_parts(c, layer)) {
+        prompt_layers(part, &p);
+        for (size_t at = 0; at < order.size();) {
+            p.n_seq = 0;
+            std::vector<PromptWork> work;
+            int64_t most = 0;
+            for (; at < order.size() && p.n_seq < kMaxBatchPerLaunch; ++at) {
+                const int32_t b = order[at], i = p.n_seq++, sq = seq_ids[b];
+                p.seq[i] = sq;
+                p.row0[i] = row0[b];
+                p.slot0[i] = c->n_slots[sq] - 1;
+                p.begin[i] = 0;
+                if (p.window > 0) {
+                    int32_t pg, in_page;
+                    window_start(c, sq, p.window, &pg, &in_page);
+                    p.begin[i] = pg * d.page_size + in_page;
+                }
+                p.first[i + 1] = p.first[i] + n_rows[b];
+                most = std::max<int64_t>(most, (int64_t)n_rows[b] * G);
+                work.push_back({(int64_t)n_rows[b] * G, 0, p.begin[i], p.slot0[i]});
             }
             const int streams = prompt_streams(d.head_dim, most);
             const int64_t slots = plan_prompt(c, work, G, prompt_tile_rows(d.head_dim, streams), false, &p);
@@ -2884,7 +3007,7 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
                     prompt_params(c, q, n_q_heads, out, scale, &last->p);
                     prompt_layers(windows[w], &last->p);
                     last->p.q_rows = B;
-                    last->p.shared = 1;
+                    last->p.shared = last->p.span = 1;
                 }
                 PromptParams &p = last->p;
                 const int32_t i = p.n_seq++, k0 = p.first[i];
@@ -2913,8 +3036,8 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
     if (kvg_status r = plan_decode(c, layer, seq_ids, B, G, w_max, &decode, 0, INT32_MAX, &part_begin); r != KVG_OK) return r;
     const int64_t own_slots = decode_slots(decode, w_max) * G;
     KVG_CUDA(use_partials(c, st));
-    KVG_CUDA(c->part_o.ensure((size_t)(own_slots + shared_slots) * d.head_dim * sizeof(float)));
-    KVG_CUDA(c->part_ml.ensure((size_t)(own_slots + shared_slots) * sizeof(float2)));
+    KVG_CUDA(c->part_o.ensure((size_t)(own_slots + shared_slots) * d.head_dim * sizeof(float), c->capturing));
+    KVG_CUDA(c->part_ml.ensure((size_t)(own_slots + shared_slots) * sizeof(float2), c->capturing));
     float *const part_o = static_cast<float *>(c->part_o.ptr);
     float2 *const part_ml = static_cast<float2 *>(c->part_ml.ptr);
     for (auto &l : launches) {

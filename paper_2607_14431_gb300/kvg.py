@@ -24,6 +24,7 @@ KVG_ERR_TIMEOUT, KVG_ERR_DEVICE_CHECK = -9, -10
 KVG_RESIDENCY_HBM, KVG_RESIDENCY_PINNED_HOST, KVG_RESIDENCY_CACHE_POOL = 0, 1, 2
 KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED = 0, 1
 KVG_ROPE_SCALING_NONE, KVG_ROPE_SCALING_LINEAR, KVG_ROPE_SCALING_YARN = 0, 1, 2
+KVG_ROPE_AXES_SECTIONS, KVG_ROPE_AXES_TURNS, KVG_ROPE_AXES_OWN = 0, 1, 2
 KVG_GRAFT_VERIFY, KVG_GRAFT_SYNC = 1, 2
 KVG_SHA256_PLAIN, KVG_SHA256_PAGED = 0, 1
 KVG_DECODE_MERGE = 1
@@ -104,6 +105,7 @@ _SIGNATURES = {
     "kvg_cache_append": ([_vp, _i32, _vp, _vp, _vp, _i32, _vp], _i32),
     "kvg_cache_append_batch": ([_vp, _vp, _i32, _vp, _vp, _vp, _vp], _i32),
     "kvg_rotary_create": ([_P(kvg_rotary_desc), _P(_vp)], _i32),
+    "kvg_rotary_create_axes": ([_P(kvg_rotary_desc), _vp, _i32, _i32, _P(_vp)], _i32),
     "kvg_rotary_destroy": ([_vp], None),
     "kvg_cache_append_qkv": ([_vp, _i32, _vp, _vp, _i32, _P(kvg_qkv), _vp, _vp, _vp, _vp], _i32),
     "kvg_cache_release": ([_vp, _i32, _vp], _i32),
@@ -118,6 +120,7 @@ _SIGNATURES = {
                                    _i32),
     "kvg_decode_state_finish": ([_vp, _i64, _i32, _vp, _vp], _i32),
     "kvg_prompt_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
+    "kvg_cross_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_decode_attention_shared": ([_vp, _i32, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_digest": ([_vp, _u64, _i32, _u64, _vp, _vp], _i32),
     "kvg_sync": ([_vp, _vp, ctypes.c_double, _P(kvg_graft_report)], _i32),
@@ -286,6 +289,13 @@ def kvg_rotary_create(desc: kvg_rotary_desc):
     return h
 
 
+def kvg_rotary_create_axes(desc: kvg_rotary_desc, sections, layout: int = KVG_ROPE_AXES_SECTIONS):
+    """sections: the pairs of each axis."""
+    h, pairs = _vp(), array("i", sections)
+    _check(lib().kvg_rotary_create_axes(ctypes.byref(desc), pairs.buffer_info()[0], len(pairs), layout, ctypes.byref(h)))
+    return h
+
+
 def kvg_rotary_destroy(rotary):
     lib().kvg_rotary_destroy(rotary)
 
@@ -427,6 +437,16 @@ def kvg_prompt_attention(cache, layer: int, seq_ids, n_rows, q_ptr: int, n_q_hea
                                       n_q_heads, out_ptr, scale, _stream(stream)))
 
 
+def kvg_cross_attention(cache, layer: int, seq_ids, n_rows, q_ptr: int, n_q_heads: int, out_ptr: int, scale: float,
+                        stream=None):
+    """Attention of n_rows[b] packed rows to every row of sequence seq_ids[b]; q and out [Lrun][sum n_rows][Hq][D]."""
+    if len(n_rows) != len(seq_ids):
+        raise ValueError("seq_ids and n_rows differ in length")
+    ids, rows = array("i", seq_ids), array("i", n_rows)
+    _check(lib().kvg_cross_attention(cache, layer, ids.buffer_info()[0], rows.buffer_info()[0], len(ids), q_ptr,
+                                     n_q_heads, out_ptr, scale, _stream(stream)))
+
+
 def kvg_decode_attention_shared(cache, layer: int, seq_ids, q_ptr: int, n_q_heads: int, out_ptr: int, scale: float,
                                 stream=None):
     """kvg_decode_attention that reads the pages which rows of the batch have in common once."""
@@ -493,15 +513,17 @@ class PoolStore(Store):
 
 
 class Rotary:
-    """Rotary positions of heads of head_dim (see kvg_rotary_desc in kvg.h)."""
+    """Rotary positions of heads of head_dim (see kvg_rotary_desc in kvg.h), on one axis, or on several with
+    `sections` pairs each (see kvg_rotary_create_axes)."""
 
     def __init__(self, head_dim: int, rotary_dim: int, theta: float = 10000.0, style: int = KVG_ROPE_HALF,
                  scaling: int = KVG_ROPE_SCALING_NONE, factor: float = 1.0, original_positions: int = 0,
-                 beta_fast: float = 32.0, beta_slow: float = 1.0, attention_factor: float = 1.0):
+                 beta_fast: float = 32.0, beta_slow: float = 1.0, attention_factor: float = 1.0, sections=None,
+                 layout: int = KVG_ROPE_AXES_SECTIONS):
         self.h = None
-        self.h = kvg_rotary_create(kvg_rotary_desc(head_dim, rotary_dim, style, scaling, float(theta), float(factor),
-                                                   float(beta_fast), float(beta_slow), original_positions,
-                                                   float(attention_factor)))
+        desc = kvg_rotary_desc(head_dim, rotary_dim, style, scaling, float(theta), float(factor), float(beta_fast),
+                               float(beta_slow), original_positions, float(attention_factor))
+        self.h = kvg_rotary_create(desc) if sections is None else kvg_rotary_create_axes(desc, sections, layout)
 
     def close(self):
         if self.h:
