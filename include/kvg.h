@@ -674,6 +674,36 @@ kvg_status kvg_cross_attention(kvg_cache *cache, int32_t layer, const int32_t *s
 kvg_status kvg_decode_attention_shared(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, int32_t B,
                                        const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
 
+/* ----------------------------------------------------------- eviction -- */
+
+/* Thins sequences to a number of their rows, so that a restored context (Sec.
+ * 4.4) takes less room: of sequence seq_ids[b]'s valid rows rows[b] are kept, the
+ * first `first`, the last `last`, and of those in between the heaviest by weight
+ * (of equal weights the earlier ones; NaN is below every weight); all of them
+ * where there are no more than rows[b].  The kept rows of every layer keep their
+ * bits, their order and their position tags, in slots 0, 1, ... without a gap.
+ * weights: device fp32 [max_seqs][max_slots], a weight for each slot, as
+ * kvg_attention_weights accumulates them; they move with the rows.
+ * dst_ids: null, or the sequences that the kept rows go to, dst_ids[b] ==
+ * seq_ids[b] in place; what another destination held is released, and its source
+ * stays as it is.  weights[dst] behind the kept rows is 0 up to where the
+ * destination's slots ended.  A destination is named once and read by no other
+ * entry; several destinations may have one source.
+ * Pages: in place the leading pages of the sequence stay its own and the others
+ * return to the free list (on `stream`, as kvg_cache_release's); another
+ * destination's own pages are used again.
+ * Pages of pool-resident blocks are never written: of a sequence that points at
+ * them, those that lie in its first rows stay shared, the others are replaced by
+ * free pages, as are the pages that a destination lacks (KVG_ERR_CAPACITY if there
+ * are too few; nothing has changed then).
+ * A windowed layer reads the last W rows that are left, so its result is what it
+ * was where `last` covers the window.  Rows that a call for layer 0 opened cannot
+ * be filled any more, and a block's digests do not fit a thinned sequence.
+ * Errors (no state change): KVG_ERR_CAPACITY, KVG_ERR_ARG (ids, rows[b] < first +
+ * last, a stream that is being captured). */
+kvg_status kvg_cache_evict(kvg_cache *cache, const int32_t *seq_ids, const int32_t *dst_ids, const int32_t *rows,
+                           int32_t B, int32_t first, int32_t last, float *weights, void *stream);
+
 /* ------------------------------------------------------------- digest -- */
 
 /* SHA-256 (FIPS 180-4) on the GPU.

@@ -411,6 +411,35 @@ struct PromptParams {
     int32_t lo[kMaxBatchPerLaunch];        // shared: first slot that it attends to
 };
 
+// ------------------------------------------------------------- eviction --
+// One sequence thinned to `kept` of its rows.
+constexpr int kMaxEvictSeqs = 128;
+struct EvictSeq {
+    int32_t src, dst;          // where the rows are, where they go (in_place: the same)
+    int32_t in_place, all;     // all: every valid row is kept
+    int32_t n_slots, gaps;     // gaps: some slots are not valid
+    int32_t kept, middle;      // rows kept, those of them chosen by weight
+    int32_t lo, hi;            // slots [lo, hi) are chosen from, the others kept
+    int32_t start;             // kept rows before this one are in their place already
+    int32_t old_slots, old_pages;  // what dst had
+    int32_t page0, n_pages;    // its new pages: EvictParams::to
+    int32_t pad;
+    int64_t list;              // its rows: EvictParams::from
+};
+struct EvictParams {
+    uint8_t *pool;
+    int64_t pool_pages;
+    int32_t *page_table, *page_fill, *positions;
+    float *weights;            // [max_seqs][max_slots]
+    int32_t *from, *to;        // scratch: pool row (within a head's plane) of each kept row; new page ids
+    int32_t max_pages, max_slots, page_size, n_kv_heads, n_planes, row_bytes, n_seq;
+    Divisor by_page;
+    DevStatus *status;
+    int32_t pid0, n_pids;      // page ids that came with the launch (0: `to` holds them already)
+    EvictSeq seq[kMaxEvictSeqs];
+    int32_t pids[kMaxPagesPerLaunch];
+};
+
 // Where the combine of a decode finds its rows' partials over the pages that
 // they share with other rows: of the launch's window group w, batch row b, the
 // group's layer l, query head h and key range i < splits[w][b] at slot at[w][b] +
@@ -552,6 +581,8 @@ cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, boo
 cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuuint64_t *dims,
                               const cuuint64_t *strides, const cuuint32_t *box);
 cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaStream_t s);
+// Selection and, with `move`, the rows; most_rows: of a sequence.
+cudaError_t launch_evict(const EvictParams &p, int64_t most_rows, bool move, int n_sm, cudaStream_t s);
 // The combine with the partials of the rows' shared pages beside the decode's.
 cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
 bool decode_supported(int head_dim, int group, bool fp8 = false);

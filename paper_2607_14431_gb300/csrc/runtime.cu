@@ -790,7 +790,7 @@ struct kvg_cache {
     // sequence, for the calls of the other layers
     std::vector<int32_t> open_slot, open_rows;
     std::vector<int32_t> layer_window;  // per layer: 0 = global attention, W > 0 = last W tokens
-    Scratch leaf, part_o, part_ml, redo;
+    Scratch leaf, part_o, part_ml, redo, evict;
     // the split-K partials are shared by every decode of the cache: a decode
     // on another stream than the previous one waits for that one's last
     // kernel (part_ev, recorded after each decode) instead of racing on them
@@ -1053,6 +1053,7 @@ extern "C" void kvg_cache_destroy(kvg_cache *c) {
     c->part_o.release();
     c->part_ml.release();
     c->redo.release();
+    c->evict.release();
     delete c;
 }
 
@@ -3065,6 +3066,201 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
             }
         }
         KVG_CUDA(launch_combine_shared(d.head_dim, p, at, st));
+    }
+    return used_partials(c, st);
+}
+
+// ---------------------------------------------------------------- eviction --
+
+extern "C" kvg_status kvg_cache_evict(kvg_cache *c, const int32_t *seq_ids, const int32_t *dst_ids, const int32_t *rows,
+                                      int32_t B, int32_t first, int32_t last, float *weights, void *stream) {
+    Trace trace_("kvg_cache_evict");
+    if (!c || !seq_ids || !rows || !weights) return fail(KVG_ERR_ARG, "kvg_cache_evict: null argument");
+    if (B <= 0 || B > 4096) return fail(KVG_ERR_ARG, "B must be in [1, 4096]");
+    if (first < 0 || last < 0) return fail(KVG_ERR_ARG, "negative first or last");
+    if (reinterpret_cast<uintptr_t>(weights) & 3) return fail(KVG_ERR_ARG, "weights must be 4-byte aligned");
+    if (!dst_ids) dst_ids = seq_ids;
+    std::vector<int32_t> reads(c->max_seqs, 0);
+    std::vector<char> written(c->max_seqs, 0);
+    for (int32_t b = 0; b < B; ++b) {
+        if (seq_ids[b] < 0 || seq_ids[b] >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", seq_ids[b]);
+        if (dst_ids[b] < 0 || dst_ids[b] >= c->max_seqs) return fail(KVG_ERR_ARG, "bad seq id %d", dst_ids[b]);
+        if (rows[b] < 0 || rows[b] < (int64_t)first + last)
+            return fail(KVG_ERR_ARG, "%d rows cannot hold the first %d and the last %d", rows[b], first, last);
+        ++reads[seq_ids[b]];
+    }
+    for (int32_t b = 0; b < B; ++b) {
+        const int32_t d = dst_ids[b];
+        if (written[d]) return fail(KVG_ERR_ARG, "sequence %d would be written twice", d);
+        written[d] = 1;
+        if (reads[d] > (seq_ids[b] == d)) return fail(KVG_ERR_ARG, "sequence %d would be read and written", d);
+    }
+    const kvg_dims &dims = c->dims;
+    const int64_t P = dims.page_size;
+    // ---- what is kept, and in which pages: nothing changes yet
+    struct Plan {
+        EvictSeq q;
+        int64_t stay;                  // leading pages that are the source's, as they are
+        int64_t fresh;                 // pages to be taken
+        std::vector<int32_t> pages;    // -1: taken
+        std::vector<int32_t> freed;    // given back
+        std::vector<int32_t> unshared; // a block's, no longer pointed at
+    };
+    std::vector<Plan> plans;
+    int64_t need = 0, n_list = 0, n_pids = 0;
+    for (int32_t b = 0; b < B; ++b) {
+        const int32_t src = seq_ids[b], dst = dst_ids[b];
+        const auto &sp = c->seq_pages[src];
+        const auto &f = c->seq_fill[src];
+        Plan plan{};
+        EvictSeq &q = plan.q;
+        q.src = src;
+        q.dst = dst;
+        q.in_place = src == dst;
+        q.n_slots = c->n_slots[src];
+        int64_t valid = 0, full = 0;  // valid rows; leading pages without a gap
+        for (size_t j = 0; j < f.size(); ++j) {
+            if (full == (int64_t)j && f[j] == P) ++full;
+            valid += f[j];
+        }
+        q.gaps = valid < q.n_slots;
+        q.kept = (int32_t)std::min<int64_t>(valid, rows[b]);
+        q.all = q.kept == valid;
+        if (q.in_place && q.all && !q.gaps) continue;  // as it is
+        q.lo = 0;
+        q.hi = q.n_slots;
+        if (!q.all) {
+            // slot of the first-th and the last-th but valid row
+            auto slot_of = [&](int64_t rank) {
+                for (size_t j = 0; j < f.size(); ++j) {
+                    if (rank < f[j]) return (int32_t)(j * P + rank);
+                    rank -= f[j];
+                }
+                return q.n_slots;
+            };
+            q.lo = slot_of(first);
+            q.hi = slot_of(valid - last);
+            q.middle = q.kept - first - last;
+        }
+        q.old_slots = c->n_slots[dst];
+        q.old_pages = (int32_t)c->seq_pages[dst].size();
+        q.n_pages = (int32_t)((q.kept + P - 1) / P);
+        // leading pages whose rows are all kept, and are in their place
+        const int64_t same = std::min<int64_t>(full, (q.all ? valid : first) / P);
+        std::vector<int32_t> own;  // of the destination's pages
+        for (int32_t pid : c->seq_pages[dst])
+            if (!c->pinned[pid]) own.push_back(pid);
+        size_t used = 0;
+        for (int64_t j = 0; j < q.n_pages; ++j) {
+            int32_t pid = -1;
+            if (j < same && (q.in_place || (c->pinned[sp[j]] && plan.stay == j))) {
+                pid = sp[j];  // (of a block where it goes to another sequence)
+                ++plan.stay;
+            } else if (q.in_place) {
+                if (!c->pinned[sp[j]]) pid = sp[j];
+            } else if (used < own.size()) {
+                pid = own[used++];
+            }
+            plan.fresh += pid < 0;
+            plan.pages.push_back(pid);
+        }
+        if (q.in_place) {
+            for (int64_t j = 0; j < (int64_t)sp.size(); ++j) {
+                if (j < q.n_pages && plan.pages[j] == sp[j]) continue;
+                (c->pinned[sp[j]] ? plan.unshared : plan.freed).push_back(sp[j]);
+            }
+        } else {
+            plan.freed.assign(own.begin() + used, own.end());
+            for (int32_t pid : c->seq_pages[dst])
+                if (c->pinned[pid]) plan.unshared.push_back(pid);
+        }
+        q.start = (int32_t)(plan.stay * P);
+        q.list = n_list;
+        q.page0 = (int32_t)n_pids;
+        n_list += q.kept;
+        n_pids += q.n_pages;
+        need += plan.fresh;
+        plans.push_back(std::move(plan));
+    }
+    if (need > (int64_t)c->free_list.size()) return fail(KVG_ERR_CAPACITY, "out of free pages");
+    if (plans.empty()) return KVG_OK;
+    DeviceGuard g(c->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    KVG_CUDA(use_partials(c, st));
+    if (c->capturing) return fail(KVG_ERR_ARG, "kvg_cache_evict cannot be captured: it changes what the host knows of the sequences");
+    KVG_CUDA(c->evict.ensure((size_t)(n_list + n_pids) * sizeof(int32_t)));
+    // ---- the host's books
+    for (Plan &plan : plans) {
+        const EvictSeq &q = plan.q;
+        const auto got = take_pages(c, plan.fresh);
+        size_t used = 0;
+        for (int32_t &pid : plan.pages)
+            if (pid < 0) pid = got[used++];
+    }
+    for (Plan &plan : plans) {
+        const EvictSeq &q = plan.q;
+        for (int32_t pid : plan.freed) c->free_list.push_back(pid);
+        for (int32_t pid : plan.unshared) --c->alias[pid];
+        if (!q.in_place)
+            for (int64_t j = 0; j < plan.stay; ++j) ++c->alias[plan.pages[j]];
+        std::vector<kvg_cache::AliasRun> runs;
+        for (kvg_cache::AliasRun r : c->seq_alias[q.src]) {
+            r.n = (int32_t)std::min<int64_t>(r.n, plan.stay - r.page0);
+            if (r.n > 0) runs.push_back(r);
+        }
+        c->seq_alias[q.dst] = std::move(runs);
+        c->seq_pages[q.dst] = plan.pages;
+        c->seq_fill[q.dst].assign(q.n_pages, (int32_t)P);
+        if (q.n_pages) c->seq_fill[q.dst].back() = (int32_t)(q.kept - (q.n_pages - 1) * P);
+        c->n_slots[q.dst] = q.kept;
+        c->open_rows[q.dst] = 0;
+    }
+    // ---- launches
+    auto p = std::make_unique<EvictParams>();
+    p->pool = c->pool;
+    p->pool_pages = c->n_pages;
+    p->page_table = c->page_table;
+    p->page_fill = c->page_fill;
+    p->positions = c->positions;
+    p->weights = weights;
+    p->status = c->status;
+    p->from = static_cast<int32_t *>(c->evict.ptr);
+    p->to = p->from + n_list;
+    p->max_pages = c->max_pages;
+    p->max_slots = c->max_slots;
+    p->page_size = dims.page_size;
+    p->n_kv_heads = dims.n_kv_heads;
+    p->n_planes = dims.n_layers * 2;
+    p->row_bytes = dims.head_dim * elem_bytes(dims);
+    p->by_page = Divisor(dims.page_size);
+    for (size_t i = 0; i < plans.size();) {
+        p->n_seq = 0;
+        p->pid0 = plans[i].q.page0;
+        p->n_pids = 0;
+        int64_t most = 0;
+        while (i < plans.size() && p->n_seq < kMaxEvictSeqs) {
+            const Plan &plan = plans[i];
+            const int32_t n = (int32_t)plan.pages.size();
+            if (n > kMaxPagesPerLaunch) {  // by themselves, ahead
+                if (p->n_seq) break;
+                for (int32_t at = 0; at < n; at += kMaxPagesPerLaunch) {
+                    IntsParams ints{};
+                    ints.dst = p->to + plan.q.page0 + at;
+                    ints.vals.n = std::min(kMaxPagesPerLaunch, n - at);
+                    std::copy_n(plan.pages.begin() + at, ints.vals.n, ints.vals.pid);
+                    KVG_CUDA(launch_write_ints(ints, st));
+                }
+            } else {
+                if (p->n_pids + n > kMaxPagesPerLaunch) break;
+                std::copy(plan.pages.begin(), plan.pages.end(), p->pids + p->n_pids);
+                p->n_pids += n;
+            }
+            p->seq[p->n_seq++] = plan.q;
+            most = std::max<int64_t>(most, plan.q.kept - plan.q.start);
+            ++i;
+            if (n > kMaxPagesPerLaunch) break;
+        }
+        KVG_CUDA(launch_evict(*p, most, most > 0, c->n_sm, st));
     }
     return used_partials(c, st);
 }

@@ -122,6 +122,7 @@ _SIGNATURES = {
     "kvg_prompt_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_cross_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_decode_attention_shared": ([_vp, _i32, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
+    "kvg_cache_evict": ([_vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp], _i32),
     "kvg_digest": ([_vp, _u64, _i32, _u64, _vp, _vp], _i32),
     "kvg_sync": ([_vp, _vp, ctypes.c_double, _P(kvg_graft_report)], _i32),
     "kvg_selftest_bounded_wait": ([_vp, _u64, _vp], _i32),
@@ -453,6 +454,16 @@ def kvg_decode_attention_shared(cache, layer: int, seq_ids, q_ptr: int, n_q_head
     ids = array("i", seq_ids)
     _check(lib().kvg_decode_attention_shared(cache, layer, ids.buffer_info()[0], len(ids), q_ptr, n_q_heads, out_ptr,
                                              scale, _stream(stream)))
+
+
+def kvg_cache_evict(cache, seq_ids, rows, first: int, last: int, weights_ptr: int, dst_ids=None, stream=None):
+    """Keeps rows[b] rows of each sequence, in place or (dst_ids) as another sequence; weights [max_seqs][max_slots]."""
+    if len(rows) != len(seq_ids) or (dst_ids is not None and len(dst_ids) != len(seq_ids)):
+        raise ValueError("seq_ids, rows and dst_ids differ in length")
+    ids, n = array("i", seq_ids), array("i", rows)
+    to = None if dst_ids is None else array("i", dst_ids)
+    _check(lib().kvg_cache_evict(cache, ids.buffer_info()[0], None if to is None else to.buffer_info()[0],
+                                 n.buffer_info()[0], len(ids), first, last, weights_ptr, _stream(stream)))
 
 
 def kvg_digest(ptr: int, n: int, mode: int, page_bytes: int, out_ptr: int, stream=None):

@@ -44,3 +44,13 @@ def test_null_arguments(lib):
 def test_the_binding_asks_for_a_count_per_sequence():
     with pytest.raises(ValueError):
         kvg.kvg_cross_attention(None, 0, [0], [1, 2], 0, 4, 0, 1.0)
+
+
+def test_eviction_refusals(lib):
+    ids = (ctypes.c_int32 * 1)(0)
+    w = ctypes.c_void_p(16)
+    assert lib.kvg_cache_evict(None, ids, None, ids, 1, 0, 0, w, None) == kvg.KVG_ERR_ARG
+    with pytest.raises(ValueError):
+        kvg.kvg_cache_evict(None, [0], [1, 2], 0, 0, 16)
+    with pytest.raises(ValueError):
+        kvg.kvg_cache_evict(None, [0], [1], 0, 0, 16, dst_ids=[1, 2])
