@@ -676,6 +676,24 @@ kvg_status kvg_decode_attention_shared(kvg_cache *cache, int32_t layer, const in
 
 /* ----------------------------------------------------------- eviction -- */
 
+/* kvg_prompt_attention that also accumulates what weight each cached row
+ * received (by which kvg_cache_evict thins a context): of sequence seq_ids[b]
+ * with n_rows[b] > 0 query rows, and each of its slots s,
+ *     weights[seq][s] = decay * weights[seq][s] + sum softmax(scale * q . k_s)
+ * summed over the layers run, the query heads and the query rows that attend to
+ * s: 0 for a slot that none attends to (before a window, after a row, unfilled).
+ * decay 0 leaves the call's own weights (what was there is not read), 1 adds
+ * them up; a sequence's slots sum to n_layers_run * n_q_heads * n_rows[b] a call.
+ * weights: device fp32 [max_seqs][max_slots], owned by the caller, who zeroes a
+ * sequence's row when the sequence starts anew.  They are formed and summed in
+ * fp32, in an order that depends on the call's arguments alone.
+ * Other arguments, out and errors as for kvg_prompt_attention (out within the
+ * rounding of the sums), plus KVG_ERR_ARG for repeated ids of sequences with rows,
+ * a decay that is not finite, and weights that are null or misaligned. */
+kvg_status kvg_attention_weights(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                 int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
+                                 float *weights, float decay, void *stream);
+
 /* Thins sequences to a number of their rows, so that a restored context (Sec.
  * 4.4) takes less room: of sequence seq_ids[b]'s valid rows rows[b] are kept, the
  * first `first`, the last `last`, and of those in between the heaviest by weight

@@ -350,7 +350,6 @@ inline int64_t decode_slots(const std::vector<DecodeParams> &plan, int64_t w_max
     return most;
 }
 
-// ---------------------------------------------------- prompt attention --
 // Division of 0 <= n < 2^31 by a number that the host knows, as a product
 // (Granlund and Montgomery, "Division by invariant integers using
 // multiplication", 1994): with l = ceil(log2 d), n / d is the product of n and
@@ -371,6 +370,32 @@ struct Divisor {
 #endif
 };
 
+// A decode that also gives what weight each row received: its scores (scale *
+// log2(e) * q.k) of run layer lr, batch row b and query head h are at
+// scores[at[b] + (lr * n_q_heads + h) * n[b] + slot].
+struct ScoreParams {
+    float *scores;
+    float *part_lx;            // beside part_ml: the sum of the weights before their rounding
+    float2 *ml;                // [n_layers_run][B][n_q_heads]: the merged maximum, one over the sum
+    int64_t at[kMaxBatchPerLaunch];
+    int32_t n[kMaxBatchPerLaunch];  // slots
+};
+// The weights of a launch's rows, added up: weights[seq][slot] becomes decay times
+// itself (0: it is not read) plus the sum over the run layers and query heads.
+struct AccumulateParams {
+    const float *scores;
+    const float2 *ml;
+    const int32_t *page_fill;
+    float *weights;            // [max_seqs][max_slots]
+    int32_t max_pages, max_slots, page_size, n_q_heads, n_layers_run, layer1, B;
+    float decay;
+    Divisor by_page;
+    int64_t at[kMaxBatchPerLaunch];
+    int32_t n[kMaxBatchPerLaunch], seq[kMaxBatchPerLaunch];
+    int32_t first[kMaxWindowGroups][kMaxBatchPerLaunch];  // first slot that was attended to
+};
+
+// ---------------------------------------------------- prompt attention --
 // Query rows of up to kMaxBatchPerLaunch sequences over layers of one window.
 // shared: "sequences" are groups of batch rows whose sequences have the same
 // first pages; a group's rows are its members, seq is one of them.
@@ -406,9 +431,29 @@ struct PromptParams {
     int64_t part0[kMaxBatchPerLaunch];     // first partial result
     float *part_o;                         // [slots][D]
     float2 *part_ml;                       // [slots] (m, l)
+    float *part_lse, *row_lse;             // kvg_attention_weights: [slots], [units][rows]: log2 of sum 2^score
     int2 *redo;                            // [items][8] (rows, entry before): rows to be computed over
     int32_t member[kMaxBatchPerLaunch];    // shared: batch row of each member
     int32_t lo[kMaxBatchPerLaunch];        // shared: first slot that it attends to
+};
+
+// What weight the rows of a prompt's launch gave each cached row: of its layers
+// [lr0, lr0 + n_lr).  A work item is a KV head, two key tiles and a range of query
+// tiles; its sums go to sums[sum0[b] + ((split * n_lr * Hkv + unit) * 2 * blocks[b]
+// + tile - tile0[b]) * 128 + column].
+struct WeighParams {
+    PromptParams p;
+    float *sums;
+    float *weights;                        // [max_seqs][max_slots]
+    int32_t max_slots, lr0, n_lr;
+    float decay;
+    int32_t met[kMaxBatchPerLaunch];       // the sequence's weights have been decayed by this call
+    int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
+    int32_t splits[kMaxBatchPerLaunch];    // ranges of query tiles
+    int32_t tile0[kMaxBatchPerLaunch];     // first key tile
+    int32_t blocks[kMaxBatchPerLaunch];    // pairs of key tiles
+    int32_t gaps[kMaxBatchPerLaunch];      // slots that hold no row
+    int64_t sum0[kMaxBatchPerLaunch];
 };
 
 // ------------------------------------------------------------- eviction --
@@ -559,6 +604,19 @@ void prompt_tiling(int page_size, int head_dim, PromptParams *p);
 cudaError_t launch_prompt(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
                           cudaStream_t s);
 cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t s);
+// The same, each row's p.row_lse (or p.part_lse) written too; then the sums of the
+// weights by key tile, and from them the weights.  q_map: the queries (16-bit
+// elements, fp16 copies for an fp8 cache) as boxes of 64 columns x the group's heads
+// x weigh_tokens() tokens.
+cudaError_t launch_prompt_lse(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
+                              cudaStream_t s);
+int weigh_tokens(int head_dim, int group);
+cudaError_t make_query_tensor_map(CUtensorMap *out, const void *q, int head_dim, int n_q_heads, int group, int tokens,
+                                  uint64_t rows);
+cudaError_t launch_query_halves(const void *q, int64_t n, void *out, int n_sm, cudaStream_t s);
+cudaError_t launch_weigh(int head_dim, bool fp8, const WeighParams &p, const CUtensorMap &k_map, const CUtensorMap &q_map,
+                         cudaStream_t s);
+cudaError_t launch_weigh_sum(const WeighParams &p, cudaStream_t s);
 // Split-decode state -> bf16 output: out[r][d] = o / l (0 where l = 0), for
 // n_rows rows of D + 4 floats.
 cudaError_t launch_state_finish(const float *state, int64_t n_rows, int head_dim, __nv_bfloat16 *out,
@@ -585,6 +643,14 @@ cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaSt
 cudaError_t launch_evict(const EvictParams &p, int64_t most_rows, bool move, int n_sm, cudaStream_t s);
 // The combine with the partials of the rows' shared pages beside the decode's.
 cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
+// Threads of a combine block over `cols` columns of a head.
+int combine_threads(int cols, const DecodeParams &p);
+// The decode with its scores, the combine beside it and the rows' weights.
+// decode_scores_max_warps(): as decode_max_warps(), of that decode kernel.
+int decode_scores_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);
+cudaError_t launch_decode_scores(int head_dim, int group, bool fp8, const DecodeParams &p, const ScoreParams &sp,
+                                 const CUtensorMap &pool_map, int n_sm, cudaStream_t s);
+cudaError_t launch_accumulate(const AccumulateParams &p, cudaStream_t s);
 bool decode_supported(int head_dim, int group, bool fp8 = false);
 int decode_tile_tokens(int head_dim, bool fp8, int page_size);
 int decode_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);
@@ -733,6 +799,16 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, i
         "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
             "r"(smem_addr(dst)),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_addr(bar))
+        : "memory");
+}
+
+// 3-D tensor copy (TMA) of one box, as above.
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z,
+                                            uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
+            "r"(smem_addr(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
         : "memory");
 }
 

@@ -790,7 +790,7 @@ struct kvg_cache {
     // sequence, for the calls of the other layers
     std::vector<int32_t> open_slot, open_rows;
     std::vector<int32_t> layer_window;  // per layer: 0 = global attention, W > 0 = last W tokens
-    Scratch leaf, part_o, part_ml, redo, evict;
+    Scratch leaf, part_o, part_ml, redo, evict, scores, halves;
     // the split-K partials are shared by every decode of the cache: a decode
     // on another stream than the previous one waits for that one's last
     // kernel (part_ev, recorded after each decode) instead of racing on them
@@ -1054,6 +1054,8 @@ extern "C" void kvg_cache_destroy(kvg_cache *c) {
     c->part_ml.release();
     c->redo.release();
     c->evict.release();
+    c->scores.release();
+    c->halves.release();
     delete c;
 }
 
@@ -2691,19 +2693,16 @@ static kvg_status prompt_partials(kvg_cache *c, int64_t slots, PromptParams *p) 
     return KVG_OK;
 }
 
-extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
-                                           int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
-                                           void *stream) {
-    Trace trace_("kvg_prompt_attention");
-    if (!n_rows) return fail(KVG_ERR_ARG, "kvg_prompt_attention: null argument");
-    int G = 0;
-    if (kvg_status r = check_decode("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, &G); r != KVG_OK) return r;
-    const kvg_dims &d = c->dims;
-    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
-    const int64_t P = d.page_size;
+// The packed rows of a prompt's call.
+struct PromptRows {
     int64_t total = 0;
     bool single = true;
-    std::vector<int32_t> order, row0(B);  // sequences with rows; first packed row
+    std::vector<int32_t> order, row0;  // sequences with rows; first packed row of each sequence
+};
+static kvg_status prompt_rows(const kvg_cache *c, const int32_t *seq_ids, const int32_t *n_rows, int32_t B,
+                              int32_t n_q_heads, PromptRows *out) {
+    const int64_t P = c->dims.page_size;
+    out->row0.resize(B);
     for (int32_t b = 0; b < B; ++b) {
         const int32_t sq = seq_ids[b];
         if (n_rows[b] < 0 || n_rows[b] > c->n_slots[sq])
@@ -2712,26 +2711,98 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
         const auto &f = c->seq_fill[sq];
         for (int64_t pg = (c->n_slots[sq] - n_rows[b]) / P; n_rows[b] && pg + 1 < (int64_t)f.size(); ++pg)
             if (f[pg] < P) return fail(KVG_ERR_ARG, "seq %d: unfilled slots among its last %d", sq, n_rows[b]);
-        row0[b] = (int32_t)total;
-        if (n_rows[b]) order.push_back(b);
-        total += n_rows[b];
-        if (total > 0x7fffffff / n_q_heads) return fail(KVG_ERR_ARG, "more than 2^31 - 1 query rows x heads");
-        single = single && n_rows[b] == 1;
+        out->row0[b] = (int32_t)out->total;
+        if (n_rows[b]) out->order.push_back(b);
+        out->total += n_rows[b];
+        if (out->total > 0x7fffffff / n_q_heads) return fail(KVG_ERR_ARG, "more than 2^31 - 1 query rows x heads");
+        out->single = out->single && n_rows[b] == 1;
     }
-    if (total == 0) return KVG_OK;
-    // prompts of one token are a decode step
-    if (single)
-        return decode_impl("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0, INT32_MAX,
-                           nullptr, 0);
+    return KVG_OK;
+}
+
+// What a prompt's launch needs to accumulate its rows' weights.
+struct PromptWeights {
+    float *weights;
+    float decay;
+    CUtensorMap q_map;         // the queries, in the products' 16 bits
+    std::vector<char> met;     // per sequence: decayed by this call
+};
+
+// Sums of weights that are kept at a time: of as many layers as fit.
+constexpr uint64_t kWeighBytes = 512ull << 20;
+
+// The work items of a launch's weights: pairs of key tiles, with the query tiles
+// split as plan_prompt splits keys.  An item costs its query tiles and kItemTiles
+// more.  Returns the floats of a layer's sums.
+static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
+    constexpr double kItemTiles = 4.0;
+    const PromptParams &p = w->p;
+    const int per = kPromptCols / p.unit;
+    auto tile_of = [&](int64_t slot) {
+        const int64_t pg = slot / p.page_size;
+        return (p.pages_per_unit ? pg / p.pages_per_unit : pg * p.units_per_page + slot % p.page_size / p.unit) / per;
+    };
+    const double at_once = (double)c->n_sm / prompt_ctas(c->dims.head_dim);
+    struct Row {
+        double longest, mean;
+    };
+    std::vector<Row> rows;
+    double longest = 1.0;
+    for (int32_t i = 0; i < p.n_seq; ++i) {
+        const int64_t n = p.first[i + 1] - p.first[i], end = p.slot0[i] + n;
+        w->tile0[i] = (int32_t)tile_of(p.begin[i]);
+        w->blocks[i] = (int32_t)((tile_of(end - 1) - w->tile0[i]) / 2 + 1);
+        const double all = std::ceil((double)n * G / kPromptCols);
+        // of `end - begin` slots those before the prompt are attended to by all of its
+        // rows, those in it by half of them; a window's rows reach each slot
+        const double before = p.slot0[i] - p.begin[i], in = (double)n;
+        double top = all, mean = (before * all + in * all / 2) / (before + in);
+        if (p.window > 0) {
+            top = std::min(top, std::ceil((double)p.window * G / kPromptCols) + 2);
+            mean = std::min(mean, top);
+        }
+        rows.push_back({std::max(top, 1.0), std::max(mean, 1.0)});
+        longest = std::max(longest, rows.back().longest);
+    }
+    double best = INFINITY, best_len = longest;
+    for (double len = longest; len >= 1.0; len *= 0.84) {
+        double items = 0, total = 0, top = 0;
+        for (int32_t i = 0; i < p.n_seq; ++i) {
+            const double s = std::max(1.0, std::ceil(rows[i].longest / len - 1e-9));
+            items += s * w->blocks[i] * p.n_units;
+            total += w->blocks[i] * p.n_units * (rows[i].mean + s * kItemTiles);
+            top = std::max(top, rows[i].longest / s + kItemTiles);
+        }
+        const double est = std::max(top, std::ceil(items / at_once) * (total / items));
+        if (est < best) {
+            best = est;
+            best_len = len;
+        }
+    }
+    int64_t floats = 0;
+    for (int32_t i = 0; i < p.n_seq; ++i) {
+        w->splits[i] = (int32_t)std::max(1.0, std::ceil(rows[i].longest / best_len - 1e-9));
+        w->sum0[i] = floats;  // (of one layer: scaled by the layers of a launch)
+        floats += (int64_t)w->splits[i] * p.n_kv_heads * 2 * w->blocks[i] * kPromptCols;
+    }
+    return floats;
+}
+
+// Prompt attention of the packed rows, with pw also their weights.
+static kvg_status prompt_impl(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                              const PromptRows &rows, const void *q, int32_t n_q_heads, void *out, float scale, int G,
+                              cudaStream_t st, PromptWeights *pw = nullptr) {
+    const kvg_dims &d = c->dims;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    const int64_t P = d.page_size;
+    const std::vector<int32_t> &row0 = rows.row0;
+    std::vector<int32_t> order = rows.order;
     // the longest work items first, so that the SMs end close together
     std::stable_sort(order.begin(), order.end(),
                      [&](int32_t a, int32_t b) { return c->n_slots[seq_ids[a]] > c->n_slots[seq_ids[b]]; });
-    DeviceGuard g(c->device);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
     PromptParams p{};
     prompt_params(c, q, n_q_heads, out, scale, &p);
-    p.q_rows = total;
-    KVG_CUDA(use_partials(c, st));
+    p.q_rows = rows.total;
     for (const WindowGroup &part : layer_parts(c, layer)) {
         prompt_layers(part, &p);
         for (size_t at = 0; at < order.size();) {
@@ -2765,10 +2836,70 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
             const int64_t slots = plan_prompt(c, work, G, prompt_tile_rows(d.head_dim, streams), false, &p);
             if (kvg_status r = prompt_items(c, prompt_tile_rows(d.head_dim, streams), G, &p); r != KVG_OK) return r;
             if (kvg_status r = prompt_partials(c, slots, &p); r != KVG_OK) return r;
-            KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
-            if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
+            if (!pw) {
+                KVG_CUDA(launch_prompt(d.head_dim, fp8, streams, p, c->prompt_map, st));
+                if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
+                continue;
+            }
+            auto w = std::make_unique<WeighParams>();
+            w->p = p;
+            w->weights = pw->weights;
+            w->max_slots = c->max_slots;
+            w->decay = pw->decay;
+            for (int32_t i = 0; i < p.n_seq; ++i) {
+                const int32_t sq = p.seq[i];
+                int64_t valid = 0;
+                for (int32_t f : c->seq_fill[sq]) valid += f;
+                w->gaps[i] = (int32_t)(c->n_slots[sq] - valid);
+                w->met[i] = pw->met[sq];
+                pw->met[sq] = 1;
+            }
+            const int64_t floats = plan_weigh(c, G, w.get());
+            const int64_t at_a_time =
+                std::max<int64_t>(1, std::min<int64_t>(p.n_layers_run, (int64_t)(kWeighBytes / sizeof(float)) / floats));
+            const int64_t n_lse = (int64_t)p.n_units * rows.total * G;
+            KVG_CUDA(c->scores.ensure((size_t)(n_lse + slots + floats * at_a_time) * sizeof(float), c->capturing));
+            w->p.row_lse = static_cast<float *>(c->scores.ptr);
+            w->p.part_lse = w->p.row_lse + n_lse;
+            w->sums = w->p.part_lse + slots;
+            KVG_CUDA(launch_prompt_lse(d.head_dim, fp8, streams, w->p, c->prompt_map, st));
+            if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, w->p, st));
+            const std::vector<int64_t> sum0(w->sum0, w->sum0 + p.n_seq);
+            for (int32_t l = 0; l < p.n_layers_run; l += w->n_lr) {
+                w->lr0 = l;
+                w->n_lr = (int32_t)std::min<int64_t>(at_a_time, p.n_layers_run - l);
+                w->item0[0] = 0;
+                for (int32_t i = 0; i < p.n_seq; ++i) {
+                    w->sum0[i] = sum0[i] * w->n_lr;
+                    w->item0[i + 1] = w->item0[i] + w->blocks[i] * w->splits[i] * w->n_lr * p.n_kv_heads;
+                    if (l) w->met[i] = 1;
+                }
+                KVG_CUDA(launch_weigh(d.head_dim, fp8, *w, c->prompt_map, pw->q_map, st));
+                KVG_CUDA(launch_weigh_sum(*w, st));
+            }
         }
     }
+    return KVG_OK;
+}
+
+extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                           int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
+                                           void *stream) {
+    Trace trace_("kvg_prompt_attention");
+    if (!n_rows) return fail(KVG_ERR_ARG, "kvg_prompt_attention: null argument");
+    int G = 0;
+    if (kvg_status r = check_decode("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, &G); r != KVG_OK) return r;
+    PromptRows rows;
+    if (kvg_status r = prompt_rows(c, seq_ids, n_rows, B, n_q_heads, &rows); r != KVG_OK) return r;
+    if (rows.total == 0) return KVG_OK;
+    // prompts of one token are a decode step
+    if (rows.single)
+        return decode_impl("kvg_prompt_attention", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0, INT32_MAX,
+                           nullptr, 0);
+    DeviceGuard g(c->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    KVG_CUDA(use_partials(c, st));
+    if (kvg_status r = prompt_impl(c, layer, seq_ids, n_rows, rows, q, n_q_heads, out, scale, G, st); r != KVG_OK) return r;
     return used_partials(c, st);
 }
 
@@ -3067,6 +3198,129 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
         }
         KVG_CUDA(launch_combine_shared(d.head_dim, p, at, st));
     }
+    return used_partials(c, st);
+}
+
+// ------------------------------------------------------- attention's weights --
+
+// Scores of a decode step that are kept at a time: all layers' of all rows, else
+// a layer's of as many rows as fit.
+constexpr uint64_t kScoreBytes = 512ull << 20;
+
+// A decode step whose rows' weights are accumulated: one launch after the other
+// leaves its scores, and what their sum needs, in the cache's scratch.
+static kvg_status decode_weights(kvg_cache *c, int32_t layer, const std::vector<int32_t> &seqs, const void *q,
+                                 int32_t n_q_heads, void *out, float scale, int G, float *weights, float decay,
+                                 cudaStream_t st) {
+    const kvg_dims &d = c->dims;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    const int32_t B = (int32_t)seqs.size();
+    const int w_max = decode_scores_max_warps(d.head_dim, G, fp8, d.page_size, c->n_sm);
+    if (w_max <= 0) return fail(KVG_ERR_CUDA, "decode kernel cannot be made resident");
+    uint64_t slots = 0;
+    for (int32_t sq : seqs) slots += c->n_slots[sq];
+    const bool together = layer >= 0 || slots * d.n_layers * n_q_heads * sizeof(float) <= kScoreBytes;
+    const int TOK = decode_tile_tokens(d.head_dim, fp8, d.page_size), tpp = (d.page_size + TOK - 1) / TOK;
+    const int32_t l0 = together ? layer : 0, l1 = together ? layer + 1 : d.n_layers;
+    for (int32_t b0 = 0, b1; b0 < B; b0 = b1) {
+        slots = 0;
+        for (b1 = b0; b1 < B; ++b1) {
+            slots += c->n_slots[seqs[b1]];
+            if (b1 > b0 && slots * n_q_heads * sizeof(float) > kScoreBytes) break;
+        }
+        for (int32_t l = l0; l < l1; ++l) {
+            std::vector<DecodeParams> plan;
+            if (kvg_status r = plan_decode(c, l, seqs.data() + b0, b1 - b0, G, w_max, &plan); r != KVG_OK) return r;
+            const size_t part = (size_t)decode_slots(plan, w_max);
+            KVG_CUDA(c->part_o.ensure(part * G * d.head_dim * sizeof(float), c->capturing));
+            KVG_CUDA(c->part_ml.ensure(part * G * sizeof(float2), c->capturing));
+            std::vector<char> met(B, 0);  // rows whose weights this layer, or these layers, have reached
+            for (DecodeParams &p : plan) {
+                decode_call(c, q, n_q_heads, out, scale, B, w_max, &p);
+                p.b0 += b0;
+                if (!together) {
+                    p.q += (int64_t)l * B * n_q_heads * d.head_dim;
+                    p.out += (int64_t)l * B * n_q_heads * d.head_dim;
+                }
+                p.part_o = static_cast<float *>(c->part_o.ptr);
+                p.part_ml = static_cast<float2 *>(c->part_ml.ptr);
+                ScoreParams sp{};
+                AccumulateParams a{};
+                int64_t n = 0;
+                for (int32_t i = 0; i < p.B; ++i) {
+                    sp.at[i] = a.at[i] = n;
+                    sp.n[i] = a.n[i] = c->n_slots[p.seq[i]];
+                    a.seq[i] = p.seq[i];
+                    n += (int64_t)sp.n[i] * n_q_heads * p.n_layers_run;
+                    for (int w = 0; w < kMaxWindowGroups; ++w) {
+                        const int32_t t0 = p.rows[w].tile0[i];
+                        a.first[w][i] = t0 / tpp * d.page_size + t0 % tpp * TOK + p.rows[w].lo[i];
+                    }
+                }
+                const size_t n_ml = (size_t)p.n_layers_run * p.B * n_q_heads;
+                KVG_CUDA(c->scores.ensure(n_ml * sizeof(float2) + (part * G + n) * sizeof(float), c->capturing));
+                sp.ml = static_cast<float2 *>(c->scores.ptr);
+                sp.part_lx = reinterpret_cast<float *>(sp.ml + n_ml);
+                sp.scores = sp.part_lx + part * G;
+                KVG_CUDA(launch_decode_scores(d.head_dim, G, fp8, p, sp, c->pool_map, c->n_sm, st));
+                a.scores = sp.scores;
+                a.ml = sp.ml;
+                a.page_fill = c->page_fill;
+                a.weights = weights;
+                a.max_pages = c->max_pages;
+                a.max_slots = c->max_slots;
+                a.page_size = d.page_size;
+                a.n_q_heads = n_q_heads;
+                a.n_layers_run = p.n_layers_run;
+                a.layer1 = p.layer1;
+                a.B = p.B;
+                a.by_page = Divisor(d.page_size);
+                a.decay = l > l0 || met[p.b0] ? 1.f : decay;
+                met[p.b0] = 1;
+                KVG_CUDA(launch_accumulate(a, st));
+            }
+        }
+    }
+    return KVG_OK;
+}
+
+extern "C" kvg_status kvg_attention_weights(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
+                                            int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
+                                            float *weights, float decay, void *stream) {
+    Trace trace_("kvg_attention_weights");
+    if (!n_rows || !weights) return fail(KVG_ERR_ARG, "kvg_attention_weights: null argument");
+    int G = 0;
+    if (kvg_status r = check_decode("kvg_attention_weights", c, layer, seq_ids, B, q, n_q_heads, out, &G); r != KVG_OK) return r;
+    if (reinterpret_cast<uintptr_t>(weights) & 3) return fail(KVG_ERR_ARG, "weights must be 4-byte aligned");
+    if (!std::isfinite(decay)) return fail(KVG_ERR_ARG, "decay must be finite");
+    PromptRows rows;
+    if (kvg_status r = prompt_rows(c, seq_ids, n_rows, B, n_q_heads, &rows); r != KVG_OK) return r;
+    std::vector<char> seen(c->max_seqs, 0);
+    for (int32_t b : rows.order) {
+        if (seen[seq_ids[b]]) return fail(KVG_ERR_ARG, "seq id %d repeated", seq_ids[b]);
+        seen[seq_ids[b]] = 1;
+    }
+    if (rows.total == 0) return KVG_OK;
+    DeviceGuard g(c->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    KVG_CUDA(use_partials(c, st));
+    if (rows.total == (int64_t)rows.order.size()) {  // a row each: a decode step
+        std::vector<int32_t> seqs;
+        for (int32_t b : rows.order) seqs.push_back(seq_ids[b]);
+        if (kvg_status r = decode_weights(c, layer, seqs, q, n_q_heads, out, scale, G, weights, decay, st); r != KVG_OK) return r;
+        return used_partials(c, st);
+    }
+    PromptWeights pw{weights, decay, {}, std::vector<char>(c->max_seqs, 0)};
+    const int64_t n_layers = layer < 0 ? c->dims.n_layers : 1, elems = n_layers * rows.total * n_q_heads * c->dims.head_dim;
+    const void *halves = q;
+    if (c->dims.kv_dtype == KVG_KV_E4M3) {  // products with the codes take them as fp16
+        KVG_CUDA(c->halves.ensure((size_t)elems * 2, c->capturing));
+        KVG_CUDA(launch_query_halves(q, elems, c->halves.ptr, c->n_sm, st));
+        halves = c->halves.ptr;
+    }
+    KVG_CUDA(make_query_tensor_map(&pw.q_map, halves, c->dims.head_dim, n_q_heads, G, weigh_tokens(c->dims.head_dim, G),
+                                   (uint64_t)(n_layers * rows.total)));
+    if (kvg_status r = prompt_impl(c, layer, seq_ids, n_rows, rows, q, n_q_heads, out, scale, G, st, &pw); r != KVG_OK) return r;
     return used_partials(c, st);
 }
 

@@ -122,6 +122,8 @@ _SIGNATURES = {
     "kvg_prompt_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_cross_attention": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
     "kvg_decode_attention_shared": ([_vp, _i32, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp], _i32),
+    "kvg_attention_weights": ([_vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp, ctypes.c_float, _vp],
+                              _i32),
     "kvg_cache_evict": ([_vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp], _i32),
     "kvg_digest": ([_vp, _u64, _i32, _u64, _vp, _vp], _i32),
     "kvg_sync": ([_vp, _vp, ctypes.c_double, _P(kvg_graft_report)], _i32),
@@ -454,6 +456,17 @@ def kvg_decode_attention_shared(cache, layer: int, seq_ids, q_ptr: int, n_q_head
     ids = array("i", seq_ids)
     _check(lib().kvg_decode_attention_shared(cache, layer, ids.buffer_info()[0], len(ids), q_ptr, n_q_heads, out_ptr,
                                              scale, _stream(stream)))
+
+
+def kvg_attention_weights(cache, layer: int, seq_ids, n_rows, q_ptr: int, n_q_heads: int, out_ptr: int, scale: float,
+                          weights_ptr: int, decay: float = 1.0, stream=None):
+    """kvg_prompt_attention that also accumulates the weight each cached row received: weights [max_seqs][max_slots]
+    fp32 becomes decay * weights + the sum over layers, heads and query rows."""
+    if len(n_rows) != len(seq_ids):
+        raise ValueError("seq_ids and n_rows differ in length")
+    ids, rows = array("i", seq_ids), array("i", n_rows)
+    _check(lib().kvg_attention_weights(cache, layer, ids.buffer_info()[0], rows.buffer_info()[0], len(ids), q_ptr,
+                                       n_q_heads, out_ptr, scale, weights_ptr, decay, _stream(stream)))
 
 
 def kvg_cache_evict(cache, seq_ids, rows, first: int, last: int, weights_ptr: int, dst_ids=None, stream=None):

@@ -54,3 +54,10 @@ def test_eviction_refusals(lib):
         kvg.kvg_cache_evict(None, [0], [1, 2], 0, 0, 16)
     with pytest.raises(ValueError):
         kvg.kvg_cache_evict(None, [0], [1], 0, 0, 16, dst_ids=[1, 2])
+
+
+def test_weights_refusals(lib):
+    f = ctypes.c_float(1.0)
+    assert lib.kvg_attention_weights(None, 0, None, None, 1, None, 4, None, f, None, f, None) == kvg.KVG_ERR_ARG
+    with pytest.raises(ValueError):
+        kvg.kvg_attention_weights(None, 0, [0], [1, 2], 0, 4, 0, 1.0, 16, 0.0)
