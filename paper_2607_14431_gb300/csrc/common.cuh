@@ -471,7 +471,11 @@ struct EvictSeq {
     int32_t pad;
     int64_t list;              // its rows: EvictParams::from
 };
-struct EvictParams {
+// SEQS, PAGES: what a launch holds (a launch copies its parameters: one sequence in
+// the larger's 13 KB took 3 us more of the host).
+template <int SEQS, int PAGES>
+struct EvictParamsOf {
+    static constexpr int kSeqs = SEQS, kPages = PAGES;
     uint8_t *pool;
     int64_t pool_pages;
     int32_t *page_table, *page_fill, *positions;
@@ -481,9 +485,11 @@ struct EvictParams {
     Divisor by_page;
     DevStatus *status;
     int32_t pid0, n_pids;      // page ids that came with the launch (0: `to` holds them already)
-    EvictSeq seq[kMaxEvictSeqs];
-    int32_t pids[kMaxPagesPerLaunch];
+    EvictSeq seq[SEQS];
+    int32_t pids[PAGES];
 };
+using EvictParams = EvictParamsOf<kMaxEvictSeqs, kMaxPagesPerLaunch>;
+using FewEvictParams = EvictParamsOf<4, 256>;
 
 // Where the combine of a decode finds its rows' partials over the pages that
 // they share with other rows: of the launch's window group w, batch row b, the
@@ -639,8 +645,9 @@ cudaError_t make_pool_tensor_map(CUtensorMap *out, void *pool, int head_dim, boo
 cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuuint64_t *dims,
                               const cuuint64_t *strides, const cuuint32_t *box);
 cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaStream_t s);
-// Selection and, with `move`, the rows; most_rows: of a sequence.
-cudaError_t launch_evict(const EvictParams &p, int64_t most_rows, bool move, int n_sm, cudaStream_t s);
+// Selection and the rows; most_slots, most_rows: of a sequence (no rows to move: selection alone).
+template <class Params>
+cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows, int n_sm, cudaStream_t s);
 // The combine with the partials of the rows' shared pages beside the decode's.
 cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
 // Threads of a combine block over `cols` columns of a head.

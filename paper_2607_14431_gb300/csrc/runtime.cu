@@ -3326,6 +3326,69 @@ extern "C" kvg_status kvg_attention_weights(kvg_cache *c, int32_t layer, const i
 
 // ---------------------------------------------------------------- eviction --
 
+struct EvictPlan {
+    EvictSeq q;
+    int64_t stay;                  // leading pages that are the source's, as they are
+    int64_t fresh;                 // pages to be taken
+    std::vector<int32_t> pages;    // -1: taken
+    std::vector<int32_t> freed;    // given back
+    std::vector<int32_t> unshared; // a block's, no longer pointed at
+};
+
+template <class Params>
+static cudaError_t run_evict(kvg_cache *c, const std::vector<EvictPlan> &plans, float *weights, int64_t n_list,
+                             cudaStream_t st) {
+    const kvg_dims &dims = c->dims;
+    Params p;  // every field is set, of the arrays what the launch reads
+    p.pool = c->pool;
+    p.pool_pages = c->n_pages;
+    p.page_table = c->page_table;
+    p.page_fill = c->page_fill;
+    p.positions = c->positions;
+    p.weights = weights;
+    p.status = c->status;
+    p.from = static_cast<int32_t *>(c->evict.ptr);
+    p.to = p.from + n_list;
+    p.max_pages = c->max_pages;
+    p.max_slots = c->max_slots;
+    p.page_size = dims.page_size;
+    p.n_kv_heads = dims.n_kv_heads;
+    p.n_planes = dims.n_layers * 2;
+    p.row_bytes = dims.head_dim * elem_bytes(dims);
+    p.by_page = Divisor(dims.page_size);
+    for (size_t i = 0; i < plans.size();) {
+        p.n_seq = 0;
+        p.pid0 = plans[i].q.page0;
+        p.n_pids = 0;
+        int64_t rows = 0, slots = 0;
+        while (i < plans.size() && p.n_seq < Params::kSeqs) {
+            const EvictPlan &plan = plans[i];
+            const int32_t n = (int32_t)plan.pages.size();
+            if (n > Params::kPages) {  // by themselves, ahead
+                if (p.n_seq) break;
+                for (int32_t at = 0; at < n; at += kMaxPagesPerLaunch) {
+                    IntsParams ints{};
+                    ints.dst = p.to + plan.q.page0 + at;
+                    ints.vals.n = std::min(kMaxPagesPerLaunch, n - at);
+                    std::copy_n(plan.pages.begin() + at, ints.vals.n, ints.vals.pid);
+                    if (cudaError_t e = launch_write_ints(ints, st); e != cudaSuccess) return e;
+                }
+            } else {
+                if (p.n_pids + n > Params::kPages) break;
+                std::copy(plan.pages.begin(), plan.pages.end(), p.pids + p.n_pids);
+                p.n_pids += n;
+            }
+            p.seq[p.n_seq++] = plan.q;
+            rows = std::max<int64_t>(rows, plan.q.kept - plan.q.start);
+            slots = std::max<int64_t>(slots, plan.q.n_slots);
+            ++i;
+            if (n > Params::kPages) break;
+        }
+        if (cudaError_t e = launch_evict(p, slots, rows, c->n_sm, st); e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
 extern "C" kvg_status kvg_cache_evict(kvg_cache *c, const int32_t *seq_ids, const int32_t *dst_ids, const int32_t *rows,
                                       int32_t B, int32_t first, int32_t last, float *weights, void *stream) {
     Trace trace_("kvg_cache_evict");
@@ -3352,21 +3415,13 @@ extern "C" kvg_status kvg_cache_evict(kvg_cache *c, const int32_t *seq_ids, cons
     const kvg_dims &dims = c->dims;
     const int64_t P = dims.page_size;
     // ---- what is kept, and in which pages: nothing changes yet
-    struct Plan {
-        EvictSeq q;
-        int64_t stay;                  // leading pages that are the source's, as they are
-        int64_t fresh;                 // pages to be taken
-        std::vector<int32_t> pages;    // -1: taken
-        std::vector<int32_t> freed;    // given back
-        std::vector<int32_t> unshared; // a block's, no longer pointed at
-    };
-    std::vector<Plan> plans;
+    std::vector<EvictPlan> plans;
     int64_t need = 0, n_list = 0, n_pids = 0;
     for (int32_t b = 0; b < B; ++b) {
         const int32_t src = seq_ids[b], dst = dst_ids[b];
         const auto &sp = c->seq_pages[src];
         const auto &f = c->seq_fill[src];
-        Plan plan{};
+        EvictPlan plan{};
         EvictSeq &q = plan.q;
         q.src = src;
         q.dst = dst;
@@ -3444,14 +3499,14 @@ extern "C" kvg_status kvg_cache_evict(kvg_cache *c, const int32_t *seq_ids, cons
     if (c->capturing) return fail(KVG_ERR_ARG, "kvg_cache_evict cannot be captured: it changes what the host knows of the sequences");
     KVG_CUDA(c->evict.ensure((size_t)(n_list + n_pids) * sizeof(int32_t)));
     // ---- the host's books
-    for (Plan &plan : plans) {
+    for (EvictPlan &plan : plans) {
         const EvictSeq &q = plan.q;
         const auto got = take_pages(c, plan.fresh);
         size_t used = 0;
         for (int32_t &pid : plan.pages)
             if (pid < 0) pid = got[used++];
     }
-    for (Plan &plan : plans) {
+    for (EvictPlan &plan : plans) {
         const EvictSeq &q = plan.q;
         for (int32_t pid : plan.freed) c->free_list.push_back(pid);
         for (int32_t pid : plan.unshared) --c->alias[pid];
@@ -3469,53 +3524,10 @@ extern "C" kvg_status kvg_cache_evict(kvg_cache *c, const int32_t *seq_ids, cons
         c->n_slots[q.dst] = q.kept;
         c->open_rows[q.dst] = 0;
     }
-    // ---- launches
-    auto p = std::make_unique<EvictParams>();
-    p->pool = c->pool;
-    p->pool_pages = c->n_pages;
-    p->page_table = c->page_table;
-    p->page_fill = c->page_fill;
-    p->positions = c->positions;
-    p->weights = weights;
-    p->status = c->status;
-    p->from = static_cast<int32_t *>(c->evict.ptr);
-    p->to = p->from + n_list;
-    p->max_pages = c->max_pages;
-    p->max_slots = c->max_slots;
-    p->page_size = dims.page_size;
-    p->n_kv_heads = dims.n_kv_heads;
-    p->n_planes = dims.n_layers * 2;
-    p->row_bytes = dims.head_dim * elem_bytes(dims);
-    p->by_page = Divisor(dims.page_size);
-    for (size_t i = 0; i < plans.size();) {
-        p->n_seq = 0;
-        p->pid0 = plans[i].q.page0;
-        p->n_pids = 0;
-        int64_t most = 0;
-        while (i < plans.size() && p->n_seq < kMaxEvictSeqs) {
-            const Plan &plan = plans[i];
-            const int32_t n = (int32_t)plan.pages.size();
-            if (n > kMaxPagesPerLaunch) {  // by themselves, ahead
-                if (p->n_seq) break;
-                for (int32_t at = 0; at < n; at += kMaxPagesPerLaunch) {
-                    IntsParams ints{};
-                    ints.dst = p->to + plan.q.page0 + at;
-                    ints.vals.n = std::min(kMaxPagesPerLaunch, n - at);
-                    std::copy_n(plan.pages.begin() + at, ints.vals.n, ints.vals.pid);
-                    KVG_CUDA(launch_write_ints(ints, st));
-                }
-            } else {
-                if (p->n_pids + n > kMaxPagesPerLaunch) break;
-                std::copy(plan.pages.begin(), plan.pages.end(), p->pids + p->n_pids);
-                p->n_pids += n;
-            }
-            p->seq[p->n_seq++] = plan.q;
-            most = std::max<int64_t>(most, plan.q.kept - plan.q.start);
-            ++i;
-            if (n > kMaxPagesPerLaunch) break;
-        }
-        KVG_CUDA(launch_evict(*p, most, most > 0, c->n_sm, st));
-    }
+    const cudaError_t e = plans.size() <= FewEvictParams::kSeqs && n_pids <= FewEvictParams::kPages
+                              ? run_evict<FewEvictParams>(c, plans, weights, n_list, st)
+                              : run_evict<EvictParams>(c, plans, weights, n_list, st);
+    KVG_CUDA(e);
     return used_partials(c, st);
 }
 

@@ -150,6 +150,21 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// What CTA `cta` of the cluster has at the place of p in its shared memory.
+__device__ __forceinline__ int load_of_cta(const int *p, int cta) {
+    int v;
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.b32 %0, [a];\n\t}"
+        : "=r"(v)
+        : "r"(smem_addr(p)), "r"(cta)
+        : "memory");
+    return v;
+}
 // All threads of the cluster's CTAs; orders their shared-memory accesses.
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
