@@ -376,22 +376,17 @@ struct Divisor {
 struct ScoreParams {
     float *scores;
     float *part_lx;            // beside part_ml: the sum of the weights before their rounding
-    float2 *ml;                // [n_layers_run][B][n_q_heads]: the merged maximum, one over the sum
     int64_t at[kMaxBatchPerLaunch];
     int32_t n[kMaxBatchPerLaunch];  // slots
 };
 // The weights of a launch's rows, added up: weights[seq][slot] becomes decay times
 // itself (0: it is not read) plus the sum over the run layers and query heads.
 struct AccumulateParams {
-    const float *scores;
-    const float2 *ml;
-    const int32_t *page_fill;
+    ScoreParams scores;
     float *weights;            // [max_seqs][max_slots]
-    int32_t max_pages, max_slots, page_size, n_q_heads, n_layers_run, layer1, B;
+    int32_t max_slots, most_slots;  // most_slots: of a row
     float decay;
     Divisor by_page;
-    int64_t at[kMaxBatchPerLaunch];
-    int32_t n[kMaxBatchPerLaunch], seq[kMaxBatchPerLaunch];
     int32_t first[kMaxWindowGroups][kMaxBatchPerLaunch];  // first slot that was attended to
 };
 
@@ -652,12 +647,11 @@ cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows,
 cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
 // Threads of a combine block over `cols` columns of a head.
 int combine_threads(int cols, const DecodeParams &p);
-// The decode with its scores, the combine beside it and the rows' weights.
+// The decode with its scores; then the combine and, beside it, the rows' weights.
 // decode_scores_max_warps(): as decode_max_warps(), of that decode kernel.
 int decode_scores_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);
-cudaError_t launch_decode_scores(int head_dim, int group, bool fp8, const DecodeParams &p, const ScoreParams &sp,
-                                 const CUtensorMap &pool_map, int n_sm, cudaStream_t s);
-cudaError_t launch_accumulate(const AccumulateParams &p, cudaStream_t s);
+cudaError_t launch_decode_weights(int head_dim, int group, bool fp8, const DecodeParams &p, const AccumulateParams &a,
+                                  const CUtensorMap &pool_map, int n_sm, cudaStream_t s);
 bool decode_supported(int head_dim, int group, bool fp8 = false);
 int decode_tile_tokens(int head_dim, bool fp8, int page_size);
 int decode_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);

@@ -240,7 +240,7 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two_codes) {
 }
 
 // SCORES: each row's scores are stored as well, and the sum of the weights as they
-// are before their rounding to 16 bits: what the weights' accumulation divides by.
+// are before their rounding to 16 bits, which the accumulated weights are divided by.
 struct NoScores {};
 template <int D, int G, bool FP8, int TOK_, bool SCORES>
 __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
@@ -690,35 +690,43 @@ __device__ __forceinline__ int64_t warp_of(int64_t t, int64_t T, int64_t W) { re
 struct Merged {
     float4 o;    // sum of o_w 2^(m_w - M) (threads of the first group)
     float M, L;  // maximum, sum of l_w 2^(m_w - M)
-    float LX;    // the same sum of part_lx (EXACT)
 };
 constexpr int kCombineMaxThreads = 512;
 
-template <int D, int COLS, bool EXACT = false>
-__device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, int col0, int b, int lr,
-                                                 const float *part_lx = nullptr) {
-    constexpr int LANES = COLS / 4;
-    __shared__ float4 sum_o[kCombineMaxThreads];
-    __shared__ float sum_l[kCombineMaxThreads / LANES];
-    __shared__ float sum_lx[EXACT ? kCombineMaxThreads / LANES : 1];
-    const int G = p.n_q_heads / p.n_kv_heads;
-    const int g = h / G, hh = h - g * G;
-    const int d4 = threadIdx.x % LANES, r = threadIdx.x / LANES, R = blockDim.x / LANES;
-    Merged res{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f, 0.f};
+// The partials of one (layer, row, KV head): n of them, from `slot` on.
+struct UnitPartials {
+    int64_t slot;
+    int n;
+};
+__device__ __forceinline__ UnitPartials unit_partials(const DecodeParams &p, int g, int b, int lr) {
     const int grp = lr >= p.layer1;
     const int32_t *pref = p.rows[grp].pref_tiles;
     const int64_t Tb = pref[b + 1] - pref[b];
-    if (Tb <= 0) {  // the whole block
-        after_previous();
-        return res;
-    }
+    if (Tb <= 0) return {0, 0};
     const int64_t T = p.group_tiles(grp), W = p.n_warps[grp];
     const int64_t unit = ((int64_t)lr * p.B + b) * p.n_kv_heads + g;
     const int64_t first = (int64_t)g * Tb +  // of the group's tiles
                           (int64_t)p.n_kv_heads * ((int64_t)(lr - (grp ? p.layer1 : 0)) * pref[p.B] + pref[b]);
     const int64_t wa = warp_of(first, T, W);
-    const int n = (int)(warp_of(first + Tb - 1, T, W) - wa) + 1;
-    const int64_t slot = unit + wa + (grp ? p.n_warps[0] : 0);
+    return {unit + wa + (grp ? p.n_warps[0] : 0), (int)(warp_of(first + Tb - 1, T, W) - wa) + 1};
+}
+
+template <int D, int COLS>
+__device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, int col0, int b, int lr) {
+    constexpr int LANES = COLS / 4;
+    __shared__ float4 sum_o[kCombineMaxThreads];
+    __shared__ float sum_l[kCombineMaxThreads / LANES];
+    const int G = p.n_q_heads / p.n_kv_heads;
+    const int g = h / G, hh = h - g * G;
+    const int d4 = threadIdx.x % LANES, r = threadIdx.x / LANES, R = blockDim.x / LANES;
+    Merged res{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+    const UnitPartials of = unit_partials(p, g, b, lr);
+    if (of.n == 0) {  // the whole block
+        after_previous();
+        return res;
+    }
+    const int n = of.n;
+    const int64_t slot = of.slot;
     const float2 *ml = p.part_ml + slot * G + hh;
     const float4 *po = reinterpret_cast<const float4 *>(p.part_o + (slot * G + hh) * D + col0) + d4;
     const int64_t step = (int64_t)G * (D / 4);  // float4 between consecutive partials
@@ -733,14 +741,12 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
         for (int i0 = r; i0 < n; i0 += U * R) {
             float4 v[U];
             float2 x[U];
-            float lx[EXACT ? U : 1];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * R;
                 if (i < n) {
                     x[u] = ml[(int64_t)i * G];
                     v[u] = po[i * step];
-                    if constexpr (EXACT) lx[u] = part_lx[(slot + i) * G + hh];
                 }
             }
 #pragma unroll
@@ -748,7 +754,6 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
                 if (i0 + u * R < n && x[u].x != -INFINITY) {
                     const float sc = exp2f(x[u].x - M);
                     res.L = __fmaf_rn(x[u].y, sc, res.L);
-                    if constexpr (EXACT) res.LX = __fmaf_rn(lx[u], sc, res.LX);
                     res.o.x = __fmaf_rn(v[u].x, sc, res.o.x);
                     res.o.y = __fmaf_rn(v[u].y, sc, res.o.y);
                     res.o.z = __fmaf_rn(v[u].z, sc, res.o.z);
@@ -760,8 +765,6 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     if (R > 1) {
         sum_o[threadIdx.x] = res.o;
         if (d4 == 0) sum_l[r] = res.L;
-        if constexpr (EXACT)
-            if (d4 == 0) sum_lx[r] = res.LX;
         __syncthreads();
         if (r == 0) {
             for (int k = 1; k < R; ++k) {
@@ -771,7 +774,6 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
                 res.o.z += v.z;
                 res.o.w += v.w;
                 res.L += sum_l[k];
-                if constexpr (EXACT) res.LX += sum_lx[k];
             }
         }
     }

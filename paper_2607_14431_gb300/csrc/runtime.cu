@@ -3244,40 +3244,28 @@ static kvg_status decode_weights(kvg_cache *c, int32_t layer, const std::vector<
                 }
                 p.part_o = static_cast<float *>(c->part_o.ptr);
                 p.part_ml = static_cast<float2 *>(c->part_ml.ptr);
-                ScoreParams sp{};
-                AccumulateParams a{};
+                AccumulateParams a;  // every field is set, of the arrays what the launch reads
                 int64_t n = 0;
+                a.most_slots = 0;
                 for (int32_t i = 0; i < p.B; ++i) {
-                    sp.at[i] = a.at[i] = n;
-                    sp.n[i] = a.n[i] = c->n_slots[p.seq[i]];
-                    a.seq[i] = p.seq[i];
-                    n += (int64_t)sp.n[i] * n_q_heads * p.n_layers_run;
+                    a.scores.at[i] = n;
+                    a.scores.n[i] = c->n_slots[p.seq[i]];
+                    a.most_slots = std::max(a.most_slots, a.scores.n[i]);
+                    n += (int64_t)a.scores.n[i] * n_q_heads * p.n_layers_run;
                     for (int w = 0; w < kMaxWindowGroups; ++w) {
                         const int32_t t0 = p.rows[w].tile0[i];
                         a.first[w][i] = t0 / tpp * d.page_size + t0 % tpp * TOK + p.rows[w].lo[i];
                     }
                 }
-                const size_t n_ml = (size_t)p.n_layers_run * p.B * n_q_heads;
-                KVG_CUDA(c->scores.ensure(n_ml * sizeof(float2) + (part * G + n) * sizeof(float), c->capturing));
-                sp.ml = static_cast<float2 *>(c->scores.ptr);
-                sp.part_lx = reinterpret_cast<float *>(sp.ml + n_ml);
-                sp.scores = sp.part_lx + part * G;
-                KVG_CUDA(launch_decode_scores(d.head_dim, G, fp8, p, sp, c->pool_map, c->n_sm, st));
-                a.scores = sp.scores;
-                a.ml = sp.ml;
-                a.page_fill = c->page_fill;
+                KVG_CUDA(c->scores.ensure((part * G + n) * sizeof(float), c->capturing));
+                a.scores.part_lx = static_cast<float *>(c->scores.ptr);
+                a.scores.scores = a.scores.part_lx + part * G;
                 a.weights = weights;
-                a.max_pages = c->max_pages;
                 a.max_slots = c->max_slots;
-                a.page_size = d.page_size;
-                a.n_q_heads = n_q_heads;
-                a.n_layers_run = p.n_layers_run;
-                a.layer1 = p.layer1;
-                a.B = p.B;
                 a.by_page = Divisor(d.page_size);
                 a.decay = l > l0 || met[p.b0] ? 1.f : decay;
                 met[p.b0] = 1;
-                KVG_CUDA(launch_accumulate(a, st));
+                KVG_CUDA(launch_decode_weights(d.head_dim, G, fp8, p, a, c->pool_map, c->n_sm, st));
             }
         }
     }
