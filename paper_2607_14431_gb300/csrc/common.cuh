@@ -434,13 +434,13 @@ struct PromptParams {
 
 // What weight the rows of a prompt's launch gave each cached row: of its layers
 // [lr0, lr0 + n_lr).  A work item is a KV head, two key tiles and a range of query
-// tiles; its sums go to sums[sum0[b] + ((split * n_lr * Hkv + unit) * 2 * blocks[b]
-// + tile - tile0[b]) * 128 + column].
+// tiles; its lines of sums go to sums[sum0[b] + (((split * n_lr * Hkv + unit) *
+// lines + line) * 2 * blocks[b] + tile - tile0[b]) * 128 + column].
 struct WeighParams {
     PromptParams p;
     float *sums;
     float *weights;                        // [max_seqs][max_slots]
-    int32_t max_slots, lr0, n_lr;
+    int32_t max_slots, lr0, n_lr, lines;   // lines: of an item's sums (weigh_lines())
     float decay;
     int32_t met[kMaxBatchPerLaunch];       // the sequence's weights have been decayed by this call
     int32_t item0[kMaxBatchPerLaunch + 1]; // prefix sums of the work items
@@ -611,12 +611,13 @@ cudaError_t launch_prompt_join(int head_dim, const PromptParams &p, cudaStream_t
 // x weigh_tokens() tokens.
 cudaError_t launch_prompt_lse(int head_dim, bool fp8, int streams, const PromptParams &p, const CUtensorMap &map,
                               cudaStream_t s);
+int weigh_lines(int head_dim);
 int weigh_tokens(int head_dim, int group);
 cudaError_t make_query_tensor_map(CUtensorMap *out, const void *q, int head_dim, int n_q_heads, int group, int tokens,
                                   uint64_t rows);
 cudaError_t launch_query_halves(const void *q, int64_t n, void *out, int n_sm, cudaStream_t s);
 cudaError_t launch_weigh(int head_dim, bool fp8, const WeighParams &p, const CUtensorMap &k_map, const CUtensorMap &q_map,
-                         cudaStream_t s);
+                         int n_sm, cudaStream_t s);
 cudaError_t launch_weigh_sum(const WeighParams &p, cudaStream_t s);
 // Split-decode state -> bf16 output: out[r][d] = o / l (0 where l = 0), for
 // n_rows rows of D + 4 floats.

@@ -2783,7 +2783,7 @@ static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     for (int32_t i = 0; i < p.n_seq; ++i) {
         w->splits[i] = (int32_t)std::max(1.0, std::ceil(rows[i].longest / best_len - 1e-9));
         w->sum0[i] = floats;  // (of one layer: scaled by the layers of a launch)
-        floats += (int64_t)w->splits[i] * p.n_kv_heads * 2 * w->blocks[i] * kPromptCols;
+        floats += (int64_t)w->splits[i] * p.n_kv_heads * w->lines * 2 * w->blocks[i] * kPromptCols;
     }
     return floats;
 }
@@ -2846,6 +2846,7 @@ static kvg_status prompt_impl(kvg_cache *c, int32_t layer, const int32_t *seq_id
             w->weights = pw->weights;
             w->max_slots = c->max_slots;
             w->decay = pw->decay;
+            w->lines = weigh_lines(d.head_dim);
             for (int32_t i = 0; i < p.n_seq; ++i) {
                 const int32_t sq = p.seq[i];
                 int64_t valid = 0;
@@ -2874,7 +2875,7 @@ static kvg_status prompt_impl(kvg_cache *c, int32_t layer, const int32_t *seq_id
                     w->item0[i + 1] = w->item0[i] + w->blocks[i] * w->splits[i] * w->n_lr * p.n_kv_heads;
                     if (l) w->met[i] = 1;
                 }
-                KVG_CUDA(launch_weigh(d.head_dim, fp8, *w, c->prompt_map, pw->q_map, st));
+                KVG_CUDA(launch_weigh(d.head_dim, fp8, *w, c->prompt_map, pw->q_map, c->n_sm, st));
                 KVG_CUDA(launch_weigh_sum(*w, st));
             }
         }

@@ -14,6 +14,10 @@
 // query tiles stream through a ring of copies; scores are double-buffered in tensor
 // memory, so that a tile's products run beside the exponentials of the one before.
 //
+// CTAs are persistent: item by item, the ring of query tiles running on from one to
+// the next, so that only an item's keys are waited for (their place is free when its
+// last products are done).
+//
 // Warps: eight form and sum weights, one loads, one thread issues products, in a
 // pair one hands the copies over to the first CTA's issuing thread.
 #include <math.h>
@@ -35,20 +39,20 @@ struct Weigh {
     static constexpr int STAGES = D == 64 ? 6 : FP8 ? 3 : 4;
     static constexpr int SUM_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, RELAY_WARP = 10;
     static constexpr int THREADS = 32 * (PAIR ? 11 : 10);
-    static constexpr int COLS = kTile * STREAMS / 2;                   // of a query tile that a summing warp has
+    static constexpr int LINES = 2 / STREAMS;                          // a key's sums: a pair's CTA has two warps to it
+    static constexpr int COLS = kTile / LINES;                         // of a query tile that a summing warp has
     static constexpr int SMEM = STREAMS * KEYS + STAGES * Q_BYTES + RAW + 1024;
     static_assert(SMEM <= 217 * 1024, "shared memory beside the barriers and the logarithms");
 };
 
 struct WeighBars {
-    uint64_t k_landed, k_ready;              // keys: there; (fp8) converted, (pair) in both CTAs
+    uint64_t k_landed, k_ready, k_free;      // keys: there; (fp8) converted, (pair) in both CTAs; multiplied
     uint64_t landed[8], ready[8], empty[8];  // query tiles: there; in both CTAs; multiplied
     uint64_t scores[2][2], taken[2][2];      // of a stream and buffer: there; read
     uint64_t drained;
     uint32_t tmem;
     int abort;
-    float lse[8][2][kTile];                  // of each summing warp: minus lse of its rows of two tiles
-    float half[kTile];                       // a pair's CTA: sums of the second half of its rows
+    alignas(16) float lse[8][2][kTile];       // of each summing warp: minus lse of its rows of two tiles
 };
 
 __device__ __forceinline__ bool wait_weigh(WeighBars &s, uint64_t *bar, uint32_t parity, DevStatus *status) {
@@ -111,6 +115,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     if (threadIdx.x == 0) {
         mbar_init(&s.k_landed, 1);
         mbar_init(&s.k_ready, CTAS * (FP8 ? C::SUM_WARPS : 1));
+        mbar_init(&s.k_free, 1);
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(&s.landed[i], 1);
             mbar_init(&s.ready[i], CTAS);
@@ -126,9 +131,6 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         fence_mbar_init();
     }
     if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
-    const WeighItem it = weigh_item(w, blockIdx.x / CTAS);
-    const int n = it.q1 - it.q0;
-    const int gs = p.log2_group, rows = (p.first[it.b + 1] - p.first[it.b]) << gs;  // of the sequence
     tc_before_sync();
     if constexpr (CTAS == 2)
         cluster_sync();
@@ -137,227 +139,250 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     tc_after_sync();
     after_previous();
     const uint32_t tmem = s.tmem;
+    const int gs = p.log2_group;
+    // The CTA's items: every (grid / CTAS)-th.  tiles: query tiles of the items before;
+    // items: how many of those had any.
+    auto each_item = [&](auto &&work) {
+        int tiles = 0, items = 0;
+        for (int at = blockIdx.x / CTAS; at < w.item0[p.n_seq]; at += gridDim.x / CTAS) {
+            const WeighItem it = weigh_item(w, at);
+            const int n = it.q1 - it.q0, rows = (p.first[it.b + 1] - p.first[it.b]) << gs;  // rows: of the sequence
+            if (!work(it, n, rows, tiles, items)) return;
+            tiles += n;
+            items += n > 0;
+        }
+    };
 
     if (warp < C::SUM_WARPS) {
-        // ---- a thread has a key
-        const int stream = STREAMS == 2 ? warp / 4 : 0, half = STREAMS == 2 ? 0 : warp / 4;
-        const int tile = it.tile + (STREAMS == 2 ? stream : rank), col = warp % 4 * 32 + lane;
-        // its slot, and the query rows [lo, hi) of the sequence that attend to it
-        int slot, lo = 0, hi = rows;
-        bool valid;
-        {
-            const int u = tile * (kTile / p.unit) + col / p.unit, c = col % p.unit;
-            int pg, r;
-            if (p.pages_per_unit) {
-                const int place = c / p.page_rows;
-                pg = u * p.pages_per_unit + place;
-                r = c - place * p.page_rows;
-                valid = place < p.pages_per_unit && r < p.page_size;
-            } else {
-                pg = u / p.units_per_page;
-                r = (u - pg * p.units_per_page) * p.unit + c;
-                valid = r < p.page_size;
-            }
-            const int slot0 = p.slot0[it.b], last = slot0 + (rows >> gs) - 1;
-            slot = pg * p.page_size + r;
-            valid = valid && slot <= last;
-            if (valid) {
-                const int32_t *fill = p.page_fill + (int64_t)p.seq[it.b] * p.max_pages;
-                valid = r < fill[pg];
-                lo = max(0, slot - slot0) << gs;
-                if (valid && p.window > 0) {
-                    // valid rows from here up to the query rows
-                    int64_t between = (int64_t)slot0 - slot;
-                    if (slot < p.solid[it.b]) {
-                        between = fill[pg] - r;
-                        const int end = slot0 / p.page_size;
-                        for (int i = pg + 1; i < end && between < p.window; ++i) between += fill[i];
-                        if (end > pg) between += slot0 - end * p.page_size;
-                        else between = slot0 - slot;
-                    }
-                    hi = (int)max((int64_t)0, min((int64_t)(rows >> gs), p.window - between)) << gs;
+        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+            // ---- a thread has a key
+            const int stream = STREAMS == 2 ? warp / 4 : 0, half = STREAMS == 2 ? 0 : warp / 4;
+            const int tile = it.tile + (STREAMS == 2 ? stream : rank), col = warp % 4 * 32 + lane;
+            // its slot, and the query rows [lo, hi) of the sequence that attend to it
+            int slot, lo = 0, hi = rows;
+            bool valid;
+            {
+                const int u = tile * (kTile / p.unit) + col / p.unit, c = col % p.unit;
+                int pg, r;
+                if (p.pages_per_unit) {
+                    const int place = c / p.page_rows;
+                    pg = u * p.pages_per_unit + place;
+                    r = c - place * p.page_rows;
+                    valid = place < p.pages_per_unit && r < p.page_size;
+                } else {
+                    pg = u / p.units_per_page;
+                    r = (u - pg * p.units_per_page) * p.unit + c;
+                    valid = r < p.page_size;
                 }
-            }
-        }
-        bool ok = true;
-        if constexpr (FP8) {  // E4M3 codes to fp16 (exact)
-            ok = wait_weigh(s, &s.k_landed, 0, p.status);
-            if (ok) {
-                constexpr int CHUNKS = D / 16;  // 16 codes each, of a key
-                for (int i = threadIdx.x; i < STREAMS * kTile * CHUNKS; i += 32 * C::SUM_WARPS) {
-                    const int u = i % CHUNKS, r = i / CHUNKS % kTile, st = i / (CHUNKS * kTile);
-                    const uint4 x = *reinterpret_cast<const uint4 *>(raw + st * (kTile * D) + u / 8 * (kTile * 128) + r * 128 +
-                                                                     ((u % 8 ^ (r & 7)) << 4));
-                    const uint32_t codes[4] = {x.x, x.y, x.z, x.w};
-                    uint32_t y[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint16_t a = (uint16_t)codes[e], b = (uint16_t)(codes[e] >> 16);
-                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(a));
-                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(b));
-                    }
-                    uint8_t *const to = keys + st * C::KEYS + u / 4 * (kTile * 128) + r * 128;
-                    const int u2 = u % 4 * 2;
-                    *reinterpret_cast<uint4 *>(to + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                    *reinterpret_cast<uint4 *>(to + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
-                }
-                fence_proxy_async_shared();
-                arrive_issuer(&s.k_ready);
-            }
-        }
-        constexpr int COLS = C::COLS, PER = COLS / 32;  // PER: logarithms that a lane fetches
-        const float *lse = p.row_lse + ((int64_t)(it.lr * p.n_kv_heads + it.g) * p.q_rows + p.row0[it.b]) * (1 << gs);
-        float *const mine[2] = {s.lse[warp][0], s.lse[warp][1]};
-        float ahead[PER];
-        auto fetch = [&](int t) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int r = t * kTile + half * COLS + i * 32 + lane;
-                ahead[i] = t < it.q1 && r < rows ? lse[r] : INFINITY;  // (2^-inf: no weight)
-            }
-        };
-        auto put = [&](int buf) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) mine[buf][i * 32 + lane] = -ahead[i];
-            __syncwarp();
-        };
-        const float c = p.negate ? -p.qscale : p.qscale;
-        const float2 c2 = make_float2(c, c);
-        const uint32_t at = tmem + ((uint32_t)(warp % 4) << 21) + stream * (2 * kTile) + half * COLS;
-        float2 sum[4] = {};
-        fetch(it.q0);
-        put(0);
-        for (int i = 0; ok && i < n; ++i) {
-            const int buf = i & 1, row0 = (it.q0 + i) * kTile + half * COLS;
-            fetch(it.q0 + i + 1);
-            ok = wait_weigh(s, &s.scores[stream][buf], (i >> 1) & 1, p.status);
-            if (!ok) break;
-            tc_after_sync();
-            const bool whole = !valid || (lo <= row0 && hi >= row0 + COLS);
-            const bool all = __all_sync(0xffffffffu, whole);
-            const int a = lo - row0, e = hi - row0;
-            float x[32];
-#pragma unroll
-            for (int j = 0; j < COLS; j += 32) {
-                tmem_ld32(at + buf * kTile + j, reinterpret_cast<uint32_t *>(x));
-                tmem_wait_ld();
-                if (j + 32 == COLS) {  // the next scores may be put there
-                    tc_before_sync();
-                    arrive_issuer(&s.taken[stream][buf]);
-                }
-                const int aj = a - j, ej = e - j;
-                const uint32_t bits = all ? ~0u
-                                          : (ej >= 32 ? ~0u : ej <= 0 ? 0u : (1u << ej) - 1) &
-                                                (aj >= 32 ? 0u : aj <= 0 ? ~0u : ~((1u << aj) - 1));
-                auto add = [&](bool masked) {
-#pragma unroll
-                    for (int r = 0; r < 32; r += 4) {
-                        const float4 l = *reinterpret_cast<const float4 *>(&mine[buf][j + r]);
-                        float2 y0 = fma2(make_float2(x[r], x[r + 1]), c2, make_float2(l.x, l.y));
-                        float2 y1 = fma2(make_float2(x[r + 2], x[r + 3]), c2, make_float2(l.z, l.w));
-                        if (masked) {
-                            y0.x = bits >> r & 1 ? y0.x : -INFINITY;
-                            y0.y = bits >> (r + 1) & 1 ? y0.y : -INFINITY;
-                            y1.x = bits >> (r + 2) & 1 ? y1.x : -INFINITY;
-                            y1.y = bits >> (r + 3) & 1 ? y1.y : -INFINITY;
+                const int slot0 = p.slot0[it.b], last = slot0 + (rows >> gs) - 1;
+                slot = pg * p.page_size + r;
+                valid = valid && slot <= last;
+                if (valid) {
+                    const int32_t *fill = p.page_fill + (int64_t)p.seq[it.b] * p.max_pages;
+                    valid = r < fill[pg];
+                    lo = max(0, slot - slot0) << gs;
+                    if (valid && p.window > 0) {
+                        // valid rows from here up to the query rows
+                        int64_t between = (int64_t)slot0 - slot;
+                        if (slot < p.solid[it.b]) {
+                            between = fill[pg] - r;
+                            const int end = slot0 / p.page_size;
+                            for (int i = pg + 1; i < end && between < p.window; ++i) between += fill[i];
+                            if (end > pg) between += slot0 - end * p.page_size;
+                            else between = slot0 - slot;
                         }
-                        sum[r / 2 % 4] = add2(sum[r / 2 % 4], make_float2(exp2_approx(y0.x), exp2_approx(y0.y)));
-                        sum[r / 2 % 4 + 1] = add2(sum[r / 2 % 4 + 1], make_float2(exp2_approx(y1.x), exp2_approx(y1.y)));
+                        hi = (int)max((int64_t)0, min((int64_t)(rows >> gs), p.window - between)) << gs;
                     }
-                };
-                if (all)
-                    add(false);
-                else
-                    add(true);
-            }
-            put(buf ^ 1);
-        }
-        const float2 total = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-        float sums = total.x + total.y;
-        if constexpr (STREAMS == 1) {
-            if (half) s.half[col] = sums;
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * C::SUM_WARPS) : "memory");
-            if (!half) sums += s.half[col];
-        }
-        if (!half) {
-            const int64_t line = (int64_t)it.split * (w.n_lr * p.n_kv_heads) + it.unit;
-            w.sums[w.sum0[it.b] + (line * 2 * w.blocks[it.b] + tile - w.tile0[it.b]) * kTile + col] = valid ? sums : 0.f;
-        }
-    } else if (warp == C::LOAD_WARP) {
-        // ---- the keys of the CTA's tiles, then its part of each query tile
-        const int64_t entry = (int64_t)p.seq[it.b] * p.max_pages;
-        const int slot_end = p.slot0[it.b] + (rows >> gs), last = (slot_end - 1) / p.page_size;
-        const int32_t base = (int32_t)(((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads + it.g) * p.page_size);
-        const int per = kTile / p.unit, unit = lane / 16, place = lane % 16;
-        constexpr int BOXES = FP8 ? D / 128 : D / 64;
-        int32_t y[STREAMS];
-        uint32_t has[STREAMS];
-        int boxes = 0;
-#pragma unroll
-        for (int st = 0; st < STREAMS; ++st) {
-            const int u = (it.tile + (STREAMS == 2 ? st : rank)) * per + unit;
-            int pg = u * p.pages_per_unit + place, sub = 0;
-            bool mine = unit < per && place < p.pages_per_unit;
-            if (!p.pages_per_unit) {
-                pg = u / p.units_per_page;
-                sub = (u - pg * p.units_per_page) * p.unit;
-                mine = unit < per && place == 0;
-            }
-            mine = mine && pg <= last;
-            int pid = 0;
-            if (mine) {
-                pid = p.page_table[entry + pg];
-                mine = p.page_fill[entry + pg] > sub;
-                if (mine && (pid < 0 || pid >= p.pool_pages)) {
-                    record_error(p.status, KVG_ERR_DEVICE_CHECK, 31);
-                    mine = false;
                 }
             }
-            y[st] = base + pid * (p.n_kv_heads * p.page_size) + sub;
-            has[st] = __ballot_sync(0xffffffffu, mine);
-            boxes += __popc(has[st]);
-        }
-        if (elect_one()) {
-            if (boxes)
-                mbar_arrive_expect_tx(&s.k_landed, boxes * p.box_rows * 128 * BOXES);
-            else
-                mbar_arrive(&s.k_landed);
-        }
-        __syncwarp();
+            bool ok = true;
+            if constexpr (FP8) {  // E4M3 codes to fp16 (exact)
+                if (n > 0) ok = wait_weigh(s, &s.k_landed, items & 1, p.status);
+                if (n > 0 && items > 0 && ok) ok = wait_weigh(s, &s.k_free, (items - 1) & 1, p.status);
+                if (n > 0 && ok) {
+                    constexpr int CHUNKS = D / 16;  // 16 codes each, of a key
+                    for (int i = threadIdx.x; i < STREAMS * kTile * CHUNKS; i += 32 * C::SUM_WARPS) {
+                        const int u = i % CHUNKS, r = i / CHUNKS % kTile, st = i / (CHUNKS * kTile);
+                        const uint4 x = *reinterpret_cast<const uint4 *>(raw + st * (kTile * D) + u / 8 * (kTile * 128) + r * 128 +
+                                                                         ((u % 8 ^ (r & 7)) << 4));
+                        const uint32_t codes[4] = {x.x, x.y, x.z, x.w};
+                        uint32_t y[8];
 #pragma unroll
-        for (int st = 0; st < STREAMS; ++st)
-            for (uint32_t left = has[st]; left; left &= left - 1) {
-                const int from = __ffs(left) - 1;
-                const int32_t row = __shfl_sync(0xffffffffu, y[st], from);
-                uint8_t *const to = (FP8 ? raw + st * (kTile * D) : keys + st * C::KEYS) +
-                                    (from / 16 * p.unit + from % 16 * p.page_rows) * 128;
-                if (elect_one())
-#pragma unroll
-                    for (int x = 0; x < BOXES; ++x)
-                        tma_load_2d(to + x * (kTile * 128), &k_map, x * (FP8 ? 128 : 64), row, &s.k_landed);
+                        for (int e = 0; e < 4; ++e) {
+                            const uint16_t a = (uint16_t)codes[e], b = (uint16_t)(codes[e] >> 16);
+                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(a));
+                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(b));
+                        }
+                        uint8_t *const to = keys + st * C::KEYS + u / 4 * (kTile * 128) + r * 128;
+                        const int u2 = u % 4 * 2;
+                        *reinterpret_cast<uint4 *>(to + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                        *reinterpret_cast<uint4 *>(to + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+                    }
+                    fence_proxy_async_shared();
+                    arrive_issuer(&s.k_ready);
+                }
             }
-        bool ok = true;
-        const int token0 = p.qlayers[it.lr] * (int)p.q_rows + p.row0[it.b] + ((rank * C::Q_ROWS) >> gs);
-        int i = 0;
-        for (; ok && i < n; ++i) {
-            const int st = i % STAGES;
-            if (i >= STAGES) ok = wait_weigh(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
-            if (!ok) break;
-            if (elect_one()) {
-                mbar_arrive_expect_tx(&s.landed[st], C::Q_BYTES);
+            constexpr int COLS = C::COLS, PER = COLS / 32;  // PER: logarithms that a lane fetches
+            const float *lse = p.row_lse + ((int64_t)(it.lr * p.n_kv_heads + it.g) * p.q_rows + p.row0[it.b]) * (1 << gs);
+            float *const mine[2] = {s.lse[warp][0], s.lse[warp][1]};
+            float ahead[PER];
+            auto fetch = [&](int t) {
 #pragma unroll
-                for (int x = 0; x < D / 64; ++x)
-                    tma_load_3d(ring + st * C::Q_BYTES + x * (C::Q_ROWS * 128), &q_map, x * 64, it.g << gs,
-                                token0 + (((it.q0 + i) * kTile) >> gs), &s.landed[st]);
+                for (int i = 0; i < PER; ++i) {
+                    const int r = t * kTile + half * COLS + i * 32 + lane;
+                    ahead[i] = t < it.q1 && r < rows ? lse[r] : INFINITY;  // (2^-inf: no weight)
+                }
+            };
+            auto put = [&](int buf) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) mine[buf][i * 32 + lane] = -ahead[i];
+                __syncwarp();
+            };
+            const float c = p.negate ? -p.qscale : p.qscale;
+            const float2 c2 = make_float2(c, c);
+            const uint32_t at = tmem + ((uint32_t)(warp % 4) << 21) + stream * (2 * kTile) + half * COLS;
+            float2 sum[4] = {};
+            fetch(it.q0);
+            put(0);
+            for (int i = 0; ok && i < n; ++i) {
+                const int buf = (tiles + i) & 1, lbuf = i & 1, row0 = (it.q0 + i) * kTile + half * COLS;
+                fetch(it.q0 + i + 1);
+                ok = wait_weigh(s, &s.scores[stream][buf], ((tiles + i) >> 1) & 1, p.status);
+                if (!ok) break;
+                tc_after_sync();
+                const bool whole = !valid || (lo <= row0 && hi >= row0 + COLS);
+                const bool all = __all_sync(0xffffffffu, whole);
+                float x[64];  // (32 at a time, the second half's loads behind the first half's exponentials: 1,560 cycles a tile)
+#pragma unroll
+                for (int j = 0; j < COLS; j += 64) {
+                    tmem_ld32(at + buf * kTile + j, reinterpret_cast<uint32_t *>(x));
+                    tmem_ld32(at + buf * kTile + j + 32, reinterpret_cast<uint32_t *>(x) + 32);
+                    tmem_wait_ld();
+                    if (j + 64 == COLS) {  // the next scores may be put there
+                        tc_before_sync();
+                        arrive_issuer(&s.taken[stream][buf]);
+                    }
+                    const int aj = lo - row0 - j, ej = hi - row0 - j;
+                    const uint64_t bits = (ej >= 64 ? ~0ull : ej <= 0 ? 0ull : (1ull << ej) - 1) &
+                                          (aj >= 64 ? 0ull : aj <= 0 ? ~0ull : ~((1ull << aj) - 1));
+                    auto add = [&](bool masked) {
+#pragma unroll
+                        for (int r = 0; r < 64; r += 4) {
+                            const float4 l = *reinterpret_cast<const float4 *>(&mine[lbuf][j + r]);
+                            float2 y0 = fma2(make_float2(x[r], x[r + 1]), c2, make_float2(l.x, l.y));
+                            float2 y1 = fma2(make_float2(x[r + 2], x[r + 3]), c2, make_float2(l.z, l.w));
+                            if (masked) {
+                                y0.x = bits >> r & 1 ? y0.x : -INFINITY;
+                                y0.y = bits >> (r + 1) & 1 ? y0.y : -INFINITY;
+                                y1.x = bits >> (r + 2) & 1 ? y1.x : -INFINITY;
+                                y1.y = bits >> (r + 3) & 1 ? y1.y : -INFINITY;
+                            }
+                            sum[r / 2 % 4] = add2(sum[r / 2 % 4], make_float2(exp2_approx(y0.x), exp2_approx(y0.y)));
+                            sum[r / 2 % 4 + 1] = add2(sum[r / 2 % 4 + 1], make_float2(exp2_approx(y1.x), exp2_approx(y1.y)));
+                        }
+                    };
+                    if (all)
+                        add(false);
+                    else
+                        add(true);
+                }
+                put(lbuf ^ 1);
+            }
+            if (!ok) return false;
+            const float2 total = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+            const int64_t line = ((int64_t)it.split * (w.n_lr * p.n_kv_heads) + it.unit) * C::LINES + half;
+            w.sums[w.sum0[it.b] + (line * 2 * w.blocks[it.b] + tile - w.tile0[it.b]) * kTile + col] =
+                valid ? total.x + total.y : 0.f;
+            return true;
+        });
+    } else if (warp == C::LOAD_WARP) {
+        bool ok = true;
+        int i = 0, k = 0;  // query tiles and keys that were asked for
+        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+            // ---- the keys of the CTA's tiles, then its part of each query tile
+            if (n == 0) return true;
+            const int64_t entry = (int64_t)p.seq[it.b] * p.max_pages;
+            const int slot_end = p.slot0[it.b] + (rows >> gs), last = (slot_end - 1) / p.page_size;
+            const int32_t base = (int32_t)(((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads + it.g) * p.page_size);
+            const int per = kTile / p.unit, unit = lane / 16, place = lane % 16;
+            constexpr int BOXES = FP8 ? D / 128 : D / 64;
+            int32_t y[STREAMS];
+            uint32_t has[STREAMS];
+            int boxes = 0;
+#pragma unroll
+            for (int st = 0; st < STREAMS; ++st) {
+                const int u = (it.tile + (STREAMS == 2 ? st : rank)) * per + unit;
+                int pg = u * p.pages_per_unit + place, sub = 0;
+                bool mine = unit < per && place < p.pages_per_unit;
+                if (!p.pages_per_unit) {
+                    pg = u / p.units_per_page;
+                    sub = (u - pg * p.units_per_page) * p.unit;
+                    mine = unit < per && place == 0;
+                }
+                mine = mine && pg <= last;
+                int pid = 0;
+                if (mine) {
+                    pid = p.page_table[entry + pg];
+                    mine = p.page_fill[entry + pg] > sub;
+                    if (mine && (pid < 0 || pid >= p.pool_pages)) {
+                        record_error(p.status, KVG_ERR_DEVICE_CHECK, 31);
+                        mine = false;
+                    }
+                }
+                y[st] = base + pid * (p.n_kv_heads * p.page_size) + sub;
+                has[st] = __ballot_sync(0xffffffffu, mine);
+                boxes += __popc(has[st]);
+            }
+            const int token0 = p.qlayers[it.lr] * (int)p.q_rows + p.row0[it.b] + ((rank * C::Q_ROWS) >> gs);
+            auto load = [&](int t) {
+                const int st = i % STAGES;
+                if (i >= STAGES) ok = wait_weigh(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
+                if (!ok) return;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&s.landed[st], C::Q_BYTES);
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x)
+                        tma_load_3d(ring + st * C::Q_BYTES + x * (C::Q_ROWS * 128), &q_map, x * 64, it.g << gs,
+                                    token0 + (((it.q0 + t) * kTile) >> gs), &s.landed[st]);
+                }
+                __syncwarp();
+                ++i;
+            };
+            // (the first query tile's place is free before the keys' is)
+            if (items > 0) load(0);
+            if (items > 0 && ok) ok = wait_weigh(s, &s.k_free, (items - 1) & 1, p.status);
+            if (!ok) return false;
+            ++k;
+            if (elect_one()) {
+                if (boxes)
+                    mbar_arrive_expect_tx(&s.k_landed, boxes * p.box_rows * 128 * BOXES);
+                else
+                    mbar_arrive(&s.k_landed);
             }
             __syncwarp();
-        }
+#pragma unroll
+            for (int st = 0; st < STREAMS; ++st)
+                for (uint32_t left = has[st]; left; left &= left - 1) {
+                    const int from = __ffs(left) - 1;
+                    const int32_t row = __shfl_sync(0xffffffffu, y[st], from);
+                    uint8_t *const to = (FP8 ? raw + st * (kTile * D) : keys + st * C::KEYS) +
+                                        (from / 16 * p.unit + from % 16 * p.page_rows) * 128;
+                    if (elect_one())
+#pragma unroll
+                        for (int x = 0; x < BOXES; ++x)
+                            tma_load_2d(to + x * (kTile * 128), &k_map, x * (FP8 ? 128 : 64), row, &s.k_landed);
+                }
+            for (int t = items > 0; ok && t < n; ++t) load(t);
+            return ok;
+        });
         // no copy may still be landing, nor a commit arriving, when the CTA ends
-        (void)mbar_wait_bounded(&s.k_landed, 0);
-        for (int k = max(0, i - STAGES); k < i; ++k) {
-            (void)mbar_wait_bounded(&s.landed[k % STAGES], (k / STAGES) & 1);
-            if (ok) ok = wait_weigh(s, &s.empty[k % STAGES], (k / STAGES) & 1, p.status);
+        if (k > 0) (void)mbar_wait_bounded(&s.k_landed, (k - 1) & 1);
+        for (int t = max(0, i - STAGES); t < i; ++t) {
+            (void)mbar_wait_bounded(&s.landed[t % STAGES], (t / STAGES) & 1);
+            if (ok) ok = wait_weigh(s, &s.empty[t % STAGES], (t / STAGES) & 1, p.status);
         }
+        if (ok && k > 0) ok = wait_weigh(s, &s.k_free, (k - 1) & 1, p.status);
+        if (rank == 1 && k > 0) (void)mbar_wait_bounded(&s.drained, 0);  // (the first CTA's commits reach this one's barriers)
     } else if (warp == C::MMA_WARP) {
         if (rank == 0 && elect_one()) {
             constexpr uint32_t KQ = mma_desc(CTAS * kTile, kTile, FP8, false);
@@ -366,43 +391,52 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, p.status);
             };
             constexpr bool DIRECT = CTAS == 1;  // the copies' own barriers
-            bool ok = wait(DIRECT && !FP8 ? &s.k_landed : &s.k_ready, 0);
-            for (int i = 0; ok && i < n; ++i) {
-                const int st = i % STAGES, buf = i & 1;
-                ok = wait(DIRECT ? &s.landed[st] : &s.ready[st], (i / STAGES) & 1);
-                for (int stream = 0; ok && stream < STREAMS; ++stream) {
-                    if (i >= 2) ok = wait(&s.taken[stream][buf], ((i >> 1) - 1) & 1);
-                    if (!ok) break;
-                    tc_after_sync();
-                    const uint32_t k = k_d + stream * (C::KEYS / 16), q = q_d + st * (C::Q_BYTES / 16);
-                    const uint32_t to = tmem + stream * (2 * kTile) + buf * kTile;
+            bool any = false;
+            each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+                if (n == 0) return true;
+                any = true;
+                bool ok = wait(DIRECT && !FP8 ? &s.k_landed : &s.k_ready, items & 1);
+                for (int i = tiles; ok && i < tiles + n; ++i) {
+                    const int st = i % STAGES, buf = i & 1;
+                    ok = wait(DIRECT ? &s.landed[st] : &s.ready[st], (i / STAGES) & 1);
+                    for (int stream = 0; ok && stream < STREAMS; ++stream) {
+                        if (i >= 2) ok = wait(&s.taken[stream][buf], ((i >> 1) - 1) & 1);
+                        if (!ok) break;
+                        tc_after_sync();
+                        const uint32_t k = k_d + stream * (C::KEYS / 16), q = q_d + st * (C::Q_BYTES / 16);
+                        const uint32_t to = tmem + stream * (2 * kTile) + buf * kTile;
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_ss<CTAS>(to, k + (x / 4 * (kTile * 128) + x % 4 * 32) / 16,
-                                     q + (x / 4 * (C::Q_ROWS * 128) + x % 4 * 32) / 16, KQ, x > 0);
-                    mma_commit<CTAS>(&s.scores[stream][buf]);
+                        for (int x = 0; x < D / 16; ++x)
+                            mma_ss<CTAS>(to, k + (x / 4 * (kTile * 128) + x % 4 * 32) / 16,
+                                         q + (x / 4 * (C::Q_ROWS * 128) + x % 4 * 32) / 16, KQ, x > 0);
+                        mma_commit<CTAS>(&s.scores[stream][buf]);
+                    }
+                    if (ok) mma_commit<CTAS>(&s.empty[st]);
                 }
-                if (ok) mma_commit<CTAS>(&s.empty[st]);
-            }
+                if (ok) mma_commit<CTAS>(&s.k_free);
+                return ok;
+            });
             // all products have completed before the tensor memory is given back
-            if (n > 0) {
+            if (any) {
                 mma_commit<CTAS>(&s.drained);
                 (void)mbar_wait_bounded(&s.drained, 0);
             }
         }
-        if (rank == 1 && n > 0) (void)mbar_wait_bounded(&s.drained, 0);
         __syncwarp();
     } else if (warp == C::RELAY_WARP) {
         // ---- a pair: what has landed here, for the first CTA's issuing thread
-        bool ok = true;
-        if constexpr (!FP8) {
-            ok = wait_weigh(s, &s.k_landed, 0, p.status);
-            if (ok) arrive_issuer(&s.k_ready);
-        }
-        for (int i = 0; ok && i < n; ++i) {
-            ok = wait_weigh(s, &s.landed[i % STAGES], (i / STAGES) & 1, p.status);
-            if (ok) arrive_issuer(&s.ready[i % STAGES]);
-        }
+        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+            bool ok = true;
+            if constexpr (!FP8) {
+                if (n > 0) ok = wait_weigh(s, &s.k_landed, items & 1, p.status);
+                if (n > 0 && ok) arrive_issuer(&s.k_ready);
+            }
+            for (int i = tiles; ok && i < tiles + n; ++i) {
+                ok = wait_weigh(s, &s.landed[i % STAGES], (i / STAGES) & 1, p.status);
+                if (ok) arrive_issuer(&s.ready[i % STAGES]);
+            }
+            return ok;
+        });
     }
     // (a pair: the other CTA's arrivals and products reach into this one's memory)
     tc_before_sync();
@@ -431,7 +465,7 @@ __global__ void __launch_bounds__(kSlots * kLines) weigh_sum_kernel(const __grid
         tile_of(p, slot, tile, col);
         tile -= w.tile0[b];
         if (tile >= 0 && slot - pg * p.page_size < p.page_fill[(int64_t)p.seq[b] * p.max_pages + pg]) {
-            const int lines = w.splits[b] * w.n_lr * p.n_kv_heads;
+            const int lines = w.splits[b] * w.n_lr * p.n_kv_heads * w.lines;
             const int64_t step = (int64_t)2 * w.blocks[b] * kTile;
             const float *s = w.sums + w.sum0[b] + (int64_t)tile * kTile + col;
 #pragma unroll 8
@@ -464,7 +498,7 @@ __global__ void __launch_bounds__(256) query_halves_kernel(const uint4 *q, int64
 }
 
 template <class C>
-cudaError_t run_weigh(const WeighParams &w, const CUtensorMap &k_map, const CUtensorMap &q_map, cudaStream_t s) {
+cudaError_t run_weigh(const WeighParams &w, const CUtensorMap &k_map, const CUtensorMap &q_map, int n_sm, cudaStream_t s) {
     static std::atomic<int> ready[kMaxDevices];  // the shared-memory attribute is per device
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -481,7 +515,7 @@ cudaError_t run_weigh(const WeighParams &w, const CUtensorMap &k_map, const CUte
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim = {C::CTAS, 1, 1};
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(w.item0[w.p.n_seq] * C::CTAS);
+    cfg.gridDim = dim3(std::min(w.item0[w.p.n_seq], n_sm / C::CTAS) * C::CTAS);
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
@@ -511,6 +545,7 @@ cudaError_t launch_prompt_lse(int head_dim, bool fp8, int streams, const PromptP
     return cudaErrorInvalidValue;
 }
 
+int weigh_lines(int head_dim) { return head_dim == 256 ? Weigh<256, false>::LINES : Weigh<128, false>::LINES; }
 int weigh_tokens(int head_dim, int group) { return (head_dim == 256 ? kTile / 2 : kTile) / group; }
 
 cudaError_t launch_query_halves(const void *q, int64_t n, void *out, int n_sm, cudaStream_t s) {
@@ -520,11 +555,11 @@ cudaError_t launch_query_halves(const void *q, int64_t n, void *out, int n_sm, c
 }
 
 cudaError_t launch_weigh(int head_dim, bool fp8, const WeighParams &w, const CUtensorMap &k_map, const CUtensorMap &q_map,
-                         cudaStream_t s) {
+                         int n_sm, cudaStream_t s) {
     switch (head_dim) {
-        case 64: return run_weigh<Weigh<64, false>>(w, k_map, q_map, s);
-        case 128: return fp8 ? run_weigh<Weigh<128, true>>(w, k_map, q_map, s) : run_weigh<Weigh<128, false>>(w, k_map, q_map, s);
-        case 256: return fp8 ? run_weigh<Weigh<256, true>>(w, k_map, q_map, s) : run_weigh<Weigh<256, false>>(w, k_map, q_map, s);
+        case 64: return run_weigh<Weigh<64, false>>(w, k_map, q_map, n_sm, s);
+        case 128: return fp8 ? run_weigh<Weigh<128, true>>(w, k_map, q_map, n_sm, s) : run_weigh<Weigh<128, false>>(w, k_map, q_map, n_sm, s);
+        case 256: return fp8 ? run_weigh<Weigh<256, true>>(w, k_map, q_map, n_sm, s) : run_weigh<Weigh<256, false>>(w, k_map, q_map, n_sm, s);
     }
     return cudaErrorInvalidValue;
 }
