@@ -10,16 +10,22 @@
 //
 // A work item is a KV head, two tiles of 128 keys and a range of query tiles (128
 // token x head rows).  For head_dim up to 128 one CTA has both key tiles; for 256 a
-// pair of CTAs has one each and half of every query tile.  Keys are loaded once,
-// query tiles stream through a ring of copies; scores are double-buffered in tensor
-// memory, so that a tile's products run beside the exponentials of the one before.
+// pair of CTAs has one each and half of every query tile.  An item's keys are put
+// into tensor memory once, query tiles stream through a ring of copies; scores have
+// two or three buffers in tensor memory, so that a tile's products run beside the
+// exponentials of the one before.
+//
+// What bounds it: with both operands in shared memory, that memory's 128 bytes a
+// cycle (a pair's products of 128 keys and 128 rows read 8 KB in their 64 cycles, the
+// copies and the rows' logarithms come on top: 1,480 cycles a tile, whether eight or
+// sixteen warps formed the weights); with the keys in tensor memory the products.
 //
 // CTAs are persistent: item by item, the ring of query tiles running on from one to
-// the next, so that only an item's keys are waited for (their place is free when its
-// last products are done).
+// the next, and the next item's keys on their way while one is worked on.
 //
-// Warps: eight form and sum weights, one loads, one thread issues products, in a
-// pair one hands the copies over to the first CTA's issuing thread.
+// Warps: eight form and sum weights, four put keys into tensor memory (of an fp8
+// cache as fp16, exact), one loads, one thread issues products, in a pair one hands
+// the query tiles over to the first CTA's issuing thread.
 #include <math.h>
 
 #include "prompt.cuh"
@@ -33,22 +39,25 @@ struct Weigh {
     static constexpr int D = D_;
     static constexpr bool FP8 = FP8_, PAIR = D == 256;
     static constexpr int CTAS = PAIR ? 2 : 1, STREAMS = PAIR ? 1 : 2;  // key tiles of a CTA
-    static constexpr int KEYS = kTile * D * 2;                         // bytes of a key tile
+    static constexpr int KEYS = kTile * D * (FP8 ? 1 : 2);             // bytes of a key tile
     static constexpr int Q_ROWS = kTile / CTAS, Q_BYTES = Q_ROWS * D * 2;  // a CTA's part of a query tile
-    static constexpr int RAW = FP8 ? STREAMS * kTile * D : 0;
-    static constexpr int STAGES = D == 64 ? 6 : FP8 ? 3 : 4;
-    static constexpr int SUM_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, RELAY_WARP = 10;
-    static constexpr int THREADS = 32 * (PAIR ? 11 : 10);
+    static constexpr int STAGES = D == 64 ? 6 : 4;
+    // tensor memory: score buffers, then the keys' (D / 2 columns a tile), of a pair two
+    static constexpr int SCORES = PAIR ? 2 : 3, KEY_SETS = PAIR ? 2 : 1, KEY_COL = SCORES * kTile;
+    static_assert(KEY_COL + KEY_SETS * STREAMS * D / 2 <= 512, "tensor memory");
+    static constexpr int SUM_WARPS = 8, KEY_WARP = 8, LOAD_WARP = 12, MMA_WARP = 13, RELAY_WARP = 14;
+    static constexpr int THREADS = 32 * (PAIR ? 15 : 14);
     static constexpr int LINES = 2 / STREAMS;                          // a key's sums: a pair's CTA has two warps to it
     static constexpr int COLS = kTile / LINES;                         // of a query tile that a summing warp has
-    static constexpr int SMEM = STREAMS * KEYS + STAGES * Q_BYTES + RAW + 1024;
+    static constexpr int SMEM = STREAMS * KEYS + STAGES * Q_BYTES + 1024;
     static_assert(SMEM <= 217 * 1024, "shared memory beside the barriers and the logarithms");
 };
 
 struct WeighBars {
-    uint64_t k_landed, k_ready, k_free;      // keys: there; (fp8) converted, (pair) in both CTAs; multiplied
+    uint64_t k_landed, k_taken;              // keys: there; their place is free
+    uint64_t k_ready[2], k_free[2];          // in tensor memory (of a pair both); multiplied
     uint64_t landed[8], ready[8], empty[8];  // query tiles: there; in both CTAs; multiplied
-    uint64_t scores[2][2], taken[2][2];      // of a stream and buffer: there; read
+    uint64_t scores[3], taken[3];            // of a buffer: there; read
     uint64_t drained;
     uint32_t tmem;
     int abort;
@@ -100,7 +109,6 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     __shared__ WeighBars s;
     uint8_t *const keys = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     uint8_t *const ring = keys + STREAMS * C::KEYS;
-    uint8_t *const raw = ring + STAGES * C::Q_BYTES;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;  // uniform in the warp
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
     auto arrive_issuer = [&](uint64_t *bar) {  // a warp, for its lanes together
@@ -114,18 +122,20 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     };
     if (threadIdx.x == 0) {
         mbar_init(&s.k_landed, 1);
-        mbar_init(&s.k_ready, CTAS * (FP8 ? C::SUM_WARPS : 1));
-        mbar_init(&s.k_free, 1);
+        mbar_init(&s.k_taken, 4);
+        for (int i = 0; i < C::KEY_SETS; ++i) {
+            mbar_init(&s.k_ready[i], CTAS * 4);
+            mbar_init(&s.k_free[i], 1);
+        }
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(&s.landed[i], 1);
             mbar_init(&s.ready[i], CTAS);
             mbar_init(&s.empty[i], 1);
         }
-        for (int i = 0; i < STREAMS; ++i)
-            for (int k = 0; k < 2; ++k) {
-                mbar_init(&s.scores[i][k], 1);
-                mbar_init(&s.taken[i][k], CTAS * C::SUM_WARPS / STREAMS);
-            }
+        for (int i = 0; i < C::SCORES; ++i) {
+            mbar_init(&s.scores[i], 1);
+            mbar_init(&s.taken[i], CTAS * C::SUM_WARPS / STREAMS);
+        }
         mbar_init(&s.drained, 1);
         s.abort = 0;
         fence_mbar_init();
@@ -196,63 +206,42 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 }
             }
             bool ok = true;
-            if constexpr (FP8) {  // E4M3 codes to fp16 (exact)
-                if (n > 0) ok = wait_weigh(s, &s.k_landed, items & 1, p.status);
-                if (n > 0 && items > 0 && ok) ok = wait_weigh(s, &s.k_free, (items - 1) & 1, p.status);
-                if (n > 0 && ok) {
-                    constexpr int CHUNKS = D / 16;  // 16 codes each, of a key
-                    for (int i = threadIdx.x; i < STREAMS * kTile * CHUNKS; i += 32 * C::SUM_WARPS) {
-                        const int u = i % CHUNKS, r = i / CHUNKS % kTile, st = i / (CHUNKS * kTile);
-                        const uint4 x = *reinterpret_cast<const uint4 *>(raw + st * (kTile * D) + u / 8 * (kTile * 128) + r * 128 +
-                                                                         ((u % 8 ^ (r & 7)) << 4));
-                        const uint32_t codes[4] = {x.x, x.y, x.z, x.w};
-                        uint32_t y[8];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint16_t a = (uint16_t)codes[e], b = (uint16_t)(codes[e] >> 16);
-                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"(a));
-                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"(b));
-                        }
-                        uint8_t *const to = keys + st * C::KEYS + u / 4 * (kTile * 128) + r * 128;
-                        const int u2 = u % 4 * 2;
-                        *reinterpret_cast<uint4 *>(to + ((u2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                        *reinterpret_cast<uint4 *>(to + (((u2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
-                    }
-                    fence_proxy_async_shared();
-                    arrive_issuer(&s.k_ready);
-                }
-            }
             constexpr int COLS = C::COLS, PER = COLS / 32;  // PER: logarithms that a lane fetches
             const float *lse = p.row_lse + ((int64_t)(it.lr * p.n_kv_heads + it.g) * p.q_rows + p.row0[it.b]) * (1 << gs);
             float *const mine[2] = {s.lse[warp][0], s.lse[warp][1]};
-            float ahead[PER];
-            auto fetch = [&](int t) {
+            // of the tile after this one, and of the one after that: their loads take as long as a tile
+            float next[PER], after[PER];
+            auto fetch = [&](int t, float (&to)[PER]) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     const int r = t * kTile + half * COLS + i * 32 + lane;
-                    ahead[i] = t < it.q1 && r < rows ? lse[r] : INFINITY;  // (2^-inf: no weight)
+                    to[i] = t < it.q1 && r < rows ? lse[r] : INFINITY;  // (2^-inf: no weight)
                 }
             };
             auto put = [&](int buf) {
+                __syncwarp();
 #pragma unroll
-                for (int i = 0; i < PER; ++i) mine[buf][i * 32 + lane] = -ahead[i];
+                for (int i = 0; i < PER; ++i) mine[buf][i * 32 + lane] = -next[i];
                 __syncwarp();
             };
             const float c = p.negate ? -p.qscale : p.qscale;
             const float2 c2 = make_float2(c, c);
-            const uint32_t at = tmem + ((uint32_t)(warp % 4) << 21) + stream * (2 * kTile) + half * COLS;
+            const uint32_t at = tmem + ((uint32_t)(warp % 4) << 21) + half * COLS;
             float2 sum[4] = {};
-            fetch(it.q0);
+            fetch(it.q0, next);
+            fetch(it.q0 + 1, after);
             put(0);
             for (int i = 0; ok && i < n; ++i) {
-                const int buf = (tiles + i) & 1, lbuf = i & 1, row0 = (it.q0 + i) * kTile + half * COLS;
-                fetch(it.q0 + i + 1);
-                ok = wait_weigh(s, &s.scores[stream][buf], ((tiles + i) >> 1) & 1, p.status);
+                const int t = (tiles + i) * STREAMS + stream, buf = t % C::SCORES, lbuf = i & 1, row0 = (it.q0 + i) * kTile + half * COLS;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) next[k] = after[k];
+                fetch(it.q0 + i + 2, after);
+                ok = wait_weigh(s, &s.scores[buf], (t / C::SCORES) & 1, p.status);
                 if (!ok) break;
                 tc_after_sync();
                 const bool whole = !valid || (lo <= row0 && hi >= row0 + COLS);
                 const bool all = __all_sync(0xffffffffu, whole);
-                float x[64];  // (32 at a time, the second half's loads behind the first half's exponentials: 1,560 cycles a tile)
+                float x[64];
 #pragma unroll
                 for (int j = 0; j < COLS; j += 64) {
                     tmem_ld32(at + buf * kTile + j, reinterpret_cast<uint32_t *>(x));
@@ -260,7 +249,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     tmem_wait_ld();
                     if (j + 64 == COLS) {  // the next scores may be put there
                         tc_before_sync();
-                        arrive_issuer(&s.taken[stream][buf]);
+                        arrive_issuer(&s.taken[buf]);
                     }
                     const int aj = lo - row0 - j, ej = hi - row0 - j;
                     const uint64_t bits = (ej >= 64 ? ~0ull : ej <= 0 ? 0ull : (1ull << ej) - 1) &
@@ -293,6 +282,47 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             const int64_t line = ((int64_t)it.split * (w.n_lr * p.n_kv_heads) + it.unit) * C::LINES + half;
             w.sums[w.sum0[it.b] + (line * 2 * w.blocks[it.b] + tile - w.tile0[it.b]) * kTile + col] =
                 valid ? total.x + total.y : 0.f;
+            return true;
+        });
+    } else if (warp < C::KEY_WARP + 4) {
+        // ---- keys from shared to tensor memory: a thread has a key of each tile, 64
+        // elements (of a bf16 cache 128 swizzled bytes, of an fp8 cache 64) at a time
+        const int row = warp % 4 * 32 + lane;
+        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+            if (n == 0) return true;
+            const int set = items % C::KEY_SETS;
+            if (!wait_weigh(s, &s.k_landed, items & 1, p.status)) return false;
+            if (items >= C::KEY_SETS && !wait_weigh(s, &s.k_free[set], (items / C::KEY_SETS - 1) & 1, p.status)) return false;
+            tc_after_sync();
+#pragma unroll
+            for (int st = 0; st < STREAMS; ++st)
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) {
+                    uint32_t y[32];
+                    const uint8_t *from = keys + st * C::KEYS + (FP8 ? x / 2 : x) * (kTile * 128) + row * 128;
+#pragma unroll
+                    for (int u = 0; u < (FP8 ? 4 : 8); ++u) {
+                        const int chunk = FP8 ? x % 2 * 4 + u : u;
+                        const uint4 v = *reinterpret_cast<const uint4 *>(from + ((chunk ^ (row & 7)) << 4));
+                        const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if constexpr (FP8) {
+                                const uint16_t a = (uint16_t)words[e], b = (uint16_t)(words[e] >> 16);
+                                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[8 * u + 2 * e]) : "h"(a));
+                                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[8 * u + 2 * e + 1]) : "h"(b));
+                            } else {
+                                y[4 * u + e] = words[e];
+                            }
+                        }
+                    }
+                    tmem_st32(tmem + ((uint32_t)(warp % 4) << 21) + C::KEY_COL + (set * STREAMS + st) * (D / 2) + x * 32, y);
+                }
+            tmem_wait_st();
+            tc_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.k_taken);
+            arrive_issuer(&s.k_ready[set]);
             return true;
         });
     } else if (warp == C::LOAD_WARP) {
@@ -348,9 +378,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 __syncwarp();
                 ++i;
             };
-            // (the first query tile's place is free before the keys' is)
-            if (items > 0) load(0);
-            if (items > 0 && ok) ok = wait_weigh(s, &s.k_free, (items - 1) & 1, p.status);
+            if (items > 0) ok = wait_weigh(s, &s.k_taken, (items - 1) & 1, p.status);
             if (!ok) return false;
             ++k;
             if (elect_one()) {
@@ -365,14 +393,13 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 for (uint32_t left = has[st]; left; left &= left - 1) {
                     const int from = __ffs(left) - 1;
                     const int32_t row = __shfl_sync(0xffffffffu, y[st], from);
-                    uint8_t *const to = (FP8 ? raw + st * (kTile * D) : keys + st * C::KEYS) +
-                                        (from / 16 * p.unit + from % 16 * p.page_rows) * 128;
+                    uint8_t *const to = keys + st * C::KEYS + (from / 16 * p.unit + from % 16 * p.page_rows) * 128;
                     if (elect_one())
 #pragma unroll
                         for (int x = 0; x < BOXES; ++x)
                             tma_load_2d(to + x * (kTile * 128), &k_map, x * (FP8 ? 128 : 64), row, &s.k_landed);
                 }
-            for (int t = items > 0; ok && t < n; ++t) load(t);
+            for (int t = 0; ok && t < n; ++t) load(t);
             return ok;
         });
         // no copy may still be landing, nor a commit arriving, when the CTA ends
@@ -381,12 +408,13 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             (void)mbar_wait_bounded(&s.landed[t % STAGES], (t / STAGES) & 1);
             if (ok) ok = wait_weigh(s, &s.empty[t % STAGES], (t / STAGES) & 1, p.status);
         }
-        if (ok && k > 0) ok = wait_weigh(s, &s.k_free, (k - 1) & 1, p.status);
+        for (int t = max(0, k - C::KEY_SETS); ok && t < k; ++t)
+            ok = wait_weigh(s, &s.k_free[t % C::KEY_SETS], (t / C::KEY_SETS) & 1, p.status);
         if (rank == 1 && k > 0) (void)mbar_wait_bounded(&s.drained, 0);  // (the first CTA's commits reach this one's barriers)
     } else if (warp == C::MMA_WARP) {
         if (rank == 0 && elect_one()) {
             constexpr uint32_t KQ = mma_desc(CTAS * kTile, kTile, FP8, false);
-            const uint32_t k_d = smem_desc(smem_addr(keys), 0), q_d = smem_desc(smem_addr(ring), 0);
+            const uint32_t q_d = smem_desc(smem_addr(ring), 0);
             auto wait = [&](uint64_t *bar, uint32_t parity) {
                 return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, p.status);
             };
@@ -395,25 +423,26 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
                 if (n == 0) return true;
                 any = true;
-                bool ok = wait(DIRECT && !FP8 ? &s.k_landed : &s.k_ready, items & 1);
+                const int set = items % C::KEY_SETS;
+                bool ok = wait(&s.k_ready[set], (items / C::KEY_SETS) & 1);
                 for (int i = tiles; ok && i < tiles + n; ++i) {
-                    const int st = i % STAGES, buf = i & 1;
+                    const int st = i % STAGES;
                     ok = wait(DIRECT ? &s.landed[st] : &s.ready[st], (i / STAGES) & 1);
                     for (int stream = 0; ok && stream < STREAMS; ++stream) {
-                        if (i >= 2) ok = wait(&s.taken[stream][buf], ((i >> 1) - 1) & 1);
+                        const int t = i * STREAMS + stream, buf = t % C::SCORES;
+                        if (t >= C::SCORES) ok = wait(&s.taken[buf], (t / C::SCORES - 1) & 1);
                         if (!ok) break;
                         tc_after_sync();
-                        const uint32_t k = k_d + stream * (C::KEYS / 16), q = q_d + st * (C::Q_BYTES / 16);
-                        const uint32_t to = tmem + stream * (2 * kTile) + buf * kTile;
+                        const uint32_t k = tmem + C::KEY_COL + (set * STREAMS + stream) * (D / 2);
+                        const uint32_t q = q_d + st * (C::Q_BYTES / 16), to = tmem + buf * kTile;
 #pragma unroll
                         for (int x = 0; x < D / 16; ++x)
-                            mma_ss<CTAS>(to, k + (x / 4 * (kTile * 128) + x % 4 * 32) / 16,
-                                         q + (x / 4 * (C::Q_ROWS * 128) + x % 4 * 32) / 16, KQ, x > 0);
-                        mma_commit<CTAS>(&s.scores[stream][buf]);
+                            mma_ts<CTAS>(to, k + x * 8, q + (x / 4 * (C::Q_ROWS * 128) + x % 4 * 32) / 16, KQ, x > 0);
+                        mma_commit<CTAS>(&s.scores[buf]);
                     }
                     if (ok) mma_commit<CTAS>(&s.empty[st]);
                 }
-                if (ok) mma_commit<CTAS>(&s.k_free);
+                if (ok) mma_commit<CTAS>(&s.k_free[set]);
                 return ok;
             });
             // all products have completed before the tensor memory is given back
@@ -424,13 +453,9 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         }
         __syncwarp();
     } else if (warp == C::RELAY_WARP) {
-        // ---- a pair: what has landed here, for the first CTA's issuing thread
+        // ---- a pair: the query tiles that have landed here, for the first CTA's issuing thread
         each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
             bool ok = true;
-            if constexpr (!FP8) {
-                if (n > 0) ok = wait_weigh(s, &s.k_landed, items & 1, p.status);
-                if (n > 0 && ok) arrive_issuer(&s.k_ready);
-            }
             for (int i = tiles; ok && i < tiles + n; ++i) {
                 ok = wait_weigh(s, &s.landed[i % STAGES], (i / STAGES) & 1, p.status);
                 if (ok) arrive_issuer(&s.ready[i % STAGES]);
