@@ -251,29 +251,35 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                         tc_before_sync();
                         arrive_issuer(&s.taken[buf]);
                     }
-                    const int aj = lo - row0 - j, ej = hi - row0 - j;
-                    const uint64_t bits = (ej >= 64 ? ~0ull : ej <= 0 ? 0ull : (1ull << ej) - 1) &
-                                          (aj >= 64 ? 0ull : aj <= 0 ? ~0ull : ~((1ull << aj) - 1));
-                    auto add = [&](bool masked) {
+                    auto add = [&](int r, float2 y0, float2 y1) {
+                        sum[r / 2 % 4] = add2(sum[r / 2 % 4], make_float2(exp2_approx(y0.x), exp2_approx(y0.y)));
+                        sum[r / 2 % 4 + 1] = add2(sum[r / 2 % 4 + 1], make_float2(exp2_approx(y1.x), exp2_approx(y1.y)));
+                    };
+                    if (all) {
+#pragma unroll
+                        for (int r = 0; r < 64; r += 4) {
+                            const float4 l = *reinterpret_cast<const float4 *>(&mine[lbuf][j + r]);
+                            add(r, fma2(make_float2(x[r], x[r + 1]), c2, make_float2(l.x, l.y)),
+                                fma2(make_float2(x[r + 2], x[r + 3]), c2, make_float2(l.z, l.w)));
+                        }
+                    } else {
+                        const int a = lo - row0 - j, e = hi - row0 - j;
+                        const uint64_t bits = (e >= 64 ? ~0ull : e <= 0 ? 0ull : (1ull << e) - 1) &
+                                              (a >= 64 ? 0ull : a <= 0 ? ~0ull : ~((1ull << a) - 1));
 #pragma unroll
                         for (int r = 0; r < 64; r += 4) {
                             const float4 l = *reinterpret_cast<const float4 *>(&mine[lbuf][j + r]);
                             float2 y0 = fma2(make_float2(x[r], x[r + 1]), c2, make_float2(l.x, l.y));
                             float2 y1 = fma2(make_float2(x[r + 2], x[r + 3]), c2, make_float2(l.z, l.w));
-                            if (masked) {
-                                y0.x = bits >> r & 1 ? y0.x : -INFINITY;
-                                y0.y = bits >> (r + 1) & 1 ? y0.y : -INFINITY;
-                                y1.x = bits >> (r + 2) & 1 ? y1.x : -INFINITY;
-                                y1.y = bits >> (r + 3) & 1 ? y1.y : -INFINITY;
-                            }
-                            sum[r / 2 % 4] = add2(sum[r / 2 % 4], make_float2(exp2_approx(y0.x), exp2_approx(y0.y)));
-                            sum[r / 2 % 4 + 1] = add2(sum[r / 2 % 4 + 1], make_float2(exp2_approx(y1.x), exp2_approx(y1.y)));
+                            y0.x = bits >> r & 1 ? y0.x : -INFINITY;
+                            y0.y = bits >> (r + 1) & 1 ? y0.y : -INFINITY;
+                            y1.x = bits >> (r + 2) & 1 ? y1.x : -INFINITY;
+                            y1.y = bits >> (r + 3) & 1 ? y1.y : -INFINITY;
+                            // (or the compiler makes one form of both, with a selection for every weight)
+                            asm volatile("" : "+f"(y0.x), "+f"(y0.y), "+f"(y1.x), "+f"(y1.y));
+                            add(r, y0, y1);
                         }
-                    };
-                    if (all)
-                        add(false);
-                    else
-                        add(true);
+                    }
                 }
                 put(lbuf ^ 1);
             }
