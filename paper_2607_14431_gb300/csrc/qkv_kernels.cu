@@ -12,13 +12,15 @@
 // decode step's few rows the launch and one dependent load do.  A CTA takes a
 // run of tokens, one after the other, the next one's rows on their way while
 // the current one's are worked on; the cos and sin of a token's position, the
-// same for all its heads, are made once, in shared memory.  A head is D / 8
-// lanes of two 8-byte pieces: of a rotated half-pair head the same 4 columns of
-// both halves, so that no pair is split over lanes.  A lane keeps its columns
-// for all rows: weights, cos and sin stay in registers.
+// same for all its heads, are made once, in shared memory.  A head is D / 16
+// lanes of two 16-byte pieces: of a rotated half-pair head the same 8 columns of
+// both halves, so that no pair is split over lanes, and two columns go through
+// each instruction (f32x2).
 // One layer of 8,191 rows of the 12B shape (268 MB): 95.6 us with a CTA per
-// token and the other half of a pair fetched by shuffles, 56.3 us this way (4.8
-// TB/s; the rest of the time is instruction issue: some 60 a piece of a row).
+// token and the other half of a pair fetched by shuffles, 56.3 us with a CTA per
+// run of tokens and two 8-byte pieces a lane (136 instructions for a warp's 256
+// columns), 47.9 us this way (98; 5.6 TB/s), with the same bits.  What is left is
+// instruction issue and the latency of a lane's chain (half of the issue slots).
 //
 // The angle: p f_i / (2 pi) turns as a 64-bit fixed-point product that wraps at
 // whole turns.  What it is off by: the fraction in fp32 2^-26 turns, and p f_i /
@@ -33,75 +35,88 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace kvg {
 
 namespace {
 
 constexpr int kQkvThreads = 256;
-constexpr int kQkvUnroll = 4;  // rows of a lane in flight
+constexpr int kQkvUnroll = 2;  // rows of a lane in flight
 constexpr int kQkvTurns = 8;   // tokens whose angles are made together
 
-// Eight columns of a row as they are handled: pairs (a[i], b[i]).  A lane's two
-// pieces hold a and b (half pairs), or pairs side by side.
+// Sixteen columns of a row as they are handled: pairs (a, b), two to an
+// instruction.  A lane's two pieces of eight hold a and b (half pairs), or pairs
+// side by side.
+struct Columns {
+    float2 a[4], b[4];
+};
+__device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 template <bool HALF>
-__device__ __forceinline__ void unpack(const uint2 &x, const uint2 &y, float (&a)[4], float (&b)[4]) {
-    const uint32_t w[4] = {x.x, x.y, y.x, y.y};
+__device__ __forceinline__ Columns unpack(const uint4 &x, const uint4 &y) {
+    const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    Columns c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
         if constexpr (HALF) {
-            (i < 2 ? a : b)[2 * i % 4] = lo;
-            (i < 2 ? a : b)[2 * i % 4 + 1] = hi;
+            c.a[i] = make_float2(lo16(w[i]), hi16(w[i]));
+            c.b[i] = make_float2(lo16(w[4 + i]), hi16(w[4 + i]));
         } else {
-            a[i] = lo;
-            b[i] = hi;
+            c.a[i] = make_float2(lo16(w[2 * i]), lo16(w[2 * i + 1]));
+            c.b[i] = make_float2(hi16(w[2 * i]), hi16(w[2 * i + 1]));
         }
     }
+    return c;
 }
 
-// The eight values in the order of their columns.
+// Neighbouring columns 2 i and 2 i + 1 of the lane's.
 template <bool HALF>
-__device__ __forceinline__ float in_order(const float (&a)[4], const float (&b)[4], int i) {
-    return HALF ? (i < 4 ? a[i % 4] : b[i % 4]) : (i % 2 ? b[i / 2] : a[i / 2]);
+__device__ __forceinline__ float2 in_order(const Columns &c, int i) {
+    if constexpr (HALF)
+        return i < 4 ? c.a[i % 4] : c.b[i % 4];
+    else
+        return i % 2 ? make_float2(c.a[i / 2].y, c.b[i / 2].y) : make_float2(c.a[i / 2].x, c.b[i / 2].x);
 }
 
 template <bool HALF>
-__device__ __forceinline__ void pack_bf16(const float (&a)[4], const float (&b)[4], uint2 &x, uint2 &y) {
-    uint32_t w[4];
+__device__ __forceinline__ void pack_bf16(const Columns &c, uint4 &x, uint4 &y) {
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(in_order<HALF>(a, b, 2 * i), in_order<HALF>(a, b, 2 * i + 1));
+    for (int i = 0; i < 8; ++i) {
+        const float2 v = in_order<HALF>(c, i);
+        const __nv_bfloat162 t = __floats2bfloat162_rn(v.x, v.y);
         w[i] = *reinterpret_cast<const uint32_t *>(&t);
     }
-    x = make_uint2(w[0], w[1]);
-    y = make_uint2(w[2], w[3]);
+    x = make_uint4(w[0], w[1], w[2], w[3]);
+    y = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
 // fp32 times the reciprocal scale (one rounding), to the E4M3 grid (nearest
 // even, saturating at +-448), as every append into an fp8 cache.
 template <bool HALF>
-__device__ __forceinline__ void pack_e4m3(const float (&a)[4], const float (&b)[4], float inv_scale, uint32_t &x, uint32_t &y) {
-    uint32_t h[4];
+__device__ __forceinline__ void pack_e4m3(const Columns &c, float inv_scale, uint2 &x, uint2 &y) {
+    uint32_t h[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float lo = __fmul_rn(in_order<HALF>(a, b, 2 * i), inv_scale);
-        const float hi = __fmul_rn(in_order<HALF>(a, b, 2 * i + 1), inv_scale);
-        uint16_t c;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
-        h[i] = c;
+    for (int i = 0; i < 8; ++i) {
+        const float2 v = mul2(in_order<HALF>(c, i), make_float2(inv_scale, inv_scale));
+        uint16_t e;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(e) : "f"(v.y), "f"(v.x));
+        h[i] = e;
     }
-    x = h[0] | (h[1] << 16);
-    y = h[2] | (h[3] << 16);
+    x = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+    y = make_uint2(h[4] | (h[5] << 16), h[6] | (h[7] << 16));
 }
 
 template <int D, bool FP8, bool HALF>
 __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid_constant__ QkvParams p) {
-    constexpr int LPR = D / 8;               // lanes of a row
+    constexpr int LPR = D / 16;              // lanes of a row
     constexpr int RPP = kQkvThreads / LPR;   // rows that the CTA's threads hold at once
     constexpr int E = FP8 ? 1 : 2;           // bytes of a cached element
-    __shared__ float2 trig[kQkvTurns][D / 2];  // of some tokens
-    __shared__ int places[2][kMaxAxes][kQkvTurns];  // positions of them and of the next
+    // A lane's eight pairs lie in four float4s, LPR apart (no bank conflicts).
+    __shared__ float4 trig[kQkvTurns][4][LPR];      // cos and sin of two pairs each, of some tokens
+    __shared__ float4 weight[2][4][LPR];            // of queries and keys, offset included: a of two pairs, b of them
+    __shared__ int places[2][kMaxAxes][kQkvTurns];  // positions of those tokens and of the next
     const int lr = blockIdx.y;
     const int lane = threadIdx.x % LPR, grp = threadIdx.x / LPR;
     // the CTA's tokens [t0, end) of the launch
@@ -117,50 +132,49 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
             hi = mid - 1;
     }
     const int P = p.page_size, R = p.rotary_dim;
-    const bool turns = 8 * lane < R;  // the lane's columns are rotated
-    // its pieces: columns [c0, c0 + 4) and [c0 + c1, c0 + c1 + 4)
-    const int c0 = HALF && turns ? 4 * lane : 8 * lane, c1 = HALF && turns ? R / 2 : 4;
+    const bool turns = 16 * lane < R;  // the lane's columns are rotated
+    // its pieces: columns [c0, c0 + 8) and [c0 + c1, c0 + c1 + 8)
+    const int c0 = HALF && turns ? 8 * lane : 16 * lane, c1 = HALF && turns ? R / 2 : 8;
     const int n_q = p.n_q_heads, n_qk = n_q + p.n_kv_heads, n_rows = n_qk + p.n_kv_heads;
     const bool norms = p.q_norm || p.k_norm;
     const float eps = p.eps, k_inv = p.k_inv_scale, v_inv = p.v_inv_scale;
     const int64_t page_elems = (int64_t)p.n_kv_heads * P * D, out_token = (int64_t)n_q * D;
 
     after_previous();
-    float wq[8], wk[8];  // weights and offset, a then b of the lane's pairs
-#pragma unroll
-    for (int i = 0; i < 8; ++i) wq[i] = wk[i] = 1.f;
-    auto weights = [&](const uint16_t *w, float (&to)[8]) {
-        w += (int64_t)lr * D + c0;
-        float a[4], d[4];
-        unpack<HALF>(*reinterpret_cast<const uint2 *>(w), *reinterpret_cast<const uint2 *>(w + c1), a, d);
+    // (the first group of lanes for queries, the second for keys)
+    if (grp < 2 && (grp ? p.k_norm : p.q_norm)) {
+        const uint16_t *const from = (grp ? p.k_norm : p.q_norm) + (int64_t)lr * D + c0;
+        const float2 offset = make_float2(p.norm_offset, p.norm_offset);
+        const Columns w = unpack<HALF>(*reinterpret_cast<const uint4 *>(from), *reinterpret_cast<const uint4 *>(from + c1));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            to[i] = a[i] + p.norm_offset;
-            to[4 + i] = d[i] + p.norm_offset;
+            const float2 a = add2(w.a[i], offset), b = add2(w.b[i], offset);
+            weight[grp][i][lane] = make_float4(a.x, a.y, b.x, b.y);
         }
-    };
-    if (p.q_norm) weights(p.q_norm, wq);
-    if (p.k_norm) weights(p.k_norm, wk);
+    }
     // Cos and sin of the tokens [t, t + kQkvTurns): all threads for all of them,
     // so that two barriers serve eight tokens and no warp waits for another's
-    // few pairs (with a barrier per token half of the stalls were there).
-    const int pairs = R / 2;
+    // few pairs (with a barrier per token half of the stalls were there).  A thread
+    // makes those of one pair.
+    const int pair = threadIdx.x % (D / 2);
+    const uint64_t turn_of = pair < R / 2 ? p.turn[pair] : 0;
     auto fetch = [&](int t, int buf) {
         const int axis = threadIdx.x / kQkvTurns, k = threadIdx.x % kQkvTurns;
         if (axis < p.n_axes && t + k < end) places[buf][axis][k] = p.pos[axis * p.n_tokens + p.tok0 + t + k];
     };
     auto turn = [&](int t, int buf) {
         __syncthreads();  // the angles before are used, the positions are there
-        const int n = min(kQkvTurns, end - t) * pairs;
-        for (int i = threadIdx.x; i < n; i += kQkvThreads) {
-            const int k = i / pairs, pair = i - k * pairs;
-            const uint64_t turn = p.turn[pair];
-            // of a turn, times 2^64
-            const uint64_t frac = (uint64_t)(int64_t)places[buf][turn >> kAxisShift][k] * (turn & (((uint64_t)1 << kAxisShift) - 1));
-            float sv, cv;
-            sincospif((float)(int32_t)(frac >> 32) * 0x1p-31f, &sv, &cv);
-            trig[k][pair] = make_float2(cv * p.attention_factor, sv * p.attention_factor);
-        }
+        const int n = min(kQkvTurns, end - t);
+        if (pair < R / 2)
+            for (int k = threadIdx.x / (D / 2); k < n; k += kQkvThreads / (D / 2)) {
+                // of a turn, times 2^64
+                const uint64_t frac = (uint64_t)(int64_t)places[buf][turn_of >> kAxisShift][k] *
+                                      (turn_of & (((uint64_t)1 << kAxisShift) - 1));
+                float sv, cv;
+                sincospif((float)(int32_t)(frac >> 32) * 0x1p-31f, &sv, &cv);
+                reinterpret_cast<float2 *>(&trig[k][pair % 8 / 2][pair / 8])[pair % 2] =
+                    make_float2(cv * p.attention_factor, sv * p.attention_factor);
+            }
         __syncthreads();
     };
 
@@ -184,12 +198,12 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
                          ? reinterpret_cast<uint8_t *>(p.q_out + (lr * p.n_tokens + p.tok0 + t0) * out_token + head * D + c0)
                          : p.pool + ((((int64_t)(p.layer0 + lr) * 2 + (kind[u] == 2)) * p.pool_pages * p.n_kv_heads + head) * P * D + c0) * E;
         }
-        auto load = [&](uint2 (&x)[kQkvUnroll][2]) {
+        auto load = [&](uint4 (&x)[kQkvUnroll][2]) {
 #pragma unroll
             for (int u = 0; u < kQkvUnroll; ++u) {
                 if (kind[u] < 3) {
-                    x[u][0] = *reinterpret_cast<const uint2 *>(src[u]);
-                    x[u][1] = *reinterpret_cast<const uint2 *>(src[u] + c1);
+                    x[u][0] = *reinterpret_cast<const uint4 *>(src[u]);
+                    x[u][1] = *reinterpret_cast<const uint4 *>(src[u] + c1);
                 }
                 src[u] += step[u];
             }
@@ -197,11 +211,11 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
         // where token t goes: kept from token to token, looked up at a page's or a segment's end
         int b = b0 - 1, seg_end = t0, pg = 0, row = P - 1, buf = 0, k = kQkvTurns;
         int64_t at_slot = 0, at_query = 0;
-        uint2 xa[kQkvUnroll][2] = {}, xb[kQkvUnroll][2] = {};
+        uint4 xa[kQkvUnroll][2] = {}, xb[kQkvUnroll][2] = {};
         __syncthreads();  // (a batch before is done with the positions)
         fetch(t0, 0);
         load(xa);
-        auto token = [&](int t, const uint2 (&x)[kQkvUnroll][2], uint2 (&ahead)[kQkvUnroll][2]) {
+        auto token = [&](int t, const uint4 (&x)[kQkvUnroll][2], uint4 (&ahead)[kQkvUnroll][2]) {
             if (k == kQkvTurns) {
                 turn(t, buf);
                 fetch(t + kQkvTurns, buf ^= 1);
@@ -230,61 +244,71 @@ __global__ void __launch_bounds__(kQkvThreads, 2) append_qkv_kernel(const __grid
                     p.page_fill[seq * p.max_pages + pg] = row + 1;
                 }
             }
-            float c[4], s[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 cs = turns ? trig[k][4 * lane + i] : make_float2(1.f, 0.f);
-                c[i] = cs.x;
-                s[i] = cs.y;
-            }
-            ++k;
             if (t + 1 < end) load(ahead);  // the next token's, while this one's are worked on
 #pragma unroll
             for (int u = 0; u < kQkvUnroll; ++u) {
-                float f[4], g[4];
-                unpack<HALF>(x[u][0], x[u][1], f, g);
+                Columns y = unpack<HALF>(x[u][0], x[u][1]);
                 if (norms && __any_sync(0xffffffffu, kind[u] < 2)) {
-                    float ss = 0.f;
+                    // the first eight columns' sum and the others', each over the row's lanes
+                    float ss[2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) ss = __fmaf_rn(f[i], f[i], __fmaf_rn(g[i], g[i], ss));
+                    for (int h = 0; h < 2; ++h) {
+                        // (columns that are not rotated: four and four of a piece)
+                        const bool side = HALF && !turns;
+                        ss[h] = 0.f;
 #pragma unroll
-                    for (int o = LPR / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                    const float rms = rsqrtf(ss * (1.f / D) + eps);
-                    auto scale = [&](const float (&w)[8]) {
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 a = h && side ? y.b[i] : y.a[2 * h + i];
+                            const float2 d = side && !h ? y.a[2 + i] : y.b[2 * h + i];
+                            ss[h] = __fmaf_rn(a.x, a.x, __fmaf_rn(d.x, d.x, ss[h]));
+                            ss[h] = __fmaf_rn(a.y, a.y, __fmaf_rn(d.y, d.y, ss[h]));
+                        }
+                    }
+                    // (the lanes' halves take one sum each from the first step on)
+                    const bool second = lane & (LPR / 2);
+                    float v = second ? ss[1] : ss[0];
+                    v += __shfl_xor_sync(0xffffffffu, second ? ss[0] : ss[1], LPR / 2);
+#pragma unroll
+                    for (int o = LPR / 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                    v += __shfl_xor_sync(0xffffffffu, v, LPR / 2);
+                    const float rms = rsqrtf(v * (1.f / D) + eps);
+                    if (kind[u] < 2 && (kind[u] ? p.k_norm : p.q_norm)) {
+                        const float2 r = make_float2(rms, rms);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            f[i] *= rms * w[i];
-                            g[i] *= rms * w[4 + i];
+                            const float4 w = weight[kind[u]][i][lane];
+                            y.a[i] = mul2(y.a[i], mul2(r, make_float2(w.x, w.y)));
+                            y.b[i] = mul2(y.b[i], mul2(r, make_float2(w.z, w.w)));
                         }
-                    };
-                    if (kind[u] == 0 && p.q_norm) scale(wq);
-                    if (kind[u] == 1 && p.k_norm) scale(wk);
+                    }
                 }
                 if (kind[u] == 3) continue;
                 if (turns && kind[u] < 2) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float a = f[i], d = g[i];
-                        f[i] = __fmaf_rn(-d, s[i], a * c[i]);
-                        g[i] = __fmaf_rn(a, s[i], d * c[i]);
+                        const float4 cs = trig[k][i][lane];
+                        const float2 a = y.a[i], d = y.b[i], c = make_float2(cs.x, cs.z);
+                        y.a[i] = fma2(d, make_float2(-cs.y, -cs.w), mul2(a, c));
+                        y.b[i] = fma2(a, make_float2(cs.y, cs.w), mul2(d, c));
                     }
                 }
                 uint8_t *const to = dst[u] + (kind[u] ? at_slot : at_query);
                 if (!FP8 && kind[u] == 2) {
-                    *reinterpret_cast<uint2 *>(to) = x[u][0];
-                    *reinterpret_cast<uint2 *>(to + 2 * c1) = x[u][1];
+                    *reinterpret_cast<uint4 *>(to) = x[u][0];
+                    *reinterpret_cast<uint4 *>(to + 2 * c1) = x[u][1];
                 } else if (FP8 && kind[u]) {
-                    uint32_t y0, y1;
-                    pack_e4m3<HALF>(f, g, kind[u] == 2 ? v_inv : k_inv, y0, y1);
-                    *reinterpret_cast<uint32_t *>(to) = y0;
-                    *reinterpret_cast<uint32_t *>(to + c1) = y1;
-                } else {
                     uint2 y0, y1;
-                    pack_bf16<HALF>(f, g, y0, y1);
+                    pack_e4m3<HALF>(y, kind[u] == 2 ? v_inv : k_inv, y0, y1);
                     *reinterpret_cast<uint2 *>(to) = y0;
-                    *reinterpret_cast<uint2 *>(to + 2 * c1) = y1;
+                    *reinterpret_cast<uint2 *>(to + c1) = y1;
+                } else {
+                    uint4 y0, y1;
+                    pack_bf16<HALF>(y, y0, y1);
+                    *reinterpret_cast<uint4 *>(to) = y0;
+                    *reinterpret_cast<uint4 *>(to + 2 * c1) = y1;
                 }
             }
+            ++k;
             at_query += out_token * 2;
         };
         for (int t = t0; t < end; t += 2) {
