@@ -2728,8 +2728,13 @@ struct PromptWeights {
     std::vector<char> met;     // per sequence: decayed by this call
 };
 
-// Sums of weights that are kept at a time: of as many layers as fit.
-constexpr uint64_t kWeighBytes = 512ull << 20;
+// What kvg_attention_weights keeps at a time: a decode step's scores of all layers
+// and rows where they fit, else of a layer's rows as many as fit; a prompt's sums of
+// as many layers as fit.
+static uint64_t weights_scratch() {
+    static const int kb = env_knob("KVG_WEIGHTS_SCRATCH_KB", 512 << 10);
+    return 1024ull * kb;
+}
 
 // The work items of a launch's weights: pairs of key tiles, with the query tiles
 // split as plan_prompt splits keys.  An item costs its query tiles and kItemTiles
@@ -2857,7 +2862,7 @@ static kvg_status prompt_impl(kvg_cache *c, int32_t layer, const int32_t *seq_id
             }
             const int64_t floats = plan_weigh(c, G, w.get());
             const int64_t at_a_time =
-                std::max<int64_t>(1, std::min<int64_t>(p.n_layers_run, (int64_t)(kWeighBytes / sizeof(float)) / floats));
+                std::max<int64_t>(1, std::min<int64_t>(p.n_layers_run, (int64_t)(weights_scratch() / sizeof(float)) / floats));
             const int64_t n_lse = (int64_t)p.n_units * rows.total * G;
             KVG_CUDA(c->scores.ensure((size_t)(n_lse + slots + floats * at_a_time) * sizeof(float), c->capturing));
             w->p.row_lse = static_cast<float *>(c->scores.ptr);
@@ -3204,10 +3209,6 @@ extern "C" kvg_status kvg_decode_attention_shared(kvg_cache *c, int32_t layer, c
 
 // ------------------------------------------------------- attention's weights --
 
-// Scores of a decode step that are kept at a time: all layers' of all rows, else
-// a layer's of as many rows as fit.
-constexpr uint64_t kScoreBytes = 512ull << 20;
-
 // A decode step whose rows' weights are accumulated: one launch after the other
 // leaves its scores, and what their sum needs, in the cache's scratch.
 static kvg_status decode_weights(kvg_cache *c, int32_t layer, const std::vector<int32_t> &seqs, const void *q,
@@ -3220,14 +3221,14 @@ static kvg_status decode_weights(kvg_cache *c, int32_t layer, const std::vector<
     if (w_max <= 0) return fail(KVG_ERR_CUDA, "decode kernel cannot be made resident");
     uint64_t slots = 0;
     for (int32_t sq : seqs) slots += c->n_slots[sq];
-    const bool together = layer >= 0 || slots * d.n_layers * n_q_heads * sizeof(float) <= kScoreBytes;
+    const bool together = layer >= 0 || slots * d.n_layers * n_q_heads * sizeof(float) <= weights_scratch();
     const int TOK = decode_tile_tokens(d.head_dim, fp8, d.page_size), tpp = (d.page_size + TOK - 1) / TOK;
     const int32_t l0 = together ? layer : 0, l1 = together ? layer + 1 : d.n_layers;
     for (int32_t b0 = 0, b1; b0 < B; b0 = b1) {
         slots = 0;
         for (b1 = b0; b1 < B; ++b1) {
             slots += c->n_slots[seqs[b1]];
-            if (b1 > b0 && slots * n_q_heads * sizeof(float) > kScoreBytes) break;
+            if (b1 > b0 && slots * n_q_heads * sizeof(float) > weights_scratch()) break;
         }
         for (int32_t l = l0; l < l1; ++l) {
             std::vector<DecodeParams> plan;

@@ -17,6 +17,9 @@ worst and sqrt(2,048) 2^-24 = 2^-18.5 for errors of no common sign.  So weights 
 within 4 (S sqrt(D) 2^-22 + 2^-18.5 + 2^-20) of themselves, the 4 for the maximum
 over many."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -380,3 +383,11 @@ def test_refusals(kvg):
     assert not out.any() and not weights.any()
     v = bed.cache.view
     assert dev_view(v.page_fill, 4, torch.int32).item() == 16
+
+
+def test_little_scratch(kvg):
+    """What does not fit the scratch at once is done layer by layer, rows by rows: the same tests with 8 KB of it."""
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", __file__, "-k",
+                        "many_sequences or layers_of_different or unfilled or plain_calls"],
+                       env=os.environ | {"KVG_WEIGHTS_SCRATCH_KB": "8"}, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-3000:]

@@ -151,6 +151,18 @@ def test_lengths_around_the_chunks(kvg, n):
         evict(bed, [0], [keep], 0, 0)
 
 
+@pytest.mark.parametrize("how", ["in place", "to another"])
+@pytest.mark.parametrize("ties", [False, True])
+def test_more_rows_than_a_cluster_holds_at_once(kvg, how, ties):
+    n = 70001
+    bed = Bed(kvg, 1, 1, 64, 64, 2200, 2, 70100)
+    bed.append(0, n)
+    w = heavy_tailed(bed.rng, n)
+    bed.set_weights(0, np.round(w) if ties else w)
+    for keep, first, last in [(66000, 4, 1000), (40000, 4, 33000), (5000, 0, 0), (33, 3, 0)]:
+        evict(bed, [0], [keep], first, last, None if how == "in place" else [1])
+
+
 WEIGHTS = {
     "all equal": lambda rng, n: np.full(n, 0.25),
     "zeros of both signs": lambda rng, n: np.where(rng.random(n) < 0.5, 0.0, -0.0),
