@@ -2615,6 +2615,10 @@ constexpr int kPromptCols = 128;  // columns of a key tile
 // With 1, 2, 3 and 5 for kItemTiles (single calls on an idle GPU): 8,192 rows of the 31B shape on 16,384
 // 1,979, 1,616, 1,617 and 1,616 us, 499 rows of the 12B shape on 8,192 79.0,
 // 79.3, 62.8 and 62.6, 37 rows of the tiny shape 15.7, 16.9, 14.4 and 14.3.
+// Cross attention's items differ in length as its sequences do, and SMs take the
+// next one when they are free, the longest first: there half an item at the end
+// stands for the last round (24 sequences of 257 to 4,099 rows of the 12B shape, 2 to
+// 5 query rows each: 86.3 us by whole rounds, which split the long ones, 81.2 so).
 // Returns the partial results' slots (0: nothing is split).
 static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &work, int G, int tile_rows, bool always,
                            PromptParams *p) {
@@ -2647,7 +2651,9 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
             top = std::max(top, r.longest / s + kItemTiles);
         }
         const double mean = total / items;
-        const double est = std::max(top, std::ceil(items / at_once) * mean) + (len < longest ? kItemTiles : 0.0);
+        const bool uneven = p->span && !p->shared;
+        const double all = uneven ? total / at_once + mean / 2 : std::ceil(items / at_once) * mean;
+        const double est = std::max(top, all) + (len < longest ? kItemTiles : 0.0);
         if (est < best) {
             best = est;
             best_len = len;
