@@ -655,8 +655,8 @@ kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *
  * kvg_decode_attention does.  A sequence may be named more than once; rows of a
  * sequence without rows get 0.  q, out, sums, layers, group sizes, fp8 queries
  * and values that are not attended to as for kvg_prompt_attention.  Where every
- * n_rows[b] is 1 this is kvg_decode_attention.  Errors: as for
- * kvg_decode_attention, and KVG_ERR_ARG for a negative n_rows[b]. */
+ * n_rows[b] is 1 this is kvg_decode_attention; a few rows a sequence are taken at a
+ * decode's rate.  Errors: as for kvg_decode_attention, and KVG_ERR_ARG for a negative n_rows[b]. */
 kvg_status kvg_cross_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
                                int32_t B, const void *q, int32_t n_q_heads, void *out, float scale, void *stream);
 

@@ -10,7 +10,7 @@ template <int D, int COLS>
 __global__ void __launch_bounds__(kCombineMaxThreads) combine_kernel(const DecodeParams p) {
     constexpr int PARTS = D / COLS;
     const int h = blockIdx.x / PARTS, col0 = blockIdx.x % PARTS * COLS, b = blockIdx.y, lr = blockIdx.z;
-    write_output<COLS>(p, merge_partials<D, COLS>(p, h, col0, b, lr), h, col0, b, lr, D);
+    write_output<COLS>(p, merge_partials<D, COLS>(p, h, col0, b, lr), out_head(p, h, b, lr), col0, D);
 }
 
 // Merge of a decode whose rows read some of their pages together
@@ -233,7 +233,7 @@ int decode_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm)
     const int tok = decode_tile_tokens(head_dim, fp8, page_size);
 #define KVG_CASE(DD, GG, FF, TT)                                        \
     if (head_dim == DD && group == GG && fp8 == FF && tok == TT)        \
-        return DecodeLaunch<DD, GG, FF, TT, false>::max_blocks_per_sm() * n_sm;
+        return DecodeLaunch<DD, GG, FF, TT>::max_blocks_per_sm() * n_sm;
     KVG_DECODE_CASES(KVG_CASE)
 #undef KVG_CASE
     return 0;
@@ -244,7 +244,7 @@ cudaError_t launch_decode(int head_dim, int group, bool fp8, const DecodeParams 
     const int tok = decode_tile_tokens(head_dim, fp8, p.page_size);
 #define KVG_CASE(DD, GG, FF, TT)                                        \
     if (head_dim == DD && group == GG && fp8 == FF && tok == TT)        \
-        return DecodeLaunch<DD, GG, FF, TT, false>::run(p, pool_map, {}, s);
+        return DecodeLaunch<DD, GG, FF, TT>::run(p, pool_map, {}, s);
     KVG_DECODE_CASES(KVG_CASE)
 #undef KVG_CASE
     return cudaErrorInvalidValue;

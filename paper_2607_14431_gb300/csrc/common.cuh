@@ -370,6 +370,15 @@ struct Divisor {
 #endif
 };
 
+// A decode whose batch rows are some query rows of a sequence each: row b has the
+// packed rows from row0[b] on, heads[b] = rows x group heads to a KV head (at most
+// kRowHeads, which the launch takes for its group).
+constexpr int kRowHeads = 8;
+struct RowParams {
+    int64_t q_rows;            // packed rows of the whole call
+    int32_t n_q_heads, log2_group;
+    int32_t row0[kMaxBatchPerLaunch], heads[kMaxBatchPerLaunch];
+};
 // A decode that also gives what weight each row received: its scores (scale *
 // log2(e) * q.k) of run layer lr, batch row b and query head h are at
 // scores[at[b] + (lr * n_q_heads + h) * n[b] + slot].
@@ -648,6 +657,10 @@ cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows,
 cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
 // Threads of a combine block over `cols` columns of a head.
 int combine_threads(int cols, const DecodeParams &p);
+// The decode of several query rows at a time and its combine.
+int decode_rows_max_warps(int head_dim, bool fp8, int page_size, int n_sm);
+cudaError_t launch_decode_rows(int head_dim, bool fp8, const DecodeParams &p, const RowParams &rows,
+                               const CUtensorMap &pool_map, int n_sm, cudaStream_t s);
 // The decode with its scores; then the combine and, beside it, the rows' weights.
 // decode_scores_max_warps(): as decode_max_warps(), of that decode kernel.
 int decode_scores_max_warps(int head_dim, int group, bool fp8, int page_size, int n_sm);

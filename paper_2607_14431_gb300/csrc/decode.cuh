@@ -150,6 +150,10 @@ __device__ __forceinline__ void next_unit(const DecodeParams &p, TilePos &r) {
     r.unit = ((int64_t)r.lr * p.B + r.b) * p.n_kv_heads + r.g;
 }
 
+// Row of q and out.
+__device__ __forceinline__ int64_t out_head(const DecodeParams &p, int h, int b, int lr) {
+    return (int64_t)(p.qlayers[lr] * p.q_row_stride_b + p.b0 + b) * p.n_q_heads + h;
+}
 // Row of q that the unit's first query head has.
 template <int G>
 __device__ __forceinline__ int64_t q_row(const DecodeParams &p, const TilePos &r) {
@@ -239,13 +243,16 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two_codes) {
     return d;
 }
 
-// SCORES: each row's scores are stored as well, and the sum of the weights as they
-// are before their rounding to 16 bits, which the accumulated weights are divided by.
-struct NoScores {};
-template <int D, int G, bool FP8, int TOK_, bool SCORES>
+// Forms beside the plain one, by what comes with the launch.  ScoreParams: each
+// row's scores are stored as well, and the sum of the weights as they are before
+// their rounding to 16 bits, which the accumulated weights are divided by.
+// RowParams: a batch row is some query rows of a sequence, their heads side by side
+// where a decode has one row's (the MMA takes eight whatever they are).
+struct Plain {};
+template <int D, int G, bool FP8, int TOK_, class Form>
 __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
-    decode_kernel(const DecodeParams p, const __grid_constant__ CUtensorMap pool_map,
-                  const __grid_constant__ std::conditional_t<SCORES, ScoreParams, NoScores> sp) {
+    decode_kernel(const DecodeParams p, const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ Form sp) {
+    constexpr bool SCORES = std::is_same_v<Form, ScoreParams>, ROWS = std::is_same_v<Form, RowParams>;
     using C = Cfg<D, FP8, TOK_>;
     constexpr int TOK = C::TOK, STAGES = C::STAGES, KS = C::KS, SUB = C::SUB, NB = C::NB, BOX = C::BOX;
     constexpr int NB8 = C::NB8;
@@ -322,7 +329,7 @@ __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
         const bool entered = cur.t >= cur.end;
         if (entered) {
             advance_to_unit();
-            if (C::WALK && cur.t != t0) {
+            if (C::WALK && !ROWS && cur.t != t0) {
                 // the unit's queries, some tiles before they are read
                 const uint8_t *qp = reinterpret_cast<const uint8_t *>(p.q + q_row<G>(p, cur.tp) * D);
 #pragma unroll
@@ -405,7 +412,10 @@ __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
     float m[2], lsum[2];  // running max / partial sum of heads 2*tq, 2*tq+1
     float lx[2];          // SCORES: the sum of the weights as they are
 
-    auto flush = [&](int64_t unit) {
+    auto flush = [&](const TilePos &at) {
+        const int64_t unit = at.unit;
+        int heads = G;
+        if constexpr (ROWS) heads = sp.heads[at.b];
         float lt[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -419,7 +429,7 @@ __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int h = 2 * tq + e;
-            if (h < G) {
+            if (h < heads) {
                 float *dst = p.part_o + (slot * G + h) * D;
 #pragma unroll
                 for (int mt = 0; mt < KS; ++mt) {
@@ -439,19 +449,28 @@ __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
     };
 
     auto begin = [&](const TilePos &tp) {
-        const __nv_bfloat16 *qrow = p.q + q_row<G>(p, tp) * D;
+        int64_t head = gq;  // of q
+        int heads = G;
+        if constexpr (ROWS) {
+            heads = sp.heads[tp.b];
+            head = (p.qlayers[tp.lr] * sp.q_rows + sp.row0[tp.b] + (gq >> sp.log2_group)) * sp.n_q_heads +
+                   (tp.g << sp.log2_group) + (gq & ((1 << sp.log2_group) - 1));
+        } else {
+            head += q_row<G>(p, tp);
+        }
+        const __nv_bfloat16 *qhead = p.q + head * D;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            if (gq < G) {
+            if (gq < heads) {
                 if constexpr (FP8) {
                     // fp16 MMAs over permuted dims: within each 16-dim step the
                     // MMA's k = 2tq, 2tq+1, 2tq+8, 2tq+9 are dims 4tq .. 4tq+3, so a
                     // key row's 4 consecutive codes fill a lane's two registers
-                    const uint32_t *q32 = reinterpret_cast<const uint32_t *>(qrow + gq * D + 16 * ks + 4 * tq);
+                    const uint32_t *q32 = reinterpret_cast<const uint32_t *>(qhead + 16 * ks + 4 * tq);
                     qb[ks][0] = pack16<true>(lo16<false>(q32[0]), hi16<false>(q32[0]));
                     qb[ks][1] = pack16<true>(lo16<false>(q32[1]), hi16<false>(q32[1]));
                 } else {
-                    const uint32_t *q32 = reinterpret_cast<const uint32_t *>(qrow + gq * D + 16 * ks + 2 * tq);
+                    const uint32_t *q32 = reinterpret_cast<const uint32_t *>(qhead + 16 * ks + 2 * tq);
                     qb[ks][0] = q32[0];
                     qb[ks][1] = q32[4];  // dims + 8
                 }
@@ -479,7 +498,7 @@ __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
         if (t == t1 - 1) let_next_start();
         const uint32_t par = (uint32_t)((i / STAGES) & 1);
         if (t >= unit_end) {
-            if (unit_end > t0) flush(rd.unit);
+            if (unit_end > t0) flush(rd);
             if (!C::WALK || unit_end == t0)
                 rd = locate(p, t);
             else
@@ -664,7 +683,7 @@ __global__ void __launch_bounds__(32, FP8 && D == 128 ? 16 : 0)
         lsum[0] = lsum[1] = 0.f;
         lx[0] = lx[1] = 0.f;
     }
-    if (unit_end > t0) flush(rd.unit);
+    if (unit_end > t0) flush(rd);
 }
 
 // Largest warp index whose range starts at or before tile t.
@@ -780,22 +799,21 @@ __device__ __forceinline__ Merged merge_partials(const DecodeParams &p, int h, i
     return res;
 }
 
-// The output columns of a merged head.
+// Columns from col0 on of a merged head, to row `head` of the outputs.
 template <int COLS>
-__device__ __forceinline__ void write_output(const DecodeParams &p, const Merged &m, int h, int col0, int b, int lr, int D) {
+__device__ __forceinline__ void write_output(const DecodeParams &p, const Merged &m, int64_t head, int col0, int D) {
     if (threadIdx.x >= COLS / 4) return;
     float r[4] = {m.o.x, m.o.y, m.o.z, m.o.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) r[e] = m.L > 0.f ? __fdiv_rn(r[e], m.L) * p.vscale : 0.f;
     const __nv_bfloat162 lo = __floats2bfloat162_rn(r[0], r[1]), hi = __floats2bfloat162_rn(r[2], r[3]);
-    uint2 *out = reinterpret_cast<uint2 *>(
-        p.out + ((int64_t)(p.qlayers[lr] * p.q_row_stride_b + p.b0 + b) * p.n_q_heads + h) * D + col0);
+    uint2 *out = reinterpret_cast<uint2 *>(p.out + head * D + col0);
     out[threadIdx.x] = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
 }
 
-template <int D, int G, bool FP8, int TOK, bool SCORES>
+template <int D, int G, bool FP8, int TOK, class Form = Plain>
 struct DecodeLaunch {
-    static constexpr auto kernel = decode_kernel<D, G, FP8, TOK, SCORES>;
+    static constexpr auto kernel = decode_kernel<D, G, FP8, TOK, Form>;
     // The shared-memory attribute is per device: set and cached per device.
     static int max_blocks_per_sm() {
         static std::atomic<int> cached[kMaxDevices];  // 0 = not yet known
@@ -812,8 +830,7 @@ struct DecodeLaunch {
         cached[dev].store(n);
         return n;
     }
-    static cudaError_t run(const DecodeParams &p, const CUtensorMap &map,
-                           const std::conditional_t<SCORES, ScoreParams, NoScores> &sp, cudaStream_t s) {
+    static cudaError_t run(const DecodeParams &p, const CUtensorMap &map, const Form &sp, cudaStream_t s) {
         if (max_blocks_per_sm() <= 0) return cudaErrorInvalidConfiguration;
         if (p.n_tiles <= 0) return cudaSuccess;
         return launch_after(kernel, p.n_warps[0] + p.n_warps[1], 32, Cfg<D, FP8, TOK>::SMEM, s, p, map, sp);

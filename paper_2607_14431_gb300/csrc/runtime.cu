@@ -2917,6 +2917,69 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
 
 // ----------------------------------------------------------- cross attention --
 
+// Whether the decode kernel takes the rows, kRowHeads heads (kRowHeads / G rows) of a
+// sequence at a time: where its keys and values are read once that way, of an fp8
+// cache of long sequences up to twice (the prompt kernel multiplies tiles of 128 or
+// 256 rows whatever is in them, and converts E4M3 codes first).  24 sequences of 257
+// to 4,099 rows with 2, 4, 8 and 12 query rows each, G = 2, by the prompt kernel and
+// so: 12B shape 79 and 75, 79 and 79, 79 and 134 us, fp8 92 and 48, 92 and 52, 92 and
+// 77, 92 and 107; 31B shape 75 and 79, 76 and 83, fp8 82 and 45, 83 and 48, 84 and 78,
+// 84 and 112; one sequence of 12,000 with 4 of the 12B shape 38 and 22, fp8 39 and 18;
+// 8 sequences of 100 to 400 with 8, fp8, 15 and 20.
+static bool few_rows(const kvg_cache *c, const int32_t *seq_ids, const int32_t *n_rows, int32_t B, int G) {
+    const int32_t at_once = kRowHeads / G;
+    int64_t once = 0, reads = 0, n = 0;  // slots, slots, sequences
+    for (int32_t b = 0; b < B; ++b) {
+        const int64_t slots = c->n_slots[seq_ids[b]];
+        if (!n_rows[b] || !slots) continue;
+        ++n;
+        once += slots;
+        reads += slots * ((n_rows[b] + at_once - 1) / at_once);
+    }
+    return reads <= once || (c->dims.kv_dtype == KVG_KV_E4M3 && once >= 1000 * n && reads <= 2 * once);
+}
+
+// The packed rows as a decode whose batch rows are kRowHeads / G query rows of a
+// sequence each.
+static kvg_status decode_rows(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows, int32_t B,
+                              const void *q, int32_t n_q_heads, void *out, float scale, int G, int64_t total,
+                              cudaStream_t st) {
+    const kvg_dims &d = c->dims;
+    const bool fp8 = d.kv_dtype == KVG_KV_E4M3;
+    const int32_t at_once = kRowHeads / G;
+    std::vector<int32_t> seqs, row0, heads;
+    for (int32_t b = 0, row = 0; b < B; row += n_rows[b++])
+        for (int32_t r = 0; r < n_rows[b]; r += at_once) {
+            seqs.push_back(seq_ids[b]);
+            row0.push_back(row + r);
+            heads.push_back(std::min(at_once, n_rows[b] - r) * G);
+        }
+    const int32_t n = (int32_t)seqs.size(), n_heads = kRowHeads * d.n_kv_heads;
+    const int w_max = decode_rows_max_warps(d.head_dim, fp8, d.page_size, c->n_sm);
+    if (w_max <= 0) return fail(KVG_ERR_CUDA, "decode kernel cannot be made resident");
+    std::vector<DecodeParams> plan;
+    if (kvg_status r = plan_decode(c, layer, seqs.data(), n, kRowHeads, w_max, &plan); r != KVG_OK) return r;
+    const size_t slots = (size_t)decode_slots(plan, w_max);
+    KVG_CUDA(c->part_o.ensure(slots * kRowHeads * d.head_dim * sizeof(float), c->capturing));
+    KVG_CUDA(c->part_ml.ensure(slots * kRowHeads * sizeof(float2), c->capturing));
+    RowParams rows;
+    rows.q_rows = total;
+    rows.n_q_heads = n_q_heads;
+    rows.log2_group = 0;
+    while (1 << rows.log2_group < G) ++rows.log2_group;
+    for (DecodeParams &p : plan) {
+        decode_call(c, q, n_heads, out, scale, n, w_max, &p);
+        p.part_o = static_cast<float *>(c->part_o.ptr);
+        p.part_ml = static_cast<float2 *>(c->part_ml.ptr);
+        for (int32_t i = 0; i < p.B; ++i) {
+            rows.row0[i] = row0[p.b0 + i];
+            rows.heads[i] = heads[p.b0 + i];
+        }
+        KVG_CUDA(launch_decode_rows(d.head_dim, fp8, p, rows, c->pool_map, c->n_sm, st));
+    }
+    return KVG_OK;
+}
+
 extern "C" kvg_status kvg_cross_attention(kvg_cache *c, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,
                                           int32_t B, const void *q, int32_t n_q_heads, void *out, float scale,
                                           void *stream) {
@@ -2942,10 +3005,15 @@ extern "C" kvg_status kvg_cross_attention(kvg_cache *c, int32_t layer, const int
     if (single)
         return decode_impl("kvg_cross_attention", c, layer, seq_ids, B, q, n_q_heads, out, scale, stream, 0, INT32_MAX,
                            nullptr, 0);
-    std::stable_sort(order.begin(), order.end(),
-                     [&](int32_t a, int32_t b) { return c->n_slots[seq_ids[a]] > c->n_slots[seq_ids[b]]; });
     DeviceGuard g(c->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (few_rows(c, seq_ids, n_rows, B, G)) {
+        KVG_CUDA(use_partials(c, st));
+        if (kvg_status r = decode_rows(c, layer, seq_ids, n_rows, B, q, n_q_heads, out, scale, G, total, st); r != KVG_OK) return r;
+        return used_partials(c, st);
+    }
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int32_t a, int32_t b) { return c->n_slots[seq_ids[a]] > c->n_slots[seq_ids[b]]; });
     const size_t row_bytes = (size_t)n_q_heads * d.head_dim * sizeof(__nv_bfloat16);
     for (int32_t b : none)
         KVG_CUDA(cudaMemset2DAsync(static_cast<uint8_t *>(out) + row0[b] * row_bytes, total * row_bytes, 0,

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kCombineMaxThreads)
     const int lr = i / (p.n_q_heads * PARTS);
     i -= lr * p.n_q_heads * PARTS;
     const int h = i / PARTS, col0 = i % PARTS * COLS, b = blockIdx.y;
-    write_output<COLS>(p, merge_partials<D, COLS>(p, h, col0, b, lr), h, col0, b, lr, D);
+    write_output<COLS>(p, merge_partials<D, COLS>(p, h, col0, b, lr), out_head(p, h, b, lr), col0, D);
 }
 
 }  // namespace
@@ -165,7 +165,7 @@ int decode_scores_max_warps(int head_dim, int group, bool fp8, int page_size, in
     const int tok = decode_tile_tokens(head_dim, fp8, page_size);
 #define KVG_CASE(DD, GG, FF, TT)                                        \
     if (head_dim == DD && group == GG && fp8 == FF && tok == TT)        \
-        return DecodeLaunch<DD, GG, FF, TT, true>::max_blocks_per_sm() * n_sm;
+        return DecodeLaunch<DD, GG, FF, TT, ScoreParams>::max_blocks_per_sm() * n_sm;
     KVG_DECODE_CASES(KVG_CASE)
 #undef KVG_CASE
     return 0;
@@ -177,7 +177,7 @@ cudaError_t launch_decode_weights(int head_dim, int group, bool fp8, const Decod
     cudaError_t e = cudaErrorInvalidValue;
 #define KVG_CASE(DD, GG, FF, TT)                                        \
     if (head_dim == DD && group == GG && fp8 == FF && tok == TT)        \
-        e = DecodeLaunch<DD, GG, FF, TT, true>::run(p, pool_map, a.scores, s);
+        e = DecodeLaunch<DD, GG, FF, TT, ScoreParams>::run(p, pool_map, a.scores, s);
     KVG_DECODE_CASES(KVG_CASE)
 #undef KVG_CASE
     if (e != cudaSuccess) return e;

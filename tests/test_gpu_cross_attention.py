@@ -98,9 +98,52 @@ def test_lengths_around_the_tiles(kvg, d, g, fp8, n):
     run(bed, g, [2, 0], [n, 3])
 
 
+@pytest.mark.parametrize("hkv,g,d,page,fp8", [
+    (2, 1, 64, 16, False), (2, 2, 64, 64, False), (1, 8, 64, 24, False), (2, 4, 64, 7, False),
+    (3, 2, 128, 64, False), (2, 4, 128, 16, False), (1, 1, 128, 48, False), (2, 1, 256, 64, False), (2, 2, 256, 16, False),
+    (2, 2, 128, 64, True), (1, 4, 128, 16, True), (2, 1, 128, 32, True), (2, 2, 256, 64, True), (1, 1, 256, 48, True)])
+def test_a_few_rows_each(kvg, hkv, g, d, page, fp8):
+    """Rows that the decode kernel takes, all of a sequence's at once or (fp8, long states) in two turns."""
+    total = [1, 900, 33, 0, 2100, 64, 1500]
+    bed = States(kvg, 2, hkv, d, page, total, fp8)
+    most = 8 // g
+    rng = np.random.default_rng(d + g)
+    for rows in ([most] * 7, list(rng.integers(0, most + 1, 7)), [0, most, 0, 1, 0, 0, most]):
+        rows = [int(x) for x in rows]
+        args = bed, hkv * g, [0, 1, 2, 3, 4, 5, 6], rows
+        assert torch.equal(run(*args, layer=-1).view(torch.int16), run(*args, layer=-1).view(torch.int16))
+        kvg.kvg_cache_set_layer_windows(bed.cache.h, [100, 0])
+        run(*args, [100, 0], layer=-1)
+        run(*args, 100, layer=0)
+        kvg.kvg_cache_set_layer_windows(bed.cache.h, [])
+    run(bed, hkv * g, [4, 6, 1], [2 * most, most + 1, 1])
+    run(bed, hkv * g, [4, 4, 0, 4], [most, 1, most, most])
+
+
+def test_a_few_rows_of_many_sequences(kvg):
+    n = 300
+    bed = States(kvg, 1, 1, 128, 16, [(b * 37) % 90 for b in range(n)])
+    run(bed, 2, list(range(n)), [(b * 13) % 5 for b in range(n)])
+
+
+def test_a_few_rows_on_grafted_blocks(kvg):
+    bed = Bed(kvg, 1, 2, 128, 64, 40, 3, 1024)
+    store = kvg.Store(bed.dims, kvg.KVG_RESIDENCY_HBM, 1 << 28)
+    bed.append(2, 150, 1)
+    block = kvg.kvg_deposit(store.h, bed.cache.h, 2, 0, 75)
+    for _ in range(3):
+        kvg.kvg_graft(store.h, block, bed.cache.h, 0)
+    bed.total = [225, 0, 150]
+    for window in (0, 70):
+        kvg.kvg_cache_set_layer_windows(bed.cache.h, [window])
+        run(bed, 4, [0, 1, 2], [4, 3, 2], window)
+
+
 def test_states_of_no_rows(kvg):
     """Rows of an empty sequence get zeros, among others and alone, in every layer."""
     bed = States(kvg, 2, 2, 128, 64, [0, 100, 0], extra=4)
+    out = run(bed, 4, [0, 1, 2], [3, 4, 2], layer=-1)  # (few)
+    assert not out[:, :3].any() and not out[:, 7:].any() and out[:, 3:7].all(-1).all()
     out = run(bed, 4, [0, 1, 2, 0], [3, 5, 70, 0], layer=-1)
     assert not out[:, :3].any() and not out[:, 8:].any() and out[:, 3:8].all(-1).all()
     assert not run(bed, 4, [0, 2], [2, 2]).any()
