@@ -2618,7 +2618,10 @@ constexpr int kPromptCols = 128;  // columns of a key tile
 // Cross attention's items differ in length as its sequences do, and SMs take the
 // next one when they are free, the longest first: there half an item at the end
 // stands for the last round (24 sequences of 257 to 4,099 rows of the 12B shape, 2 to
-// 5 query rows each: 86.3 us by whole rounds, which split the long ones, 81.2 so).
+// 5 query rows each: 86.3 us by whole rounds, which split the long ones, 81.2 so),
+// and what partial results take to write and read (at 5 TB/s, a key tile 1.3 us) is
+// counted: 8,191 rows of the 31B shape on 12,001 would be split for it to even out
+// the last round, 1,252 us instead of 1,066.
 // Returns the partial results' slots (0: nothing is split).
 static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &work, int G, int tile_rows, bool always,
                            PromptParams *p) {
@@ -2643,16 +2646,19 @@ static int64_t plan_prompt(const kvg_cache *c, const std::vector<PromptWork> &wo
     }
     double best = INFINITY, best_len = longest;
     for (double len = longest; len >= 1.0; len *= 0.84) {
-        double items = 0, total = 0, top = 0;
-        for (const Row &r : rows) {
+        double items = 0, total = 0, top = 0, partials = 0;  // partials: of rows
+        for (size_t i = 0; i < rows.size(); ++i) {
+            const Row &r = rows[i];
             const double s = std::max(1.0, std::ceil(r.longest / len - 1e-9));
+            if (s > 1) partials += s * work[i].rows * p->n_units;
             items += s * r.tiles * p->n_units;
             total += r.tiles * p->n_units * (r.mean + s * kItemTiles);
             top = std::max(top, r.longest / s + kItemTiles);
         }
         const double mean = total / items;
         const bool uneven = p->span && !p->shared;
-        const double all = uneven ? total / at_once + mean / 2 : std::ceil(items / at_once) * mean;
+        const double moved = partials * c->dims.head_dim * 8 / 5e6 / 1.3;  // in key tiles
+        const double all = uneven ? total / at_once + mean / 2 + moved : std::ceil(items / at_once) * mean;
         const double est = std::max(top, all) + (len < longest ? kItemTiles : 0.0);
         if (est < best) {
             best = est;
