@@ -2934,14 +2934,16 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
 // 8 sequences of 100 to 400 with 8, fp8, 15 and 20.
 static bool few_rows(const kvg_cache *c, const int32_t *seq_ids, const int32_t *n_rows, int32_t B, int G) {
     const int32_t at_once = kRowHeads / G;
-    int64_t once = 0, reads = 0, n = 0;  // slots, slots, sequences
+    int64_t once = 0, reads = 0, n = 0, items = 0;  // slots, slots, sequences, batch rows of the decode
     for (int32_t b = 0; b < B; ++b) {
-        const int64_t slots = c->n_slots[seq_ids[b]];
+        const int64_t slots = c->n_slots[seq_ids[b]], times = ((int64_t)n_rows[b] + at_once - 1) / at_once;
+        items += times;
         if (!n_rows[b] || !slots) continue;
         ++n;
         once += slots;
-        reads += slots * ((n_rows[b] + at_once - 1) / at_once);
+        reads += slots * times;
     }
+    if (items > 4 * (int64_t)B) return false;  // (many rows of short or empty sequences beside long ones)
     return reads <= once || (c->dims.kv_dtype == KVG_KV_E4M3 && once >= 1000 * n && reads <= 2 * once);
 }
 

@@ -164,6 +164,13 @@ def test_few_rows_on_long_states(kvg, d, g, fp8):
     run(bed, 2 * g, [1, 0], [300, 2])
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_many_rows_of_empty_and_short_states_beside_long_ones(kvg, fp8):
+    bed = States(kvg, 2, 2, 128, 64, [0, 5000, 3], fp8)
+    run(bed, 4, [0, 1, 2], [2000, 4, 2], layer=-1)
+    run(bed, 4, [0, 1, 2], [5, 4, 900], layer=-1)
+
+
 def test_layers_of_different_windows_in_one_call(kvg):
     bed = States(kvg, 4, 2, 128, 64, [570, 333])
     windows = [0, 100, 0, 30]
