@@ -409,7 +409,6 @@ struct PromptParams {
     int32_t n_kv_heads, page_size, n_q_heads, n_layers_run;
     const int32_t *page_table, *page_fill;
     int32_t max_pages, n_seq, window, shared;
-    int32_t span;              // every row of a sequence attends to the slots [begin, slot0] (shared: [lo, slot0])
     int32_t n_units;           // run layers x KV heads
     int32_t log2_group;        // of the query heads to a KV head
     Divisor by_units, by_kv_heads, by_page, by_pages;  // n_units, n_kv_heads, page_size, pages_per_unit or units_per_page
@@ -435,10 +434,11 @@ struct PromptParams {
     int64_t part0[kMaxBatchPerLaunch];     // first partial result
     float *part_o;                         // [slots][D]
     float2 *part_ml;                       // [slots] (m, l)
-    float *part_lse, *row_lse;             // kvg_attention_weights: [slots], [units][rows]: log2 of sum 2^score
     int2 *redo;                            // [items][8] (rows, entry before): rows to be computed over
     int32_t member[kMaxBatchPerLaunch];    // shared: batch row of each member
     int32_t lo[kMaxBatchPerLaunch];        // shared: first slot that it attends to
+    int32_t span;                          // every row of a sequence attends to the slots [begin, slot0] (shared: [lo, slot0])
+    float *part_lse, *row_lse;             // kvg_attention_weights: [slots], [units][rows]: log2 of sum 2^score
 };
 
 // What weight the rows of a prompt's launch gave each cached row: of its layers

@@ -185,9 +185,10 @@ __device__ __forceinline__ int first_slot(const PromptParams &p, int tile) {
                             : p.by_pages.div(u) * p.page_size + (u - p.by_pages.div(u) * p.units_per_page) * p.unit;
 }
 
-// First slot that the row at `slot` attends to.
+// First slot that the row at `slot` attends to (span: that any row does).
 __device__ __forceinline__ int window_first(const PromptParams &p, int b, int slot) {
     if (p.window <= 0) return 0;
+    if (p.span) return p.begin[b];
     const int from = max(0, slot - p.window + 1);
     if (from >= p.solid[b]) return from;
     // pages that are not full lie in between: count valid rows back
@@ -200,7 +201,7 @@ __device__ __forceinline__ int window_first(const PromptParams &p, int b, int sl
     return pg * p.page_size + max(0, n - left);
 }
 __device__ __forceinline__ int row_first(const PromptParams &p, const Item &it, int tok) {
-    return p.shared ? p.lo[p.row0[it.b] + tok] : p.span ? p.begin[it.b] : window_first(p, it.b, p.slot0[it.b] + tok);
+    return p.shared ? p.lo[p.row0[it.b] + tok] : window_first(p, it.b, p.slot0[it.b] + tok);
 }
 __device__ __forceinline__ int row_last(const PromptParams &p, const Item &it, int tok) {
     return p.slot0[it.b] + (p.span ? 0 : tok);
@@ -763,8 +764,10 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     const float a = rescale ? exp2_approx((m - top) * c) : 1.f;
                     sum.x *= a;
                     sum.y *= a;
-                    exact.x *= a;
-                    exact.y *= a;
+                    if constexpr (C::LSE && !FP8) {
+                        exact.x *= a;
+                        exact.y *= a;
+                    }
                     // (two streams: the scores came after the previous product)
                     if (STREAMS == 1) ok = wait_bar(s, &s.out[0], (J - 1) & 1, p.status);
                     if (!ok) break;

@@ -2448,7 +2448,8 @@ extern "C" kvg_status kvg_cache_set_layer_windows(kvg_cache *c, const int32_t *w
 // that is being captured does not (its replays are the caller's to order).
 static cudaError_t use_partials(kvg_cache *c, cudaStream_t st) {
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    if (cudaError_t e = cudaStreamIsCapturing(st, &capture); e != cudaSuccess) return e;
+    if (st)  // (the null stream cannot be; asking takes 0.3 us)
+        if (cudaError_t e = cudaStreamIsCapturing(st, &capture); e != cudaSuccess) return e;
     c->capturing = capture != cudaStreamCaptureStatusNone;
     if (c->capturing) return cudaSuccess;
     if (!c->part_ev)
