@@ -14,15 +14,16 @@
 // certain ones before it and as many of the ties before it as are kept.  The
 // sequence's tags, weights and tables move in the same pass, all of the slots at
 // hand read before any is written, and nothing is written behind them.  Latency
-// bounds it: with one CTA and 16 slots a thread it took 28 us for 16,384 rows (the
-// loads of a chunk at a time: 37) and 15 for 293, where four slots took 5.
+// bounds it: three sequences of 16,384 rows take 15 us (one CTA each, 16 slots a
+// thread: 28, four slots at a time: 37), one of 293 rows 9.
 //
 // Move: a CTA takes one KV head of a layer's keys or values of a sequence, chunk
 // by chunk of kept rows in order: a chunk's rows come from behind the chunk before
 // it, so a barrier between a chunk's loads and its stores is all that moving rows
 // within a sequence's own pages takes.  Rows that go to another sequence's pages
 // are divided among several CTAs.  Memory bounds it: each kept row is read and
-// written once, with the next chunk's loads in flight while one is stored.
+// written once, with the next chunk's loads in flight while one is stored (403 MB of
+// the 12B shape's rows read and written in 119 us, 6.8 TB/s).
 #include <algorithm>
 
 #include "tcgen05.cuh"

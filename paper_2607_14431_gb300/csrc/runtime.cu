@@ -2750,8 +2750,14 @@ static uint64_t weights_scratch() {
 }
 
 // The work items of a launch's weights: pairs of key tiles, with the query tiles
-// split as plan_prompt splits keys.  An item costs its query tiles and kItemTiles
-// more.  Returns the floats of a layer's sums.
+// split where that evens out the SMs' shares.  The CTAs go through the items in
+// turn, every other round backwards (weigh_kernel), as is done here: few items are
+// shared out one by one, of many half an item stands for the difference.  An item
+// costs its query tiles and kItemTiles more.  (2,047 rows of the 12B shape on 6,145:
+// 76 pairs of CTAs with whole items have 98 tiles at most, with every round forwards
+// 113, so that halves were better, 105: 251 us for the call and 257.  27 prompts of up
+// to 490 with a window: whole items 131 us, halves, which 2 for kItemTiles takes, 134.)
+// Returns the floats of a layer's sums.
 static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     constexpr double kItemTiles = 4.0;
     const PromptParams &p = w->p;
@@ -2760,38 +2766,60 @@ static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
         const int64_t pg = slot / p.page_size;
         return (p.pages_per_unit ? pg / p.pages_per_unit : pg * p.units_per_page + slot % p.page_size / p.unit) / per;
     };
-    const double at_once = (double)c->n_sm / prompt_ctas(c->dims.head_dim);
-    struct Row {
-        double longest, mean;
+    auto slot_of = [&](int64_t tile) {  // its first
+        const int64_t u = tile * per;
+        return p.pages_per_unit ? u * p.pages_per_unit * p.page_size
+                                : u / p.units_per_page * p.page_size + u % p.units_per_page * p.unit;
     };
-    std::vector<Row> rows;
-    double longest = 1.0;
+    std::vector<int32_t> tiles, longest(p.n_seq);  // query tiles of each block, of a sequence the most
+    int64_t blocks = 0, sum = 0;
+    int32_t most = 1;
     for (int32_t i = 0; i < p.n_seq; ++i) {
-        const int64_t n = p.first[i + 1] - p.first[i], end = p.slot0[i] + n;
+        const int64_t n = p.first[i + 1] - p.first[i], slot0 = p.slot0[i];
         w->tile0[i] = (int32_t)tile_of(p.begin[i]);
-        w->blocks[i] = (int32_t)((tile_of(end - 1) - w->tile0[i]) / 2 + 1);
-        const double all = std::ceil((double)n * G / kPromptCols);
-        // of `end - begin` slots those before the prompt are attended to by all of its
-        // rows, those in it by half of them; a window's rows reach each slot
-        const double before = p.slot0[i] - p.begin[i], in = (double)n;
-        double top = all, mean = (before * all + in * all / 2) / (before + in);
-        if (p.window > 0) {
-            top = std::min(top, std::ceil((double)p.window * G / kPromptCols) + 2);
-            mean = std::min(mean, top);
+        w->blocks[i] = (int32_t)((tile_of(slot0 + n - 1) - w->tile0[i]) / 2 + 1);
+        for (int32_t b = 0; b < w->blocks[i]; ++b) {  // (as weigh_item())
+            const int64_t tile = w->tile0[i] + 2 * b, t0 = std::max<int64_t>(0, slot_of(tile) - slot0);
+            const int64_t t1 = p.window > 0 ? std::min<int64_t>(n, slot_of(tile + 2) - 1 + p.window - slot0 + w->gaps[i]) : n;
+            const int64_t len = t0 < t1 ? (t1 * G + kPromptCols - 1) / kPromptCols - t0 * G / kPromptCols : 0;
+            tiles.push_back((int32_t)len);
+            sum += len;
+            longest[i] = std::max(longest[i], (int32_t)len);
         }
-        rows.push_back({std::max(top, 1.0), std::max(mean, 1.0)});
-        longest = std::max(longest, rows.back().longest);
+        blocks += w->blocks[i];
+        most = std::max(most, longest[i]);
     }
-    double best = INFINITY, best_len = longest;
-    for (double len = longest; len >= 1.0; len *= 0.84) {
-        double items = 0, total = 0, top = 0;
-        for (int32_t i = 0; i < p.n_seq; ++i) {
-            const double s = std::max(1.0, std::ceil(rows[i].longest / len - 1e-9));
-            items += s * w->blocks[i] * p.n_units;
-            total += w->blocks[i] * p.n_units * (rows[i].mean + s * kItemTiles);
-            top = std::max(top, rows[i].longest / s + kItemTiles);
+    const int at_once = c->n_sm / prompt_ctas(c->dims.head_dim);
+    auto splits_of = [&](int32_t i, double len) { return std::max(1, (int32_t)std::ceil(longest[i] / len - 1e-9)); };
+    double best = INFINITY, best_len = most;
+    int64_t before = 0;  // items of the length before
+    std::vector<double> load;
+    for (double len = most; len >= 1.0; len *= 0.84) {
+        int64_t items = 0;
+        for (int32_t i = 0; i < p.n_seq; ++i) items += (int64_t)splits_of(i, len) * w->blocks[i] * p.n_units;
+        if (items == before) continue;
+        before = items;
+        double est = (double)(sum * p.n_units) / at_once + kItemTiles * items / at_once;
+        if (items > 8 * at_once) {
+            est += 0.5 * sum * p.n_units / items;
+        } else {
+            load.assign(at_once, 0.0);
+            int at = 0, step = 1;
+            const int32_t *of = tiles.data();
+            for (int32_t i = 0; i < p.n_seq; ++i) {
+                const int32_t s = splits_of(i, len);
+                for (int32_t b = 0; b < w->blocks[i]; ++b, ++of)
+                    for (int32_t k = 0; k < s; ++k) {
+                        const double cost = (*of * (k + 1) / s - *of * k / s) + kItemTiles;
+                        for (int32_t u = 0; u < p.n_units; ++u) {
+                            load[at] += cost;
+                            at += step;
+                            if (at < 0 || at >= at_once) at -= step, step = -step;
+                        }
+                    }
+            }
+            est = *std::max_element(load.begin(), load.end());
         }
-        const double est = std::max(top, std::ceil(items / at_once) * (total / items));
         if (est < best) {
             best = est;
             best_len = len;
@@ -2799,7 +2827,7 @@ static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     }
     int64_t floats = 0;
     for (int32_t i = 0; i < p.n_seq; ++i) {
-        w->splits[i] = (int32_t)std::max(1.0, std::ceil(rows[i].longest / best_len - 1e-9));
+        w->splits[i] = splits_of(i, best_len);
         w->sum0[i] = floats;  // (of one layer: scaled by the layers of a launch)
         floats += (int64_t)w->splits[i] * p.n_kv_heads * w->lines * 2 * w->blocks[i] * kPromptCols;
     }

@@ -15,12 +15,12 @@
 // two or three buffers in tensor memory, so that a tile's products run beside the
 // exponentials of the one before.
 //
-// What bounds it: the products, and the exponentials close behind.  2,047 rows of the
-// 12B shape on 6,145: 91 us, of which the products alone are 59; 77 with the hand-overs
-// between the warps but no sums, 84 with the sums but without the rows' logarithms
-// from shared memory.  Sixteen summing warps are no faster than eight.  With both
-// operands in shared memory that memory's 128 bytes a cycle bounded it (a pair's
-// products of 128 keys and 128 rows read 8 KB in their 64 cycles): 1,480 cycles a tile.
+// What bounds it: the products, and the hand-overs between warps.  2,047 rows of the
+// 12B shape on 6,145: 86 us, of which the products alone are 59; with the CTAs' shares
+// less even than now 92, of that 77 without sums, 84 without the rows' logarithms
+// from shared memory, and 92 with sixteen summing warps or a third score buffer too.
+// With both operands in shared memory that memory's 128 bytes a cycle bounded it (a
+// pair's products of 128 keys and 128 rows read 8 KB in their 64 cycles).
 //
 // CTAs are persistent: item by item, the ring of query tiles running on from one to
 // the next, and the next item's keys on their way while one is worked on.
@@ -152,11 +152,15 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     after_previous();
     const uint32_t tmem = s.tmem;
     const int gs = p.log2_group;
-    // The CTA's items: every (grid / CTAS)-th.  tiles: query tiles of the items before;
-    // items: how many of those had any.
+    // The CTA's items: one of each round of grid / CTAS, every other round backwards (the
+    // items of a sequence get shorter).  tiles: query tiles of the items before; items:
+    // how many of those had any.
     auto each_item = [&](auto &&work) {
         int tiles = 0, items = 0;
-        for (int at = blockIdx.x / CTAS; at < w.item0[p.n_seq]; at += gridDim.x / CTAS) {
+        const int n_at = gridDim.x / CTAS, me = blockIdx.x / CTAS;
+        for (int round = 0;; ++round) {
+            const int at = round * n_at + (round & 1 ? n_at - 1 - me : me);
+            if (at >= w.item0[p.n_seq]) return;
             const WeighItem it = weigh_item(w, at);
             const int n = it.q1 - it.q0, rows = (p.first[it.b + 1] - p.first[it.b]) << gs;  // rows: of the sequence
             if (!work(it, n, rows, tiles, items)) return;
