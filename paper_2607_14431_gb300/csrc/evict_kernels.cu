@@ -14,8 +14,8 @@
 // certain ones before it and as many of the ties before it as are kept.  The
 // sequence's tags, weights and tables move in the same pass, all of the slots at
 // hand read before any is written, and nothing is written behind them.  Latency
-// bounds it: three sequences of 16,384 rows take 15 us (one CTA each, 16 slots a
-// thread: 28, four slots at a time: 37), one of 293 rows 9.
+// bounds it: three sequences of up to 16,384 rows take 15 us (one CTA each, 16 slots
+// a thread: 28, four slots at a time: 37), one of 293 rows 9.
 //
 // Move: a CTA takes one KV head of a layer's keys or values of a sequence, chunk
 // by chunk of kept rows in order: a chunk's rows come from behind the chunk before
