@@ -52,9 +52,51 @@ struct Weigh {
     static constexpr int LINES = 2 / STREAMS;                          // a key's sums: a pair's CTA has two warps to it
     static constexpr int COLS = kTile / LINES;                         // of a query tile that a summing warp has
     static constexpr int SMEM = STREAMS * KEYS + STAGES * Q_BYTES + 1024;
-    static_assert(SMEM <= 217 * 1024, "shared memory beside the barriers and the logarithms");
+    static_assert(SMEM <= 210 * 1024, "shared memory beside the barriers, the logarithms and the items");
 };
 
+// Of the launch: a KV head of a layer, a pair of key tiles, a range of query tiles.
+struct WeighItem {
+    int n, q0;               // query tiles [q0, q0 + n)
+    int rows;                // query rows of the sequence, token x head
+    int tile;                // first key tile
+    int seq, slot0, solid, head;  // head: first query head
+    int token, key;          // first row of the queries; of the KV head's plane in the pool
+    int line, pad;           // floats between the lines of sums
+    int64_t lse, sums;       // the sequence's logarithms; the first line of sums, its first key
+};
+__device__ __forceinline__ WeighItem weigh_item(const WeighParams &w, int at) {
+    const PromptParams &p = w.p;
+    WeighItem it;
+    const int b = search(w.item0, p.n_seq, at), splits = w.splits[b];
+    const int units = w.n_lr * p.n_kv_heads, of_seq = at - w.item0[b], of_unit = of_seq / units;
+    const int unit = of_seq - of_unit * units, lr = w.lr0 + unit / p.n_kv_heads, g = unit % p.n_kv_heads;
+    const int block = of_unit / splits, split = of_unit - block * splits, gs = p.log2_group;
+    const int n = p.first[b + 1] - p.first[b], row0 = p.row0[b];
+    it.rows = n << gs;
+    it.tile = w.tile0[b] + 2 * block;
+    it.seq = p.seq[b];
+    it.slot0 = p.slot0[b];
+    it.solid = p.solid[b];
+    it.head = g << gs;
+    it.token = p.qlayers[lr] * (int)p.q_rows + row0;
+    it.key = (int)(((int64_t)p.layers[lr] * 2 * p.pool_pages * p.n_kv_heads + g) * p.page_size);
+    it.line = 2 * w.blocks[b] * kTile;
+    it.pad = 0;
+    it.lse = ((int64_t)(lr * p.n_kv_heads + g) * p.q_rows + row0) << gs;
+    it.sums = w.sum0[b] + ((int64_t)split * units + unit) * w.lines * it.line + 2 * block * kTile;
+    // the tokens that may attend to its slots
+    const int from = first_slot(p, it.tile), end = first_slot(p, it.tile + 2);
+    const int t0 = max(0, from - it.slot0);
+    const int64_t reach = p.window > 0 ? (int64_t)end - 1 + p.window - it.slot0 + w.gaps[b] : n;
+    const int t1 = (int)min((int64_t)n, max(reach, (int64_t)0));
+    const int a = (t0 << gs) / kTile, e = max(a, ((t1 << gs) + kTile - 1) / kTile), len = e - a;
+    it.q0 = a + (int)((int64_t)len * split / splits);
+    it.n = t0 < t1 ? a + (int)((int64_t)len * (split + 1) / splits) - it.q0 : 0;
+    return it;
+}
+
+constexpr int kItemsAhead = 96;  // of a CTA, worked out at its start, a thread each
 struct WeighBars {
     uint64_t k_landed, k_taken;              // keys: there; their place is free
     uint64_t k_ready[2], k_free[2];          // in tensor memory (of a pair both); multiplied
@@ -63,41 +105,13 @@ struct WeighBars {
     uint64_t drained;
     uint32_t tmem;
     int abort;
-    alignas(16) float lse[8][2][kTile];       // of each summing warp: minus lse of its rows of two tiles
+    alignas(16) float lse[8][2][kTile];      // of each summing warp: minus lse of its rows of two tiles
+    alignas(16) WeighItem items[kItemsAhead];
 };
 
 __device__ __forceinline__ bool wait_weigh(WeighBars &s, uint64_t *bar, uint32_t parity, DevStatus *status) {
     const bool ok = mbar_try_wait(bar, parity) || wait_slow(bar, parity, &s.abort, status);
     return __all_sync(0xffffffffu, ok);
-}
-
-// Of the launch: a KV head of a layer, a pair of key tiles, a range of query tiles.
-struct WeighItem {
-    int b, unit, lr, g, split, tile;  // tile: the first key tile
-    int q0, q1;                       // query tiles
-};
-__device__ __forceinline__ WeighItem weigh_item(const WeighParams &w, int at) {
-    const PromptParams &p = w.p;
-    WeighItem it;
-    it.b = search(w.item0, p.n_seq, at);
-    const int units = w.n_lr * p.n_kv_heads, of_seq = at - w.item0[it.b], of_unit = of_seq / units;
-    it.unit = of_seq - of_unit * units;
-    it.lr = w.lr0 + it.unit / p.n_kv_heads;
-    it.g = it.unit % p.n_kv_heads;
-    const int block = of_unit / w.splits[it.b];
-    it.split = of_unit - block * w.splits[it.b];
-    it.tile = w.tile0[it.b] + 2 * block;
-    // the tokens that may attend to its slots
-    const int n = p.first[it.b + 1] - p.first[it.b], slot0 = p.slot0[it.b];
-    const int from = first_slot(p, it.tile), end = first_slot(p, it.tile + 2);
-    const int t0 = max(0, from - slot0);
-    const int64_t reach = p.window > 0 ? (int64_t)end - 1 + p.window - slot0 + w.gaps[it.b] : n;
-    const int t1 = (int)min((int64_t)n, max(reach, (int64_t)0));
-    const int a = (t0 << p.log2_group) / kTile, e = max(a, ((t1 << p.log2_group) + kTile - 1) / kTile), len = e - a;
-    it.q0 = a + (int)((int64_t)len * it.split / w.splits[it.b]);
-    it.q1 = a + (int)((int64_t)len * (it.split + 1) / w.splits[it.b]);
-    if (t0 >= t1) it.q1 = it.q0;
-    return it;
 }
 
 template <class C>
@@ -142,6 +156,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         s.abort = 0;
         fence_mbar_init();
     }
+    // The CTA's items: one of each round of grid / CTAS, every other round backwards (the
+    // items of a sequence get shorter).  Working one out takes 3,000 cycles where the
+    // launch's parameters are not in the constant cache.
+    const int n_at = gridDim.x / CTAS, me = blockIdx.x / CTAS, n_items = w.item0[p.n_seq];
+    auto item_of = [&](int round) { return round * n_at + (round & 1 ? n_at - 1 - me : me); };
+    if (threadIdx.x < kItemsAhead && item_of(threadIdx.x) < n_items) s.items[threadIdx.x] = weigh_item(w, item_of(threadIdx.x));
     if (warp == C::MMA_WARP) tmem_alloc<512, CTAS>(&s.tmem);
     tc_before_sync();
     if constexpr (CTAS == 2)
@@ -152,78 +172,80 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     after_previous();
     const uint32_t tmem = s.tmem;
     const int gs = p.log2_group;
-    // The CTA's items: one of each round of grid / CTAS, every other round backwards (the
-    // items of a sequence get shorter).  tiles: query tiles of the items before; items:
-    // how many of those had any.
+    // tiles: query tiles of the items before; items: how many of those had any.
     auto each_item = [&](auto &&work) {
         int tiles = 0, items = 0;
-        const int n_at = gridDim.x / CTAS, me = blockIdx.x / CTAS;
         for (int round = 0;; ++round) {
-            const int at = round * n_at + (round & 1 ? n_at - 1 - me : me);
-            if (at >= w.item0[p.n_seq]) return;
-            const WeighItem it = weigh_item(w, at);
-            const int n = it.q1 - it.q0, rows = (p.first[it.b + 1] - p.first[it.b]) << gs;  // rows: of the sequence
-            if (!work(it, n, rows, tiles, items)) return;
-            tiles += n;
-            items += n > 0;
+            const int at = item_of(round);
+            if (at >= n_items) return;
+            WeighItem it;
+            if (round < kItemsAhead)
+                it = s.items[round];
+            else
+                it = weigh_item(w, at);
+            if (!work(it, tiles, items)) return;
+            tiles += it.n;
+            items += it.n > 0;
         }
     };
 
     if (warp < C::SUM_WARPS) {
-        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+        each_item([&](const WeighItem &it, int tiles, int items) {
             // ---- a thread has a key
             const int stream = STREAMS == 2 ? warp / 4 : 0, half = STREAMS == 2 ? 0 : warp / 4;
-            const int tile = it.tile + (STREAMS == 2 ? stream : rank), col = warp % 4 * 32 + lane;
-            // its slot, and the query rows [lo, hi) of the sequence that attend to it
-            int slot, lo = 0, hi = rows;
+            const int shift = STREAMS == 2 ? stream : rank, col = warp % 4 * 32 + lane, n = it.n, rows = it.rows;
+            // its slot
+            const int u = (it.tile + shift) * (kTile / p.unit) + col / p.unit, c0 = col % p.unit;
+            int pg, r0;
             bool valid;
-            {
-                const int u = tile * (kTile / p.unit) + col / p.unit, c = col % p.unit;
-                int pg, r;
-                if (p.pages_per_unit) {
-                    const int place = c / p.page_rows;
-                    pg = u * p.pages_per_unit + place;
-                    r = c - place * p.page_rows;
-                    valid = place < p.pages_per_unit && r < p.page_size;
-                } else {
-                    pg = u / p.units_per_page;
-                    r = (u - pg * p.units_per_page) * p.unit + c;
-                    valid = r < p.page_size;
-                }
-                const int slot0 = p.slot0[it.b], last = slot0 + (rows >> gs) - 1;
-                slot = pg * p.page_size + r;
-                valid = valid && slot <= last;
-                if (valid) {
-                    const int32_t *fill = p.page_fill + (int64_t)p.seq[it.b] * p.max_pages;
-                    valid = r < fill[pg];
-                    lo = max(0, slot - slot0) << gs;
-                    if (valid && p.window > 0) {
-                        // valid rows from here up to the query rows
-                        int64_t between = (int64_t)slot0 - slot;
-                        if (slot < p.solid[it.b]) {
-                            between = fill[pg] - r;
-                            const int end = slot0 / p.page_size;
-                            for (int i = pg + 1; i < end && between < p.window; ++i) between += fill[i];
-                            if (end > pg) between += slot0 - end * p.page_size;
-                            else between = slot0 - slot;
-                        }
-                        hi = (int)max((int64_t)0, min((int64_t)(rows >> gs), p.window - between)) << gs;
-                    }
-                }
+            if (p.pages_per_unit) {
+                const int place = c0 / p.page_rows;
+                pg = u * p.pages_per_unit + place;
+                r0 = c0 - place * p.page_rows;
+                valid = place < p.pages_per_unit && r0 < p.page_size;
+            } else {
+                pg = p.by_pages.div(u);
+                r0 = (u - pg * p.units_per_page) * p.unit + c0;
+                valid = r0 < p.page_size;
             }
+            const int slot0 = it.slot0, slot = pg * p.page_size + r0;
+            valid = valid && slot < slot0 + (rows >> gs);
+            const int32_t *fill = p.page_fill + (int64_t)it.seq * p.max_pages;
+            const int filled = valid ? fill[pg] : 0;
+            // the logarithms of the first tiles, beside it
             bool ok = true;
             constexpr int COLS = C::COLS, PER = COLS / 32;  // PER: logarithms that a lane fetches
-            const float *lse = p.row_lse + ((int64_t)(it.lr * p.n_kv_heads + it.g) * p.q_rows + p.row0[it.b]) * (1 << gs);
+            const float *lse = p.row_lse + it.lse;
             float *const mine[2] = {s.lse[warp][0], s.lse[warp][1]};
             // of the tile after this one, and of the one after that: their loads take as long as a tile
             float next[PER], after[PER];
-            auto fetch = [&](int t, float (&to)[PER]) {
+            auto fetch = [&](int i, float (&to)[PER]) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int r = t * kTile + half * COLS + i * 32 + lane;
-                    to[i] = t < it.q1 && r < rows ? lse[r] : INFINITY;  // (2^-inf: no weight)
+                for (int k = 0; k < PER; ++k) {
+                    const int r = (it.q0 + i) * kTile + half * COLS + k * 32 + lane;
+                    to[k] = i < n && r < rows ? lse[r] : INFINITY;  // (2^-inf: no weight)
                 }
             };
+            fetch(0, next);
+            fetch(1, after);
+            // the query rows [lo, hi) of the sequence that attend to it
+            int lo = 0, hi = rows;
+            valid = r0 < filled;
+            if (valid) {
+                lo = max(0, slot - slot0) << gs;
+                if (p.window > 0) {
+                    // valid rows from here up to the query rows
+                    int64_t between = (int64_t)slot0 - slot;
+                    if (slot < it.solid) {
+                        between = filled - r0;
+                        const int end = slot0 / p.page_size;
+                        for (int i = pg + 1; i < end && between < p.window; ++i) between += fill[i];
+                        if (end > pg) between += slot0 - end * p.page_size;
+                        else between = slot0 - slot;
+                    }
+                    hi = (int)max((int64_t)0, min((int64_t)(rows >> gs), p.window - between)) << gs;
+                }
+            }
             auto put = [&](int buf) {
                 __syncwarp();
 #pragma unroll
@@ -234,14 +256,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             const float2 c2 = make_float2(c, c);
             const uint32_t at = tmem + ((uint32_t)(warp % 4) << 21) + half * COLS;
             float2 sum[4] = {};
-            fetch(it.q0, next);
-            fetch(it.q0 + 1, after);
             put(0);
             for (int i = 0; ok && i < n; ++i) {
                 const int t = (tiles + i) * STREAMS + stream, buf = t % C::SCORES, lbuf = i & 1, row0 = (it.q0 + i) * kTile + half * COLS;
 #pragma unroll
                 for (int k = 0; k < PER; ++k) next[k] = after[k];
-                fetch(it.q0 + i + 2, after);
+                fetch(i + 2, after);
                 ok = wait_weigh(s, &s.scores[buf], (t / C::SCORES) & 1, p.status);
                 if (!ok) break;
                 tc_after_sync();
@@ -250,10 +270,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 float x[64];
 #pragma unroll
                 for (int j = 0; j < COLS; j += 64) {
+                    const int left = rows - row0 - j;  // of the sequence's rows
+                    if (j > 0 && left <= 0) break;
                     tmem_ld32(at + buf * kTile + j, reinterpret_cast<uint32_t *>(x));
                     tmem_ld32(at + buf * kTile + j + 32, reinterpret_cast<uint32_t *>(x) + 32);
                     tmem_wait_ld();
-                    if (j + 64 == COLS) {  // the next scores may be put there
+                    if (j + 64 == COLS || left <= 64) {  // the next scores may be put there
                         tc_before_sync();
                         arrive_issuer(&s.taken[buf]);
                     }
@@ -291,17 +313,15 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
             if (!ok) return false;
             const float2 total = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-            const int64_t line = ((int64_t)it.split * (w.n_lr * p.n_kv_heads) + it.unit) * C::LINES + half;
-            w.sums[w.sum0[it.b] + (line * 2 * w.blocks[it.b] + tile - w.tile0[it.b]) * kTile + col] =
-                valid ? total.x + total.y : 0.f;
+            w.sums[it.sums + half * it.line + shift * kTile + col] = valid ? total.x + total.y : 0.f;
             return true;
         });
     } else if (warp < C::KEY_WARP + 4) {
         // ---- keys from shared to tensor memory: a thread has a key of each tile, 64
         // elements (of a bf16 cache 128 swizzled bytes, of an fp8 cache 64) at a time
         const int row = warp % 4 * 32 + lane;
-        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
-            if (n == 0) return true;
+        each_item([&](const WeighItem &it, int tiles, int items) {
+            if (it.n == 0) return true;
             const int set = items % C::KEY_SETS;
             if (!wait_weigh(s, &s.k_landed, items & 1, p.status)) return false;
             if (items >= C::KEY_SETS && !wait_weigh(s, &s.k_free[set], (items / C::KEY_SETS - 1) & 1, p.status)) return false;
@@ -340,12 +360,12 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     } else if (warp == C::LOAD_WARP) {
         bool ok = true;
         int i = 0, k = 0;  // query tiles and keys that were asked for
-        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+        each_item([&](const WeighItem &it, int tiles, int items) {
             // ---- the keys of the CTA's tiles, then its part of each query tile
+            const int n = it.n;
             if (n == 0) return true;
-            const int64_t entry = (int64_t)p.seq[it.b] * p.max_pages;
-            const int slot_end = p.slot0[it.b] + (rows >> gs), last = (slot_end - 1) / p.page_size;
-            const int32_t base = (int32_t)(((int64_t)p.layers[it.lr] * 2 * p.pool_pages * p.n_kv_heads + it.g) * p.page_size);
+            const int64_t entry = (int64_t)it.seq * p.max_pages;
+            const int slot_end = it.slot0 + (it.rows >> gs), last = (slot_end - 1) / p.page_size;
             const int per = kTile / p.unit, unit = lane / 16, place = lane % 16;
             constexpr int BOXES = FP8 ? D / 128 : D / 64;
             int32_t y[STREAMS];
@@ -371,11 +391,11 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                         mine = false;
                     }
                 }
-                y[st] = base + pid * (p.n_kv_heads * p.page_size) + sub;
+                y[st] = it.key + pid * (p.n_kv_heads * p.page_size) + sub;
                 has[st] = __ballot_sync(0xffffffffu, mine);
                 boxes += __popc(has[st]);
             }
-            const int token0 = p.qlayers[it.lr] * (int)p.q_rows + p.row0[it.b] + ((rank * C::Q_ROWS) >> gs);
+            const int token0 = it.token + ((rank * C::Q_ROWS) >> gs);
             auto load = [&](int t) {
                 const int st = i % STAGES;
                 if (i >= STAGES) ok = wait_weigh(s, &s.empty[st], (i / STAGES - 1) & 1, p.status);
@@ -384,7 +404,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     mbar_arrive_expect_tx(&s.landed[st], C::Q_BYTES);
 #pragma unroll
                     for (int x = 0; x < D / 64; ++x)
-                        tma_load_3d(ring + st * C::Q_BYTES + x * (C::Q_ROWS * 128), &q_map, x * 64, it.g << gs,
+                        tma_load_3d(ring + st * C::Q_BYTES + x * (C::Q_ROWS * 128), &q_map, x * 64, it.head,
                                     token0 + (((it.q0 + t) * kTile) >> gs), &s.landed[st]);
                 }
                 __syncwarp();
@@ -432,7 +452,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             };
             constexpr bool DIRECT = CTAS == 1;  // the copies' own barriers
             bool any = false;
-            each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+            each_item([&](const WeighItem &it, int tiles, int items) {
+                const int n = it.n;
                 if (n == 0) return true;
                 any = true;
                 const int set = items % C::KEY_SETS;
@@ -466,9 +487,9 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         __syncwarp();
     } else if (warp == C::RELAY_WARP) {
         // ---- a pair: the query tiles that have landed here, for the first CTA's issuing thread
-        each_item([&](const WeighItem &it, int n, int rows, int tiles, int items) {
+        each_item([&](const WeighItem &it, int tiles, int items) {
             bool ok = true;
-            for (int i = tiles; ok && i < tiles + n; ++i) {
+            for (int i = tiles; ok && i < tiles + it.n; ++i) {
                 ok = wait_weigh(s, &s.landed[i % STAGES], (i / STAGES) & 1, p.status);
                 if (ok) arrive_issuer(&s.ready[i % STAGES]);
             }
