@@ -204,6 +204,18 @@ def test_many_sequences(kvg, most):
     run(bed, 2, list(range(n)), rows, decay=0.5, before=torch.rand(n, 96, device="cuda"))
 
 
+@pytest.mark.parametrize("d,page,window", [(64, 1, 0), (64, 1, 70), (256, 1, 0)])
+def test_more_work_than_an_sm_looks_ahead(kvg, d, page, window):
+    """Some 20,000 pairs of key tiles, of 16 slots each, for few rows each."""
+    n_l, hkv, per = 4, 8, 32
+    lens = [(500 + 17 * i, 2 + i % 3) for i in range(28 if d == 64 else 16)]
+    if window:
+        lens = [(a, n) for a, n in lens] * 4
+    assert window or sum(-(-(a + n) // per) for a, n in lens) * hkv * n_l > 96 * (152 if d == 64 else 76)
+    bed = bed_of(kvg, (hkv, 1, d, page, window, False, lens), n_layers=n_l)
+    run(bed, hkv, list(range(len(lens))), [n for _, n in lens], window, layer=-1)
+
+
 @pytest.mark.parametrize("window", [0, 70])
 @pytest.mark.parametrize("rows", [100, 1])
 def test_unfilled_page_tails_between_grafted_blocks(kvg, window, rows):
