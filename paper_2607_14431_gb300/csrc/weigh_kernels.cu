@@ -16,11 +16,15 @@
 // exponentials of the one before.
 //
 // What bounds it: the products, and the hand-overs between warps.  2,047 rows of the
-// 12B shape on 6,145: 86 us, of which the products alone are 59; with the CTAs' shares
-// less even than now 92, of that 77 without sums, 84 without the rows' logarithms
+// 12B shape on 6,145: 81 us, of which the products alone are 59; with the CTAs' shares
+// less even than now, and their items worked out one by one, 92, of that 77 without sums, 84 without the rows' logarithms
 // from shared memory, and 92 with sixteen summing warps or a third score buffer too.
 // With both operands in shared memory that memory's 128 bytes a cycle bounded it (a
 // pair's products of 128 keys and 128 rows read 8 KB in their 64 cycles).
+//
+// Few rows on long contexts are bound by what an item costs beside its products: 17
+// sequences of 65 to 125 rows on 3,872 to 5,027 of the 31B shape 308 us a call with
+// items worked out one by one, 265 so.
 //
 // CTAs are persistent: item by item, the ring of query tiles running on from one to
 // the next, and the next item's keys on their way while one is worked on.
