@@ -475,11 +475,7 @@ struct EvictSeq {
     int32_t pad;
     int64_t list;              // its rows: EvictParams::from
 };
-// SEQS, PAGES: what a launch holds (a launch copies its parameters: one sequence in
-// the larger's 13 KB took 3 us more of the host).
-template <int SEQS, int PAGES>
-struct EvictParamsOf {
-    static constexpr int kSeqs = SEQS, kPages = PAGES;
+struct EvictParams {
     uint8_t *pool;
     int64_t pool_pages;
     int32_t *page_table, *page_fill, *positions;
@@ -489,11 +485,9 @@ struct EvictParamsOf {
     Divisor by_page;
     DevStatus *status;
     int32_t pid0, n_pids;      // page ids that came with the launch (0: `to` holds them already)
-    EvictSeq seq[SEQS];
-    int32_t pids[PAGES];
+    EvictSeq seq[kMaxEvictSeqs];
+    int32_t pids[kMaxPagesPerLaunch];
 };
-using EvictParams = EvictParamsOf<kMaxEvictSeqs, kMaxPagesPerLaunch>;
-using FewEvictParams = EvictParamsOf<4, 256>;
 
 // Where the combine of a decode finds its rows' partials over the pages that
 // they share with other rows: of the launch's window group w, batch row b, the
@@ -651,8 +645,7 @@ cudaError_t encode_tensor_map(CUtensorMap *out, int rank, void *base, const cuui
                               const cuuint64_t *strides, const cuuint32_t *box);
 cudaError_t launch_combine(int head_dim, const DecodeParams &p, int n_sm, cudaStream_t s);
 // Selection and the rows; most_slots, most_rows: of a sequence (no rows to move: selection alone).
-template <class Params>
-cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows, int n_sm, cudaStream_t s);
+cudaError_t launch_evict(const EvictParams &p, int64_t most_slots, int64_t most_rows, int n_sm, cudaStream_t s);
 // The combine with the partials of the rows' shared pages beside the decode's.
 cudaError_t launch_combine_shared(int head_dim, const DecodeParams &p, const SharedParts &parts, cudaStream_t s);
 // Threads of a combine block over `cols` columns of a head.

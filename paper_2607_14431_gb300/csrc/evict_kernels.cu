@@ -45,8 +45,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
 }
 
-template <class Params>
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
     __shared__ int hist[2][256];     // of a digit, this CTA's rows
     __shared__ int all_hist[256];    // the cluster's
     __shared__ int found[2];         // digit, rows that have larger ones
@@ -216,8 +215,8 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
 }
 
 // SHIFT: log2 of a row's bytes.
-template <int SHIFT, class Params>
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ Params p) {
+template <int SHIFT>
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictParams p) {
     constexpr int U = kMoveUnroll, ROWS = kMoveThreads * U * 16 >> SHIFT;  // of a chunk
     const EvictSeq q = p.seq[blockIdx.y];
     const int part = blockIdx.z;
@@ -269,8 +268,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
 
 }  // namespace
 
-template <class Params>
-cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows, int n_sm, cudaStream_t s) {
+cudaError_t launch_evict(const EvictParams &p, int64_t most_slots, int64_t most_rows, int n_sm, cudaStream_t s) {
     // a slot to each thread, up to a cluster's CTAs
     int cluster = 1;
     while (cluster < kMaxCluster && (int64_t)cluster * kSelectThreads < most_slots) cluster *= 2;
@@ -285,7 +283,7 @@ cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows,
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel<Params>, p);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel, p);
     count_launches(1);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess || most_rows <= 0) return e;
@@ -295,14 +293,12 @@ cudaError_t launch_evict(const Params &p, int64_t most_slots, int64_t most_rows,
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({chunks, 32 * (int64_t)n_sm / units, 65535}));
     const dim3 grid((unsigned)(p.n_planes * p.n_kv_heads), p.n_seq, (unsigned)parts);
     switch (p.row_bytes) {
-        case 64: return launch_after(evict_move_kernel<6, Params>, grid, kMoveThreads, 0, s, p);
-        case 128: return launch_after(evict_move_kernel<7, Params>, grid, kMoveThreads, 0, s, p);
-        case 256: return launch_after(evict_move_kernel<8, Params>, grid, kMoveThreads, 0, s, p);
-        case 512: return launch_after(evict_move_kernel<9, Params>, grid, kMoveThreads, 0, s, p);
+        case 64: return launch_after(evict_move_kernel<6>, grid, kMoveThreads, 0, s, p);
+        case 128: return launch_after(evict_move_kernel<7>, grid, kMoveThreads, 0, s, p);
+        case 256: return launch_after(evict_move_kernel<8>, grid, kMoveThreads, 0, s, p);
+        case 512: return launch_after(evict_move_kernel<9>, grid, kMoveThreads, 0, s, p);
     }
     return cudaErrorInvalidValue;
 }
-template cudaError_t launch_evict(const EvictParams &, int64_t, int64_t, int, cudaStream_t);
-template cudaError_t launch_evict(const FewEvictParams &, int64_t, int64_t, int, cudaStream_t);
 
 }  // namespace kvg

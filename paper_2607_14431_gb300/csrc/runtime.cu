@@ -3436,11 +3436,10 @@ struct EvictPlan {
     std::vector<int32_t> unshared; // a block's, no longer pointed at
 };
 
-template <class Params>
 static cudaError_t run_evict(kvg_cache *c, const std::vector<EvictPlan> &plans, float *weights, int64_t n_list,
                              cudaStream_t st) {
     const kvg_dims &dims = c->dims;
-    Params p;  // every field is set, of the arrays what the launch reads
+    EvictParams p;  // every field is set, of the arrays what the launch reads
     p.pool = c->pool;
     p.pool_pages = c->n_pages;
     p.page_table = c->page_table;
@@ -3462,10 +3461,10 @@ static cudaError_t run_evict(kvg_cache *c, const std::vector<EvictPlan> &plans, 
         p.pid0 = plans[i].q.page0;
         p.n_pids = 0;
         int64_t rows = 0, slots = 0;
-        while (i < plans.size() && p.n_seq < Params::kSeqs) {
+        while (i < plans.size() && p.n_seq < kMaxEvictSeqs) {
             const EvictPlan &plan = plans[i];
             const int32_t n = (int32_t)plan.pages.size();
-            if (n > Params::kPages) {  // by themselves, ahead
+            if (n > kMaxPagesPerLaunch) {  // by themselves, ahead
                 if (p.n_seq) break;
                 for (int32_t at = 0; at < n; at += kMaxPagesPerLaunch) {
                     IntsParams ints{};
@@ -3475,7 +3474,7 @@ static cudaError_t run_evict(kvg_cache *c, const std::vector<EvictPlan> &plans, 
                     if (cudaError_t e = launch_write_ints(ints, st); e != cudaSuccess) return e;
                 }
             } else {
-                if (p.n_pids + n > Params::kPages) break;
+                if (p.n_pids + n > kMaxPagesPerLaunch) break;
                 std::copy(plan.pages.begin(), plan.pages.end(), p.pids + p.n_pids);
                 p.n_pids += n;
             }
@@ -3483,7 +3482,7 @@ static cudaError_t run_evict(kvg_cache *c, const std::vector<EvictPlan> &plans, 
             rows = std::max<int64_t>(rows, plan.q.kept - plan.q.start);
             slots = std::max<int64_t>(slots, plan.q.n_slots);
             ++i;
-            if (n > Params::kPages) break;
+            if (n > kMaxPagesPerLaunch) break;
         }
         if (cudaError_t e = launch_evict(p, slots, rows, c->n_sm, st); e != cudaSuccess) return e;
     }
@@ -3625,10 +3624,7 @@ extern "C" kvg_status kvg_cache_evict(kvg_cache *c, const int32_t *seq_ids, cons
         c->n_slots[q.dst] = q.kept;
         c->open_rows[q.dst] = 0;
     }
-    const cudaError_t e = plans.size() <= FewEvictParams::kSeqs && n_pids <= FewEvictParams::kPages
-                              ? run_evict<FewEvictParams>(c, plans, weights, n_list, st)
-                              : run_evict<EvictParams>(c, plans, weights, n_list, st);
-    KVG_CUDA(e);
+    KVG_CUDA(run_evict(c, plans, weights, n_list, st));
     return used_partials(c, st);
 }
 
