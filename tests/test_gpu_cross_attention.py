@@ -150,6 +150,20 @@ def test_states_of_no_rows(kvg):
     assert not run(bed, 4, [0], [1]).any()
 
 
+def test_rows_past_2_gib_of_a_layer_without_states(kvg):
+    bed = States(kvg, 2, 8, 256, 64, [0, 70])
+    n, hq = [262_150, 3], 16  # a layer's outputs: 2^31 bytes and more
+    q = torch.zeros(2, sum(n), hq, 256, dtype=torch.bfloat16, device="cuda")
+    q[:, -3:] = normal(3, 2, 3, hq, 256)
+    out = torch.full_like(q, float("nan"))
+    kvg.kvg_cross_attention(bed.cache.h, -1, [0, 1], n, q.data_ptr(), hq, out.data_ptr(), 1 / 16)
+    torch.cuda.synchronize()
+    kvg.kvg_sync(bed.cache.h)
+    assert not out[:, :-3].any()
+    for l in range(2):
+        check(out[l, -3:], reference(bed, 1, l, q[l, -3:], 0, 1 / 16), f"layer {l}")
+
+
 def test_a_sequence_named_more_than_once(kvg):
     bed = States(kvg, 1, 2, 128, 64, [333, 90])
     q = normal(4, 1, 60, 4, 128)
