@@ -3052,15 +3052,9 @@ extern "C" kvg_status kvg_cross_attention(kvg_cache *c, int32_t layer, const int
     std::stable_sort(order.begin(), order.end(),
                      [&](int32_t a, int32_t b) { return c->n_slots[seq_ids[a]] > c->n_slots[seq_ids[b]]; });
     const size_t row_bytes = (size_t)n_q_heads * d.head_dim * sizeof(__nv_bfloat16);
-    const size_t layer_bytes = total * row_bytes, n_run = layer < 0 ? d.n_layers : 1;
-    for (int32_t b : none) {
-        uint8_t *const rows = static_cast<uint8_t *>(out) + row0[b] * row_bytes;
-        if (layer_bytes <= 0x7fffffff)  // (the most that a pitch may be)
-            KVG_CUDA(cudaMemset2DAsync(rows, layer_bytes, 0, n_rows[b] * row_bytes, n_run, st));
-        else
-            for (size_t l = 0; l < n_run; ++l)
-                KVG_CUDA(cudaMemsetAsync(rows + l * layer_bytes, 0, n_rows[b] * row_bytes, st));
-    }
+    for (int32_t b : none)
+        KVG_CUDA(cudaMemset2DAsync(static_cast<uint8_t *>(out) + row0[b] * row_bytes, total * row_bytes, 0,
+                                   n_rows[b] * row_bytes, layer < 0 ? d.n_layers : 1, st));
     if (order.empty()) return KVG_OK;
     PromptParams p{};
     prompt_params(c, q, n_q_heads, out, scale, &p);
