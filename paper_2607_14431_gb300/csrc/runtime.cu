@@ -2755,8 +2755,9 @@ static uint64_t weights_scratch() {
 // shared out one by one, of many half an item stands for the difference.  An item
 // costs its query tiles and kItemTiles more.  (2,047 rows of the 12B shape on 6,145:
 // 76 pairs of CTAs with whole items have 98 tiles at most, with every round forwards
-// 113, so that halves were better, 105: 251 us for the call and 257.  27 prompts of up
-// to 490 with a window: whole items 131 us, halves, which 2 for kItemTiles takes, 134.)
+// 113, so that halves were better, 105: 251 us for the call and 257.  What an item
+// costs need not be known well: with 0.5 to 6 for kItemTiles a dozen calls of 18 to
+// 265 us took the same within 1%.)
 // Returns the floats of a layer's sums.
 static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     constexpr double kItemTiles = 4.0;
