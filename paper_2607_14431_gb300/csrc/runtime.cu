@@ -183,11 +183,17 @@ struct Scratch {
     size_t cap = 0;
     bool captured = false;
     std::vector<void *> kept;
-    // capturing: the call is being captured, where nothing can be allocated
-    cudaError_t ensure(size_t bytes, bool capturing = false) {
+    // capturing: the call is being captured, where nothing can be allocated.
+    // grows: what is asked for grows with every token of a sequence, so a buffer is
+    // followed by one half as large again (of `grows` bytes at most, where they
+    // are enough): few steps allocate, which waits for the device, and what graphs
+    // keep is less than twice what there is.
+    cudaError_t ensure(size_t bytes, bool capturing = false, size_t grows = 0) {
         if (bytes > cap && capturing) return cudaErrorStreamCaptureUnsupported;
         captured = captured || capturing;
         if (bytes <= cap) return cudaSuccess;
+        size_t want = std::max(bytes, (size_t)1 << 20), more = want;
+        if (grows) more = std::max(want, bytes <= grows ? std::min(cap + cap / 2, grows) : cap + cap / 2);
         if (ptr && captured)
             kept.push_back(ptr);
         else if (ptr)
@@ -195,10 +201,13 @@ struct Scratch {
         captured = false;
         ptr = nullptr;
         cap = 0;
-        size_t want = std::max(bytes, (size_t)1 << 20);
-        cudaError_t e = cudaMalloc(&ptr, want);
+        cudaError_t e = cudaMalloc(&ptr, more);
+        if (e != cudaSuccess && more > want) {
+            cudaGetLastError();
+            e = cudaMalloc(&ptr, more = want);
+        }
         if (e != cudaSuccess) return e;
-        cap = want;
+        cap = more;
         return cudaSuccess;
     }
     void release() {
@@ -2906,7 +2915,8 @@ static kvg_status prompt_impl(kvg_cache *c, int32_t layer, const int32_t *seq_id
             const int64_t at_a_time =
                 std::max<int64_t>(1, std::min<int64_t>(p.n_layers_run, (int64_t)(weights_scratch() / sizeof(float)) / floats));
             const int64_t n_lse = (int64_t)p.n_units * rows.total * G;
-            KVG_CUDA(c->scores.ensure((size_t)(n_lse + slots + floats * at_a_time) * sizeof(float), c->capturing));
+            KVG_CUDA(c->scores.ensure((size_t)(n_lse + slots + floats * at_a_time) * sizeof(float), c->capturing,
+                                       weights_scratch()));
             w->p.row_lse = static_cast<float *>(c->scores.ptr);
             w->p.part_lse = w->p.row_lse + n_lse;
             w->sums = w->p.part_lse + slots;
@@ -3371,7 +3381,7 @@ static kvg_status decode_weights(kvg_cache *c, int32_t layer, const std::vector<
                         a.first[w][i] = t0 / tpp * d.page_size + t0 % tpp * TOK + p.rows[w].lo[i];
                     }
                 }
-                KVG_CUDA(c->scores.ensure((part * G + n) * sizeof(float), c->capturing));
+                KVG_CUDA(c->scores.ensure((part * G + n) * sizeof(float), c->capturing, weights_scratch()));
                 a.scores.part_lx = static_cast<float *>(c->scores.ptr);
                 a.scores.scores = a.scores.part_lx + part * G;
                 a.weights = weights;
