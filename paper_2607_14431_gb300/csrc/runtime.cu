@@ -2752,10 +2752,34 @@ struct PromptWeights {
 
 // What kvg_attention_weights keeps at a time: a decode step's scores of all layers
 // and rows where they fit, else of a layer's rows as many as fit; a prompt's sums of
-// as many layers as fit.
+// as many sequences as fit, and of those as many layers.  (One row's scores of a
+// layer, and one sequence's sums, are kept whatever they take.  Beside them, what
+// goes by the queries: 4 bytes for each of their heads and key ranges, and of an fp8
+// cache the queries as fp16.)
 static uint64_t weights_scratch() {
     static const int kb = env_knob("KVG_WEIGHTS_SCRATCH_KB", 512 << 10);
     return 1024ull * kb;
+}
+
+// Key tile of a slot, and a tile's first slot.
+static int64_t key_tile(const PromptParams &p, int64_t slot) {
+    const int64_t pg = slot / p.page_size;
+    return (p.pages_per_unit ? pg / p.pages_per_unit : pg * p.units_per_page + slot % p.page_size / p.unit) /
+           (kPromptCols / p.unit);
+}
+static int64_t tile_slot(const PromptParams &p, int64_t tile) {
+    const int64_t u = tile * (kPromptCols / p.unit);
+    return p.pages_per_unit ? u * p.pages_per_unit * p.page_size
+                            : u / p.units_per_page * p.page_size + u % p.units_per_page * p.unit;
+}
+// Pairs of key tiles of a launch's sequence, and the floats of its sums of a layer
+// where its query tiles are not split.
+static int32_t weigh_blocks(const PromptParams &p, int32_t i) {
+    const int64_t last = (int64_t)p.slot0[i] + p.first[i + 1] - p.first[i] - 1;
+    return (int32_t)((key_tile(p, last) - key_tile(p, p.begin[i])) / 2 + 1);
+}
+static int64_t weigh_floats(const PromptParams &p, int32_t blocks, int32_t lines) {
+    return (int64_t)p.n_kv_heads * lines * 2 * blocks * kPromptCols;
 }
 
 // The work items of a launch's weights: pairs of key tiles, with the query tiles
@@ -2771,26 +2795,16 @@ static uint64_t weights_scratch() {
 static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     constexpr double kItemTiles = 4.0;
     const PromptParams &p = w->p;
-    const int per = kPromptCols / p.unit;
-    auto tile_of = [&](int64_t slot) {
-        const int64_t pg = slot / p.page_size;
-        return (p.pages_per_unit ? pg / p.pages_per_unit : pg * p.units_per_page + slot % p.page_size / p.unit) / per;
-    };
-    auto slot_of = [&](int64_t tile) {  // its first
-        const int64_t u = tile * per;
-        return p.pages_per_unit ? u * p.pages_per_unit * p.page_size
-                                : u / p.units_per_page * p.page_size + u % p.units_per_page * p.unit;
-    };
     std::vector<int32_t> tiles, longest(p.n_seq);  // query tiles of each block, of a sequence the most
     int64_t blocks = 0, sum = 0;
     int32_t most = 1;
     for (int32_t i = 0; i < p.n_seq; ++i) {
         const int64_t n = p.first[i + 1] - p.first[i], slot0 = p.slot0[i];
-        w->tile0[i] = (int32_t)tile_of(p.begin[i]);
-        w->blocks[i] = (int32_t)((tile_of(slot0 + n - 1) - w->tile0[i]) / 2 + 1);
+        w->tile0[i] = (int32_t)key_tile(p, p.begin[i]);
+        w->blocks[i] = weigh_blocks(p, i);
         for (int32_t b = 0; b < w->blocks[i]; ++b) {  // (as weigh_item())
-            const int64_t tile = w->tile0[i] + 2 * b, t0 = std::max<int64_t>(0, slot_of(tile) - slot0);
-            const int64_t t1 = p.window > 0 ? std::min<int64_t>(n, slot_of(tile + 2) - 1 + p.window - slot0 + w->gaps[i]) : n;
+            const int64_t tile = w->tile0[i] + 2 * b, t0 = std::max<int64_t>(0, tile_slot(p, tile) - slot0);
+            const int64_t t1 = p.window > 0 ? std::min<int64_t>(n, tile_slot(p, tile + 2) - 1 + p.window - slot0 + w->gaps[i]) : n;
             const int64_t len = t0 < t1 ? (t1 * G + kPromptCols - 1) / kPromptCols - t0 * G / kPromptCols : 0;
             tiles.push_back((int32_t)len);
             sum += len;
@@ -2805,9 +2819,13 @@ static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     int64_t before = 0;  // items of the length before
     std::vector<double> load;
     for (double len = most; len >= 1.0; len *= 0.84) {
-        int64_t items = 0;
-        for (int32_t i = 0; i < p.n_seq; ++i) items += (int64_t)splits_of(i, len) * w->blocks[i] * p.n_units;
+        int64_t items = 0, floats = 0;
+        for (int32_t i = 0; i < p.n_seq; ++i) {
+            items += (int64_t)splits_of(i, len) * w->blocks[i] * p.n_units;
+            floats += splits_of(i, len) * weigh_floats(p, w->blocks[i], w->lines);
+        }
         if (items == before) continue;
+        if (before && floats * sizeof(float) > weights_scratch()) break;
         before = items;
         double est = (double)(sum * p.n_units) / at_once + kItemTiles * items / at_once;
         if (items > 8 * at_once) {
@@ -2839,7 +2857,7 @@ static int64_t plan_weigh(const kvg_cache *c, int G, WeighParams *w) {
     for (int32_t i = 0; i < p.n_seq; ++i) {
         w->splits[i] = splits_of(i, best_len);
         w->sum0[i] = floats;  // (of one layer: scaled by the layers of a launch)
-        floats += (int64_t)w->splits[i] * p.n_kv_heads * w->lines * 2 * w->blocks[i] * kPromptCols;
+        floats += w->splits[i] * weigh_floats(p, w->blocks[i], w->lines);
     }
     return floats;
 }
@@ -2897,43 +2915,68 @@ static kvg_status prompt_impl(kvg_cache *c, int32_t layer, const int32_t *seq_id
                 if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
                 continue;
             }
-            auto w = std::make_unique<WeighParams>();
-            w->p = p;
-            w->weights = pw->weights;
-            w->max_slots = c->max_slots;
-            w->decay = pw->decay;
-            w->lines = weigh_lines(d.head_dim);
-            for (int32_t i = 0; i < p.n_seq; ++i) {
-                const int32_t sq = p.seq[i];
-                int64_t valid = 0;
-                for (int32_t f : c->seq_fill[sq]) valid += f;
-                w->gaps[i] = (int32_t)(c->n_slots[sq] - valid);
-                w->met[i] = pw->met[sq];
-                pw->met[sq] = 1;
-            }
-            const int64_t floats = plan_weigh(c, G, w.get());
-            const int64_t at_a_time =
-                std::max<int64_t>(1, std::min<int64_t>(p.n_layers_run, (int64_t)(weights_scratch() / sizeof(float)) / floats));
-            const int64_t n_lse = (int64_t)p.n_units * rows.total * G;
-            KVG_CUDA(c->scores.ensure((size_t)(n_lse + slots + floats * at_a_time) * sizeof(float), c->capturing,
-                                       weights_scratch()));
-            w->p.row_lse = static_cast<float *>(c->scores.ptr);
-            w->p.part_lse = w->p.row_lse + n_lse;
-            w->sums = w->p.part_lse + slots;
-            KVG_CUDA(launch_prompt_lse(d.head_dim, fp8, streams, w->p, c->prompt_map, st));
-            if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, w->p, st));
-            const std::vector<int64_t> sum0(w->sum0, w->sum0 + p.n_seq);
-            for (int32_t l = 0; l < p.n_layers_run; l += w->n_lr) {
-                w->lr0 = l;
-                w->n_lr = (int32_t)std::min<int64_t>(at_a_time, p.n_layers_run - l);
-                w->item0[0] = 0;
-                for (int32_t i = 0; i < p.n_seq; ++i) {
-                    w->sum0[i] = sum0[i] * w->n_lr;
-                    w->item0[i + 1] = w->item0[i] + w->blocks[i] * w->splits[i] * w->n_lr * p.n_kv_heads;
-                    if (l) w->met[i] = 1;
+            // the launch's sequences, as many at a time as the scratch takes sums of
+            std::vector<std::unique_ptr<WeighParams>> passes;
+            std::vector<int64_t> at_a_time;  // layers
+            const int32_t lines = weigh_lines(d.head_dim);
+            const int64_t most_floats = (int64_t)(weights_scratch() / sizeof(float));
+            int64_t sums = 0;
+            for (int32_t i0 = 0, i1; i0 < p.n_seq; i0 = i1) {
+                int64_t floats = 0;
+                for (i1 = i0; i1 < p.n_seq; ++i1) {
+                    floats += weigh_floats(p, weigh_blocks(p, i1), lines);
+                    if (i1 > i0 && floats > most_floats) break;
                 }
-                KVG_CUDA(launch_weigh(d.head_dim, fp8, *w, c->prompt_map, pw->q_map, c->n_sm, st));
-                KVG_CUDA(launch_weigh_sum(*w, st));
+                passes.push_back(std::make_unique<WeighParams>());
+                WeighParams &w = *passes.back();
+                w.p = p;
+                w.p.n_seq = i1 - i0;
+                w.weights = pw->weights;
+                w.max_slots = c->max_slots;
+                w.decay = pw->decay;
+                w.lines = lines;
+                for (int32_t i = 0; i < w.p.n_seq; ++i) {
+                    const int32_t sq = p.seq[i0 + i];
+                    w.p.seq[i] = sq;
+                    w.p.row0[i] = p.row0[i0 + i];
+                    w.p.slot0[i] = p.slot0[i0 + i];
+                    w.p.begin[i] = p.begin[i0 + i];
+                    w.p.solid[i] = p.solid[i0 + i];
+                    w.p.first[i] = p.first[i0 + i];
+                    w.p.first[i + 1] = p.first[i0 + i + 1];
+                    int64_t valid = 0;
+                    for (int32_t f : c->seq_fill[sq]) valid += f;
+                    w.gaps[i] = (int32_t)(c->n_slots[sq] - valid);
+                    w.met[i] = pw->met[sq];
+                    pw->met[sq] = 1;
+                }
+                floats = plan_weigh(c, G, &w);
+                at_a_time.push_back(std::max<int64_t>(1, std::min<int64_t>(p.n_layers_run, most_floats / floats)));
+                sums = std::max(sums, floats * at_a_time.back());
+            }
+            const int64_t n_lse = (int64_t)p.n_units * rows.total * G;
+            KVG_CUDA(c->scores.ensure((size_t)(n_lse + slots + sums) * sizeof(float), c->capturing, weights_scratch()));
+            p.row_lse = static_cast<float *>(c->scores.ptr);
+            p.part_lse = p.row_lse + n_lse;
+            KVG_CUDA(launch_prompt_lse(d.head_dim, fp8, streams, p, c->prompt_map, st));
+            if (slots) KVG_CUDA(launch_prompt_join(d.head_dim, p, st));
+            for (size_t k = 0; k < passes.size(); ++k) {
+                WeighParams &w = *passes[k];
+                w.p.row_lse = p.row_lse;
+                w.sums = p.part_lse + slots;
+                const std::vector<int64_t> sum0(w.sum0, w.sum0 + w.p.n_seq);
+                for (int32_t l = 0; l < p.n_layers_run; l += w.n_lr) {
+                    w.lr0 = l;
+                    w.n_lr = (int32_t)std::min<int64_t>(at_a_time[k], p.n_layers_run - l);
+                    w.item0[0] = 0;
+                    for (int32_t i = 0; i < w.p.n_seq; ++i) {
+                        w.sum0[i] = sum0[i] * w.n_lr;
+                        w.item0[i + 1] = w.item0[i] + w.blocks[i] * w.splits[i] * w.n_lr * p.n_kv_heads;
+                        if (l) w.met[i] = 1;
+                    }
+                    KVG_CUDA(launch_weigh(d.head_dim, fp8, w, c->prompt_map, pw->q_map, c->n_sm, st));
+                    KVG_CUDA(launch_weigh_sum(w, st));
+                }
             }
         }
     }
