@@ -346,8 +346,10 @@ void kvg_rotary_destroy(kvg_rotary *rotary);
  *     of axis a has f = theta^(-j / sections[a]).
  * Scaling applies to each pair's f.  One axis is kvg_rotary_create.
  * A call that is given such a rotary takes positions [n_axes][T]; the position
- * tags of the rows are those of axis 0, and a relocated graft (delta != 0),
- * which turns whole heads by one position, does not fit them.
+ * tags of the rows are those of axis 0.  A relocated graft (delta != 0) turns
+ * whole heads by one position, which moves every axis by delta: it fits rows of
+ * KVG_ROPE_AXES_SECTIONS and _TURNS as it does those of one axis (above), not
+ * several axes with ladders of their own (nothing refuses it).
  * n_axes in [1, KVG_ROPE_MAX_AXES]; KVG_ERR_ARG otherwise. */
 kvg_status kvg_rotary_create_axes(const kvg_rotary_desc *desc, const int32_t *sections, int32_t n_axes,
                                   int32_t layout, kvg_rotary **out);
