@@ -642,8 +642,8 @@ kvg_status kvg_decode_attention_noalloc(kvg_cache *cache, int32_t layer, const i
  * group sizes as for kvg_decode_attention.  A value row
  * that a query does not attend to does not reach its output, whatever bits it
  * holds.  Products with an fp8 cache take q as fp16, as the decode's do: past
- * 65,504 an element is infinite.  Where every n_rows[b] is 1 this is
- * kvg_decode_attention.
+ * 65,504 an element is infinite, below 2^-17 it is off by up to 2^-25, between
+ * them it is exact.  Where every n_rows[b] is 1 this is kvg_decode_attention.
  * Errors: KVG_ERR_ARG as for kvg_decode_attention, for more query rows than
  * slots, and where a graft left unfilled slots among a sequence's query rows. */
 kvg_status kvg_prompt_attention(kvg_cache *cache, int32_t layer, const int32_t *seq_ids, const int32_t *n_rows,

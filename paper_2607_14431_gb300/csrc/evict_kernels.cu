@@ -23,7 +23,10 @@
 // within a sequence's own pages takes.  Rows that go to another sequence's pages
 // are divided among several CTAs.  Memory bounds it: each kept row is read and
 // written once, with the next chunk's loads in flight while one is stored (403 MB of
-// the 12B shape's rows read and written in 119 us, 6.8 TB/s).
+// the 12B shape's rows read and written in 119 us, 6.8 TB/s).  In place there are no
+// more CTAs than planes and heads, and each one's chunks in turn bound it until those
+// fill the SMs: 4,096 of 8,192 rows of the 12B shape take 243 us for 1 or 4 layers and
+// 567 for 40 (bytes 10, 40 and 396), to another sequence 32, 65 and 423.
 #include <algorithm>
 
 #include "tcgen05.cuh"

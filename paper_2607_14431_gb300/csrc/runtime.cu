@@ -2457,7 +2457,7 @@ extern "C" kvg_status kvg_cache_set_layer_windows(kvg_cache *c, const int32_t *w
 // that is being captured does not (its replays are the caller's to order).
 static cudaError_t use_partials(kvg_cache *c, cudaStream_t st) {
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    if (st)  // (the null stream cannot be; asking takes 0.3 us)
+    if (st)  // (the null stream cannot be; asking takes 0.03 us)
         if (cudaError_t e = cudaStreamIsCapturing(st, &capture); e != cudaSuccess) return e;
     c->capturing = capture != cudaStreamCaptureStatusNone;
     if (c->capturing) return cudaSuccess;
@@ -2788,7 +2788,8 @@ static int64_t weigh_floats(const PromptParams &p, int32_t blocks, int32_t lines
 // shared out one by one, of many half an item stands for the difference.  An item
 // costs its query tiles and kItemTiles more.  (2,047 rows of the 12B shape on 6,145:
 // 76 pairs of CTAs with whole items have 98 tiles at most, with every round forwards
-// 113, so that halves were better, 105: 251 us for the call and 257.  What an item
+// 113, so that halves were better, 105: 251 us for the call and 257, before items were
+// worked out at a CTA's start, 232 now.  What an item
 // costs need not be known well: with 0.5 to 6 for kItemTiles a dozen calls of 18 to
 // 265 us took the same within 1%.)
 // Returns the floats of a layer's sums.
@@ -3009,7 +3010,9 @@ extern "C" kvg_status kvg_prompt_attention(kvg_cache *c, int32_t layer, const in
 // Whether the decode kernel takes the rows, kRowHeads heads (kRowHeads / G rows) of a
 // sequence at a time: where its keys and values are read once that way, of an fp8
 // cache of long sequences up to twice (the prompt kernel multiplies tiles of 128 or
-// 256 rows whatever is in them, and converts E4M3 codes first).  24 sequences of 257
+// 256 rows whatever is in them, and converts E4M3 codes first).  The rule is made for
+// fp8, for few sequences and for head_dim 256; many bf16 sequences of head_dim 128
+// lose 5 to 9% by it.  The whole batch goes one way.  24 sequences of 257
 // to 4,099 rows with 2, 4, 8 and 12 query rows each, G = 2, by the prompt kernel and
 // so: 12B shape 79 and 75, 79 and 79, 79 and 134 us, fp8 92 and 48, 92 and 52, 92 and
 // 77, 92 and 107; 31B shape 75 and 79, 76 and 83, fp8 82 and 45, 83 and 48, 84 and 78,

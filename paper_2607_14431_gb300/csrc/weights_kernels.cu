@@ -5,14 +5,14 @@
 // s_ij the scores scaled by log2(e), m_i a row's maximum, l_i its sum of 2^(s_ij -
 // m_i), all in fp32 (the attention's own sums add 16-bit weights).
 //
-// A decode step's scores are 2 G / D of its keys' and values' bytes: the decode
-// kernel stores them on its way.  Behind it one launch merges its partial results
-// into outputs (the blocks of the combine) and adds up a slot's weights over layers
-// and heads, in a fixed order, so that keys are read once and results are bitwise
-// reproducible.  A block of the latter has up to 128 slots of a batch row and finds (m, l)
-// of all its heads itself, a few partials each: as a launch of its own behind the
-// combine, which had merged them, one token on 2,111 rows of the 31B shape took
-// 13.9 us.
+// A decode step's scores are G / D of its keys' and values' bytes (fp8: 2 G / D), to
+// be written and read once: the decode kernel stores them on its way.  Behind it one
+// launch merges its partial results into outputs (the blocks of the combine) and adds
+// up a slot's weights over layers and heads, in a fixed order, so that keys are read
+// once and results are bitwise reproducible.  A block of the latter has up to 128 slots
+// of a batch row and finds (m, l) of all its heads itself, a few partials each: as a
+// launch of its own behind the combine, which had merged them, one token on 2,111 rows
+// of the 31B shape took 13.9 us.
 #include <algorithm>
 
 #include "decode.cuh"
@@ -181,7 +181,8 @@ cudaError_t launch_decode_weights(int head_dim, int group, bool fp8, const Decod
     KVG_DECODE_CASES(KVG_CASE)
 #undef KVG_CASE
     if (e != cudaSuccess) return e;
-    // (the combine's blocks are those of launch_combine, so that outputs are those of the decode alone)
+    // (the combine's blocks are those of launch_combine: outputs are those of the decode alone, bit for bit, where
+    // both split the tiles alike, among as many warps and over the same layers and rows; else within the sums' rounding)
     const int cols = (int64_t)p.n_q_heads * p.B * p.n_layers_run <= n_sm ? 64 : head_dim;
     const int n = combine_threads(cols, p), slots = block_slots(n);
     const int64_t outputs = (int64_t)p.n_q_heads * (head_dim / cols) * p.n_layers_run;
